@@ -23,6 +23,7 @@
 #ifndef MAP_GB300_H
 #define MAP_GB300_H
 
+#include <stddef.h>
 #include <stdint.h>
 
 #ifdef __cplusplus
@@ -157,6 +158,25 @@ int map_assemble(map_ctx *ctx, const void *vis_feats, const int32_t *keep_idx,
                  int pos_offset, void *seq, int32_t *pos_ids, void *stream);
 
 /*
+ * The hand-off for a language model whose rotary positions have three axes (time, height,
+ * width), as image and video models use them: map_assemble_ragged's rows, with position ids
+ * on each axis.  Image b is a grid of T x H x W visual tokens, its rows 0 .. T H W - 1 of
+ * vis_feats in time-major order (H W per frame, W per row of a frame).
+ *   kept token n:     (n / (H W)) * t_step,  (n / W) % H,  n % W
+ *   question token m: max((T - 1) * t_step + 1, H, W) + m  on every axis
+ * each plus pos_offset: a pruned image's question sits where the whole image's would.
+ *   grids    int32 [B, 3] HOST array: T, H, W >= 1 of each image, T H W <= N, k <= T H W.
+ *   t_step   int32 [B] HOST array: positions from one frame to the next, >= 0; NULL: 1.
+ *   pos_ids  int32 [3, sum_b (k + lens[b])] output (device): time, height, width.
+ * Everything else as for map_assemble.  An index outside [0, T H W) is not copied: its ids are
+ * -1 and map_status reports MAP_EINTERNAL.  Positions must stay below 2^31 (MAP_EUNSUPPORTED).
+ */
+int map_assemble_axes(map_ctx *ctx, const void *vis_feats, const int32_t *keep_idx,
+                      const void *text_feats, const int32_t *lens, const int32_t *grids,
+                      const int32_t *t_step, int B, int N, int k, int pos_offset, void *seq,
+                      int32_t *pos_ids, void *stream);
+
+/*
  * map_select without allocating memory in the call (the paper has no counterpart; this
  * is a deployment variant of map_select).  Same arguments and limits as map_select, and
  * the same exact greedy picks (a near-tie below fp32 resolution may go either way, as
@@ -284,6 +304,168 @@ typedef struct {
 int map_distill_grad(map_ctx *ctx, const void *text_feats, const void *vis_feats,
                      const int32_t *lens, const float *teacher, int B, int N, float *loss,
                      const map_grads *grads, void *stream);
+
+/* ---------------------------------------------------------------- queries and keys
+ * What a language model does with the hand-off sequence before its attention: the norm of
+ * each query and key head and the rotation by position, forward and backward.  Context-free
+ * like map_qcts: no map_init, no device workspace of the library's own.
+ */
+
+/* Element types of the calls below. */
+#define MAP_BF16 0
+#define MAP_F16  1
+#define MAP_F32  2
+
+/* Heads of `heads` vectors a row: element (r, h, i) at p[r * row + h * head + i] (strides in
+ * elements, >= 0).  A view of one projection's output, or [heads, rows, dh] arrays, need no copy. */
+typedef struct {
+    void *p;
+    long long row, head;
+    int heads;
+} map_heads;
+
+/*
+ * A rotation plan: host memory only, immutable, usable from any thread, stream and device.
+ *   dh        head width, 1 .. 256.
+ *   rot       columns that are rotated, the first of each head: even, 0 .. dh.
+ *   adjacent  0: pair i is columns (i, i + rot / 2); 1: columns (2 i, 2 i + 1).
+ *   n_axes    position axes, 1 .. 4.
+ *   inv_freq  double [rot / 2] HOST: radians per position of each pair, finite.
+ *   axis      int32 [rot / 2] HOST: the axis whose position turns the pair, 0 .. n_axes - 1
+ *             (time, height and width in runs, by turns, or any other way); NULL: axis 0.
+ *   eps       added to the mean square of a head before its root, >= 0.
+ * The angle pos * inv_freq is reduced modulo 2 pi exactly (64-bit fixed point), for any int32
+ * position.  Returns MAP_EINVAL for arguments outside these ranges.
+ */
+typedef struct map_rope map_rope;
+int map_rope_init(int dh, int rot, int adjacent, int n_axes, const double *inv_freq, const int32_t *axis,
+                  double eps, map_rope **out);
+void map_rope_destroy(map_rope *rope);
+
+/*
+ * Per head x of q and k:  z = x * (mean_i x_i^2 + eps)^(-1/2) * w   (z = x where w is NULL),
+ * then pair (a, b) of the rotated columns:  (z_a cos t - z_b sin t, z_b cos t + z_a sin t),
+ * t = pos[axis, row] * inv_freq.  Computed in fp32, rounded once to the output's type.
+ *   type      MAP_BF16, MAP_F16 or MAP_F32: of q, k, wq, wk and the outputs.
+ *   pos       int32 [n_axes, rows] (device); NULL only if rot = 0.
+ *   q, k      inputs; either may be absent (NULL or heads = 0).
+ *   wq, wk    [dh] norm weights (device) or NULL: no norm of that side.
+ *   q_out, k_out  outputs with the inputs' heads; they may be the inputs themselves (same p,
+ *             row and head), else must not overlap them.  Vectors of one output must not
+ *             overlap each other (MAP_EINVAL).
+ * rows >= 0 (0: no-op), rows * heads < 2^31 per side.  16-byte aligned bases, strides that are
+ * multiples of 8 elements and dh and rot / 2 that are multiples of 8 take the widest accesses.
+ */
+int map_qk_rotate(const map_rope *rope, int type, long long rows, const int32_t *pos, const map_heads *q,
+                  const map_heads *k, const void *wq, const void *wk, const map_heads *q_out,
+                  const map_heads *k_out, void *stream);
+
+/*
+ * Gradient of map_qk_rotate.  dq_out, dk_out: gradients of its outputs; q, k: its inputs (only
+ * read where wq / wk is given; else may be NULL); dq, dk: outputs, of `type` (may be dq_out,
+ * dk_out themselves); dwq, dwk: float [dh] outputs, overwritten, for the sides with a norm:
+ * sums over all rows and heads in fp32, in a fixed order.  ws: device scratch of
+ * map_qk_rotate_grad_workspace(rope) bytes, 16-byte aligned, the caller's until the call's work
+ * completes (may be NULL without norms).  Other arguments as for map_qk_rotate.  rows = 0 zeroes
+ * dwq and dwk.
+ */
+size_t map_qk_rotate_grad_workspace(const map_rope *rope);
+int map_qk_rotate_grad(const map_rope *rope, int type, long long rows, const int32_t *pos,
+                       const map_heads *dq_out, const map_heads *dk_out, const map_heads *q, const map_heads *k,
+                       const void *wq, const void *wk, const map_heads *dq, const map_heads *dk, float *dwq,
+                       float *dwk, void *ws, void *stream);
+
+/* ---------------------------------------------------------------- pages of a cache
+ * Keys and values of the sequences that a language model is answering, in pages of a pool that
+ * all layers share one page table for.  Sequences of one image share its pages: a question
+ * takes the parent's rows with its own kept visual tokens (map_cache_fork) and frees them when
+ * answered.  Everything below is device memory of the caller, initially zero but for the pool;
+ * the calls keep no other state, never synchronise and may be captured.  Calls on one cache
+ * are ordered by the caller (one stream, or events).
+ *   pool    [layers][2: K, V][pages][heads][page][dh] of `type`, 16-byte aligned.
+ *   table   int32 [seqs, max_pages]: the pages of each sequence; only the first
+ *           ceil(len / page) entries of a row mean anything.
+ *   len     int32 [seqs]: rows of each sequence.
+ *   refs    int32 [pages]: sequences that hold the page; 0: free.
+ *   status  int32 [2]: error bits for map_cache_status; a word for the calls' own use.
+ * type MAP_BF16 or MAP_F16; dh a multiple of 8 up to 256; page 1 .. 1024; pages <= 1048576;
+ * seqs <= 262144; max_pages * page < 2^31 (MAP_EUNSUPPORTED beyond these).  New pages are the free ones with the lowest numbers, in the order of the
+ * call's entries: results do not depend on timing.
+ * A call that names a bad sequence, names one twice where that is not allowed, or needs more
+ * pages than are free or than a table row holds, changes no length and no page: map_cache_status
+ * then reports it.
+ */
+typedef struct {
+    void *pool;
+    int32_t *table, *len, *refs, *status;
+    int type, layers, pages, heads, page, dh, seqs, max_pages;
+} map_cache;
+
+/*
+ * Appends rows: entry i adds counts[i] rows to sequence seqs[i], taking pages where they are
+ * needed, and gives them their slots (page * cache->page + row in the page), packed in the
+ * entries' order: slots [rows], those past the last entry's rows are -1.
+ *   seqs, counts  int32 [n] (device).  seqs[i] = -1: the entry is padding, without rows.  A
+ *                 sequence may appear once.  counts >= 0, sum <= rows (else the call is refused
+ *                 as above and every slot is -1).  counts = NULL, for a decoding step: one row
+ *                 each, entry i's is row i, a padding entry's slot is -1; rows >= n.
+ *   n <= 4096, rows <= 1048576 (MAP_EUNSUPPORTED).
+ */
+int map_cache_extend(const map_cache *cache, const int32_t *seqs, const int32_t *counts, int n, long long rows,
+                     int32_t *slots, void *stream);
+
+/*
+ * map_qk_rotate whose keys go to the cache: row r's rotated k and its v (copied) are written to
+ * slot slots[r] of `layer`, its rotated q to q_out.  k and v have cache->heads heads of
+ * cache->dh = the plan's dh columns, and the cache's type.  A row with slot -1 is padding:
+ * nothing of it is written.  A slot outside the pool is skipped like padding and reported by
+ * map_cache_status.  No slot may appear twice.
+ */
+int map_qk_rotate_append(const map_rope *rope, const map_cache *cache, int layer, long long rows,
+                         const int32_t *pos, const int32_t *slots, const map_heads *q, const map_heads *k,
+                         const map_heads *v, const void *wq, const void *wk, const map_heads *q_out, void *stream);
+
+/*
+ * Forks sequences: the empty sequence children[i] gets the rows of parents[i] in all layers.
+ *   keep = NULL  all rows.
+ *   keep int32 [n, k] (device), base, span int32 [n] (device): rows base .. base + span - 1 of
+ *        the parent (its visual tokens) are replaced by its rows base + keep[i, 0 .. k); the rows
+ *        before and after stay.  keep is map_select's keep_idx: a question's own pruned view of
+ *        an image that stays cached whole.  base, span >= 0, base + span <= the parent's
+ *        length.  An index outside [0, span) gives a row of zeros and is reported.
+ * Pages that are full and end before the first replaced row are shared (not copied); the other
+ * rows are copied to new pages.  parents may repeat, children may not, and no child may be a
+ * parent.  Compaction in place is a fork of the kept rows followed by map_cache_free of the
+ * parent.  n <= 4096, 0 <= k <= 2^24 (MAP_EUNSUPPORTED beyond).
+ */
+int map_cache_fork(const map_cache *cache, const int32_t *parents, const int32_t *children, int n,
+                   const int32_t *keep, int k, const int32_t *base, const int32_t *span, void *stream);
+
+/* Frees sequences: each page loses one holder, the length becomes 0.  seqs int32 [n] (device);
+ * -1 is padding, a sequence that is empty or appears again is left alone.  n <= 1048576
+ * (MAP_EUNSUPPORTED beyond). */
+int map_cache_free(const map_cache *cache, const int32_t *seqs, int n, void *stream);
+
+/*
+ * Attention of single tokens over the cache: for query row i of sequence s = seqs[i] and head h,
+ *   out[i, h] = sum_t softmax_t(scale <q[i, h], K[t, h / G]>) V[t, h / G],  t < len[s],
+ * G = q heads / cache->heads (a whole number).  Scores, softmax statistics and sums in fp32.
+ *   q, out    heads of cache->dh columns in the cache's type, [n] rows; 16-byte aligned, strides
+ *             that are multiples of 8; out must not overlap q.
+ *   seqs      int32 [n] (device); -1: padding, that row of out is left as it was.  A sequence
+ *             without rows gives zeros.  A sequence may appear in several rows.
+ *   ws        device scratch of map_cache_attend_workspace(cache) bytes, 16-byte aligned, the
+ *             caller's until the call's work completes.
+ * dh 64, 80, 96, 128, 192 or 256 (MAP_EUNSUPPORTED otherwise); n <= 65535.
+ */
+size_t map_cache_attend_workspace(const map_cache *cache);
+int map_cache_attend(const map_cache *cache, int layer, const map_heads *q, const int32_t *seqs, int n, float scale,
+                     const map_heads *out, void *ws, void *stream);
+
+/* Synchronises `stream` and returns the error recorded by calls on this cache since the last
+ * call (MAP_ENOMEM: no free page or a full table row; MAP_EINTERNAL: a bad sequence, slot, count or index),
+ * clearing it; else a CUDA error as MAP_ECUDA; else MAP_OK. */
+int map_cache_status(const map_cache *cache, void *stream);
 
 /* Synchronises `stream` and returns the first deferred device-side error recorded by
  * this context since the last call (MAP_ETIMEOUT, MAP_EINTERNAL), clearing it; else a

@@ -9,7 +9,8 @@ from __future__ import annotations
 
 import ctypes
 import os
-from ctypes import POINTER, c_double, c_float, c_int, c_int32, c_longlong, c_void_p
+import struct
+from ctypes import POINTER, c_double, c_float, c_int, c_int32, c_longlong, c_size_t, c_void_p
 
 import numpy as np
 import torch
@@ -62,6 +63,22 @@ SIGNATURES = {
                                  c_int, c_void_p, c_void_p, c_void_p, c_void_p]),
     "map_assemble_ragged": (c_int, [c_void_p, c_void_p, c_void_p, c_void_p, POINTER(c_int32), POINTER(c_int32),
                                     c_int, c_int, c_int, c_int, c_void_p, c_void_p, c_void_p]),
+    "map_assemble_axes": (c_int, [c_void_p, c_void_p, c_void_p, c_void_p, POINTER(c_int32), POINTER(c_int32),
+                                  POINTER(c_int32), c_int, c_int, c_int, c_int, c_void_p, c_void_p, c_void_p]),
+    "map_rope_init": (c_int, [c_int, c_int, c_int, c_int, POINTER(c_double), POINTER(c_int32), c_double,
+                              POINTER(c_void_p)]),
+    "map_rope_destroy": (None, [c_void_p]),
+    # map_heads and map_cache are passed as packed bytes (c_void_p): see _heads and Cache
+    "map_qk_rotate": (c_int, [c_void_p, c_int, c_longlong] + [c_void_p] * 8),
+    "map_qk_rotate_grad_workspace": (c_size_t, [c_void_p]),
+    "map_qk_rotate_grad": (c_int, [c_void_p, c_int, c_longlong] + [c_void_p] * 13),
+    "map_cache_extend": (c_int, [c_void_p, c_void_p, c_void_p, c_int, c_longlong, c_void_p, c_void_p]),
+    "map_qk_rotate_append": (c_int, [c_void_p, c_void_p, c_int, c_longlong] + [c_void_p] * 9),
+    "map_cache_fork": (c_int, [c_void_p, c_void_p, c_void_p, c_int, c_void_p, c_int, c_void_p, c_void_p, c_void_p]),
+    "map_cache_free": (c_int, [c_void_p, c_void_p, c_int, c_void_p]),
+    "map_cache_attend_workspace": (c_size_t, [c_void_p]),
+    "map_cache_attend": (c_int, [c_void_p, c_int, c_void_p, c_void_p, c_int, c_float, c_void_p, c_void_p, c_void_p]),
+    "map_cache_status": (c_int, [c_void_p, c_void_p]),
     "map_distill_grad": (c_int, [c_void_p, c_void_p, c_void_p, POINTER(c_int32), c_void_p, c_int, c_int, c_void_p,
                                  POINTER(MapGrads), c_void_p]),
     "map_prune": (c_int, [c_void_p, c_void_p, c_void_p, POINTER(c_int32), c_int, c_int, c_int, c_void_p,
@@ -217,6 +234,26 @@ class Context:
                                 _ptr(pos), _stream(stream)), "map_assemble")
         return seq, pos
 
+    def assemble_axes(self, vis, keep, text, lens, grids, t_step=None, pos_offset: int = 0, seq=None, pos=None,
+                      stream=None):
+        """map_assemble_axes: the hand-off sequence with position ids [3, rows] (time, height, width) of images
+        that are grids of grids[b] = (T, H, W) tokens, t_step[b] positions from frame to frame (default 1)."""
+        B, N, D = vis.shape
+        k = keep.shape[1]
+        arr, lp = _lens(lens)
+        ga, gp = _lens(grids)
+        sa, sp = _lens(t_step) if t_step is not None else (None, None)
+        if arr.shape != (B,) or ga.shape != (B, 3) or (sa is not None and sa.shape != (B,)) or keep.shape[0] != B:
+            raise ValueError("lens and t_step have one entry an image, grids three, keep one row")
+        rows = B * k + int(arr.sum())
+        if seq is None:
+            seq = torch.empty((rows, D), dtype=vis.dtype, device=vis.device)
+        if pos is None:
+            pos = torch.empty((3, rows), dtype=torch.int32, device=vis.device)
+        _check(lib.map_assemble_axes(self.h, _ptr(vis), _ptr(keep), _ptr(text), lp, gp, sp, B, N, k, pos_offset,
+                                     _ptr(seq), _ptr(pos), _stream(stream)), "map_assemble_axes")
+        return seq, pos
+
     # -- ragged batches (padded layout, n_valid tokens per image) ---------------------------
     def score_ragged(self, text, vis, lens, n_valid, scores=None, stream=None):
         B, N = vis.shape[0], vis.shape[1]
@@ -346,3 +383,252 @@ def qcts(attn, lens, attn_ref, L: int, H: int, N: int, p=None, p_ref=None, js=No
     _check(lib.map_qcts(_ptr(attn), lp, _ptr(attn_ref), M_ref, B, L, H, N, _ptr(p), _ptr(p_ref), _ptr(js),
                         _ptr(teacher), _ptr(teacher_p), _stream(stream)), "map_qcts")
     return p, p_ref, js, teacher, teacher_p
+
+
+# ------------------------------------------------------------------ queries, keys and a cache's pages
+# These calls run on the device of the tensors they are given, whichever is current, and on that device's current
+# stream unless `stream` is given; scratch and outputs that are not given are allocated on the stream that uses them.
+
+TYPES = {torch.bfloat16: 0, torch.float16: 1, torch.float32: 2}      # MAP_BF16, MAP_F16, MAP_F32
+_pack_heads = struct.Struct("@Pqqi4x").pack                          # map_heads
+_pack_cache = struct.Struct("@5P8i").pack                            # map_cache
+
+
+class _on:
+    """The device of a call made current, and its stream (`.s`, a cudaStream_t as an int); with a stream of the
+    caller's, torch allocates on that one meanwhile."""
+    __slots__ = ("device", "stream", "s", "guards")
+
+    def __init__(self, device, stream):
+        if device.type != "cuda":
+            raise ValueError("tensors passed to libmap_gb300 must be on a CUDA device")
+        self.device, self.stream, self.guards = device, stream, ()
+
+    def __enter__(self):
+        d = self.device.index
+        if self.stream is not None:
+            if self.stream.device != self.device:
+                raise ValueError("the stream is not on the tensors' device")
+            g = torch.cuda.stream(self.stream)
+            g.__enter__()
+            self.guards = (g,)
+            self.s = self.stream.cuda_stream
+        else:
+            if torch.cuda.current_device() != d:
+                g = torch.cuda.device(d)
+                g.__enter__()
+                self.guards = (g,)
+            self.s = torch.cuda.current_stream(d).cuda_stream
+        return self
+
+    def __exit__(self, *exc):
+        for g in self.guards:
+            g.__exit__(*exc)
+        return False
+
+
+def _heads(t, rows: int, dh: int, dtype, device):
+    """map_heads of a [rows, heads, dh] tensor with any strides but dh's."""
+    n, h, d = t.shape
+    if n != rows or d != dh or t.dtype != dtype or t.device != device:
+        raise ValueError(f"heads must be [{rows}, heads, {dh}] {dtype} on {device}: got {tuple(t.shape)} {t.dtype} on {t.device}")
+    sr, sh, sd = t.stride()
+    if sd != 1 and d > 1:
+        raise ValueError("a head's columns must be adjacent in memory")
+    return _pack_heads(t.data_ptr(), sr, sh, h)
+
+
+def _dense(t, dtype, device, shape=None, what="tensor"):
+    """Pointer of a contiguous tensor of the wanted type, place and shape (None: NULL)."""
+    if t is None:
+        return None
+    if t.dtype != dtype or t.device != device or not t.is_contiguous() or (shape is not None and tuple(t.shape) != shape):
+        raise ValueError(f"{what} must be a contiguous {dtype} tensor on {device}" + (f" of shape {shape}" if shape else ""))
+    return t.data_ptr()
+
+
+class Rope:
+    """A rotation plan (map_rope_init): heads of dh columns, their first 2 * len(inv_freq) rotated; pair i is turned by
+    pos[axis[i]] * inv_freq[i].  Serves any stream and device."""
+
+    def __init__(self, dh: int, inv_freq, axis=None, n_axes: int | None = None, adjacent: bool = False, eps: float = 1e-6):
+        f = np.ascontiguousarray(np.asarray(inv_freq, dtype=np.float64).reshape(-1))
+        a = np.zeros(f.shape[0], np.int32) if axis is None else np.ascontiguousarray(np.asarray(axis, dtype=np.int32).reshape(-1))
+        if a.shape != f.shape:
+            raise ValueError("axis has one entry a pair")
+        self.dh, self.rot = int(dh), 2 * f.shape[0]
+        self.n_axes = int(n_axes) if n_axes is not None else (int(a.max()) + 1 if a.size else 1)
+        h = c_void_p()
+        _check(lib.map_rope_init(self.dh, self.rot, int(bool(adjacent)), self.n_axes, f.ctypes.data_as(POINTER(c_double)),
+                                 a.ctypes.data_as(POINTER(c_int32)), float(eps), ctypes.byref(h)), "map_rope_init")
+        self.h = h
+        self._grad_ws = int(lib.map_qk_rotate_grad_workspace(h))
+
+    def close(self) -> None:
+        if self.h:
+            lib.map_rope_destroy(self.h)
+            self.h = c_void_p()
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    def _common(self, x, pos):
+        if x.dtype not in TYPES:
+            raise ValueError(f"unsupported element type {x.dtype}")
+        rows = x.shape[0]
+        return TYPES[x.dtype], rows, _dense(pos, torch.int32, x.device, (self.n_axes, rows), "pos")
+
+    def rotate(self, q, k, pos, wq=None, wk=None, q_out=None, k_out=None, stream=None):
+        """map_qk_rotate: (q_out, k_out) of q [rows, heads, dh] and k (either may be None), pos int32 [n_axes, rows],
+        norm weights wq, wk [dh] or None (no norm of that side).  Outputs not given are new, contiguous tensors."""
+        x = q if q is not None else k
+        dt, dev = x.dtype, x.device
+        typ, rows, pp = self._common(x, pos)
+        with _on(dev, stream) as on:
+            if q is not None and q_out is None:
+                q_out = torch.empty(q.shape, dtype=dt, device=dev)
+            if k is not None and k_out is None:
+                k_out = torch.empty(k.shape, dtype=dt, device=dev)
+            a, b, oa, ob = (None if t is None else _heads(t, rows, self.dh, dt, dev) for t in (q, k, q_out, k_out))
+            _check(lib.map_qk_rotate(self.h, typ, rows, pp, a, b, _dense(wq, dt, dev, (self.dh,), "wq"),
+                                     _dense(wk, dt, dev, (self.dh,), "wk"), oa, ob, on.s), "map_qk_rotate")
+        return q_out, k_out
+
+    def grad(self, dq_out, dk_out, pos, q=None, k=None, wq=None, wk=None, dq=None, dk=None, dwq=None, dwk=None,
+             stream=None):
+        """map_qk_rotate_grad: (dq, dk, dwq, dwk) from the gradients of rotate's outputs; q and k (rotate's inputs) are
+        needed where wq and wk are given, dwq and dwk are float32 (None without a norm)."""
+        x = dq_out if dq_out is not None else dk_out
+        dt, dev = x.dtype, x.device
+        typ, rows, pp = self._common(x, pos)
+        with _on(dev, stream) as on:
+            if dq_out is not None and dq is None:
+                dq = torch.empty(dq_out.shape, dtype=dt, device=dev)
+            if dk_out is not None and dk is None:
+                dk = torch.empty(dk_out.shape, dtype=dt, device=dev)
+            if dq_out is not None and wq is not None and dwq is None:
+                dwq = torch.empty(self.dh, dtype=torch.float32, device=dev)
+            if dk_out is not None and wk is not None and dwk is None:
+                dwk = torch.empty(self.dh, dtype=torch.float32, device=dev)
+            ws = torch.empty(self._grad_ws, dtype=torch.uint8, device=dev) if dwq is not None or dwk is not None else None
+            a, b, xa, xb, oa, ob = (None if t is None else _heads(t, rows, self.dh, dt, dev)
+                                    for t in (dq_out, dk_out, q, k, dq, dk))
+            _check(lib.map_qk_rotate_grad(self.h, typ, rows, pp, a, b, xa, xb, _dense(wq, dt, dev, (self.dh,), "wq"),
+                                          _dense(wk, dt, dev, (self.dh,), "wk"), oa, ob,
+                                          _dense(dwq, torch.float32, dev, (self.dh,), "dwq"),
+                                          _dense(dwk, torch.float32, dev, (self.dh,), "dwk"),
+                                          None if ws is None else ws.data_ptr(), on.s), "map_qk_rotate_grad")
+        return dq, dk, dwq, dwk
+
+    def append(self, q, k, v, pos, cache, layer: int, slots, wq=None, wk=None, q_out=None, stream=None):
+        """map_qk_rotate_append: rotated k, and v, into the cache's slots (Cache.extend); returns the rotated q."""
+        dt, dev = k.dtype, k.device
+        if dt != cache.pool.dtype or dev != cache.pool.device:
+            raise ValueError("k has the cache's type and device")
+        _, rows, pp = self._common(k, pos)
+        with _on(dev, stream) as on:
+            if q is not None and q_out is None:
+                q_out = torch.empty(q.shape, dtype=dt, device=dev)
+            a, b, c, oa = (None if t is None else _heads(t, rows, self.dh, dt, dev) for t in (q, k, v, q_out))
+            _check(lib.map_qk_rotate_append(self.h, cache.desc, layer, rows, pp, _dense(slots, torch.int32, dev, (rows,), "slots"),
+                                            a, b, c, _dense(wq, dt, dev, (self.dh,), "wq"),
+                                            _dense(wk, dt, dev, (self.dh,), "wk"), oa, on.s), "map_qk_rotate_append")
+        return q_out
+
+
+class Cache:
+    """Pages of a key/value cache (map_cache) over the caller's tensors: pool [layers, 2, pages, heads, page, dh] bf16 or
+    fp16, table int32 [seqs, max_pages], length int32 [seqs], refs int32 [pages], status int32 [2], the last four
+    initially zero (`Cache.empty` makes all of them)."""
+
+    def __init__(self, pool, table, length, refs, status=None):
+        dev = pool.device
+        if pool.dim() != 6 or pool.shape[1] != 2 or pool.dtype not in TYPES or not pool.is_contiguous():
+            raise ValueError("pool must be a contiguous [layers, 2, pages, heads, page, dh] tensor")
+        if status is None:
+            status = torch.zeros(2, dtype=torch.int32, device=dev)
+        layers, _, pages, heads, page, dh = pool.shape
+        if table.dim() != 2:
+            raise ValueError("table must be [seqs, max_pages]")
+        seqs, max_pages = table.shape
+        ptrs = (_dense(table, torch.int32, dev, None, "table"), _dense(length, torch.int32, dev, (seqs,), "length"),
+                _dense(refs, torch.int32, dev, (pages,), "refs"), _dense(status, torch.int32, dev, (2,), "status"))
+        self.pool, self.table, self.length, self.refs, self.status_word = pool, table, length, refs, status
+        self.heads, self.page, self.dh = heads, page, dh
+        self.desc = _pack_cache(pool.data_ptr(), *ptrs, TYPES[pool.dtype], layers, pages, heads, page, dh, seqs, max_pages)
+        self._attend_ws = int(lib.map_cache_attend_workspace(self.desc))
+
+    @classmethod
+    def empty(cls, layers: int, pages: int, heads: int, page: int, dh: int, seqs: int, max_pages: int,
+              dtype=torch.bfloat16, device="cuda"):
+        def ints(*shape):
+            return torch.zeros(shape, dtype=torch.int32, device=device)
+        return cls(torch.empty((layers, 2, pages, heads, page, dh), dtype=dtype, device=device), ints(seqs, max_pages),
+                   ints(seqs), ints(pages))
+
+    def extend(self, seqs, counts=None, rows: int | None = None, slots=None, stream=None):
+        """map_cache_extend: slots int32 [rows] for counts[i] new rows (default 1) of each sequence seqs[i] (device
+        int32); `rows` (or the size of `slots`) is at least their sum and must be given with counts."""
+        dev = self.pool.device
+        n = seqs.shape[0]
+        if rows is None:
+            if slots is not None:
+                rows = slots.shape[0]
+            elif counts is None:
+                rows = n
+            else:
+                raise ValueError("rows must be given with counts")
+        with _on(dev, stream) as on:
+            if slots is None:
+                slots = torch.empty(rows, dtype=torch.int32, device=dev)
+            _check(lib.map_cache_extend(self.desc, _dense(seqs, torch.int32, dev, (n,), "seqs"),
+                                        _dense(counts, torch.int32, dev, (n,), "counts"), n, rows,
+                                        _dense(slots, torch.int32, dev, (rows,), "slots"), on.s), "map_cache_extend")
+        return slots
+
+    def fork(self, parents, children, keep=None, base=None, span=None, stream=None) -> None:
+        """map_cache_fork: children[i] (empty) gets parents[i]'s rows, with keep int32 [n, k] those of rows
+        base[i] .. base[i] + span[i] that keep[i] names (all int32 on the device)."""
+        dev = self.pool.device
+        n = parents.shape[0]
+        if keep is not None and (keep.dim() != 2 or base is None or span is None):
+            raise ValueError("keep is [n, k] and comes with base and span")
+        k = 0 if keep is None else keep.shape[1]
+        with _on(dev, stream) as on:
+            _check(lib.map_cache_fork(self.desc, _dense(parents, torch.int32, dev, (n,), "parents"),
+                                      _dense(children, torch.int32, dev, (n,), "children"), n,
+                                      _dense(keep, torch.int32, dev, (n, k), "keep"), k,
+                                      _dense(base, torch.int32, dev, (n,), "base"),
+                                      _dense(span, torch.int32, dev, (n,), "span"), on.s), "map_cache_fork")
+
+    def free(self, seqs, stream=None) -> None:
+        """map_cache_free: the pages of seqs (int32 [n] on the device) lose a holder, the lengths become 0."""
+        dev = self.pool.device
+        n = seqs.shape[0]
+        with _on(dev, stream) as on:
+            _check(lib.map_cache_free(self.desc, _dense(seqs, torch.int32, dev, (n,), "seqs"), n, on.s), "map_cache_free")
+
+    def attend(self, q, seqs, layer: int, scale: float | None = None, out=None, stream=None):
+        """map_cache_attend: attention of q [n, heads, dh], row i over sequence seqs[i] (int32 on the device);
+        scale defaults to dh ** -0.5."""
+        dev, dt = self.pool.device, self.pool.dtype
+        n = seqs.shape[0]
+        with _on(dev, stream) as on:
+            if out is None:
+                out = torch.empty(q.shape, dtype=dt, device=dev)
+            ws = torch.empty(self._attend_ws, dtype=torch.uint8, device=dev)
+            _check(lib.map_cache_attend(self.desc, layer, _heads(q, n, self.dh, dt, dev),
+                                        _dense(seqs, torch.int32, dev, (n,), "seqs"), n,
+                                        self.dh ** -0.5 if scale is None else scale, _heads(out, n, self.dh, dt, dev),
+                                        ws.data_ptr(), on.s), "map_cache_attend")
+        return out
+
+    def status(self, stream=None) -> int:
+        with _on(self.pool.device, stream) as on:
+            return lib.map_cache_status(self.desc, on.s)
+
+    def check(self, stream=None) -> None:
+        _check(self.status(stream), "map_cache_status")

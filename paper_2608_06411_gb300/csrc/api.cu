@@ -597,6 +597,30 @@ int assemble_impl(map_ctx* ctx, const void* vis_feats, const int32_t* keep_idx, 
   return MAP_OK;
 }
 
+int assemble_axes_impl(map_ctx* ctx, const void* vis_feats, const int32_t* keep_idx, const void* text_feats,
+                       const int32_t* lens, const int32_t* grids, const int32_t* t_step, int B, int N, int k,
+                       int pos_offset, void* seq, int32_t* pos_ids, cudaStream_t st) {
+  if (!ctx || !vis_feats || !text_feats || !lens || !grids) return MAP_EINVAL;
+  if (B < 1 || N < 1 || k < 0 || k > N) return MAP_EINVAL;
+  long long rows = 0, last = 0;                       // last: largest position, without the offset
+  for (int b = 0; b < B; ++b) {
+    const long long T = grids[3 * b], H = grids[3 * b + 1], W = grids[3 * b + 2], step = t_step ? t_step[b] : 1;
+    if (lens[b] < 0 || T < 1 || H < 1 || W < 1 || step < 0) return MAP_EINVAL;
+    if (T > N || H > N || W > N || H * W > N || T * H * W > N || k > T * H * W) return MAP_EINVAL;
+    last = std::max(last, std::max((T - 1) * step + 1, std::max(H, W)) + lens[b]);
+    rows += k + lens[b];
+  }
+  if (last + std::max(pos_offset, 0) >= (1ll << 31) || rows >= (1ll << 31)) return MAP_EUNSUPPORTED;
+  if (rows == 0) return MAP_OK;
+  if (!seq || !pos_ids || (k > 0 && !keep_idx)) return MAP_EINVAL;
+  if (!aligned16(vis_feats) || !aligned16(text_feats) || !aligned16(seq)) return MAP_EINVAL;
+  CU_TRY(cudaSetDevice(ctx->device));
+  ++ctx->counters.launches;
+  CU_TRY(mapk::launch_assemble_axes(vis_feats, keep_idx, text_feats, lens, grids, t_step, B, N, k, ctx->cfg.D,
+                                    pos_offset, seq, pos_ids, ctx->status, st));
+  return MAP_OK;
+}
+
 bool is_device_ptr(const void* p) {
   cudaPointerAttributes a;
   if (cudaPointerGetAttributes(&a, p) != cudaSuccess) {
@@ -728,6 +752,13 @@ int map_assemble(map_ctx* ctx, const void* vis_feats, const int32_t* keep_idx, c
                  void* stream) {
   return assemble_impl(ctx, vis_feats, keep_idx, text_feats, lens, nullptr, B, N, k, pos_offset, seq, pos_ids,
                        static_cast<cudaStream_t>(stream));
+}
+
+int map_assemble_axes(map_ctx* ctx, const void* vis_feats, const int32_t* keep_idx, const void* text_feats,
+                      const int32_t* lens, const int32_t* grids, const int32_t* t_step, int B, int N, int k,
+                      int pos_offset, void* seq, int32_t* pos_ids, void* stream) {
+  return assemble_axes_impl(ctx, vis_feats, keep_idx, text_feats, lens, grids, t_step, B, N, k, pos_offset, seq,
+                            pos_ids, static_cast<cudaStream_t>(stream));
 }
 
 int map_assemble_ragged(map_ctx* ctx, const void* vis_feats, const int32_t* keep_idx, const void* text_feats,

@@ -1,0 +1,410 @@
+// Pages of a language model's key/value cache: rows appended (map_cache_extend), sequences forked whole or with the
+// kept visual tokens of a question (map_cache_fork), and freed (map_cache_free).
+//
+// Bookkeeping runs on the device, so that a kept set or a count computed there needs no trip to the host and
+// every call can be captured.  One CTA does it for a whole call: the entries' needs are added up in shared memory, the
+// free pages are those with a reference count of zero, and the r-th lowest of them goes to the r-th need.  Nothing but
+// the counts says what is free, so results follow from the state alone, and a fork that is freed leaves it as it was.
+// A call is checked whole before it changes a length or a count; until then it writes only table entries past a length.
+#include "handoff.h"
+
+namespace mapk {
+
+int check_cache(const map_cache* c) {
+  if (!c || !c->pool || !c->table || !c->len || !c->refs || !c->status) return MAP_EINVAL;
+  if (c->type != MAP_BF16 && c->type != MAP_F16) return MAP_EINVAL;
+  if (c->layers < 1 || c->pages < 1 || c->heads < 1 || c->page < 1 || c->dh < 1 || c->seqs < 1 || c->max_pages < 1)
+    return MAP_EINVAL;
+  if (!aligned16(c->pool)) return MAP_EINVAL;
+  if (c->dh % 8 || c->dh > kMaxHead || c->page > 1024 || c->seqs > 262144) return MAP_EUNSUPPORTED;
+  if (c->pages > (1 << 20)) return MAP_EUNSUPPORTED;            // block_scan adds 1024 needs of at most so many pages
+  if (static_cast<long long>(c->max_pages) * c->page >= (1ll << 31)) return MAP_EUNSUPPORTED;
+  return MAP_OK;
+}
+
+namespace {
+
+constexpr int kPlanThreads = 1024;
+constexpr int kMaxEntries = 4096;
+constexpr int kMaxFree = 1 << 20;
+
+// What a fork makes of a parent: rows kept as they are, shared whole pages, length.
+struct ForkShape { int base, span, k, shared, len; };
+__device__ __forceinline__ ForkShape fork_shape(int parent_len, int page, bool kept, int base, int span, int k) {
+  if (!kept) return {parent_len, 0, 0, parent_len / page, parent_len};
+  return {base, span, k, base / page, parent_len - span + k};
+}
+
+// Exclusive prefix sums of v over the block, and their total (every thread gets it).
+__device__ __forceinline__ int block_scan(int v, int* warp_sums, int* total) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  int s = v;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int u = __shfl_up_sync(0xffffffffu, s, o);
+    if (lane >= o) s += u;
+  }
+  if (lane == 31) warp_sums[warp] = s;
+  __syncthreads();
+  int before = 0, all = 0;
+  for (int w = 0; w < kPlanThreads / 32; ++w) {
+    const int x = warp_sums[w];
+    before += w < warp ? x : 0;
+    all += x;
+  }
+  __syncthreads();
+  *total = all;
+  return before + s - v;
+}
+
+// Last i in [0, n) with start[i] <= x (start ascending, start[0] = 0).
+__device__ __forceinline__ int entry_of(const int* start, int n, int x) {
+  int lo = 0, hi = n;
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (start[mid] <= x) lo = mid; else hi = mid;
+  }
+  return lo;
+}
+
+// The total lowest free pages into the table: need r of entry i (start[i] <= r < start[i + 1]) is column
+// col[i] + r - start[i] of row seq[i].  False if there are fewer.  Counts are left as they are.
+__device__ bool take_pages(const map_cache& c, const int* start, const int* col, const int* seq, int n, int total,
+                           int* warp_sums) {
+  int found = 0;
+  for (int p0 = 0; p0 < c.pages && found < total; p0 += kPlanThreads) {
+    const int p = p0 + threadIdx.x;
+    const bool free_page = p < c.pages && c.refs[p] == 0;
+    int got;
+    const int r = found + block_scan(free_page, warp_sums, &got);
+    if (free_page && r < total) {
+      const int i = entry_of(start, n, r);
+      c.table[static_cast<long long>(seq[i]) * c.max_pages + col[i] + r - start[i]] = p;
+    }
+    found += got;
+  }
+  __syncthreads();
+  return found >= total;
+}
+
+// counts[i] more rows for sequence seqs[i], and their slots.  Without counts entry i has row i, padding or not.
+__global__ void __launch_bounds__(kPlanThreads) extend_kernel(const map_cache c, const int32_t* __restrict__ seqs,
+                                                              const int32_t* __restrict__ counts, int n, int rows,
+                                                              int32_t* __restrict__ slots) {
+  extern __shared__ int sh[];
+  int* start = sh;                         // [n + 1] pages needed before entry i
+  int* row0 = start + n + 1;               // [n + 1] rows before entry i
+  int* col = row0 + n + 1;                 // [n] first new page
+  int* seq = col + n;                      // [n]
+  int* old = seq + n;                      // [n] length before, -1: padding
+  unsigned* seen = reinterpret_cast<unsigned*>(old + n);   // bitmap of the sequences
+  __shared__ int warp_sums[kPlanThreads / 32];
+  __shared__ int error;
+  pdl_enter();
+  for (int i = threadIdx.x; i < (c.seqs + 31) / 32; i += kPlanThreads) seen[i] = 0;
+  if (threadIdx.x == 0) error = 0;
+  __syncthreads();
+  int pages0 = 0, rows0 = 0;
+  for (int i0 = 0; i0 < n; i0 += kPlanThreads) {
+    const int i = i0 + threadIdx.x;
+    int need = 0, add = 0;
+    if (i < n) {
+      const int s = seqs[i];
+      seq[i] = col[i] = 0;
+      old[i] = -1;
+      add = counts ? (s == -1 ? 0 : counts[i]) : 1;
+      if (s != -1) {
+        if (s < 0 || s >= c.seqs || add < 0 || add > rows ||
+            (atomicOr(&seen[s >> 5], 1u << (s & 31)) >> (s & 31) & 1u)) {
+          atomicOr(&error, ST_BADINDEX);
+          add = 0;
+        } else {
+          const int len = c.len[s];
+          const long long pages = (static_cast<long long>(len) + add + c.page - 1) / c.page;
+          if (pages > c.max_pages) {
+            atomicOr(&error, ST_NOPAGES);
+            add = 0;
+          } else {
+            seq[i] = s;
+            old[i] = len;
+            col[i] = (len + c.page - 1) / c.page;
+            need = static_cast<int>(pages) - col[i];
+          }
+        }
+      }
+    }
+    int all;
+    const int rs = rows0 + block_scan(add, warp_sums, &all);
+    if (i < n) row0[i] = rs;
+    rows0 += all;                          // 1024 counts of at most 2^20 rows
+    const int ps = pages0 + block_scan(need, warp_sums, &all);
+    if (i < n) start[i] = ps;
+    pages0 += all;
+    if (rows0 > rows) {
+      if (threadIdx.x == 0) atomicOr(&error, ST_BADINDEX);
+      rows0 = pages0 = 0;
+    }
+  }
+  if (threadIdx.x == 0) { start[n] = pages0; row0[n] = rows0; }
+  __syncthreads();
+  const bool ok = error == 0;
+  const bool enough = ok && take_pages(c, start, col, seq, n, pages0, warp_sums);
+  if (!enough) {
+    if (threadIdx.x == 0) atomicOr(c.status, ok ? ST_NOPAGES : error);
+    for (int r = threadIdx.x; r < rows; r += kPlanThreads) slots[r] = -1;
+    return;
+  }
+  for (int r = threadIdx.x; r < pages0; r += kPlanThreads) {
+    const int i = entry_of(start, n, r);
+    c.refs[c.table[static_cast<long long>(seq[i]) * c.max_pages + col[i] + r - start[i]]] = 1;
+  }
+  for (int i = threadIdx.x; i < n; i += kPlanThreads)
+    if (old[i] >= 0) c.len[seq[i]] = old[i] + row0[i + 1] - row0[i];
+  for (int r = threadIdx.x; r < rows; r += kPlanThreads) {
+    int slot = -1;
+    if (r < rows0) {
+      const int i = entry_of(row0, n, r), t = old[i] + r - row0[i];
+      if (old[i] >= 0) slot = c.table[static_cast<long long>(seq[i]) * c.max_pages + t / c.page] * c.page + t % c.page;
+    }
+    slots[r] = slot;
+  }
+}
+
+// Tables, counts and lengths of the children.  status[1]: whether fork_copy_kernel is to copy.
+__global__ void __launch_bounds__(kPlanThreads) fork_plan_kernel(const map_cache c, const int32_t* __restrict__ parents,
+                                                                 const int32_t* __restrict__ children, int n, int kept,
+                                                                 int k, const int32_t* __restrict__ base,
+                                                                 const int32_t* __restrict__ span) {
+  extern __shared__ int sh[];
+  int* start = sh;                         // [n + 1] pages needed before entry i
+  int* col = start + n + 1;                // [n] pages shared with the parent
+  int* seq = col + n;                      // [n] child
+  int* len = seq + n;                      // [n] its length
+  int* par = len + n;                      // [n]
+  unsigned* seen = reinterpret_cast<unsigned*>(par + n);
+  __shared__ int warp_sums[kPlanThreads / 32];
+  __shared__ int error;
+  pdl_enter();
+  for (int i = threadIdx.x; i < (c.seqs + 31) / 32; i += kPlanThreads) seen[i] = 0;
+  if (threadIdx.x == 0) error = 0;
+  __syncthreads();
+  int pages0 = 0;
+  for (int i0 = 0; i0 < n; i0 += kPlanThreads) {
+    const int i = i0 + threadIdx.x;
+    int need = 0;
+    if (i < n) {
+      const int p = parents[i], s = children[i];
+      par[i] = seq[i] = col[i] = len[i] = 0;
+      if (p < 0 || p >= c.seqs || s < 0 || s >= c.seqs || c.len[s] != 0 ||
+          (atomicOr(&seen[s >> 5], 1u << (s & 31)) >> (s & 31) & 1u)) {
+        atomicOr(&error, ST_BADINDEX);
+      } else {
+        const int plen = c.len[p], b = kept ? base[i] : 0, sp = kept ? span[i] : 0;
+        if (b < 0 || sp < 0 || static_cast<long long>(b) + sp > plen) {
+          atomicOr(&error, ST_BADINDEX);
+        } else {
+          // a child longer than its parent (keep may repeat rows) can pass its table row, or 2^31
+          const long long pages = (static_cast<long long>(plen) - sp + (kept ? k : 0) + c.page - 1) / c.page;
+          if (pages > c.max_pages) {
+            atomicOr(&error, ST_NOPAGES);
+          } else {
+            const ForkShape f = fork_shape(plen, c.page, kept, b, sp, k);
+            par[i] = p;
+            seq[i] = s;
+            col[i] = f.shared;
+            len[i] = f.len;
+            need = static_cast<int>(pages) - f.shared;
+          }
+        }
+      }
+    }
+    int all;
+    const int ps = pages0 + block_scan(need, warp_sums, &all);
+    if (i < n) start[i] = ps;
+    pages0 += all;
+    if (pages0 > c.pages) {                // more than there are: no sum past this one
+      if (threadIdx.x == 0) atomicOr(&error, ST_NOPAGES);
+      pages0 = 0;
+    }
+  }
+  if (threadIdx.x == 0) start[n] = pages0;
+  __syncthreads();
+  for (int i = threadIdx.x; i < n; i += kPlanThreads)       // no child may be a parent
+    if (seen[par[i] >> 5] >> (par[i] & 31) & 1u && error == 0) atomicOr(&error, ST_BADINDEX);
+  __syncthreads();
+  const bool ok = error == 0;
+  const bool enough = ok && take_pages(c, start, col, seq, n, pages0, warp_sums);
+  if (threadIdx.x == 0) {
+    c.status[1] = enough;
+    if (!enough) atomicOr(c.status, ok ? ST_NOPAGES : error);
+  }
+  if (!enough) return;
+  for (int r = threadIdx.x; r < pages0; r += kPlanThreads) {
+    const int i = entry_of(start, n, r);
+    c.refs[c.table[static_cast<long long>(seq[i]) * c.max_pages + col[i] + r - start[i]]] = 1;
+  }
+  for (int i = threadIdx.x >> 5; i < n; i += kPlanThreads / 32) {        // a warp an entry
+    const int32_t* from = c.table + static_cast<long long>(par[i]) * c.max_pages;
+    int32_t* to = c.table + static_cast<long long>(seq[i]) * c.max_pages;
+    for (int j = threadIdx.x & 31; j < col[i]; j += 32) {
+      to[j] = from[j];
+      atomicAdd(&c.refs[from[j]], 1);
+    }
+    if ((threadIdx.x & 31) == 0) c.len[seq[i]] = len[i];
+  }
+}
+
+// The rows of the children's own pages: a unit is one new page of one plane (K or V of a layer).
+constexpr int kCopyThreads = 256;
+__global__ void __launch_bounds__(kCopyThreads) fork_copy_kernel(const map_cache c, const int32_t* __restrict__ parents,
+                                                                 const int32_t* __restrict__ children, int n,
+                                                                 const int32_t* __restrict__ keep, int k,
+                                                                 const int32_t* __restrict__ base,
+                                                                 const int32_t* __restrict__ span) {
+  extern __shared__ int sh[];
+  int* start = sh;                         // [n + 1] new pages before entry i
+  int* from = sh + n + 1;                  // [page] source slot of each row: -1 none, -2 a bad index
+  pdl_enter();
+  if (c.status[1] == 0) return;
+  if (threadIdx.x == 0) {
+    int s = 0;
+    for (int i = 0; i < n; ++i) {
+      start[i] = s;
+      const ForkShape f = fork_shape(c.len[parents[i]], c.page, base != nullptr, base ? base[i] : 0, span ? span[i] : 0, k);
+      s += (f.len + c.page - 1) / c.page - f.shared;
+    }
+    start[n] = s;
+  }
+  __syncthreads();
+  const int planes = 2 * c.layers, vec = c.dh / 8, per_plane = c.heads * c.page * vec;
+  const long long units = static_cast<long long>(start[n]) * planes;
+  for (long long u = blockIdx.x; u < units; u += gridDim.x) {
+    const int r = static_cast<int>(u / planes), plane = static_cast<int>(u % planes), i = entry_of(start, n, r);
+    const int32_t* ptab = c.table + static_cast<long long>(parents[i]) * c.max_pages;
+    const ForkShape f = fork_shape(c.len[parents[i]], c.page, base != nullptr, base ? base[i] : 0, span ? span[i] : 0, k);
+    const int colm = f.shared + r - start[i];
+    __syncthreads();
+    for (int t = threadIdx.x; t < c.page; t += kCopyThreads) {
+      const int j = colm * c.page + t;
+      int src = j;
+      bool bad = false;
+      if (j >= f.base && base) {
+        if (j < f.base + k) {
+          const int x = keep[static_cast<long long>(i) * k + j - f.base];
+          bad = x < 0 || x >= f.span;
+          src = f.base + x;
+        } else {
+          src = j - k + f.span;
+        }
+      }
+      if (j >= f.len) from[t] = -1;
+      else if (bad) { from[t] = -2; if (plane == 0) atomicOr(c.status, ST_BADINDEX); }
+      else from[t] = ptab[src / c.page] * c.page + src % c.page;
+    }
+    __syncthreads();
+    uint4* pool = static_cast<uint4*>(c.pool) + static_cast<long long>(plane) * c.pages * per_plane;
+    uint4* to = pool + static_cast<long long>(c.table[static_cast<long long>(children[i]) * c.max_pages + colm]) * per_plane;
+    for (int v = threadIdx.x; v < per_plane; v += kCopyThreads) {
+      const int x = v % vec, t = v / vec % c.page, h = v / vec / c.page, s = from[t];
+      if (s == -1) continue;
+      to[v] = s < 0 ? make_uint4(0, 0, 0, 0)
+                    : pool[static_cast<long long>(s / c.page) * per_plane + (h * c.page + s % c.page) * vec + x];
+    }
+  }
+}
+
+// A warp a sequence; the first to take its length frees its pages.
+__global__ void __launch_bounds__(256) free_kernel(const map_cache c, const int32_t* __restrict__ seqs, int n) {
+  pdl_enter();
+  const int i = (blockIdx.x * 256 + threadIdx.x) >> 5, lane = threadIdx.x & 31;
+  if (i >= n) return;
+  const int s = seqs[i];
+  if (s < 0 || s >= c.seqs) {
+    if (s != -1 && lane == 0) atomicOr(c.status, ST_BADINDEX);
+    return;
+  }
+  int len = lane == 0 ? atomicExch(&c.len[s], 0) : 0;
+  len = __shfl_sync(0xffffffffu, len, 0);
+  const int32_t* row = c.table + static_cast<long long>(s) * c.max_pages;
+  for (int j = lane; j < (len + c.page - 1) / c.page; j += 32) atomicSub(&c.refs[row[j]], 1);
+}
+
+cudaError_t allow_smem(const void* kern, size_t bytes) {
+  if (bytes <= 48 * 1024) return cudaSuccess;
+  return cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(bytes));
+}
+
+int launch_err(cudaError_t e) {
+  if (e == cudaSuccess) return MAP_OK;
+  cudaGetLastError();
+  return MAP_ECUDA;
+}
+
+}  // namespace
+}  // namespace mapk
+
+using namespace mapk;
+
+extern "C" {
+
+int map_cache_extend(const map_cache* c, const int32_t* seqs, const int32_t* counts, int n, long long rows,
+                     int32_t* slots, void* stream) {
+  const int rc = check_cache(c);
+  if (rc != MAP_OK) return rc;
+  if (n < 0 || rows < 0 || (n > 0 && !seqs) || (rows > 0 && !slots)) return MAP_EINVAL;
+  if (n > kMaxEntries || rows > (1 << 20)) return MAP_EUNSUPPORTED;
+  if (n == 0 && rows == 0) return MAP_OK;
+  const size_t smem = (2 * (n + 1) + 3 * static_cast<size_t>(n) + (c->seqs + 31) / 32) * 4;
+  cudaError_t e = allow_smem(reinterpret_cast<const void*>(extend_kernel), smem);
+  if (e == cudaSuccess)
+    e = launch_k(extend_kernel, dim3(1), dim3(kPlanThreads), smem, static_cast<cudaStream_t>(stream), *c, seqs, counts,
+                 n, static_cast<int>(rows), slots);
+  return launch_err(e);
+}
+
+int map_cache_fork(const map_cache* c, const int32_t* parents, const int32_t* children, int n, const int32_t* keep,
+                   int k, const int32_t* base, const int32_t* span, void* stream) {
+  const int rc = check_cache(c);
+  if (rc != MAP_OK) return rc;
+  if (n < 0 || k < 0) return MAP_EINVAL;
+  if (n == 0) return MAP_OK;
+  if (!parents || !children) return MAP_EINVAL;
+  if ((base == nullptr) != (span == nullptr) || (keep && !base) || (k > 0 && !keep)) return MAP_EINVAL;
+  if (n > kMaxEntries || k > (1 << 24)) return MAP_EUNSUPPORTED;
+  const size_t smem = (n + 1 + 4 * static_cast<size_t>(n) + (c->seqs + 31) / 32) * 4;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  cudaError_t e = allow_smem(reinterpret_cast<const void*>(fork_plan_kernel), smem);
+  if (e == cudaSuccess)
+    e = launch_k(fork_plan_kernel, dim3(1), dim3(kPlanThreads), smem, st, *c, parents, children, n,
+                 base != nullptr ? 1 : 0, k, base, span);
+  if (e == cudaSuccess)
+    e = launch_k(fork_copy_kernel, dim3(1216), dim3(kCopyThreads), (n + 1 + static_cast<size_t>(c->page)) * 4, st, *c,
+                 parents, children, n, keep, k, base, span);
+  return launch_err(e);
+}
+
+int map_cache_free(const map_cache* c, const int32_t* seqs, int n, void* stream) {
+  const int rc = check_cache(c);
+  if (rc != MAP_OK) return rc;
+  if (n < 0 || (n > 0 && !seqs)) return MAP_EINVAL;
+  if (n > kMaxFree) return MAP_EUNSUPPORTED;
+  if (n == 0) return MAP_OK;
+  return launch_err(launch_k(free_kernel, dim3((n + 7) / 8), dim3(256), 0, static_cast<cudaStream_t>(stream), *c, seqs, n));
+}
+
+int map_cache_status(const map_cache* c, void* stream) {
+  const int rc = check_cache(c);
+  if (rc != MAP_OK) return rc;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  int32_t bits = 0;
+  cudaError_t e = cudaMemcpyAsync(&bits, c->status, sizeof(bits), cudaMemcpyDeviceToHost, st);
+  if (e == cudaSuccess) e = cudaStreamSynchronize(st);
+  if (e == cudaSuccess && bits) {
+    e = cudaMemsetAsync(c->status, 0, sizeof(bits), st);
+    if (e == cudaSuccess) e = cudaStreamSynchronize(st);
+  }
+  if (e != cudaSuccess) return launch_err(e);
+  return bits & ST_BADINDEX ? MAP_EINTERNAL : bits & ST_NOPAGES ? MAP_ENOMEM : bits ? MAP_EINTERNAL : MAP_OK;
+}
+
+}  // extern "C"

@@ -176,6 +176,12 @@ cudaError_t launch_assemble(const void* V, const int32_t* idx, const void* T, co
                             int B, int N, int k, int D, int pos_offset, void* seq, int32_t* pos, int* status,
                             cudaStream_t st);
 
+// The same with positions on three axes, pos [3][rows]: grids (host) [B][3] = frames, height, width of each image,
+// t_step (host) [B] or nullptr (1).
+cudaError_t launch_assemble_axes(const void* V, const int32_t* idx, const void* T, const int32_t* lens,
+                                 const int32_t* grids, const int32_t* t_step, int B, int N, int k, int D,
+                                 int pos_offset, void* seq, int32_t* pos, int* status, cudaStream_t st);
+
 // ------------------------------------------------------------------ distillation step (fp32)
 // A bf16 operand of a contraction: element (i, k) = p[i * cols + k] (mn = 0) or p[k * cols + i]
 // (mn = 1), `rows` array rows.  seg > 0: an fp32 operand as three bf16 terms hi, mid, lo at columns

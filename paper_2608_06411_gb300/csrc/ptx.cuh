@@ -14,6 +14,7 @@ namespace mapk {
 constexpr int ST_TIMEOUT  = 1;
 constexpr int ST_INTERNAL = 2;
 constexpr int ST_BADINDEX = 4;
+constexpr int ST_NOPAGES  = 8;
 
 constexpr unsigned long long kWaitLimitNs = 2000000000ull;   // 2 s per wait
 

@@ -206,6 +206,49 @@ __global__ void assemble_kernel(const __grid_constant__ AssembleChunk m, const u
   for (int v = threadIdx.x; v < vec_per_row; v += blockDim.x) d[v] = __ldg(src + v);
 }
 
+struct AxesChunk {
+  int b0, count, N, k, pos_offset;
+  long long rows;                   // of all images: distance of the axes in pos
+  int32_t lens[kAsmImages];
+  int32_t frames[kAsmImages], height[kAsmImages], width[kAsmImages], t_step[kAsmImages];
+  long long text_row[kAsmImages];
+  long long seq_row[kAsmImages];
+};
+
+// The same with positions on three axes: kept token n of a frames x height x width grid at
+// (n / (height width) t_step, n / width % height, n % width), the question after the grid's largest position.
+__global__ void assemble_axes_kernel(const __grid_constant__ AxesChunk m, const uint4* __restrict__ V,
+                                     const int32_t* __restrict__ idx, const uint4* __restrict__ T, int vec_per_row,
+                                     uint4* __restrict__ seq, int32_t* __restrict__ pos, int* status) {
+  pdl_enter();
+  const int i = blockIdx.y, j = blockIdx.x;
+  const long long b = m.b0 + i;
+  if (j >= m.k + m.lens[i]) return;
+  const long long r = m.seq_row[i] + j;
+  const int F = m.frames[i], H = m.height[i], W = m.width[i];
+  const uint4* src;
+  int pt, ph, pw;
+  if (j < m.k) {
+    const int t = __ldg(idx + b * m.k + j);
+    if (t < 0 || t >= F * H * W) {
+      if (threadIdx.x < 3) pos[threadIdx.x * m.rows + r] = -1;
+      if (threadIdx.x == 0) atomicOr(status, ST_BADINDEX);
+      return;
+    }
+    src = V + (b * m.N + t) * vec_per_row;
+    pt = t / (H * W) * m.t_step[i];
+    ph = t / W % H;
+    pw = t % W;
+  } else {
+    src = T + (m.text_row[i] + (j - m.k)) * vec_per_row;
+    pt = ph = pw = max((F - 1) * m.t_step[i] + 1, max(H, W)) + (j - m.k);
+  }
+  if (threadIdx.x < 3)
+    pos[threadIdx.x * m.rows + r] = (threadIdx.x == 0 ? pt : threadIdx.x == 1 ? ph : pw) + m.pos_offset;
+  uint4* d = seq + r * vec_per_row;
+  for (int v = threadIdx.x; v < vec_per_row; v += blockDim.x) d[v] = __ldg(src + v);
+}
+
 __global__ void flags_to_host_kernel(const int32_t* a, const int* b, volatile int32_t* ah, volatile int* bh) {
   pdl_enter();
   *ah = *a;
@@ -269,6 +312,43 @@ cudaError_t launch_assemble(const void* V, const int32_t* idx, const void* T, co
     }
     if (max_rows == 0) continue;
     const cudaError_t e = launch_k(assemble_kernel, dim3(max_rows, m.count), dim3(128), 0, st, m,
+                                   static_cast<const uint4*>(V), idx, static_cast<const uint4*>(T), D / 8,
+                                   static_cast<uint4*>(seq), pos, status);
+    if (e != cudaSuccess) return e;
+  }
+  return cudaSuccess;
+}
+
+cudaError_t launch_assemble_axes(const void* V, const int32_t* idx, const void* T, const int32_t* lens,
+                                 const int32_t* grids, const int32_t* t_step, int B, int N, int k, int D,
+                                 int pos_offset, void* seq, int32_t* pos, int* status, cudaStream_t st) {
+  if (D % 8 != 0) return cudaErrorInvalidValue;
+  long long trow = 0, srow = 0, rows = 0;
+  for (int b = 0; b < B; ++b) rows += k + lens[b];
+  for (int b0 = 0; b0 < B; b0 += kAsmImages) {
+    AxesChunk m;
+    m.b0 = b0;
+    m.count = B - b0 < kAsmImages ? B - b0 : kAsmImages;
+    m.N = N;
+    m.k = k;
+    m.pos_offset = pos_offset;
+    m.rows = rows;
+    int max_rows = 0;
+    for (int i = 0; i < m.count; ++i) {
+      const int b = b0 + i;
+      m.lens[i] = lens[b];
+      m.frames[i] = grids[3 * b];
+      m.height[i] = grids[3 * b + 1];
+      m.width[i] = grids[3 * b + 2];
+      m.t_step[i] = t_step ? t_step[b] : 1;
+      m.text_row[i] = trow;
+      m.seq_row[i] = srow;
+      trow += lens[b];
+      srow += k + lens[b];
+      max_rows = std::max(max_rows, k + lens[b]);
+    }
+    if (max_rows == 0) continue;
+    const cudaError_t e = launch_k(assemble_axes_kernel, dim3(max_rows, m.count), dim3(128), 0, st, m,
                                    static_cast<const uint4*>(V), idx, static_cast<const uint4*>(T), D / 8,
                                    static_cast<uint4*>(seq), pos, status);
     if (e != cudaSuccess) return e;

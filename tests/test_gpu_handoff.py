@@ -1,0 +1,728 @@
+"""The language-model hand-off on the GPU against the 64-bit models of oracle/handoff_oracle.py.
+
+Tolerances.  u = eps / 2 of the output's type is its one rounding.  Rotation: z = x r w carries the error of r (rsqrtf
+2 ulp, a sum of dh squares in at most 16 + 8 steps, halved by the root, the division and eps: 2 + 12 + 2) and of two
+products; cos and sin carry their argument's rounding, pi 2^-24, and 2 ulp; the turn adds 3 roundings: under 32 * 2^-24
+of |z_a| + |z_b|.  fp16 results below 2^-14 are rounded to multiples of 2^-24.
+"""
+import numpy as np
+import pytest
+import torch
+
+from oracle import handoff_oracle as H
+from oracle import map_oracle as O
+
+pytestmark = pytest.mark.gpu
+
+DEV = "cuda"
+TYPES = {"bf16": torch.bfloat16, "f16": torch.float16, "f32": torch.float32}
+E24 = 2.0 ** -24
+
+
+@pytest.fixture(scope="module")
+def mb():
+    if not torch.cuda.is_available():
+        pytest.skip("needs a GPU")
+    from paper_2608_06411_gb300 import binding
+    return binding
+
+
+def f64(t):
+    return None if t is None else t.detach().cpu().double().numpy()
+
+
+def half_step(typ):
+    return torch.finfo(typ).eps / 2
+
+
+def tiny(typ):
+    return 2.0 ** -25 if typ == torch.float16 else 1e-37
+
+
+def gen(seed):
+    return torch.Generator(device=DEV).manual_seed(seed)
+
+
+def randn(g, *shape, typ):
+    return torch.randn(*shape, generator=g, device=DEV, dtype=torch.float32).to(typ)
+
+
+def ints(x):
+    return torch.tensor(x, dtype=torch.int32, device=DEV)
+
+
+# ----------------------------------------------------------------------------- layouts
+
+def place(x, layout):
+    """A tensor of x's values laid out as `layout` says, and the storage it is a view of."""
+    rows, heads, dh = x.shape
+    if layout == "dense":
+        base = x.clone()
+        return base, base
+    if layout == "packed":                       # between other columns of a projection's row
+        base = torch.full((rows, (heads + 3) * dh), 7.0, dtype=x.dtype, device=x.device)
+        view = base[:, 2 * dh: (2 + heads) * dh].unflatten(1, (heads, dh))
+    elif layout == "heads_first":
+        base = torch.full((heads, rows, dh), 7.0, dtype=x.dtype, device=x.device)
+        view = base.transpose(0, 1)
+    else:                                        # "odd": odd offset and strides
+        base = torch.full((rows * (heads * (dh + 3) + 5) + 1,), 7.0, dtype=x.dtype, device=x.device)
+        view = base[1:].as_strided((rows, heads, dh), (heads * (dh + 3) + 5, dh + 3, 1), 1)
+    view.copy_(x)
+    return view, base
+
+
+ROTATIONS = [
+    # type, rows, hq, hk, dh, rot, axes, adjacent, norm, layout, far
+    ("bf16", 1, 28, 4, 128, 128, 3, False, True, "packed", 5000),
+    ("bf16", 37, 8, 2, 128, 128, 3, True, True, "dense", 5000),
+    ("f16", 130, 4, 4, 64, 32, 1, False, True, "heads_first", 5000),
+    ("f32", 65, 5, 1, 80, 80, 2, False, True, "packed", 5000),
+    ("f32", 19, 16, 16, 72, 72, 2, True, False, "dense", 60),
+    ("f32", 19, 16, 3, 72, 72, 2, False, True, "dense", 60),
+    ("bf16", 33, 3, 3, 96, 96, 4, False, False, "odd", 5000),
+    ("bf16", 9, 1, 1, 256, 256, 3, False, True, "dense", 2 ** 31),
+    ("f32", 9, 2, 1, 256, 128, 3, True, True, "heads_first", 2 ** 31),
+    ("f16", 21, 2, 2, 37, 36, 2, False, True, "dense", 5000),
+    ("bf16", 21, 2, 2, 37, 2, 2, True, True, "odd", 5000),
+    ("f32", 7, 3, 2, 1, 0, 1, False, True, "dense", 5000),
+    ("f16", 7, 3, 2, 20, 20, 3, False, True, "odd", 5000),
+    ("bf16", 7, 3, 2, 20, 12, 3, True, True, "packed", 5000),
+    ("bf16", 7, 3, 2, 48, 24, 3, False, False, "packed", 5000),
+    ("f16", 700, 7, 1, 192, 64, 2, False, True, "packed", 100000),
+    ("bf16", 2500, 32, 32, 128, 128, 3, False, True, "packed", 8192),
+    ("f32", 1027, 4, 4, 128, 96, 2, False, False, "packed", 8192),
+    ("f32", 3, 1, 2, 254, 254, 1, False, True, "dense", 8192),
+]
+IDS = ["-".join(str(v) for v in c) for c in ROTATIONS]
+
+
+def rotation(mb, case, seed=1):
+    typ, rows, hq, hk, dh, rot, axes, adjacent, norm, layout, far = case
+    typ, g = TYPES[typ], gen(seed)
+    q, k = randn(g, rows, hq, dh, typ=typ) * 2, randn(g, rows, hk, dh, typ=typ) * 2
+    wq, wk = ((1 + 0.3 * torch.randn(dh, generator=g, device=DEV)).to(typ) for _ in range(2)) if norm else (None, None)
+    pos = torch.randint(-far, far, (axes, rows), generator=g, device=DEV, dtype=torch.int64).to(torch.int32)
+    half = rot // 2
+    inv = [10000.0 ** (-2.0 * i / max(rot, 1)) for i in range(half)]
+    ax = [i % axes if adjacent else i * axes // max(half, 1) for i in range(half)]
+    plan = mb.Rope(dh, inv, axis=ax, n_axes=axes, adjacent=adjacent, eps=1e-6)
+    return typ, q, k, wq, wk, pos, inv, ax, plan
+
+
+def check_rotated(got, x, w, pos, inv, ax, adjacent, typ):
+    y, z = H.rotate(f64(x), f64(w), pos.cpu().numpy(), inv, ax, adjacent, 1e-6)
+    size = np.abs(z)
+    a, b = H.pairs_of(2 * len(inv), adjacent)
+    both = size[..., a] + size[..., b]
+    size[..., a], size[..., b] = both, both
+    off = np.abs(f64(got) - y)
+    tol = half_step(typ) * np.abs(y) * 1.001 + 32 * E24 * size + tiny(typ)
+    assert (off <= tol).all(), float((off / tol).max())
+
+
+@pytest.mark.parametrize("case", ROTATIONS, ids=IDS)
+def test_rotate_matches_the_formula(mb, case):
+    typ, q, k, wq, wk, pos, inv, ax, plan = rotation(mb, case)
+    layout, adjacent = case[9], case[7]
+    (qv, _), (kv, _) = place(q, layout), place(k, layout)
+    (qo, qbase), (ko, kbase) = place(torch.full_like(q, 7.0), layout), place(torch.full_like(k, 7.0), layout)
+    plan.rotate(qv, kv, pos, wq, wk, qo, ko)
+    check_rotated(qo, q, wq, pos, inv, ax, adjacent, typ)
+    check_rotated(ko, k, wk, pos, inv, ax, adjacent, typ)
+    got_q, got_k = qo.clone(), ko.clone()
+    qo.fill_(7.0), ko.fill_(7.0)                     # nothing but the heads was written
+    assert bool((qbase == 7.0).all()) and bool((kbase == 7.0).all())
+    assert torch.equal(qv, q) and torch.equal(kv, k)
+    plan.rotate(qv, kv, pos, wq, wk, qv, kv)         # in place: the same
+    assert torch.equal(qv, got_q) and torch.equal(kv, got_k)
+    only_q, none = plan.rotate(q, None, pos, wq)     # one side alone, dense
+    assert none is None
+    check_rotated(only_q, q, wq, pos, inv, ax, adjacent, typ)
+    none, only_k = plan.rotate(None, k, pos, None, wk)
+    assert none is None
+    check_rotated(only_k, k, wk, pos, inv, ax, adjacent, typ)
+
+
+def test_rotate_edges(mb):
+    inv = [0.5, 0.25]
+    plan = mb.Rope(8, inv, axis=[0, 1], n_axes=2)
+    pos = ints([[2 ** 31 - 1, -2 ** 31, 0], [5, 6, 7]])
+    x = torch.randn(3, 2, 8, device=DEV)
+    x[1, 0, 3] = float("nan")
+    x[2, 1] = float("inf")
+    y, _ = plan.rotate(x, None, pos, torch.ones(8, device=DEV))
+    assert bool(torch.isnan(y[1, 0]).all()) and bool(torch.isnan(y[2, 1]).all())      # a bad head spoils itself alone
+    keep = torch.ones(3, 2, dtype=torch.bool)
+    keep[1, 0] = keep[2, 1] = False
+    assert bool(torch.isfinite(y[keep.to(DEV)]).all())
+    y, z = H.rotate(f64(x[:1]), None, pos.cpu().numpy()[:, :1], inv, [0, 1], False, 0.0)
+    got, _ = plan.rotate(x[:1], None, pos[:, :1].contiguous())
+    assert np.abs(f64(got) - y).max() < 1e-5
+    for rows in (0,):
+        q, k = plan.rotate(x[:rows], x[:rows], pos[:, :rows].contiguous())
+        assert q.shape == (0, 2, 8) and k.shape == (0, 2, 8)
+    # heads broadcast over rows are a valid input
+    one = x[:1].expand(3, 2, 8)
+    got, _ = plan.rotate(one, None, pos)
+    want, _ = plan.rotate(one.contiguous(), None, pos)
+    assert torch.equal(got, want)
+    with pytest.raises(mb.MapError):
+        plan.rotate(x, None, pos, q_out=torch.empty(1, 2, 8, device=DEV).expand(3, 2, 8))
+    with pytest.raises(ValueError):
+        plan.rotate(x, None, pos[:1])
+    with pytest.raises(ValueError):
+        plan.rotate(x, x.half(), pos)
+    with pytest.raises(ValueError):
+        plan.rotate(x.transpose(1, 2), None, pos)
+    with pytest.raises(ValueError):
+        plan.rotate(x.double(), None, pos)
+
+
+def check_grad(dx, dw, dy, x, w, pos, inv, ax, adjacent, typ):
+    """dx: r (g w - n mean(g w n)); errors as above, and of the mean: dh products in 24 steps and the roundings of both
+    factors, 40 steps.  dw: a term's 24 steps (g 20 and n 3), and the additions of its sum, each at most 2^-24 of the sum
+    of magnitudes: rows * heads / (blocks * heads in flight) in a thread, under 64, 32 heads of a block and 608 blocks."""
+    x64, w64, p = f64(x), f64(w), pos.cpu().numpy()
+    want, wdw = H.rotate_grad(f64(dy), x64, w64, p, inv, ax, adjacent, 1e-6)
+    g = np.abs(H.rotate(f64(dy), None, p, -np.asarray(inv), ax, adjacent, 0.0)[0])
+    size = np.abs(f64(dy))
+    a, b = H.pairs_of(2 * len(inv), adjacent)
+    both = size[..., a] + size[..., b]
+    size[..., a], size[..., b] = both, both                      # bounds g
+    if w is not None:
+        r = 1 / np.sqrt((x64 ** 2).mean(-1, keepdims=True) + 1e-6)
+        n = np.abs(x64 * r)
+        gsize = size
+        size = r * (gsize * np.abs(w64) + n * (gsize * np.abs(w64) * n).mean(-1, keepdims=True))
+    tol = half_step(typ) * np.abs(want) * 1.001 + 64 * E24 * size + tiny(typ)
+    off = np.abs(f64(dx) - want)
+    assert (off <= tol).all(), float((off / tol).max())
+    if w is not None:
+        tol = (24 + 64 + 32 + 608) * E24 * (gsize * n).sum((0, 1)) + 1e-37
+        off = np.abs(f64(dw) - wdw)
+        assert (off <= tol).all(), float((off / tol).max())
+    else:
+        assert dw is None
+
+
+@pytest.mark.parametrize("case", ROTATIONS, ids=IDS)
+def test_rotate_grad_matches_the_formula(mb, case):
+    typ, q, k, wq, wk, pos, inv, ax, plan = rotation(mb, case)
+    layout, adjacent = case[9], case[7]
+    g = gen(9)
+    dq, dk = randn(g, *q.shape, typ=typ), randn(g, *k.shape, typ=typ)
+    (qv, _), (kv, _), (dqv, _), (dkv, _) = (place(t, layout) for t in (q, k, dq, dk))
+    (qo, qbase), (ko, kbase) = place(torch.full_like(q, 7.0), layout), place(torch.full_like(k, 7.0), layout)
+    _, _, dwq, dwk = plan.grad(dqv, dkv, pos, qv, kv, wq, wk, dq=qo, dk=ko)
+    check_grad(qo, dwq, dq, q, wq, pos, inv, ax, adjacent, typ)
+    check_grad(ko, dwk, dk, k, wk, pos, inv, ax, adjacent, typ)
+    a, b = qo.clone(), ko.clone()
+    again = plan.grad(dqv, dkv, pos, qv, kv, wq, wk, dq=qo, dk=ko)   # the same again, sums too (fixed order)
+    assert torch.equal(a, qo) and torch.equal(b, ko)
+    assert wq is None or torch.equal(dwq, again[2]) and torch.equal(dwk, again[3])
+    dense = plan.grad(dq, dk, pos, q, k, wq, wk)
+    check_grad(dense[0], dense[2], dq, q, wq, pos, inv, ax, adjacent, typ)
+    check_grad(dense[1], dense[3], dk, k, wk, pos, inv, ax, adjacent, typ)
+    qo.fill_(7.0), ko.fill_(7.0)
+    assert bool((qbase == 7.0).all()) and bool((kbase == 7.0).all())
+    plan.grad(dqv, dkv, pos, qv, kv, wq, wk, dq=dqv, dk=dkv)         # in place
+    assert torch.equal(dqv, a) and torch.equal(dkv, b)
+
+
+def test_rotate_grad_against_differences(mb):
+    """<grad, d> = (loss(x + h d) - loss(x - h d)) / 2h in fp32: the difference is off by h^2 / 6 of the third derivative
+    (of order 10 for heads of unit norm: 2e-4 at h = 1e-2 times the sum's size) and by fp32 roundings over h (a sum of
+    1e3 terms of size 1: 1e3 * 2^-24 * 32 / 1e-2 = 0.2 of a gradient of size 30)."""
+    rows, heads, dh = 5, 3, 64
+    inv = [10000.0 ** (-2.0 * i / dh) for i in range(dh // 2)]
+    plan = mb.Rope(dh, inv, axis=[i % 3 for i in range(dh // 2)])
+    g = gen(3)
+    x, dy, d, w = (randn(g, rows, heads, dh, typ=torch.float32) for _ in range(4))
+    w = 1 + 0.2 * w[0, 0]
+    pos = torch.randint(0, 500, (3, rows), generator=g, device=DEV, dtype=torch.int32)
+    dx, _, dw, _ = plan.grad(dy, None, pos, x, None, w)
+    h = 1e-2
+
+    def loss(x, w):
+        return float((plan.rotate(x, None, pos, w)[0].double() * dy.double()).sum())
+
+    num = (loss(x + h * d, w) - loss(x - h * d, w)) / (2 * h)
+    assert abs(num - float((dx.double() * d.double()).sum())) < 0.3
+    e = d[0, 0]
+    num = (loss(x, w + h * e) - loss(x, w - h * e)) / (2 * h)
+    assert abs(num - float((dw.double() * e.double()).sum())) < 0.3
+
+
+def test_rotate_grad_of_no_rows_and_one_side(mb):
+    plan = mb.Rope(64, [1.0] * 32)
+    z = torch.zeros(0, 2, 64, device=DEV)
+    w = torch.ones(64, device=DEV)
+    pos = torch.zeros(1, 0, dtype=torch.int32, device=DEV)
+    dq, dk, dwq, dwk = plan.grad(z, None, pos, z, None, w, dwq=torch.full((64,), 3.0, device=DEV))
+    assert dk is None and dwk is None and dq.shape == z.shape and bool((dwq == 0).all())
+
+
+# ----------------------------------------------------------------------------- positions
+
+@pytest.mark.parametrize("grids,lens,k,step,off,N", [
+    ([(1, 24, 24)], [32], 32, None, 0, 576),
+    ([(1, 24, 24), (4, 6, 5), (3, 1, 40), (1, 1, 33)], [5, 0, 77, 1], 33, [1, 3, 0, 9], 35, 600),
+    ([(2, 3, 4)] * 3, [2, 0, 1], 0, [2, 2, 2], -3, 24),
+    ([(1, 2, 3)], [0], 6, None, 0, 6),
+    ([(2, 2, 2)] * 700, [i % 3 for i in range(700)], 3, list(range(700)), 1, 8),
+])
+def test_assemble_axes(mb, grids, lens, k, step, off, N):
+    D, B = 512, len(grids)
+    ctx = handoff_context(mb, D)
+    rng = np.random.default_rng(3)
+    vis = rng.integers(0, 2 ** 16, size=(B, N, D), dtype=np.uint16)
+    text = rng.integers(0, 2 ** 16, size=(max(1, sum(lens)), D), dtype=np.uint16)
+    keep = np.stack([np.sort(rng.choice(t * h * w, k, replace=False)) for t, h, w in grids]).astype(np.int32)
+    seq, pos = ctx.assemble_axes(torch.from_numpy(vis.view(np.int16)).to(DEV), torch.from_numpy(keep).to(DEV),
+                                 torch.from_numpy(text.view(np.int16)).to(DEV), lens, grids, step, off)
+    ctx.check()
+    ref, _ = O.assemble(vis, keep, text[: sum(lens)], lens)
+    np.testing.assert_array_equal(seq.cpu().numpy().view(np.uint16), ref)
+    np.testing.assert_array_equal(pos.cpu().numpy(), H.axis_positions(keep, lens, grids, step, off))
+
+
+def test_assemble_axes_reports_a_bad_index(mb):
+    ctx = handoff_context(mb, 512)
+    vis, text = torch.zeros((2, 9, 512), dtype=torch.int16, device=DEV), torch.ones((2, 512), dtype=torch.int16, device=DEV)
+    seq = torch.full((6, 512), 5, dtype=torch.int16, device=DEV)
+    _, pos = ctx.assemble_axes(vis, ints([[0, 8], [6, -1]]), text, [1, 1], [(2, 2, 2), (1, 3, 3)], seq=seq)
+    assert ctx.status() == mb.MAP_EINTERNAL and ctx.status() == mb.MAP_OK
+    assert pos.cpu().tolist() == [[0, -1, 2, 0, -1, 3], [0, -1, 2, 2, -1, 3], [0, -1, 2, 0, -1, 3]]
+    assert seq[:, 0].cpu().tolist() == [0, 5, 1, 0, 5, 1]
+    with pytest.raises(ValueError):
+        ctx.assemble_axes(vis, ints([[0, 8], [6, -1]]), text, [1, 1], [(2, 2, 2)])
+
+
+_CONTEXTS = {}
+
+
+def handoff_context(mb, D):
+    if D not in _CONTEXTS:
+        shapes = {"wT1": (256, D), "bT1": (256,), "wT2": (256, 256), "bT2": (256,), "wQ": (64, 256)}
+        shapes.update({n.replace("T", "V").replace("Q", "K"): s for n, s in shapes.items()})
+        _CONTEXTS[D] = mb.Context({n: torch.zeros(s, dtype=torch.int16, device=DEV) for n, s in shapes.items()}, D, 256, 64)
+    return _CONTEXTS[D]
+
+
+# ----------------------------------------------------------------------------- pages
+
+def rows_of(pool, slots):
+    """[layers, 2, rows, heads, dh] at the given slots."""
+    page = pool.shape[4]
+    s = torch.tensor(slots, dtype=torch.int64, device=pool.device)
+    return pool[:, :, s // page, :, s % page].permute(1, 2, 0, 3, 4) if len(slots) else pool[:, :, :0, 0, 0]
+
+
+def same_state(cache, model):
+    assert cache.length.cpu().tolist() == model.length
+    assert cache.refs.cpu().tolist() == model.refs
+    table = cache.table.cpu().tolist()
+    for s, pages in enumerate(model.table):
+        assert table[s][: len(pages)] == pages, s
+
+
+@pytest.mark.parametrize("page,dh,hk,layers,seed", [(16, 128, 2, 2, 0), (1, 8, 1, 1, 1), (5, 40, 3, 2, 2), (64, 64, 8, 1, 3),
+                                                    (1024, 16, 1, 1, 4), (7, 256, 1, 3, 5)])
+def test_page_calls_follow_the_model(mb, page, dh, hk, layers, seed):
+    """A long run of extensions, appended rows, forks, pruned forks and frees, good and refused ones."""
+    import random
+    r = random.Random(seed)
+    pages, seqs, max_pages = r.randint(20, 45), 9, 8
+    cache = mb.Cache.empty(layers, pages, hk, page, dh, seqs, max_pages, torch.float16)
+    cache.pool.normal_(generator=gen(seed))
+    model = H.Pages(pages, page, seqs, max_pages)
+    plan = mb.Rope(dh, [0.3, 0.1], n_axes=1)
+    refused = copied = 0
+    for step in range(120):
+        op = r.choice(["extend", "extend", "fork", "prune", "free"])
+        before = cache.pool.clone()
+        if op == "extend":
+            n = r.randint(0, 4)
+            who = [r.choice([-1] + list(range(seqs))) if r.random() < 0.97 else r.choice([seqs, -2]) for _ in range(n)]
+            counts = [r.choice([0, 1, 1, page, r.randint(0, 2 * page + 1)]) if r.random() < 0.97 else -1 for _ in range(n)]
+            rows = max(0, sum(c for c, w in zip(counts, who) if w != -1)) + r.choice([0, 0, 3])
+            rows = max(0, rows - (1 if r.random() < 0.05 else 0))
+            if r.random() < 0.3:
+                counts, rows = None, n + r.choice([0, 0, 2, -1 if n else 0])
+            want = model.extend(who, counts, rows)
+            got = cache.extend(ints(who), None if counts is None else ints(counts), rows=rows)
+            assert got.cpu().tolist() == (want if want is not None else [-1] * rows)
+            named = [w for w in who if w != -1]
+            ok = want is not None
+            if ok and rows and r.random() < 0.5:
+                layer = r.randrange(layers)
+                k, v, q = (randn(gen(step), rows, h, dh, typ=torch.float16) for h in (hk, hk, 2))
+                pos = torch.arange(rows, dtype=torch.int32, device=DEV)[None]
+                qo = torch.full_like(q, 3.0)
+                plan.append(q, k, v, pos, cache, layer, got, q_out=qo)
+                rq, rk = plan.rotate(q, k, pos)
+                real = [i for i, s in enumerate(want) if s >= 0]
+                pad = [i for i, s in enumerate(want) if s < 0]
+                assert torch.equal(qo[real], rq[real]) and bool((qo[pad] == 3.0).all())
+                at = torch.tensor([want[i] for i in real], dtype=torch.int64, device=DEV)
+                before[layer, 0][at // page, :, at % page] = rk[real]
+                before[layer, 1][at // page, :, at % page] = v[real]
+        elif op in ("fork", "prune"):
+            n = r.randint(0, 3)
+            par = [r.randrange(seqs) if r.random() < 0.98 else seqs + 3 for _ in range(n)]
+            empty = [s for s in range(seqs) if model.length[s] == 0]
+            chi = [r.choice(empty) if empty and r.random() < 0.97 else r.randrange(seqs) for _ in range(n)]
+            keep = base = span = None
+            k = r.choice([0, 1, 2, page + 3])
+            if op == "prune":
+                base, span = [], []
+                for p in par:
+                    have = model.length[p] if p < seqs else 4
+                    b = r.randint(0, have)
+                    base.append(b if r.random() < 0.98 else -1)
+                    span.append(r.randint(0, have - b) + (1 if r.random() < 0.02 else 0))
+                keep = [[r.randint(0, max(0, s - 1)) if r.random() < 0.97 else s + 2 for _ in range(k)] for s in span]
+            dev = [None if keep is None else ints(keep).reshape(n, k), *(None if x is None else ints(x) for x in (base, span))]
+            want = model.fork(par, chi, keep, base, span)
+            cache.fork(ints(par), ints(chi), *dev)
+            ok = want is not None
+            bad_index = ok and any(s < 0 for _, s in want)
+            if ok:
+                copied += len(want)
+                for to, at in want:
+                    src = 0.0 if at < 0 else before[:, :, at // page, :, at % page].clone()
+                    before[:, :, to // page, :, to % page] = src
+            if bad_index:
+                assert cache.status() == mb.MAP_EINTERNAL
+        else:
+            who = [r.choice([-1] + list(range(seqs))) for _ in range(r.randint(0, 3))]
+            model.free(who)
+            cache.free(ints(who))
+            ok = True
+        if not ok:
+            refused += 1
+            assert cache.status() in (mb.MAP_ENOMEM, mb.MAP_EINTERNAL)
+        assert cache.status() == mb.MAP_OK
+        same_state(cache, model)
+        assert torch.equal(cache.pool, before), (step, op)
+    assert refused > 5 and copied > 5
+
+
+def test_many_entries_and_a_large_pool(mb):
+    """4096 sequences extended in one call, over pages whose free ones lie behind used ones; freed in one call."""
+    n, page = 4096, 4
+    cache = mb.Cache.empty(1, 40000, 1, page, 8, n + 2, 4)
+    model = H.Pages(40000, page, n + 2, 4)
+    first = [n, n + 1]
+    assert cache.extend(ints(first), ints([16, 9]), rows=25).cpu().tolist() == model.extend(first, [16, 9], 25)
+    counts = [(i * 7) % 14 for i in range(n)]
+    got = cache.extend(ints(list(range(n))), ints(counts), rows=sum(counts) + 5).cpu().tolist()
+    assert got == model.extend(list(range(n)), counts, sum(counts) + 5)
+    same_state(cache, model)
+    cache.free(ints(list(range(0, n, 2)) * 2 + [-1]))
+    model.free(range(0, n, 2))
+    got = cache.extend(ints(list(range(0, n, 2)))).cpu().tolist()
+    assert got == model.extend(list(range(0, n, 2)), [1] * (n // 2), n // 2)
+    same_state(cache, model)
+    cache.check()
+
+
+def test_append_reports_bad_slots_and_skips_them(mb):
+    cache = mb.Cache.empty(1, 2, 1, 4, 8, 2, 2)
+    cache.pool.fill_(5.0)
+    plan = mb.Rope(8, [], n_axes=1)
+    x = torch.arange(5 * 8, device=DEV).reshape(5, 1, 8).to(torch.bfloat16)
+    qo = torch.full_like(x, 9.0)
+    pos = torch.zeros(1, 5, dtype=torch.int32, device=DEV)
+    plan.append(x, x, x + 1, pos, cache, 0, ints([3, -1, 8, -2, 4]), q_out=qo)
+    assert cache.status() == mb.MAP_EINTERNAL and cache.status() == mb.MAP_OK
+    assert torch.equal(qo[[0, 4]], x[[0, 4]]) and bool((qo[1:4] == 9).all())
+    assert torch.equal(cache.pool[0, 0, 0, 0, 3], x[0, 0]) and torch.equal(cache.pool[0, 1, 1, 0, 0], x[4, 0] + 1)
+    assert int((cache.pool != 5).any(-1).sum()) == 4
+    plan.append(None, x, x, pos, cache, 0, ints([0, 1, 2, 3, 4]))           # keys and values alone
+    assert torch.equal(cache.pool[0, 1, 0, 0], x[:4, 0])
+
+
+# ----------------------------------------------------------------------------- attention
+
+def filled(mb, typ, dh, hk, page, lens, seed, layers=1, spare=2, extra_seqs=0):
+    """A cache whose sequences have the given lengths, pages at random places, NaN wherever no row is."""
+    g = gen(seed)
+    used = [-(-t // page) for t in lens]
+    pages, max_pages = sum(used) + spare, max([1] + used)
+    cache = mb.Cache.empty(layers, pages, hk, page, dh, len(lens) + extra_seqs, max_pages, typ)
+    cache.pool.fill_(float("nan"))
+    order = torch.randperm(pages, generator=g, device=DEV).to(torch.int32)
+    at = 0
+    for s, (n, t) in enumerate(zip(used, lens)):
+        mine = order[at: at + n]
+        cache.table[s, :n] = mine
+        cache.refs[mine.long()] = 1
+        at += n
+        if t:
+            i = torch.arange(t, device=DEV)
+            for l in range(layers):
+                for kv in (0, 1):
+                    cache.pool[l, kv][mine[i // page].long(), :, i % page] = randn(g, t, hk, dh, typ=typ)
+    cache.length[: len(lens)] = ints(lens)
+    return cache
+
+
+def check_attend(got, q, cache, layer, seqs, scale, typ):
+    """Scores: tensor-core sums lose up to an ulp (2^-23) of their magnitude per 16 terms, plus the product with scale:
+    dz = (dh / 16 + 3) 2^-23 of sum |q k| scale; exp turns that into a relative error of p, twice (p and their sum),
+    with 2^-21 for exp2 and its argument (|z| up to 40: 40 * 2^-24).  p as two halves of the cache's type keeps 2^-16;
+    the sum over n rows loses an ulp per 16, and a few joins of parts."""
+    table, lens = cache.table.cpu().tolist(), cache.length.cpu().tolist()
+    page = cache.page
+    for i, s in enumerate(seqs):
+        if s < 0:
+            continue
+        slots = [table[s][t // page] * page + t % page for t in range(lens[s])]
+        k, v = (f64(rows_of(cache.pool[layer: layer + 1], slots))[0, j] for j in (0, 1)) if slots else \
+            (np.zeros((0, cache.heads, cache.dh)),) * 2
+        want, mag, dz = H.attend(f64(q[i]), k, v, scale)
+        e = 2 * (cache.dh / 16 + 3) * 2.0 ** -23 * dz + 2.0 ** -19 + 2.0 ** -16 + (len(slots) / 16 + 64) * 2.0 ** -23
+        tol = half_step(typ) * np.abs(want) * 1.001 + e * mag + tiny(typ)
+        off = np.abs(f64(got[i]) - want)
+        assert (off <= tol).all(), (i, float((off / np.maximum(tol, 1e-30)).max()))
+
+
+ATTENDS = [
+    # type, dh, hk, group, page, lens
+    ("bf16", 128, 2, 4, 16, [0, 1, 15, 16, 17, 63, 64, 65, 300]),
+    ("f16", 64, 1, 1, 16, [5, 0, 1000]),
+    ("bf16", 80, 3, 2, 8, [33, 129, 2]),
+    ("f16", 96, 2, 8, 32, [200, 31]),
+    ("bf16", 192, 1, 3, 64, [1, 700]),
+    ("f16", 256, 2, 2, 16, [129, 64, 2000]),
+    ("bf16", 128, 1, 16, 5, [77, 13, 0]),
+    ("bf16", 64, 1, 40, 1, [50, 3]),
+    ("f16", 128, 4, 7, 48, [9000]),
+    ("bf16", 128, 8, 4, 16, [200 + 37 * i for i in range(40)]),
+    ("bf16", 64, 2, 17, 1024, [1500, 1023, 1024, 1025]),
+    ("f16", 128, 1, 1, 3, [2, 1] * 150),
+]
+
+
+@pytest.mark.parametrize("case", ATTENDS, ids=["-".join(str(v) for v in c[:5]) for c in ATTENDS])
+def test_attend_matches_the_formula(mb, case):
+    typ, dh, hk, group, page, lens = case
+    typ = TYPES[typ]
+    cache = filled(mb, typ, dh, hk, page, lens, 5, layers=2)
+    seqs = list(range(len(lens) - 1, -1, -1)) + [-1, 0]
+    q = randn(gen(6), len(seqs), hk * group, dh, typ=typ) * 1.5
+    out = torch.full_like(q, 3.0)
+    cache.attend(q, ints(seqs), 1, out=out)
+    check_attend(out, q, cache, 1, seqs, dh ** -0.5, typ)
+    assert bool((out[len(lens)] == 3.0).all())                       # the padding row
+    for i, s in enumerate(seqs):
+        assert s < 0 or lens[s] or bool((out[i] == 0).all())         # an empty sequence
+    assert torch.equal(cache.attend(q, ints(seqs), 1, out=torch.full_like(q, 3.0)), out)      # repeatable
+    (qv, _), (ov, base) = place(q, "packed"), place(torch.full_like(q, 7.0), "packed")
+    cache.attend(qv, ints(seqs), 1, out=ov)
+    ok = [i for i, s in enumerate(seqs) if s >= 0]
+    assert torch.equal(ov[ok], out[ok])
+    ov.fill_(7.0)
+    assert bool((base == 7.0).all())
+    cache.check()
+
+
+def test_attend_values_at_the_edges(mb):
+    cache = filled(mb, torch.bfloat16, 64, 1, 16, [100, 3, 40], 2)
+    q = randn(gen(1), 3, 2, 64, typ=torch.bfloat16)
+    out = cache.attend(q, ints([0, 1, 2]), 0, scale=0.0)             # equal weights: the mean
+    check_attend(out, q, cache, 0, [0, 1, 2], 0.0, torch.bfloat16)
+    out = cache.attend(q, ints([0, 1, 2]), 0, scale=-0.125)
+    check_attend(out, q, cache, 0, [0, 1, 2], -0.125, torch.bfloat16)
+    out = cache.attend(q * 1e4, ints([0, 1, 2]), 0)                  # one row takes all
+    assert bool(torch.isfinite(out).all())
+    cache.pool[0, 1][cache.table[1, 0].long(), 0, 1] = float("inf")  # an infinite value: sequence 1 alone has it
+    out = cache.attend(q, ints([0, 1, 2]), 0)
+    assert bool(torch.isinf(out[1]).all()) and bool(torch.isfinite(out[[0, 2]]).all())
+    cache.pool[0, 0][cache.table[2, 0].long(), 0, 7] = float("nan")  # a visible NaN key
+    out = cache.attend(q, ints([0, 1, 2]), 0)
+    assert bool(torch.isnan(out[2]).all()) and bool(torch.isfinite(out[0]).all())
+    out = torch.full_like(q, 4.0)
+    cache.attend(q, ints([5, 0, -3]), 0, out=out)
+    assert cache.status() == mb.MAP_EINTERNAL and bool((out[[0, 2]] == 4.0).all()) and bool(torch.isfinite(out[1]).all())
+    with pytest.raises(ValueError):
+        cache.attend(q.half(), ints([0, 1, 2]), 0)
+    with pytest.raises(mb.MapError):
+        cache.attend(q, ints([0, 1, 2]), 1)
+    assert cache.attend(q[:0], ints([]), 0).shape == (0, 2, 64)
+
+
+def test_pool_offsets_past_32_bits(mb):
+    """The last pages of a pool of 2^33 bytes: appended, attended, forked and freed."""
+    dh, hk, page = 128, 8, 64
+    pages = (1 << 32) // (4 * hk * page * dh) + 3                    # 2 layers, K and V: over 2^32 elements
+    cache = mb.Cache.empty(2, pages, hk, page, dh, 3, 4)
+    cache.refs[: pages - 3] = 1                                      # the free pages are the last
+    plan = mb.Rope(dh, [1.0] * 64)
+    g = gen(4)
+    k, v, q = (randn(g, 70, h, dh, typ=torch.bfloat16) for h in (hk, hk, 16))
+    slots = cache.extend(ints([0]), ints([70]), rows=70)
+    pos = torch.arange(70, dtype=torch.int32, device=DEV)[None]
+    plan.append(q, k, v, pos, cache, 1, slots)
+    rk = plan.rotate(None, k, pos)[1]
+    cache.fork(ints([0]), ints([1]))
+    cache.check()
+    assert cache.table[1, :2].cpu().tolist() == [pages - 3, pages - 1]
+    for s in (0, 1):
+        at = cache.table[s, :2].cpu().tolist()
+        sl = [at[t // page] * page + t % page for t in range(70)]
+        got = rows_of(cache.pool[1:], sl)[0]
+        assert torch.equal(got[0], rk) and torch.equal(got[1], v)
+    out = cache.attend(q[:2], ints([1, 0]), 1)
+    check_attend(out, q[:2], cache, 1, [1, 0], dh ** -0.5, torch.bfloat16)
+
+
+# ----------------------------------------------------------------------------- streams, graphs, the whole path
+
+def test_calls_on_a_stream_of_the_callers(mb):
+    case = ROTATIONS[0]
+    typ, q, k, wq, wk, pos, inv, ax, plan = rotation(mb, case)
+    cache = filled(mb, typ, 128, 4, 16, [40, 20], 3)
+    want = plan.rotate(q, k, pos, wq, wk)
+    wgrad = plan.grad(q, k, pos, q, k, wq, wk)
+    watt = cache.attend(q.expand(2, -1, -1), ints([0, 1]), 0)
+    torch.cuda.synchronize()
+    s = torch.cuda.Stream()
+    got = plan.rotate(q, k, pos, wq, wk, stream=s)
+    ggrad = plan.grad(q, k, pos, q, k, wq, wk, stream=s)
+    gatt = cache.attend(q.expand(2, -1, -1), ints([0, 1]), 0, stream=s)
+    s.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip((*want, *wgrad, watt), (*got, *ggrad, gatt)))
+
+
+def test_a_decoding_step_captured_and_replayed(mb):
+    """extend, append and attend of a padded batch in one graph, replayed with new rows and another set of sequences."""
+    dh, hk, hq, n = 64, 2, 8, 4
+    caches = [filled(mb, torch.float16, dh, hk, 16, [30, 0, 15, 16, 47], 8, spare=30) for _ in range(2)]
+    for c in caches:                                                 # room for longer rows
+        wide = torch.zeros(5, 9, dtype=torch.int32, device=DEV)
+        wide[:, : c.table.shape[1]] = c.table
+        c.__init__(c.pool, wide, c.length, c.refs)
+    plan = mb.Rope(dh, [0.9 ** i for i in range(32)])
+    seqs = ints([0, 1, 2, -1])
+    q, k, v = (randn(gen(1), n, h, dh, typ=torch.float16) for h in (hq, hk, hk))
+    pos = ints([[30, 0, 15, 0]])
+    out = torch.full((n, hq, dh), 3.0, dtype=torch.float16, device=DEV)
+
+    def step(c, out):
+        slots = c.extend(seqs)
+        qr = plan.append(q, k, v, pos, c, 0, slots)
+        c.attend(qr, seqs, 0, out=out)
+
+    want = [out.clone() for _ in range(3)]
+    inputs = [(ints([0, 1, 2, -1]), 1), (ints([4, -1, 0, 1]), 2), (ints([0, 1, 2, 3]), 3)]
+
+    def feed(i):
+        seqs.copy_(inputs[i][0])
+        for t, h in ((q, hq), (k, hk), (v, hk)):
+            t.copy_(randn(gen(10 * inputs[i][1] + h), n, h, dh, typ=torch.float16))
+
+    for i in range(3):
+        feed(i)
+        step(caches[0], want[i])
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    warm = torch.cuda.Stream()
+    warm.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.graph(g, stream=warm):
+        step(caches[1], out)
+    for i in range(3):
+        feed(i)
+        out.fill_(3.0)
+        g.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want[i]), i
+    assert torch.equal(caches[0].length, caches[1].length) and torch.equal(caches[0].refs, caches[1].refs)
+    caches[1].check()
+
+
+def test_gradient_captured_and_replayed_beside_an_eager_one(mb):
+    typ, q, k, wq, wk, pos, inv, ax, plan = rotation(mb, ROTATIONS[15])
+    dq, dk = torch.randn_like(q), torch.randn_like(k)
+    g = torch.cuda.CUDAGraph()
+    plan.grad(dq, dk, pos, q, k, wq, wk)
+    torch.cuda.synchronize()
+    with torch.cuda.graph(g):
+        held = plan.grad(dq, dk, pos, q, k, wq, wk)
+    for seed in (1, 2):
+        dq.copy_(randn(gen(seed), *dq.shape, typ=typ))
+        g.replay()
+        eager = plan.grad(dq, dk, pos, q, k, wq, wk)
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(held, eager))
+
+
+def test_an_image_answered_twice_from_one_cache(mb):
+    """The whole path: score, select and assemble an image's tokens; its full prompt and two questions, each with its own
+    kept tokens, in one cache; every layer's pages hold what the pruned prompt alone would give, and attention over
+    the fork is attention over those rows."""
+    from paper_2608_06411_gb300 import workloads as W
+    dims = W.PredictorDims(D=512, Dh=256, dp=64)
+    w = W.make_weights(dims, seed=7)
+    wl = W.WORKLOADS["c0"]
+    grid, K, dh, hk, hq, page = (2, 10, 12), 31, 64, 2, 8, 16
+    N = grid[0] * grid[1] * grid[2]
+    vis = np.stack([W.make_image(wl, 0, N=N, D=512)] * 2)
+    lens = np.array([5, 9], np.int32)
+    text = np.concatenate([W.make_text(wl, b, int(lens[b]), D=512) for b in range(2)])
+    ctx = mb.Context({k: torch.from_numpy(v.view(np.int16)).to(DEV) for k, v in w.items()}, 512, 256, 64)
+    vis_t, text_t = (torch.from_numpy(a.view(np.int16)).to(DEV) for a in (vis, text))
+    keep, _ = ctx.select(ctx.score(text_t, vis_t, lens), vis_t, K)
+    head = 7                                                         # rows of a system prompt before the image
+    seq, pos = ctx.assemble_axes(vis_t, keep, text_t, lens, [grid] * 2, t_step=[2, 2], pos_offset=head)
+    whole = torch.arange(N, dtype=torch.int32, device=DEV)[None]
+    full, fpos = ctx.assemble_axes(vis_t[:1], whole, text_t[:1], [0], [grid], t_step=[2], pos_offset=head)
+    ctx.check()
+    # one layer's projection, and the system prompt's rows
+    g = gen(2)
+    proj = torch.randn(512, (hq + 2 * hk) * dh, generator=g, device=DEV) / 512 ** 0.5
+    sys_rows = torch.randn(head, 512, generator=g, device=DEV)
+    rows = torch.cat((sys_rows, full.view(torch.bfloat16).float()))
+    rpos = torch.cat((torch.arange(head, dtype=torch.int32, device=DEV).expand(3, -1), fpos), 1).contiguous()
+    wq, wk = ((1 + 0.1 * torch.randn(dh, generator=g, device=DEV)).bfloat16() for _ in range(2))
+    inv = [10000.0 ** (-2.0 * i / dh) for i in range(dh // 2)]
+    ax = [i % 3 for i in range(dh // 2)]
+    plan = mb.Rope(dh, inv, axis=ax)
+    cache = mb.Cache.empty(1, 64, hk, page, dh, 4, 24)
+
+    def heads(x):
+        y = (x @ proj).bfloat16()
+        return y[:, : hq * dh].unflatten(1, (hq, dh)), y[:, hq * dh: -hk * dh].unflatten(1, (hk, dh)), \
+            y[:, -hk * dh:].unflatten(1, (hk, dh))
+
+    q, k, v = heads(rows)
+    slots = cache.extend(ints([3]), ints([len(rows)]), rows=len(rows))
+    plan.append(q, k, v, rpos, cache, 0, slots, wq, wk)
+    cache.fork(ints([3, 3]), ints([0, 1]), keep, ints([head] * 2), ints([N] * 2))
+    at = 0
+    for b in range(2):                                               # the question's rows behind the kept ones
+        m = int(lens[b])
+        ids = pos[:, at + K: at + K + m].contiguous()
+        tq, tk, tv = heads(seq[at + K: at + K + m].view(torch.bfloat16).float())
+        s = cache.extend(ints([b]), ints([m]), rows=m)
+        tq = plan.append(tq, tk, tv, ids, cache, 0, s, wq, wk)
+        out = cache.attend(tq[-1:], ints([b]), 0)
+        cache.check()
+        # the same from the definition, in 64 bits
+        kept = keep[b].long()
+        kk = torch.cat((k[:head], k[head + kept], tk)).double().cpu().numpy()
+        vv = torch.cat((v[:head], v[head + kept], tv)).double().cpu().numpy()
+        kpos = torch.cat((rpos[:, :head], pos[:, at: at + K + m]), 1).cpu().numpy()
+        ref, _ = H.rotate(kk, f64(wk), kpos, inv, ax, False, 1e-6)
+        sl = [int(x) for t in range(-(-(head + K + m) // page)) for x in [cache.table[b, t]]]
+        sl = [sl[t // page] * page + t % page for t in range(head + K + m)]
+        got = rows_of(cache.pool, sl)[0]
+        assert np.abs(f64(got[0]) - ref).max() <= 2 ** -8 * np.abs(ref).max() and (f64(got[1]) == vv).all()
+        check_attend(out, tq[-1:], cache, 0, [b], dh ** -0.5, torch.bfloat16)
+        at += K + m
+    assert cache.length.cpu().tolist() == [head + K + 5, head + K + 9, 0, head + N]
+    cache.free(ints([0, 1, 3]))
+    assert int(cache.refs.sum()) == 0
+    ctx.close()
