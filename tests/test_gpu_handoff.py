@@ -159,6 +159,16 @@ def test_rotate_edges(mb):
     y, z = H.rotate(f64(x[:1]), None, pos.cpu().numpy()[:, :1], inv, [0, 1], False, 0.0)
     got, _ = plan.rotate(x[:1], None, pos[:, :1].contiguous())
     assert np.abs(f64(got) - y).max() < 1e-5
+    for adjacent in (False, True):                                   # columns past rot do not touch each other
+        for extra in (0, 1):                                         # (vectors, and any alignment)
+            wide = mb.Rope(64, [0.5] * 16, adjacent=adjacent)
+            x = torch.ones(2 * 64 + extra, device=DEV)[extra:].view(2, 1, 64)
+            x[0, 0, 40] = float("inf")
+            y, _ = wide.rotate(x, None, ints([[3, 4]]))
+            assert int(torch.isfinite(y).sum()) == 127 and bool(torch.isinf(y[0, 0, 40]))
+            y = wide.grad(x, None, ints([[3, 4]]))[0]
+            assert int(torch.isfinite(y).sum()) == 127 and bool(torch.isinf(y[0, 0, 40]))
+    x = torch.randn(3, 2, 8, device=DEV)
     for rows in (0,):
         q, k = plan.rotate(x[:rows], x[:rows], pos[:, :rows].contiguous())
         assert q.shape == (0, 2, 8) and k.shape == (0, 2, 8)
