@@ -63,8 +63,7 @@ SIGNATURES = {
                                  c_int, c_void_p, c_void_p, c_void_p, c_void_p]),
     "map_assemble_ragged": (c_int, [c_void_p, c_void_p, c_void_p, c_void_p, POINTER(c_int32), POINTER(c_int32),
                                     c_int, c_int, c_int, c_int, c_void_p, c_void_p, c_void_p]),
-    "map_assemble_axes": (c_int, [c_void_p, c_void_p, c_void_p, c_void_p, POINTER(c_int32), POINTER(c_int32),
-                                  POINTER(c_int32), c_int, c_int, c_int, c_int, c_void_p, c_void_p, c_void_p]),
+    "map_assemble_axes": (c_int, [c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_int, c_int, c_int, c_int, c_void_p, c_void_p, c_void_p]),
     "map_rope_init": (c_int, [c_int, c_int, c_int, c_int, POINTER(c_double), POINTER(c_int32), c_double,
                               POINTER(c_void_p)]),
     "map_rope_destroy": (None, [c_void_p]),
@@ -240,18 +239,20 @@ class Context:
         that are grids of grids[b] = (T, H, W) tokens, t_step[b] positions from frame to frame (default 1)."""
         B, N, D = vis.shape
         k = keep.shape[1]
-        arr, lp = _lens(lens)
-        ga, gp = _lens(grids)
-        sa, sp = _lens(t_step) if t_step is not None else (None, None)
-        if arr.shape != (B,) or ga.shape != (B, 3) or (sa is not None and sa.shape != (B,)) or keep.shape[0] != B:
+        m = np.array(lens, np.int32)
+        g = np.array(grids, np.int32)
+        t = None if t_step is None else np.array(t_step, np.int32)
+        if m.shape != (B,) or g.shape != (B, 3) or (t is not None and t.shape != (B,)) or keep.shape[0] != B:
             raise ValueError("lens and t_step have one entry an image, grids three, keep one row")
-        rows = B * k + int(arr.sum())
+        rows = B * k + int(m.sum())
         if seq is None:
             seq = torch.empty((rows, D), dtype=vis.dtype, device=vis.device)
         if pos is None:
             pos = torch.empty((3, rows), dtype=torch.int32, device=vis.device)
-        _check(lib.map_assemble_axes(self.h, _ptr(vis), _ptr(keep), _ptr(text), lp, gp, sp, B, N, k, pos_offset,
-                                     _ptr(seq), _ptr(pos), _stream(stream)), "map_assemble_axes")
+        s = _current_stream(vis.device.index) if stream is None else stream.cuda_stream
+        _check(lib.map_assemble_axes(self.h, _ptr(vis), _ptr(keep), _ptr(text), m.tobytes(), g.tobytes(),
+                                     None if t is None else t.tobytes(), B, N, k, pos_offset, _ptr(seq), _ptr(pos), s),
+               "map_assemble_axes")
         return seq, pos
 
     # -- ragged batches (padded layout, n_valid tokens per image) ---------------------------
@@ -394,37 +395,32 @@ _pack_heads = struct.Struct("@Pqqi4x").pack                          # map_heads
 _pack_cache = struct.Struct("@5P8i").pack                            # map_cache
 
 
+_current_device = torch._C._cuda_getDevice              # as torch.cuda.current_device and current_stream, without their
+_current_stream = torch._C._cuda_getCurrentRawStream    # Python objects: 1.5 us a call less
+
+
 class _on:
-    """The device of a call made current, and its stream (`.s`, a cudaStream_t as an int); with a stream of the
-    caller's, torch allocates on that one meanwhile."""
-    __slots__ = ("device", "stream", "s", "guards")
+    """A device made current, and with a stream of the caller's that one for torch's allocations too."""
 
     def __init__(self, device, stream):
         if device.type != "cuda":
             raise ValueError("tensors passed to libmap_gb300 must be on a CUDA device")
-        self.device, self.stream, self.guards = device, stream, ()
+        if stream is not None and stream.device != device:
+            raise ValueError("the stream is not on the tensors' device")
+        self.guard = torch.cuda.stream(stream) if stream is not None else torch.cuda.device(device)
 
     def __enter__(self):
-        d = self.device.index
-        if self.stream is not None:
-            if self.stream.device != self.device:
-                raise ValueError("the stream is not on the tensors' device")
-            g = torch.cuda.stream(self.stream)
-            g.__enter__()
-            self.guards = (g,)
-            self.s = self.stream.cuda_stream
-        else:
-            if torch.cuda.current_device() != d:
-                g = torch.cuda.device(d)
-                g.__enter__()
-                self.guards = (g,)
-            self.s = torch.cuda.current_stream(d).cuda_stream
-        return self
+        return self.guard.__enter__()
 
     def __exit__(self, *exc):
-        for g in self.guards:
-            g.__exit__(*exc)
-        return False
+        return self.guard.__exit__(*exc)
+
+
+def _type(dtype) -> int:
+    t = TYPES.get(dtype)
+    if t is None:
+        raise ValueError(f"unsupported element type {dtype}")
+    return t
 
 
 def _heads(t, rows: int, dh: int, dtype, device):
@@ -475,26 +471,27 @@ class Rope:
         except Exception:
             pass
 
-    def _common(self, x, pos):
-        if x.dtype not in TYPES:
-            raise ValueError(f"unsupported element type {x.dtype}")
-        rows = x.shape[0]
-        return TYPES[x.dtype], rows, _dense(pos, torch.int32, x.device, (self.n_axes, rows), "pos")
-
     def rotate(self, q, k, pos, wq=None, wk=None, q_out=None, k_out=None, stream=None):
         """map_qk_rotate: (q_out, k_out) of q [rows, heads, dh] and k (either may be None), pos int32 [n_axes, rows],
         norm weights wq, wk [dh] or None (no norm of that side).  Outputs not given are new, contiguous tensors."""
         x = q if q is not None else k
-        dt, dev = x.dtype, x.device
-        typ, rows, pp = self._common(x, pos)
-        with _on(dev, stream) as on:
-            if q is not None and q_out is None:
+        dev = x.device
+        if stream is not None or dev.index != _current_device():
+            with _on(dev, stream):
+                return self.rotate(q, k, pos, wq, wk, q_out, k_out)
+        dt, dh, rows = x.dtype, self.dh, x.shape[0]
+        a = b = oa = ob = None
+        if q is not None:
+            if q_out is None:
                 q_out = torch.empty(q.shape, dtype=dt, device=dev)
-            if k is not None and k_out is None:
+            a, oa = _heads(q, rows, dh, dt, dev), _heads(q_out, rows, dh, dt, dev)
+        if k is not None:
+            if k_out is None:
                 k_out = torch.empty(k.shape, dtype=dt, device=dev)
-            a, b, oa, ob = (None if t is None else _heads(t, rows, self.dh, dt, dev) for t in (q, k, q_out, k_out))
-            _check(lib.map_qk_rotate(self.h, typ, rows, pp, a, b, _dense(wq, dt, dev, (self.dh,), "wq"),
-                                     _dense(wk, dt, dev, (self.dh,), "wk"), oa, ob, on.s), "map_qk_rotate")
+            b, ob = _heads(k, rows, dh, dt, dev), _heads(k_out, rows, dh, dt, dev)
+        _check(lib.map_qk_rotate(self.h, _type(dt), rows, _dense(pos, torch.int32, dev, (self.n_axes, rows), "pos"), a, b,
+                                 _dense(wq, dt, dev, (dh,), "wq"), _dense(wk, dt, dev, (dh,), "wk"), oa, ob,
+                                 _current_stream(dev.index)), "map_qk_rotate")
         return q_out, k_out
 
     def grad(self, dq_out, dk_out, pos, q=None, k=None, wq=None, wk=None, dq=None, dk=None, dwq=None, dwk=None,
@@ -502,40 +499,59 @@ class Rope:
         """map_qk_rotate_grad: (dq, dk, dwq, dwk) from the gradients of rotate's outputs; q and k (rotate's inputs) are
         needed where wq and wk are given, dwq and dwk are float32 (None without a norm)."""
         x = dq_out if dq_out is not None else dk_out
-        dt, dev = x.dtype, x.device
-        typ, rows, pp = self._common(x, pos)
-        with _on(dev, stream) as on:
-            if dq_out is not None and dq is None:
+        dev = x.device
+        if stream is not None or dev.index != _current_device():
+            with _on(dev, stream):
+                return self.grad(dq_out, dk_out, pos, q, k, wq, wk, dq, dk, dwq, dwk)
+        dt, dh, rows, f32 = x.dtype, self.dh, x.shape[0], torch.float32
+        a = b = xa = xb = oa = ob = ws = None
+        if dq_out is not None:
+            if dq is None:
                 dq = torch.empty(dq_out.shape, dtype=dt, device=dev)
-            if dk_out is not None and dk is None:
+            a, oa = _heads(dq_out, rows, dh, dt, dev), _heads(dq, rows, dh, dt, dev)
+            if wq is not None:
+                if q is None:
+                    raise ValueError("q is needed with wq")
+                xa = _heads(q, rows, dh, dt, dev)
+                if dwq is None:
+                    dwq = torch.empty(dh, dtype=f32, device=dev)
+        if dk_out is not None:
+            if dk is None:
                 dk = torch.empty(dk_out.shape, dtype=dt, device=dev)
-            if dq_out is not None and wq is not None and dwq is None:
-                dwq = torch.empty(self.dh, dtype=torch.float32, device=dev)
-            if dk_out is not None and wk is not None and dwk is None:
-                dwk = torch.empty(self.dh, dtype=torch.float32, device=dev)
-            ws = torch.empty(self._grad_ws, dtype=torch.uint8, device=dev) if dwq is not None or dwk is not None else None
-            a, b, xa, xb, oa, ob = (None if t is None else _heads(t, rows, self.dh, dt, dev)
-                                    for t in (dq_out, dk_out, q, k, dq, dk))
-            _check(lib.map_qk_rotate_grad(self.h, typ, rows, pp, a, b, xa, xb, _dense(wq, dt, dev, (self.dh,), "wq"),
-                                          _dense(wk, dt, dev, (self.dh,), "wk"), oa, ob,
-                                          _dense(dwq, torch.float32, dev, (self.dh,), "dwq"),
-                                          _dense(dwk, torch.float32, dev, (self.dh,), "dwk"),
-                                          None if ws is None else ws.data_ptr(), on.s), "map_qk_rotate_grad")
+            b, ob = _heads(dk_out, rows, dh, dt, dev), _heads(dk, rows, dh, dt, dev)
+            if wk is not None:
+                if k is None:
+                    raise ValueError("k is needed with wk")
+                xb = _heads(k, rows, dh, dt, dev)
+                if dwk is None:
+                    dwk = torch.empty(dh, dtype=f32, device=dev)
+        if xa is not None or xb is not None:
+            ws = torch.empty(self._grad_ws, dtype=torch.uint8, device=dev)
+        _check(lib.map_qk_rotate_grad(self.h, _type(dt), rows, _dense(pos, torch.int32, dev, (self.n_axes, rows), "pos"), a, b,
+                                      xa, xb, _dense(wq, dt, dev, (dh,), "wq"), _dense(wk, dt, dev, (dh,), "wk"), oa, ob,
+                                      _dense(dwq, f32, dev, (dh,), "dwq"), _dense(dwk, f32, dev, (dh,), "dwk"),
+                                      None if ws is None else ws.data_ptr(), _current_stream(dev.index)), "map_qk_rotate_grad")
         return dq, dk, dwq, dwk
 
     def append(self, q, k, v, pos, cache, layer: int, slots, wq=None, wk=None, q_out=None, stream=None):
-        """map_qk_rotate_append: rotated k, and v, into the cache's slots (Cache.extend); returns the rotated q."""
-        dt, dev = k.dtype, k.device
+        """map_qk_rotate_append: rotated k, and v, into the cache's slots (Cache.extend); returns the rotated q (None
+        without q)."""
+        dev = k.device
+        if stream is not None or dev.index != _current_device():
+            with _on(dev, stream):
+                return self.append(q, k, v, pos, cache, layer, slots, wq, wk, q_out)
+        dt, dh, rows = k.dtype, self.dh, k.shape[0]
         if dt != cache.pool.dtype or dev != cache.pool.device:
             raise ValueError("k has the cache's type and device")
-        _, rows, pp = self._common(k, pos)
-        with _on(dev, stream) as on:
-            if q is not None and q_out is None:
+        a = oa = None
+        if q is not None:
+            if q_out is None:
                 q_out = torch.empty(q.shape, dtype=dt, device=dev)
-            a, b, c, oa = (None if t is None else _heads(t, rows, self.dh, dt, dev) for t in (q, k, v, q_out))
-            _check(lib.map_qk_rotate_append(self.h, cache.desc, layer, rows, pp, _dense(slots, torch.int32, dev, (rows,), "slots"),
-                                            a, b, c, _dense(wq, dt, dev, (self.dh,), "wq"),
-                                            _dense(wk, dt, dev, (self.dh,), "wk"), oa, on.s), "map_qk_rotate_append")
+            a, oa = _heads(q, rows, dh, dt, dev), _heads(q_out, rows, dh, dt, dev)
+        _check(lib.map_qk_rotate_append(self.h, cache.desc, layer, rows, _dense(pos, torch.int32, dev, (self.n_axes, rows), "pos"),
+                                        _dense(slots, torch.int32, dev, (rows,), "slots"), a, _heads(k, rows, dh, dt, dev),
+                                        _heads(v, rows, dh, dt, dev), _dense(wq, dt, dev, (dh,), "wq"),
+                                        _dense(wk, dt, dev, (dh,), "wk"), oa, _current_stream(dev.index)), "map_qk_rotate_append")
         return q_out
 
 
@@ -557,7 +573,7 @@ class Cache:
         ptrs = (_dense(table, torch.int32, dev, None, "table"), _dense(length, torch.int32, dev, (seqs,), "length"),
                 _dense(refs, torch.int32, dev, (pages,), "refs"), _dense(status, torch.int32, dev, (2,), "status"))
         self.pool, self.table, self.length, self.refs, self.status_word = pool, table, length, refs, status
-        self.heads, self.page, self.dh = heads, page, dh
+        self.device, self.heads, self.page, self.dh = dev, heads, page, dh
         self.desc = _pack_cache(pool.data_ptr(), *ptrs, TYPES[pool.dtype], layers, pages, heads, page, dh, seqs, max_pages)
         self._attend_ws = int(lib.map_cache_attend_workspace(self.desc))
 
@@ -570,9 +586,13 @@ class Cache:
                    ints(seqs), ints(pages))
 
     def extend(self, seqs, counts=None, rows: int | None = None, slots=None, stream=None):
-        """map_cache_extend: slots int32 [rows] for counts[i] new rows (default 1) of each sequence seqs[i] (device
-        int32); `rows` (or the size of `slots`) is at least their sum and must be given with counts."""
-        dev = self.pool.device
+        """map_cache_extend: slots int32 [rows] for counts[i] new rows of each sequence seqs[i] (device int32), or with
+        counts None for one row each, entry i's at i.  `rows` (or the size of `slots`) is at least their sum and must
+        be given with counts."""
+        dev = self.device
+        if stream is not None or dev.index != _current_device():
+            with _on(dev, stream):
+                return self.extend(seqs, counts, rows, slots)
         n = seqs.shape[0]
         if rows is None:
             if slots is not None:
@@ -581,54 +601,62 @@ class Cache:
                 rows = n
             else:
                 raise ValueError("rows must be given with counts")
-        with _on(dev, stream) as on:
-            if slots is None:
-                slots = torch.empty(rows, dtype=torch.int32, device=dev)
-            _check(lib.map_cache_extend(self.desc, _dense(seqs, torch.int32, dev, (n,), "seqs"),
-                                        _dense(counts, torch.int32, dev, (n,), "counts"), n, rows,
-                                        _dense(slots, torch.int32, dev, (rows,), "slots"), on.s), "map_cache_extend")
+        if slots is None:
+            slots = torch.empty(rows, dtype=torch.int32, device=dev)
+        _check(lib.map_cache_extend(self.desc, _dense(seqs, torch.int32, dev, (n,), "seqs"),
+                                    _dense(counts, torch.int32, dev, (n,), "counts"), n, rows,
+                                    _dense(slots, torch.int32, dev, (rows,), "slots"), _current_stream(dev.index)),
+               "map_cache_extend")
         return slots
 
     def fork(self, parents, children, keep=None, base=None, span=None, stream=None) -> None:
         """map_cache_fork: children[i] (empty) gets parents[i]'s rows, with keep int32 [n, k] those of rows
         base[i] .. base[i] + span[i] that keep[i] names (all int32 on the device)."""
-        dev = self.pool.device
-        n = parents.shape[0]
+        dev = self.device
+        if stream is not None or dev.index != _current_device():
+            with _on(dev, stream):
+                return self.fork(parents, children, keep, base, span)
+        n, i32 = parents.shape[0], torch.int32
         if keep is not None and (keep.dim() != 2 or base is None or span is None):
             raise ValueError("keep is [n, k] and comes with base and span")
         k = 0 if keep is None else keep.shape[1]
-        with _on(dev, stream) as on:
-            _check(lib.map_cache_fork(self.desc, _dense(parents, torch.int32, dev, (n,), "parents"),
-                                      _dense(children, torch.int32, dev, (n,), "children"), n,
-                                      _dense(keep, torch.int32, dev, (n, k), "keep"), k,
-                                      _dense(base, torch.int32, dev, (n,), "base"),
-                                      _dense(span, torch.int32, dev, (n,), "span"), on.s), "map_cache_fork")
+        _check(lib.map_cache_fork(self.desc, _dense(parents, i32, dev, (n,), "parents"),
+                                  _dense(children, i32, dev, (n,), "children"), n, _dense(keep, i32, dev, (n, k), "keep"), k,
+                                  _dense(base, i32, dev, (n,), "base"), _dense(span, i32, dev, (n,), "span"),
+                                  _current_stream(dev.index)), "map_cache_fork")
 
     def free(self, seqs, stream=None) -> None:
         """map_cache_free: the pages of seqs (int32 [n] on the device) lose a holder, the lengths become 0."""
-        dev = self.pool.device
+        dev = self.device
+        if stream is not None or dev.index != _current_device():
+            with _on(dev, stream):
+                return self.free(seqs)
         n = seqs.shape[0]
-        with _on(dev, stream) as on:
-            _check(lib.map_cache_free(self.desc, _dense(seqs, torch.int32, dev, (n,), "seqs"), n, on.s), "map_cache_free")
+        _check(lib.map_cache_free(self.desc, _dense(seqs, torch.int32, dev, (n,), "seqs"), n, _current_stream(dev.index)),
+               "map_cache_free")
 
     def attend(self, q, seqs, layer: int, scale: float | None = None, out=None, stream=None):
         """map_cache_attend: attention of q [n, heads, dh], row i over sequence seqs[i] (int32 on the device);
         scale defaults to dh ** -0.5."""
-        dev, dt = self.pool.device, self.pool.dtype
-        n = seqs.shape[0]
-        with _on(dev, stream) as on:
-            if out is None:
-                out = torch.empty(q.shape, dtype=dt, device=dev)
-            ws = torch.empty(self._attend_ws, dtype=torch.uint8, device=dev)
-            _check(lib.map_cache_attend(self.desc, layer, _heads(q, n, self.dh, dt, dev),
-                                        _dense(seqs, torch.int32, dev, (n,), "seqs"), n,
-                                        self.dh ** -0.5 if scale is None else scale, _heads(out, n, self.dh, dt, dev),
-                                        ws.data_ptr(), on.s), "map_cache_attend")
+        dev = self.device
+        if stream is not None or dev.index != _current_device():
+            with _on(dev, stream):
+                return self.attend(q, seqs, layer, scale, out)
+        dt, n, dh = self.pool.dtype, seqs.shape[0], self.dh
+        if out is None:
+            out = torch.empty(q.shape, dtype=dt, device=dev)
+        ws = torch.empty(self._attend_ws, dtype=torch.uint8, device=dev)
+        _check(lib.map_cache_attend(self.desc, layer, _heads(q, n, dh, dt, dev), _dense(seqs, torch.int32, dev, (n,), "seqs"),
+                                    n, dh ** -0.5 if scale is None else scale, _heads(out, n, dh, dt, dev), ws.data_ptr(),
+                                    _current_stream(dev.index)), "map_cache_attend")
         return out
 
     def status(self, stream=None) -> int:
-        with _on(self.pool.device, stream) as on:
-            return lib.map_cache_status(self.desc, on.s)
+        dev = self.device
+        if stream is not None or dev.index != _current_device():
+            with _on(dev, stream):
+                return self.status()
+        return lib.map_cache_status(self.desc, _current_stream(dev.index))
 
     def check(self, stream=None) -> None:
         _check(self.status(stream), "map_cache_status")

@@ -16,7 +16,7 @@ struct RopeTab {
   unsigned long long turn[kMaxHead / 2];
   uint8_t axis[kMaxHead / 2];
   int dh, rot, adjacent, axes;
-  float eps;
+  float eps, inv_dh;
 };
 
 __device__ __forceinline__ float to_f32(float x) { return x; }

@@ -26,7 +26,8 @@ namespace mapk {
 namespace {
 
 constexpr int kThreads = 256, kWarps = kThreads / 32;
-constexpr int kGradBlocks = 608;     // partial sums of dw: at most this many blocks a side (4 for each of 152 SMs)
+constexpr int kRotateCtas = 3, kGradCtas = 2;  // CTAs an SM
+constexpr int kGradBlocks = 152 * kGradCtas;   // blocks of a gradient's sides, each with a partial sum of dw
 
 struct Side {                        // one tensor's heads: input, output, norm weight
   const void* x; long long xrow, xhead;
@@ -63,19 +64,18 @@ __device__ __forceinline__ float2 turn_of(const RopeTab& t, int pair, const int3
   return make_float2(c, s);
 }
 
-// Where head h of row `row` goes; nullptr: nowhere (a padding row, or a slot outside the pool).
+// Whether a row is written: not for slot -1 (padding), nor for one outside the pool, which is reported.
+__device__ __forceinline__ bool good_slot(const Job& job, int slot) {
+  if (slot >= 0 && slot < job.pages * job.page) return true;
+  if (slot != -1) atomicOr(job.status, ST_BADINDEX);
+  return false;
+}
+// Where head h of row `row` goes.
 template <typename T, bool APPEND>
-__device__ __forceinline__ T* out_of(const RopeTab& tab, const Job& job, const Side& sd, long long row, int h) {
-  if (APPEND) {
-    const int slot = __ldg(job.slots + row);
-    if (slot < 0 || slot >= job.pages * job.page) {
-      if (slot != -1) atomicOr(job.status, ST_BADINDEX);
-      return nullptr;
-    }
-    if (sd.kind != kRowsOut)
-      return static_cast<T*>(sd.y) +
-             ((static_cast<long long>(slot / job.page) * sd.heads + h) * job.page + slot % job.page) * tab.dh;
-  }
+__device__ __forceinline__ T* out_of(const RopeTab& tab, const Job& job, const Side& sd, long long row, int h, int slot) {
+  if (APPEND && sd.kind != kRowsOut)
+    return static_cast<T*>(sd.y) +
+           ((static_cast<long long>(slot / job.page) * sd.heads + h) * job.page + slot % job.page) * tab.dh;
   return static_cast<T*>(sd.y) + row * sd.yrow + h * sd.yhead;
 }
 
@@ -104,8 +104,9 @@ __global__ void __launch_bounds__(kThreads) rotate_any_kernel(const __grid_const
   const long long row = item / sd.heads;
   const int h = static_cast<int>(item - row * sd.heads);
   const T* x = static_cast<const T*>(sd.x) + row * sd.xrow + h * sd.xhead;
-  T* y = out_of<T, APPEND>(tab, job, sd, row, h);
-  if (y == nullptr) return;
+  const int slot = APPEND ? __ldg(job.slots + row) : 0;
+  if (APPEND && !good_slot(job, slot)) return;
+  T* y = out_of<T, APPEND>(tab, job, sd, row, h, slot);
   const T* w = static_cast<const T*>(sd.w);
   const int np = (tab.dh + 1) >> 1;
   float a[4], b[4], ss = 0.f;
@@ -234,271 +235,500 @@ __global__ void __launch_bounds__(kThreads) grad_any_kernel(const __grid_constan
   }
 }
 
-// ------------------------------------------------------------------ vectors of V columns
-// V columns as one access (16 bytes; 8 for V = 4 of a 16-bit type).
+// ------------------------------------------------------------------ vectors of V columns: a warp a row's heads
+// (Scalar instructions: the two-wide ones took as many moves between registers as they saved, and 0.92 of the speed.)
+__device__ __forceinline__ float2 neg2(float2 a) { return make_float2(-a.x, -a.y); }
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) { return make_float2(a.x * b.x, a.y * b.y); }
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) { return make_float2(fmaf(a.x, b.x, c.x), fmaf(a.y, b.y, c.y)); }
+
+// V columns as one access (16 bytes; 8 for V = 4 of a 16-bit type), and as V / 2 pairs of floats.
 template <typename T, int V> struct Vec;
 template <> struct Vec<float, 4> {
   float4 r;
-  __device__ __forceinline__ void load(const float* p) { r = *reinterpret_cast<const float4*>(p); }
-  __device__ __forceinline__ void get(float (&v)[4]) const { v[0] = r.x; v[1] = r.y; v[2] = r.z; v[3] = r.w; }
-  static __device__ __forceinline__ void store(float* p, const float (&v)[4]) {
-    *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]);
+  __device__ __forceinline__ void load(const void* p) { r = *static_cast<const float4*>(p); }
+  __device__ __forceinline__ void get(float2 (&v)[2]) const { v[0] = make_float2(r.x, r.y); v[1] = make_float2(r.z, r.w); }
+  static __device__ __forceinline__ void store(float* p, const float2 (&v)[2]) {
+    const float2 a = v[0], b = v[1];
+    *reinterpret_cast<float4*>(p) = make_float4(a.x, a.y, b.x, b.y);
   }
 };
 __device__ __forceinline__ float2 unpack2(uint32_t w, __nv_bfloat16) {
   return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
 }
-__device__ __forceinline__ float2 unpack2(uint32_t w, __half) { return __half22float2(*reinterpret_cast<const __half2*>(&w)); }
-__device__ __forceinline__ uint32_t pack2(float x, float y, __nv_bfloat16) {
-  const __nv_bfloat162 h = __floats2bfloat162_rn(x, y);
+__device__ __forceinline__ float2 unpack2(uint32_t w, __half) {
+  const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w));
+  return make_float2(f.x, f.y);
+}
+__device__ __forceinline__ uint32_t pack2(float2 v, __nv_bfloat16) {
+  const __nv_bfloat162 h = __float22bfloat162_rn(v);
   return *reinterpret_cast<const uint32_t*>(&h);
 }
-__device__ __forceinline__ uint32_t pack2(float x, float y, __half) {
-  const __half2 h = __floats2half2_rn(x, y);
+__device__ __forceinline__ uint32_t pack2(float2 v, __half) {
+  const __half2 h = __float22half2_rn(v);
   return *reinterpret_cast<const uint32_t*>(&h);
 }
 template <typename T> struct Vec<T, 8> {
   uint4 r;
-  __device__ __forceinline__ void load(const T* p) { r = *reinterpret_cast<const uint4*>(p); }
-  __device__ __forceinline__ void get(float (&v)[8]) const {
-    const uint32_t w[4] = {r.x, r.y, r.z, r.w};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const float2 f = unpack2(w[i], T());
-      v[2 * i] = f.x;
-      v[2 * i + 1] = f.y;
-    }
+  __device__ __forceinline__ void load(const void* p) { r = *static_cast<const uint4*>(p); }
+  __device__ __forceinline__ void get(float2 (&v)[4]) const {
+    v[0] = unpack2(r.x, T());
+    v[1] = unpack2(r.y, T());
+    v[2] = unpack2(r.z, T());
+    v[3] = unpack2(r.w, T());
   }
-  static __device__ __forceinline__ void store(T* p, const float (&v)[8]) {
-    *reinterpret_cast<uint4*>(p) = make_uint4(pack2(v[0], v[1], T()), pack2(v[2], v[3], T()), pack2(v[4], v[5], T()), pack2(v[6], v[7], T()));
+  static __device__ __forceinline__ void store(T* p, const float2 (&v)[4]) {
+    *reinterpret_cast<uint4*>(p) = make_uint4(pack2(v[0], T()), pack2(v[1], T()), pack2(v[2], T()), pack2(v[3], T()));
   }
 };
 template <typename T> struct Vec<T, 4> {
   uint2 r;
-  __device__ __forceinline__ void load(const T* p) { r = *reinterpret_cast<const uint2*>(p); }
-  __device__ __forceinline__ void get(float (&v)[4]) const {
-    const float2 a = unpack2(r.x, T()), b = unpack2(r.y, T());
-    v[0] = a.x; v[1] = a.y; v[2] = b.x; v[3] = b.y;
-  }
-  static __device__ __forceinline__ void store(T* p, const float (&v)[4]) {
-    *reinterpret_cast<uint2*>(p) = make_uint2(pack2(v[0], v[1], T()), pack2(v[2], v[3], T()));
+  __device__ __forceinline__ void load(const void* p) { r = *static_cast<const uint2*>(p); }
+  __device__ __forceinline__ void get(float2 (&v)[2]) const { v[0] = unpack2(r.x, T()); v[1] = unpack2(r.y, T()); }
+  static __device__ __forceinline__ void store(T* p, const float2 (&v)[2]) {
+    *reinterpret_cast<uint2*>(p) = make_uint2(pack2(v[0], T()), pack2(v[1], T()));
   }
 };
 
-// A lane holds two vectors of a head, those of its pairs: V columns from a and V from b, pairs (a + i, b + i), or for
-// adjacent pairs 2 V columns in a row.  `lanes` (a power of two, the last ones without columns) share a head.
-struct Lane { int a, b, turned; bool on, two; };       // turned: how many of the lane's V pairs turn
+// A lane holds two vectors of a head, those of its V pairs: V columns from a and V from b, pairs (a + i, b + i), or for
+// adjacent pairs 2 V columns in a row.  2^shift lanes (the last ones may be without columns) share a head, 32 >> shift
+// heads a warp.
+struct Lane { int j, a, b, turned; bool on, two; };     // turned: how many of the lane's pairs turn
 template <int V, bool ADJ>
 __device__ __forceinline__ Lane lane_of(const RopeTab& t, int shift) {
   Lane l;
-  const int j = threadIdx.x & ((1 << shift) - 1), nr = ADJ ? 0 : t.rot / (2 * V);
-  l.turned = ADJ ? min(V, max(0, (t.rot >> 1) - j * V)) : j < nr ? V : 0;
-  l.a = j < nr ? j * V : 2 * j * V;
-  l.b = j < nr ? (t.rot >> 1) + j * V : l.a + V;
+  const int nr = ADJ ? 0 : t.rot / (2 * V);
+  l.j = threadIdx.x & ((1 << shift) - 1);
+  l.turned = ADJ ? min(V, max(0, (t.rot >> 1) - l.j * V)) : l.j < nr ? V : 0;
+  l.a = l.j < nr ? l.j * V : 2 * l.j * V;
+  l.b = l.j < nr ? (t.rot >> 1) + l.j * V : l.a + V;
   l.on = l.a < t.dh;
   l.two = l.b < t.dh;
   return l;
 }
 
-// (cos, sin) of the pairs of `n` rows from row0 on, where the lanes of a
-// warp read them without bank conflicts: pair j V + i of row r is entry ((r V / 2 + i / 2) np + j) 2 + i % 2.  They are
-// computed once a block, not once a head: a head takes 16 instructions a pair without them.
+// The plan's frequencies and axes where lanes read different ones at once (the parameter bank serves one a cycle).
+struct Freqs {
+  unsigned long long turn[kMaxHead / 2];
+  int axis[kMaxHead / 2];
+};
+__device__ __forceinline__ void fill_freqs(Freqs& f, const RopeTab& t) {
+  for (int p = threadIdx.x; p < t.rot >> 1; p += kThreads) {
+    f.turn[p] = t.turn[p];
+    f.axis[p] = t.axis[p];
+  }
+  __syncthreads();
+}
+
+// cos and sin of the lane's V pairs at one row, two pairs at a time.  A warp computes each pair once (a head's
+// lanes would repeat it for every head of the warp) and hands them round through its part of shared memory.
 template <int V>
-__device__ __forceinline__ void fill_turns(float2* cs, const RopeTab& t, const Job& job, long long row0, int n, int np) {
-  const int half = t.rot >> 1;
-  for (int e = threadIdx.x; e < n * half; e += kThreads) {
-    const int r = e / half, p = e - r * half, j = p / V, i = p % V;
-    if (row0 + r < job.rows) cs[((r * (V / 2) + i / 2) * np + j) * 2 + i % 2] = turn_of(t, p, job.pos, job.rows, row0 + r);
-  }
-}
-
-// The lane's pairs turned by row r's entries (SIGN = 1) or back (-1); columns past rot are left as they are.
-template <int V, bool ADJ, int SIGN>
-__device__ __forceinline__ void turn_pairs(float (&a)[V], float (&b)[V], const float2* cs, int r, int np, int j, int turned) {
-  if (turned == 0) return;
-  const float4* c4 = reinterpret_cast<const float4*>(cs) + r * (V / 2) * np + j;
+struct Turns {
+  float2 c[V / 2], s[V / 2];
+  // at: the row's position on axis `lane` (lane < axes)
+  __device__ __forceinline__ void make(const RopeTab& t, const Freqs& f, int at, int lane, const Lane& ln, float* buf) {
+    const int half = t.rot >> 1;
+    __syncwarp();
+    for (int p0 = 0; p0 < half; p0 += 32) {
+      const int p = p0 + lane;
+      const int x = __shfl_sync(0xffffffffu, at, p < half ? f.axis[p] : 0);
+      if (p >= half) break;
+      const unsigned long long ph = f.turn[p] * static_cast<unsigned long long>(static_cast<long long>(x));
+      float si, co;
+      sincospif(static_cast<float>(static_cast<int>(ph >> 32)) * 0x1p-31f, &si, &co);
+      buf[(p >> 1) * 4 + (p & 1)] = co;                // (c, c, s, s) of two pairs
+      buf[(p >> 1) * 4 + 2 + (p & 1)] = si;
+    }
+    __syncwarp();
 #pragma unroll
-  for (int i = 0; i < V; i += 2) {
-    const float4 c = c4[(i / 2) * np];
-#pragma unroll
-    for (int k = 0; k < 2; ++k) {
-      const int q = i + k;
-      if (ADJ && q >= turned) continue;
-      const float co = k ? c.z : c.x, si = SIGN * (k ? c.w : c.y);
-      float& x = ADJ ? (q < V / 2 ? a[2 * q] : b[2 * q - V]) : a[q];
-      float& y = ADJ ? (q < V / 2 ? a[2 * q + 1] : b[2 * q + 1 - V]) : b[q];
-      const float u = x * co - y * si;
-      y = y * co + x * si;
-      x = u;
+    for (int i = 0; i < V / 2; ++i) {
+      const int at = min(ln.j * (V / 2) + i, kMaxHead / 4 - 1);
+      const float4 x = reinterpret_cast<const float4*>(buf)[at];
+      c[i] = make_float2(x.x, x.y);
+      s[i] = make_float2(x.z, x.w);
     }
   }
-}
-
-// U heads a lane, all loaded before the turns are computed.
-template <typename T, int V, bool ADJ, int U, bool APPEND>
-__global__ void __launch_bounds__(kThreads) rotate_kernel(const __grid_constant__ RopeTab tab,
-                                                          const __grid_constant__ Job job, int shift, int turn_rows) {
-  extern __shared__ float2 cs[];
-  pdl_enter();
-  const int si = side_of_block(job);
-  const Side& sd = job.s[si];
-  const Lane ln = lane_of<V, ADJ>(tab, shift);
-  const unsigned per = kThreads >> shift, heads = sd.heads, base = (blockIdx.x - job.first[si]) * (per * U);
-  const unsigned total = static_cast<unsigned>(job.rows) * heads, row0 = base / heads;
-  const int j = threadIdx.x & ((1 << shift) - 1), np = (tab.dh / V + 1) >> 1;
-  Vec<T, V> va[U], vb[U];
-  unsigned row[U], h[U];
+  // The lane's pairs turned (SIGN = 1) or turned back (-1); columns past rot are left as they are.
+  template <bool ADJ, int SIGN>
+  __device__ __forceinline__ void turn(float2 (&a)[V / 2], float2 (&b)[V / 2], int turned, bool all) const {
+    if constexpr (!ADJ) {
+      if (!all && turned == 0) return;
 #pragma unroll
-  for (int u = 0; u < U; ++u) {
-    const unsigned hv = base + u * per + (threadIdx.x >> shift);
-    row[u] = hv / heads;
-    h[u] = hv - row[u] * heads;
-    va[u].r = {};
-    vb[u].r = {};
-    if (hv < total && ln.on) {
-      const T* x = static_cast<const T*>(sd.x) + row[u] * sd.xrow + h[u] * sd.xhead;
-      va[u].load(x + ln.a);
-      if (ln.two) vb[u].load(x + ln.b);
-    }
-  }
-  const bool turns = sd.kind != kValues;
-  if (turns) {
-    fill_turns<V>(cs, tab, job, row0, turn_rows, np);
-    __syncthreads();
-  }
-  const T* w = static_cast<const T*>(sd.w);
-  float wa[V], wb[V];
-  if (w && ln.on) {
-    Vec<T, V> t;
-    t.load(w + ln.a);
-    t.get(wa);
-    if (ln.two) t.load(w + ln.b);
-    t.get(wb);
-  }
+      for (int i = 0; i < V / 2; ++i) {
+        const float2 u = fma2(a[i], c[i], mul2(b[i], SIGN > 0 ? neg2(s[i]) : s[i]));
+        b[i] = fma2(b[i], c[i], mul2(a[i], SIGN > 0 ? s[i] : neg2(s[i])));
+        a[i] = u;
+      }
+    } else {
 #pragma unroll
-  for (int u = 0; u < U; ++u) {
-    float a[V], b[V];
-    va[u].get(a);
-    vb[u].get(b);
-    if (w) {
-      float ss = 0.f;
-#pragma unroll
-      for (int i = 0; i < V; ++i) ss = fmaf(a[i], a[i], fmaf(b[i], b[i], ss));
-      for (int o = 1 << shift >> 1; o > 0; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
-      const float r = rsqrtf(ss / static_cast<float>(tab.dh) + tab.eps);
-#pragma unroll
-      for (int i = 0; i < V; ++i) {
-        a[i] *= r * wa[i];
-        b[i] *= r * wb[i];
+      for (int q = 0; q < V; ++q) {
+        if (q >= turned) continue;
+        const float2 cc = c[q / 2], ss = s[q / 2];
+        const float co = q & 1 ? cc.y : cc.x, si = SIGN * (q & 1 ? ss.y : ss.x);
+        float2& v = q < V / 2 ? a[q] : b[q - V / 2];
+        const float2 x = v;
+        v = make_float2(x.x * co - x.y * si, x.y * co + x.x * si);
       }
     }
-    if (base + u * per + (threadIdx.x >> shift) >= total || !ln.on) continue;
-    T* y = out_of<T, APPEND>(tab, job, sd, row[u], h[u]);
-    if (y == nullptr) continue;
-    if (turns) turn_pairs<V, ADJ, 1>(a, b, cs, row[u] - row0, np, j, ln.turned);
-    Vec<T, V>::store(y + ln.a, a);
-    if (ln.two) Vec<T, V>::store(y + ln.b, b);
+  }
+};
+
+template <int N>
+__device__ __forceinline__ float dot2(const float2 (&a)[N], const float2 (&b)[N], float add) {
+  float2 s = make_float2(add, 0.f);
+#pragma unroll
+  for (int i = 0; i < N; ++i) s = fma2(a[i], b[i], s);
+  const float2 f = s;
+  return f.x + f.y;
+}
+// Sum over the lanes of a head times 2^(5 - shift): steps past the head's lanes add a lane's sum to itself, which is
+// exact and costs less than branches around them.
+struct LaneSum {
+  int m[5];
+  __device__ __forceinline__ explicit LaneSum(int shift) {
+#pragma unroll
+    for (int i = 0; i < 5; ++i) m[i] = i < shift ? 1 << i : 0;
+  }
+  __device__ __forceinline__ float operator()(float x) const {
+#pragma unroll
+    for (int i = 0; i < 5; ++i) x += __shfl_xor_sync(0xffffffffu, x, m[i]);
+    return x;
+  }
+};
+
+// A norm weight as floats in shared memory: a pass reads it from there, for registers are what its heads need.
+template <typename T>
+__device__ __forceinline__ void fill_weight(float* to, const T* w, int dh) {
+  if (w)
+    for (int c = threadIdx.x; c < dh; c += kThreads) to[c] = to_f32(w[c]);
+}
+template <int V>
+__device__ __forceinline__ void weight_at(const float* w, float2 (&v)[V / 2]) {
+#pragma unroll
+  for (int i = 0; i < V / 4; ++i) {
+    const float4 x = reinterpret_cast<const float4*>(w)[i];
+    v[2 * i] = make_float2(x.x, x.y);
+    v[2 * i + 1] = make_float2(x.z, x.w);
   }
 }
 
-// A block takes every blocks-th group of heads of its side; its lanes keep their columns, so the sums of g n stay in
-// registers until the end.
-template <typename T, int V, bool ADJ>
-__global__ void __launch_bounds__(kThreads) grad_kernel(const __grid_constant__ RopeTab tab,
-                                                        const __grid_constant__ Job job, int shift, int turn_rows) {
-  extern __shared__ float2 cs[];               // two groups' turns
-  __shared__ float red[kWarps][kMaxHead];
+// Loads in flight, without registers: a lane copies its vectors to places of its own in shared memory (no other lane
+// reads them, so no barrier is needed), kAhead passes ahead.  Places that a lane never fills hold zeros.
+template <int BYTES>
+__device__ __forceinline__ void copy_vec(uint32_t dst, const char* src) {
+  if (BYTES == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+  else asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(dst), "l"(src) : "memory");
+}
+__device__ __forceinline__ void copy_int(uint32_t dst, const int32_t* src) {
+  asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst), "l"(src) : "memory");
+}
+constexpr int kStages = 4, kAhead = kStages - 1;
+
+// A pass is 32 >> shift heads of one row.  A warp takes runs of `run` passes of a row, the runs first, first + stride,
+// ...: it makes the row's turns once a run, and from pass to pass only adds to its addresses.
+constexpr int kRuns = 4;             // runs a warp, at least, where a row has several (the last ones leave warps idle)
+struct Passes {
+  unsigned row, k, end, at, rows, of_row, run, of_run, drow, dat;
+  __device__ __forceinline__ Passes(unsigned first, unsigned stride, long long rows_, unsigned of_row_)
+      : rows(static_cast<unsigned>(rows_)), of_row(of_row_) {
+    const unsigned long long most = static_cast<unsigned long long>(rows) * of_row / (stride * kRuns);
+    const unsigned cap = most < 1 ? 1 : most < of_row ? static_cast<unsigned>(most) : of_row, runs = (of_row + cap - 1) / cap;
+    run = (of_row + runs - 1) / runs;
+    of_run = (of_row + run - 1) / run;
+    row = first / of_run;
+    at = first % of_run;
+    drow = stride / of_run;
+    dat = stride % of_run;
+    enter();
+  }
+  __device__ __forceinline__ void enter() {
+    k = at * run;
+    end = min(k + run, of_row);
+  }
+  __device__ __forceinline__ bool left() const { return row < rows; }
+  // The next pass; whether it begins a run.
+  __device__ __forceinline__ bool next() {
+    if (++k < end) return false;
+    row += drow;
+    at += dat;
+    if (at >= of_run) { at -= of_run; ++row; }
+    enter();
+    return true;
+  }
+};
+
+// Addresses in bytes of a lane's first vector of a head.
+struct Heads {
+  const char* p; long long row, head;
+  template <typename T>
+  __device__ __forceinline__ Heads(const void* base, long long row_, long long head_, int a, T)
+      : p(static_cast<const char*>(base) + a * static_cast<int>(sizeof(T))), row(row_ * static_cast<int>(sizeof(T))),
+        head(head_ * static_cast<int>(sizeof(T))) {}
+  __device__ __forceinline__ const char* at(unsigned r, int h) const { return p + r * row + h * head; }
+};
+template <typename T, int V>
+__device__ __forceinline__ void store_vec(const char* y, const float2 (&v)[V / 2]) {
+  Vec<T, V>::store(reinterpret_cast<T*>(const_cast<char*>(y)), v);
+}
+
+// A block's warps take the passes of one side.  HBM-bound (q and k once in, once out).
+template <typename T, int V, bool ADJ, bool APPEND>
+__global__ void __launch_bounds__(kThreads, kRotateCtas) rotate_kernel(const __grid_constant__ RopeTab tab,
+                                                                       const __grid_constant__ Job job, int shift) {
+  constexpr int VB = V * sizeof(T);
+  __shared__ Freqs freqs;
+  __shared__ __align__(16) float turns_buf[kWarps][kMaxHead];
+  __shared__ __align__(16) float weight[kMaxHead];
+  __shared__ int row_buf[kWarps][kStages][8];  // positions on up to 4 axes, slot
+  extern __shared__ uint4 stages[];            // [kWarps][kStages][2][32]
   pdl_enter();
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, per = 32 >> shift;
   const int si = side_of_block(job);
   const Side& sd = job.s[si];
   const Lane ln = lane_of<V, ADJ>(tab, shift);
   const unsigned blk = blockIdx.x - job.first[si], blocks = job.first[si + 1] - job.first[si];
-  const unsigned per = kThreads >> shift, heads = sd.heads, total = static_cast<unsigned>(job.rows) * heads;
-  const int j = threadIdx.x & ((1 << shift) - 1), np = (tab.dh / V + 1) >> 1;
-  const T* w = static_cast<const T*>(sd.w);
-  float wa[V], wb[V], da[V] = {}, db[V] = {};
-  if (w && ln.on) {
-    Vec<T, V> t;
-    t.load(w + ln.a);
-    t.get(wa);
-    if (ln.two) t.load(w + ln.b);
-    t.get(wb);
-  }
-  int side = 0;
-  for (unsigned long long base64 = static_cast<unsigned long long>(blk) * per; base64 < total;
-       base64 += static_cast<unsigned long long>(blocks) * per, side ^= 1) {
-    const unsigned base = static_cast<unsigned>(base64), row0 = base / heads, hv = base + (threadIdx.x >> shift);
-    const unsigned row = hv / heads, h = hv - row * heads;
-    const bool on = hv < total && ln.on;
-    Vec<T, V> ga, gb, xa, xb;
-    ga.r = {}; gb.r = {}; xa.r = {}; xb.r = {};
-    if (on) {
-      const T* g = static_cast<const T*>(sd.g) + row * sd.grow + h * sd.ghead;
-      ga.load(g + ln.a);
-      if (ln.two) gb.load(g + ln.b);
-      if (w) {
-        const T* x = static_cast<const T*>(sd.x) + row * sd.xrow + h * sd.xhead;
-        xa.load(x + ln.a);
-        if (ln.two) xb.load(x + ln.b);
+  const bool values = APPEND && sd.kind == kValues, paged = APPEND && sd.kind != kRowsOut, norm = sd.w != nullptr;
+  const int heads = ln.on ? sd.heads : 0;      // of this lane
+  const int heads2 = ln.two ? heads : 0;
+  const int gap = (ln.b - ln.a) * static_cast<int>(sizeof(T));
+  uint4* mine = stages + warp * (kStages * 64) + lane;
+#pragma unroll
+  for (int n = 0; n < 2 * kStages; ++n) mine[n * 32] = make_uint4(0, 0, 0, 0);
+  __syncthreads();                             // before the copies to the same places
+  const uint32_t mine_at = smem_u32(mine), row_at = smem_u32(row_buf[warp][0]);
+  const Heads in(sd.x, sd.xrow, sd.xhead, ln.a, T());
+  const Heads out(sd.y, paged ? 0 : sd.yrow, paged ? static_cast<long long>(job.page) * tab.dh : sd.yhead, ln.a, T());
+  const long long in_step = per * in.head, out_step = per * out.head;
+  Passes ld(warp * blocks + blk, blocks * kWarps, job.rows, (sd.heads + per - 1) / per), cp = ld;
+  int lh = 0, ch = 0;                          // head of the lane in the pass loaded and in the one computed
+  const char* lx = nullptr;
+  char* cy = nullptr;
+  bool enter = true;
+  const auto load = [&](int stage) {
+    {
+      if (enter && !ld.left()) { enter = false; lh = 1 << 30; }
+      if (enter) {
+        lh = ld.k * per + (lane >> shift);
+        lx = in.at(ld.row, lh);
+        if (lane < tab.axes && tab.rot > 0 && !values) copy_int(row_at + (stage * 8 + lane) * 4, job.pos + lane * job.rows + ld.row);
+        if (APPEND && lane == 4) copy_int(row_at + (stage * 8 + 4) * 4, job.slots + ld.row);
+      }
+      if (lh < heads) copy_vec<VB>(mine_at + stage * 1024, lx);
+      if (lh < heads2) copy_vec<VB>(mine_at + stage * 1024 + 512, lx + gap);
+      lh += per;
+      lx += in_step;
+    }
+    if (ld.left()) enter = ld.next();
+    cp_async_commit();
+  };
+#pragma unroll
+  for (int n = 0; n < kAhead; ++n) load(n);
+  fill_weight(weight, static_cast<const T*>(sd.w), tab.dh);
+  fill_freqs(freqs, tab);                      // and a barrier
+  const float* w_a = weight + (ln.on ? ln.a : 0);
+  const float* w_b = weight + (ln.two ? ln.b : 0);
+  const LaneSum lane_sum(shift);
+  const float inv = tab.inv_dh * static_cast<float>(1 << shift) * 0.03125f;
+  Turns<V> turns;
+  unsigned turned_row = 0xffffffffu;
+  bool begins = true, write = true;
+  for (int stage = 0; cp.left(); stage = stage + 1 == kStages ? 0 : stage + 1) {
+    cp_async_wait_group<kAhead - 1>();
+    load(stage == 0 ? kStages - 1 : stage - 1);        // read by this lane in the round before
+    if (begins) {
+      const int at = lane < 8 ? row_buf[warp][stage][lane] : 0;  // lanes read what they copied
+      ch = cp.k * per + (lane >> shift);
+      cy = const_cast<char*>(out.at(cp.row, ch));
+      if (APPEND) {
+        const int slot = __shfl_sync(0xffffffffu, at, 4);
+        write = good_slot(job, slot);
+        if (paged && write)
+          cy += (static_cast<long long>(slot / job.page) * sd.heads * job.page + slot % job.page) * tab.dh * static_cast<int>(sizeof(T));
+      }
+      if (!values && cp.row != turned_row) {
+        turns.make(tab, freqs, at, lane, ln, turns_buf[warp]);
+        turned_row = cp.row;
       }
     }
-    float2* c = cs + side * turn_rows * np * V;
-    fill_turns<V>(c, tab, job, row0, turn_rows, np);
-    __syncthreads();                           // the other half is read by no one past this barrier
-    float a[V], b[V];
-    ga.get(a);
-    gb.get(b);
-    if (on) turn_pairs<V, ADJ, -1>(a, b, c, row - row0, np, j, ln.turned);
-    if (w) {
-      float na[V], nb[V], ss = 0.f, dot = 0.f;
-      xa.get(na);
-      xb.get(nb);
+    if (!APPEND || write) {
+      Vec<T, V> va, vb;
+      va.load(mine + stage * 64);
+      vb.load(mine + stage * 64 + 32);
+      float2 a[V / 2], b[V / 2];
+      va.get(a);
+      vb.get(b);
+      if (norm) {
+        const float ss = lane_sum(dot2(a, a, dot2(b, b, 0.f)));
+        const float r = rsqrtf(fmaf(ss, inv, tab.eps));
+        const float2 r2 = make_float2(r, r);
+        float2 wa[V / 2], wb[V / 2];
+        weight_at<V>(w_a, wa);
+        weight_at<V>(w_b, wb);
 #pragma unroll
-      for (int i = 0; i < V; ++i) ss = fmaf(na[i], na[i], fmaf(nb[i], nb[i], ss));
-      if (on) {
-#pragma unroll
-        for (int i = 0; i < V; ++i) dot = fmaf(a[i] * wa[i], na[i], fmaf(b[i] * (ln.two ? wb[i] : 0.f), nb[i], dot));
-      }
-      for (int o = 1 << shift >> 1; o > 0; o >>= 1) {
-        ss += __shfl_xor_sync(0xffffffffu, ss, o);
-        dot += __shfl_xor_sync(0xffffffffu, dot, o);
-      }
-      if (on) {
-        const float r = rsqrtf(ss / static_cast<float>(tab.dh) + tab.eps), m = dot * r / static_cast<float>(tab.dh);
-#pragma unroll
-        for (int i = 0; i < V; ++i) {
-          na[i] *= r;
-          nb[i] *= r;
-          da[i] = fmaf(a[i], na[i], da[i]);
-          db[i] = fmaf(b[i], nb[i], db[i]);
-          a[i] = r * (a[i] * wa[i] - na[i] * m);
-          b[i] = r * (b[i] * wb[i] - nb[i] * m);
+        for (int i = 0; i < V / 2; ++i) {
+          a[i] = mul2(a[i], mul2(r2, wa[i]));
+          b[i] = mul2(b[i], mul2(r2, wb[i]));
         }
       }
+      if (!values) turns.template turn<ADJ, 1>(a, b, ln.turned, tab.rot == tab.dh);
+      if (ch < heads) store_vec<T, V>(cy, a);
+      if (ch < heads2) store_vec<T, V>(cy + gap, b);
     }
-    if (on) {
-      T* y = static_cast<T*>(sd.y) + row * sd.yrow + h * sd.yhead;
-      Vec<T, V>::store(y + ln.a, a);
-      if (ln.two) Vec<T, V>::store(y + ln.b, b);
-    }
+    ch += per;
+    cy += out_step;
+    begins = cp.next();
   }
-  if (!w) return;
+}
+
+// The same passes; the lanes' sums of g n stay in registers until the end.  HBM-bound (q, k and the gradients of both
+// once in, their gradients once out).
+template <typename T, int V, bool ADJ>
+__global__ void __launch_bounds__(kThreads, kGradCtas) grad_kernel(const __grid_constant__ RopeTab tab,
+                                                                   const __grid_constant__ Job job, int shift) {
+  constexpr int VB = V * sizeof(T);
+  __shared__ Freqs freqs;
+  __shared__ __align__(16) float turns_buf[kWarps][kMaxHead];
+  __shared__ __align__(16) float weight[kMaxHead];
+  __shared__ int row_buf[kWarps][kStages][4];
+  extern __shared__ uint4 stages[];            // [kWarps][kStages][4][32]
+  pdl_enter();
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, per = 32 >> shift;
+  const int si = side_of_block(job);
+  const Side& sd = job.s[si];
+  const Lane ln = lane_of<V, ADJ>(tab, shift);
+  const unsigned blk = blockIdx.x - job.first[si], blocks = job.first[si + 1] - job.first[si];
+  const bool norm = sd.w != nullptr;
+  const int heads = ln.on ? sd.heads : 0, heads2 = ln.two ? heads : 0;
+  const int gap = (ln.b - ln.a) * static_cast<int>(sizeof(T));
+  uint4* mine = stages + warp * (kStages * 128) + lane;
 #pragma unroll
-  for (int i = 0; i < V; ++i) {
-    for (int o = 16; o >= 1 << shift; o >>= 1) {
-      da[i] += __shfl_xor_sync(0xffffffffu, da[i], o);
-      db[i] += __shfl_xor_sync(0xffffffffu, db[i], o);
+  for (int n = 0; n < 4 * kStages; ++n) mine[n * 32] = make_uint4(0, 0, 0, 0);
+  __syncthreads();                             // before the copies to the same places
+  const uint32_t mine_at = smem_u32(mine), row_at = smem_u32(row_buf[warp][0]);
+  const Heads ing(sd.g, sd.grow, sd.ghead, ln.a, T()), inx(sd.x, sd.xrow, sd.xhead, ln.a, T()), out(sd.y, sd.yrow, sd.yhead, ln.a, T());
+  const long long g_step = per * ing.head, x_step = per * inx.head, out_step = per * out.head;
+  Passes ld(warp * blocks + blk, blocks * kWarps, job.rows, (sd.heads + per - 1) / per), cp = ld;
+  int lh = 0, ch = 0;
+  const char *lg = nullptr, *lx = nullptr;
+  char* cy = nullptr;
+  bool enter = true;
+  const auto load = [&](int stage) {
+    {
+      if (enter && !ld.left()) { enter = false; lh = 1 << 30; }
+      if (enter) {
+        lh = ld.k * per + (lane >> shift);
+        lg = ing.at(ld.row, lh);
+        lx = inx.at(ld.row, lh);
+        if (lane < tab.axes && tab.rot > 0) copy_int(row_at + (stage * 4 + lane) * 4, job.pos + lane * job.rows + ld.row);
+      }
+      const uint32_t to = mine_at + stage * 2048;
+      if (lh < heads) {
+        copy_vec<VB>(to, lg);
+        if (norm) copy_vec<VB>(to + 1024, lx);
+      }
+      if (lh < heads2) {
+        copy_vec<VB>(to + 512, lg + gap);
+        if (norm) copy_vec<VB>(to + 1536, lx + gap);
+      }
+      lh += per;
+      lg += g_step;
+      lx += x_step;
     }
-    if ((threadIdx.x & 31) >> shift == 0 && ln.on) {
-      red[threadIdx.x >> 5][ln.a + i] = da[i];
-      if (ln.two) red[threadIdx.x >> 5][ln.b + i] = db[i];
+    if (ld.left()) enter = ld.next();
+    cp_async_commit();
+  };
+#pragma unroll
+  for (int n = 0; n < kAhead; ++n) load(n);
+  fill_weight(weight, static_cast<const T*>(sd.w), tab.dh);
+  fill_freqs(freqs, tab);                      // and a barrier
+  const float* w_a = weight + (ln.on ? ln.a : 0);
+  const float* w_b = weight + (ln.two ? ln.b : 0);
+  float2 da[V / 2], db[V / 2];
+#pragma unroll
+  for (int i = 0; i < V / 2; ++i) da[i] = db[i] = make_float2(0.f, 0.f);
+  const LaneSum lane_sum(shift);
+  const float inv = tab.inv_dh * static_cast<float>(1 << shift) * 0.03125f;
+  Turns<V> turns;
+  unsigned turned_row = 0xffffffffu;
+  bool begins = true;
+  for (int stage = 0; cp.left(); stage = stage + 1 == kStages ? 0 : stage + 1) {
+    cp_async_wait_group<kAhead - 1>();
+    load(stage == 0 ? kStages - 1 : stage - 1);        // read by this lane in the round before
+    if (begins) {
+      ch = cp.k * per + (lane >> shift);
+      cy = const_cast<char*>(out.at(cp.row, ch));
+      if (cp.row != turned_row) {
+        turns.make(tab, freqs, lane < 4 ? row_buf[warp][stage][lane] : 0, lane, ln, turns_buf[warp]);
+        turned_row = cp.row;
+      }
+    }
+    const uint4* from = mine + stage * 128;
+    Vec<T, V> va, vb;
+    va.load(from);
+    vb.load(from + 32);
+    float2 a[V / 2], b[V / 2];
+    va.get(a);
+    vb.get(b);
+    turns.template turn<ADJ, -1>(a, b, ln.turned, tab.rot == tab.dh);
+    if (norm) {
+      float2 na[V / 2], nb[V / 2], ha[V / 2], hb[V / 2];     // x, later n = x r; g w
+      va.load(from + 64);
+      vb.load(from + 96);
+      va.get(na);
+      vb.get(nb);
+      weight_at<V>(w_a, ha);
+      weight_at<V>(w_b, hb);
+#pragma unroll
+      for (int i = 0; i < V / 2; ++i) {
+        ha[i] = mul2(a[i], ha[i]);
+        hb[i] = mul2(b[i], hb[i]);
+      }
+      const float ss = lane_sum(dot2(na, na, dot2(nb, nb, 0.f)));
+      const float r = rsqrtf(fmaf(ss, inv, tab.eps));
+      const float m = lane_sum(dot2(ha, na, dot2(hb, nb, 0.f))) * r * -inv;        // -mean(g w n)
+      const float2 r2 = make_float2(r, r), m2 = make_float2(m, m);
+#pragma unroll
+      for (int i = 0; i < V / 2; ++i) {
+        na[i] = mul2(na[i], r2);
+        nb[i] = mul2(nb[i], r2);
+        if (ch < heads) {                      // elsewhere n may be 0 times an infinite r
+          da[i] = fma2(a[i], na[i], da[i]);
+          db[i] = fma2(b[i], nb[i], db[i]);
+        }
+        a[i] = mul2(r2, fma2(na[i], m2, ha[i]));
+        b[i] = mul2(r2, fma2(nb[i], m2, hb[i]));
+      }
+    }
+    if (ch < heads) store_vec<T, V>(cy, a);
+    if (ch < heads2) store_vec<T, V>(cy + gap, b);
+    ch += per;
+    cy += out_step;
+    begins = cp.next();
+  }
+  if (!norm) return;
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < V / 2; ++i) {
+    float2 fa = da[i], fb = db[i];
+    for (int o = 16; o >= 1 << shift; o >>= 1) {
+      fa.x += __shfl_xor_sync(0xffffffffu, fa.x, o);
+      fa.y += __shfl_xor_sync(0xffffffffu, fa.y, o);
+      fb.x += __shfl_xor_sync(0xffffffffu, fb.x, o);
+      fb.y += __shfl_xor_sync(0xffffffffu, fb.y, o);
+    }
+    if (lane >> shift == 0 && ln.on) {
+      turns_buf[warp][ln.a + 2 * i] = fa.x;
+      turns_buf[warp][ln.a + 2 * i + 1] = fa.y;
+      if (ln.two) {
+        turns_buf[warp][ln.b + 2 * i] = fb.x;
+        turns_buf[warp][ln.b + 2 * i + 1] = fb.y;
+      }
     }
   }
   __syncthreads();
   for (int c = threadIdx.x; c < tab.dh; c += kThreads) {
     float s = 0.f;
 #pragma unroll
-    for (int k = 0; k < kWarps; ++k) s += red[k][c];
+    for (int k = 0; k < kWarps; ++k) s += turns_buf[k][c];
     sd.part[static_cast<long long>(blk) * tab.dh + c] = s;
   }
 }
@@ -594,32 +824,27 @@ int shift_of(const RopeTab& t, int v) {
   return s;
 }
 
-// Rows whose turns a group of `vectors` heads of a side needs.
-int rows_spanned(int vectors, int heads, long long rows) {
-  const long long n = (vectors - 1) / heads + 2;
-  return static_cast<int>(n < rows ? n : rows);
+// Blocks of the sides: `limit` in proportion to their passes of `per` heads, at most one for kWarps passes.
+void spread_blocks(Job& job, int sides, int per, int limit) {
+  long long passes[3] = {}, all = 0;
+  for (int i = 0; i < sides; ++i) all += passes[i] = job.rows * ((job.s[i].heads + per - 1) / per);
+  unsigned at = 0;
+  for (int i = 0; i < 4; ++i) {
+    job.first[i] = at;
+    if (i >= sides) continue;
+    const long long share = std::max(1ll, limit * passes[i] / all), most = (passes[i] + kWarps - 1) / kWarps;
+    at += static_cast<unsigned>(std::min(share, most));
+  }
 }
 
-template <typename T, int V, bool ADJ, int U, bool APPEND>
+template <typename T, int V, bool ADJ, bool APPEND>
 cudaError_t run_rotate(const RopeTab& t, Job& job, int sides, cudaStream_t st) {
-  const int shift = shift_of(t, V), per = (kThreads >> shift) * U;
-  unsigned blocks = 0;
-  int rows = 0;
-  for (int i = 0; i < 3; ++i) {
-    job.first[i] = blocks;
-    if (i >= sides) continue;
-    blocks += static_cast<unsigned>((job.rows * job.s[i].heads + per - 1) / per);
-    if (job.s[i].kind != kValues) rows = std::max(rows, rows_spanned(per, job.s[i].heads, job.rows));
-  }
-  job.first[3] = blocks;
-  for (int i = sides; i < 3; ++i) job.first[i] = blocks;
-  const size_t smem = static_cast<size_t>(rows) * ((t.dh / V + 1) / 2) * V * sizeof(float2);
-  if (smem > 48 * 1024) {
-    const cudaError_t e = cudaFuncSetAttribute(rotate_kernel<T, V, ADJ, U, APPEND>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                               static_cast<int>(smem));
-    if (e != cudaSuccess) return e;
-  }
-  return launch_k(rotate_kernel<T, V, ADJ, U, APPEND>, dim3(blocks), dim3(kThreads), smem, st, t, job, shift, rows);
+  const int shift = shift_of(t, V);
+  spread_blocks(job, sides, 32 >> shift, 152 * kRotateCtas);
+  constexpr size_t smem = kWarps * kStages * 64 * sizeof(uint4);
+  const cudaError_t e = cudaFuncSetAttribute(rotate_kernel<T, V, ADJ, APPEND>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+  if (e != cudaSuccess) return e;
+  return launch_k(rotate_kernel<T, V, ADJ, APPEND>, dim3(job.first[3]), dim3(kThreads), smem, st, t, job, shift);
 }
 
 template <typename T, bool APPEND>
@@ -634,7 +859,7 @@ cudaError_t run_rotate_any(const RopeTab& t, Job& job, int sides, cudaStream_t s
 
 template <typename T, int V, bool APPEND>
 cudaError_t rotate_width(const RopeTab& t, Job& job, int sides, cudaStream_t st) {
-  return t.adjacent ? run_rotate<T, V, true, 2, APPEND>(t, job, sides, st) : run_rotate<T, V, false, 2, APPEND>(t, job, sides, st);
+  return t.adjacent ? run_rotate<T, V, true, APPEND>(t, job, sides, st) : run_rotate<T, V, false, APPEND>(t, job, sides, st);
 }
 
 template <typename T, bool APPEND>
@@ -646,32 +871,14 @@ cudaError_t rotate_job(const RopeTab& t, Job& job, int sides, cudaStream_t st) {
   return run_rotate_any<T, APPEND>(t, job, sides, st);
 }
 
-// Blocks of a gradient's sides: in proportion to their heads, at most kGradBlocks a side and one a group.
-void grad_blocks(Job& job, int sides, int per) {
-  long long heads = 0;
-  for (int i = 0; i < sides; ++i) heads += job.s[i].heads;
-  unsigned at = 0;
-  for (int i = 0; i < 4; ++i) {
-    job.first[i] = at;
-    if (i >= sides) continue;
-    const long long groups = (job.rows * job.s[i].heads + per - 1) / per;
-    const long long share = (kGradBlocks * job.s[i].heads + heads - 1) / heads;
-    at += static_cast<unsigned>(std::min(groups, share));
-  }
-}
-
 template <typename T, int V, bool ADJ>
 cudaError_t run_grad(const RopeTab& t, Job& job, int sides, cudaStream_t st) {
-  const int shift = shift_of(t, V), per = kThreads >> shift;
-  grad_blocks(job, sides, per);
-  int rows = 0;
-  for (int i = 0; i < sides; ++i) rows = std::max(rows, rows_spanned(per, job.s[i].heads, job.rows));
-  const size_t smem = 2 * static_cast<size_t>(rows) * ((t.dh / V + 1) / 2) * V * sizeof(float2);
-  if (smem > 40 * 1024) {                       // beside 8 KB of static shared memory
-    const cudaError_t e = cudaFuncSetAttribute(grad_kernel<T, V, ADJ>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
-    if (e != cudaSuccess) return e;
-  }
-  return launch_k(grad_kernel<T, V, ADJ>, dim3(job.first[3]), dim3(kThreads), smem, st, t, job, shift, rows);
+  const int shift = shift_of(t, V);
+  spread_blocks(job, sides, 32 >> shift, kGradBlocks);
+  constexpr size_t smem = kWarps * kStages * 128 * sizeof(uint4);
+  const cudaError_t e = cudaFuncSetAttribute(grad_kernel<T, V, ADJ>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+  if (e != cudaSuccess) return e;
+  return launch_k(grad_kernel<T, V, ADJ>, dim3(job.first[3]), dim3(kThreads), smem, st, t, job, shift);
 }
 
 template <typename T>
@@ -680,7 +887,7 @@ cudaError_t grad_job(const RopeTab& t, Job& job, int sides, cudaStream_t st) {
   if (v == 4) return t.adjacent ? run_grad<T, 4, true>(t, job, sides, st) : run_grad<T, 4, false>(t, job, sides, st);
   if constexpr (sizeof(T) == 2)
     if (v == 8) return t.adjacent ? run_grad<T, 8, true>(t, job, sides, st) : run_grad<T, 8, false>(t, job, sides, st);
-  grad_blocks(job, sides, kWarps);
+  spread_blocks(job, sides, 1, kGradBlocks);
   return launch_k(grad_any_kernel<T>, dim3(job.first[3]), dim3(kThreads), 0, st, t, job);
 }
 
@@ -709,6 +916,7 @@ int map_rope_init(int dh, int rot, int adjacent, int n_axes, const double* inv_f
   t.adjacent = adjacent;
   t.axes = n_axes;
   t.eps = static_cast<float>(eps);
+  t.inv_dh = 1.f / static_cast<float>(dh);
   for (int i = 0; i < rot / 2; ++i) {
     const double turns = inv_freq[i] * 0.15915494309189533577;     // 1 / 2 pi
     t.turn[i] = static_cast<unsigned long long>(std::ldexp(turns - std::floor(turns), 64));
