@@ -387,7 +387,7 @@ int map_qk_rotate_grad(const map_rope *rope, int type, long long rows, const int
  *           ceil(len / page) entries of a row mean anything.
  *   len     int32 [seqs]: rows of each sequence.
  *   refs    int32 [pages]: sequences that hold the page; 0: free.
- *   status  int32 [2]: error bits for map_cache_status; a word for the calls' own use.
+ *   status  int32 [MAP_CACHE_STATUS_WORDS]: error bits for map_cache_status; the calls' own counters.
  * type MAP_BF16 or MAP_F16; dh a multiple of 8 up to 256; page 1 .. 1024; pages <= 1048576;
  * seqs <= 262144; max_pages * page < 2^31 (MAP_EUNSUPPORTED beyond these).  New pages are the free ones with the lowest numbers, in the order of the
  * call's entries: results do not depend on timing.
@@ -395,6 +395,7 @@ int map_qk_rotate_grad(const map_rope *rope, int type, long long rows, const int
  * pages than are free or than a table row holds, changes no length and no page: map_cache_status
  * then reports it.
  */
+#define MAP_CACHE_STATUS_WORDS 1024
 typedef struct {
     void *pool;
     int32_t *table, *len, *refs, *status;

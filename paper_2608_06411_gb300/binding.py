@@ -391,6 +391,7 @@ def qcts(attn, lens, attn_ref, L: int, H: int, N: int, p=None, p_ref=None, js=No
 # stream unless `stream` is given; scratch and outputs that are not given are allocated on the stream that uses them.
 
 TYPES = {torch.bfloat16: 0, torch.float16: 1, torch.float32: 2}      # MAP_BF16, MAP_F16, MAP_F32
+CACHE_STATUS_WORDS = 1024                                            # MAP_CACHE_STATUS_WORDS
 _pack_heads = struct.Struct("@Pqqi4x").pack                          # map_heads
 _pack_cache = struct.Struct("@5P8i").pack                            # map_cache
 
@@ -557,21 +558,21 @@ class Rope:
 
 class Cache:
     """Pages of a key/value cache (map_cache) over the caller's tensors: pool [layers, 2, pages, heads, page, dh] bf16 or
-    fp16, table int32 [seqs, max_pages], length int32 [seqs], refs int32 [pages], status int32 [2], the last four
-    initially zero (`Cache.empty` makes all of them)."""
+    fp16, table int32 [seqs, max_pages], length int32 [seqs], refs int32 [pages], status int32 [CACHE_STATUS_WORDS], the last
+    four initially zero (`Cache.empty` makes all of them)."""
 
     def __init__(self, pool, table, length, refs, status=None):
         dev = pool.device
         if pool.dim() != 6 or pool.shape[1] != 2 or pool.dtype not in TYPES or not pool.is_contiguous():
             raise ValueError("pool must be a contiguous [layers, 2, pages, heads, page, dh] tensor")
         if status is None:
-            status = torch.zeros(2, dtype=torch.int32, device=dev)
+            status = torch.zeros(CACHE_STATUS_WORDS, dtype=torch.int32, device=dev)
         layers, _, pages, heads, page, dh = pool.shape
         if table.dim() != 2:
             raise ValueError("table must be [seqs, max_pages]")
         seqs, max_pages = table.shape
         ptrs = (_dense(table, torch.int32, dev, None, "table"), _dense(length, torch.int32, dev, (seqs,), "length"),
-                _dense(refs, torch.int32, dev, (pages,), "refs"), _dense(status, torch.int32, dev, (2,), "status"))
+                _dense(refs, torch.int32, dev, (pages,), "refs"), _dense(status, torch.int32, dev, (CACHE_STATUS_WORDS,), "status"))
         self.pool, self.table, self.length, self.refs, self.status_word = pool, table, length, refs, status
         self.device, self.heads, self.page, self.dh = dev, heads, page, dh
         self.desc = _pack_cache(pool.data_ptr(), *ptrs, TYPES[pool.dtype], layers, pages, heads, page, dh, seqs, max_pages)

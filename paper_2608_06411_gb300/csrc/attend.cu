@@ -9,8 +9,10 @@
 // head; the 64-row tiles of all items form one list, and every CTA takes an equal run of it (the lengths are read on the
 // device, so one long sequence and many short ones fill the chip alike).  A CTA's four warps take 16 rows of a tile
 // each, with a ring of tiles of their own filled by cp.async, and join once an item ends: no barrier in the loop over
-// tiles.  Runs that begin or end inside an item leave (m, l, o) in the workspace and a second kernel joins them in
-// list order, so results do not depend on timing.
+// tiles.  Runs that begin or end inside an item leave (m, l, o) in the workspace; the last CTA of an item to do so
+// (counted in the cache's status words) joins them in list order, so results do not depend on timing.  (A second
+// kernel for that took 7 to 8 us of 53 to 56.)
+#include <algorithm>
 #include <cmath>
 
 #include "handoff.h"
@@ -22,7 +24,9 @@ constexpr int kWarps = 4, kThreads = kWarps * 32;
 constexpr int kTok = 16;                       // rows a warp takes of a tile
 constexpr int kTile = kWarps * kTok;
 constexpr int kRows = 16;                      // query heads of an item: the M of an mma.m16n8k16
-constexpr int kMaxGrid = 304;                  // two CTAs for each of 152 SMs
+constexpr int kMaxGrid = 456;                  // three CTAs for each of 152 SMs
+constexpr int kGroup = 16;                     // parts that one CTA joins
+static_assert(2 + 2 * kMaxGrid <= MAP_CACHE_STATUS_WORDS, "counters of an item's groups and of their parts");
 
 // A partial result: m [16], l [16], o [16][dh].
 __host__ __device__ constexpr int part_floats(int dh) { return kRows * (dh + 2); }
@@ -34,6 +38,7 @@ struct AttendArgs {
   map_heads q, out;
   const int32_t* seqs;
   int n, group, subs;                          // query heads a key head, items a key head
+  int page_shift;                              // log2 of the page, -1: no power of two
   float scale2;                                // scale log2(e)
   float* ws;
 };
@@ -43,23 +48,39 @@ __device__ __forceinline__ int seq_len(const AttendArgs& a, int i) {
   return s >= 0 && s < a.c.seqs ? max(0, __ldg(a.c.len + s)) : 0;
 }
 
-// Tiles before entry i (i = n: all) of the list, per item; all threads call it.
-__device__ __forceinline__ long long tiles_before(const AttendArgs& a, int i, long long* red) {
-  long long sum = 0;
-  for (int e = threadIdx.x; e < i; e += kThreads) sum += (seq_len(a, e) + kTile - 1) / kTile;
+__device__ __forceinline__ int seq_tiles(const AttendArgs& a, int i) { return (seq_len(a, i) + kTile - 1) / kTile; }
+
+// Sum over the block's threads before this one, and over all (red: kWarps words).
+__device__ __forceinline__ long long block_prefix(long long v, long long* red, long long* total) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  long long s = v;
 #pragma unroll
-  for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+  for (int o = 1; o < 32; o <<= 1) {
+    const long long u = __shfl_up_sync(0xffffffffu, s, o);
+    if (lane >= o) s += u;
+  }
+  if (lane == 31) red[warp] = s;
   __syncthreads();
-  if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = sum;
-  __syncthreads();
-  sum = 0;
+  long long before = 0, all = 0;
 #pragma unroll
-  for (int w = 0; w < kWarps; ++w) sum += red[w];
-  return sum;
+  for (int w = 0; w < kWarps; ++w) {
+    before += w < warp ? red[w] : 0;
+    all += red[w];
+  }
+  *total = all;
+  return before + s - v;
 }
 
+__device__ __forceinline__ void cp_async16_at(uint32_t dst, const void* src) {
+  asm volatile("cp.async.cg.shared.global.L2::128B [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
 __device__ __forceinline__ void cp_async16_or_zero(uint32_t dst, const void* src, bool on) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(on ? 16 : 0) : "memory");
+}
+__device__ __forceinline__ float exp2_fast(float x) {       // 2 ulp; 0 at -inf
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
 }
 __device__ __forceinline__ void ldsm4(uint32_t (&r)[4], uint32_t addr) {
   asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];"
@@ -119,104 +140,200 @@ struct Place {
   }
 };
 
+// A row of a tile in shared memory, 16 bytes longer than its columns: eight rows' vector x meet distinct banks.  (An
+// exclusive or of the vector with the row saves the padding but its addresses are not constants: 58 against 53 us.)
+template <int DH>
+struct Tile {
+  static constexpr int kVecs = DH / 8;
+  static constexpr int kRow = DH * 2 + 16;
+  static constexpr int kStage = 2 * kTok * kRow;             // K and V rows of one warp's part of a tile
+  static __device__ __forceinline__ uint32_t at(int row, int x) { return row * kRow + x * 16; }
+};
+// Joins `count` parts, of CTAs c, c + stride, ... (the first one's slot `slot0`, the others' slot 0), in order: into out,
+// or into the first part where out is nullptr.  All of the block's threads, one for four columns of a row, with kGroup
+// parts in flight, for all that a join takes is latency.
+template <typename T, int DH>
+__device__ __noinline__ void join_parts(const AttendArgs& a, int c, int stride, int slot0, int count, int have, T* out,
+                                        float* tops, float* sums) {
+  const auto part = [&](int p) { return a.ws + (2 * static_cast<long long>(c + p * stride) + (p == 0 ? slot0 : 0)) * part_floats(DH); };
+  for (int e = threadIdx.x; e < have * (DH / 4); e += kThreads) {
+    const int r = e / (DH / 4), x = 4 * (e % (DH / 4));
+    float top = -INFINITY, sum = 0.f;
+    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int p0 = 0; p0 < count; p0 += kGroup) {
+      float4 y[kGroup];
+      float m[kGroup], l[kGroup], next = top;
+#pragma unroll
+      for (int k = 0; k < kGroup; ++k) {
+        const bool on = p0 + k < count;
+        const float* q = part(on ? p0 + k : 0);
+        m[k] = on ? __ldcg(q + r) : -INFINITY;
+        l[k] = on ? __ldcg(q + kRows + r) : 0.f;
+        y[k] = on ? __ldcg(reinterpret_cast<const float4*>(q + 2 * kRows + r * DH + x)) : make_float4(0.f, 0.f, 0.f, 0.f);
+      }
+#pragma unroll
+      for (int k = 0; k < kGroup; ++k) next = fmaxf(next, m[k]);
+      const float at = next == -INFINITY ? 0.f : next, f0 = exp2_fast(top - at);
+      top = next;
+      sum *= f0;
+      v = make_float4(v.x * f0, v.y * f0, v.z * f0, v.w * f0);
+#pragma unroll
+      for (int k = 0; k < kGroup; ++k) {
+        const float f = exp2_fast(m[k] - at);
+        sum = fmaf(f, l[k], sum);
+        v.x = fmaf(f, y[k].x, v.x);
+        v.y = fmaf(f, y[k].y, v.y);
+        v.z = fmaf(f, y[k].z, v.z);
+        v.w = fmaf(f, y[k].w, v.w);
+      }
+    }
+    if (out) {
+      T* o = out + r * a.out.head + x;
+      o[0] = from_f32<T>(v.x / sum);
+      o[1] = from_f32<T>(v.y / sum);
+      o[2] = from_f32<T>(v.z / sum);
+      o[3] = from_f32<T>(v.w / sum);
+    } else {
+      *reinterpret_cast<float4*>(part(0) + 2 * kRows + r * DH + x) = v;
+      if (x == 0) {
+        tops[r] = top;
+        sums[r] = sum;
+      }
+    }
+  }
+  if (out) return;
+  __syncthreads();                             // the first part's m and l have been read
+  if (threadIdx.x < have) {
+    part(0)[threadIdx.x] = tops[threadIdx.x];
+    part(0)[kRows + threadIdx.x] = sums[threadIdx.x];
+  }
+}
+
+// Whether this block is the last of `count` to come here after writing a part (its writes are then visible to the last,
+// and theirs to it).  The counter is zero between uses.
+__device__ __forceinline__ bool is_last(int* counter, int count, int* flag) {
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    __threadfence();
+    const bool last = count == 1 || atomicAdd(counter, 1) == count - 1;
+    if (last && count > 1) {
+      *counter = 0;
+      __threadfence();
+    }
+    *flag = last;
+  }
+  __syncthreads();
+  return *flag;
+}
+
 template <typename T, int DH, int STAGES>
-__global__ void __launch_bounds__(kThreads) attend_kernel(const __grid_constant__ AttendArgs a) {
-  constexpr int RS = DH * 2 + 16;              // row of a tile in shared memory: eight rows meet distinct banks
-  constexpr int VPR = DH / 8;                  // 16-byte vectors of a row
-  constexpr int KSTEPS = DH / 16;
+__global__ void __launch_bounds__(kThreads, DH <= 80 ? 3 : DH <= 192 ? 2 : 1) attend_kernel(const __grid_constant__ AttendArgs a) {
+  using R = Tile<DH>;
+  constexpr int VPR = R::kVecs, KSTEPS = DH / 16;
   constexpr bool QREG = DH <= 128;             // query fragments stay in registers
-  constexpr int kStage = 2 * kTok * RS;        // K and V rows of one warp's part of a tile
   extern __shared__ __align__(16) unsigned char sh[];
   __shared__ float sm[kWarps][kRows], sl[kWarps][kRows];
-  __shared__ long long red[kWarps];
+  __shared__ long long red[kWarps + kRows / 2];  // and 16 floats
   __shared__ int first_entry;
   __shared__ long long first_tile;
+  __shared__ int last_part;
   pdl_enter();
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int tid = threadIdx.x, lane = tid & 31;
+  const int warp = __shfl_sync(0xffffffffu, tid >> 5, 0);              // one value a warp, as the compiler then knows
   const int rows = min(a.group, kRows), items = a.c.heads * a.subs;
 
-  // this CTA's run of the list
-  const long long total = tiles_before(a, a.n, red) * items;
+  // this CTA's run of the list, and where it begins: a thread counts a run of the entries
+  const int each = (a.n + kThreads - 1) / kThreads, e0 = tid * each, e1 = min(a.n, e0 + each);
+  long long mine = 0, total;
+  for (int e = e0; e < e1; ++e) mine += static_cast<long long>(seq_tiles(a, e)) * items;
+  long long at0 = block_prefix(mine, red, &total);
   const long long per = (total + gridDim.x - 1) / gridDim.x, t0 = per * blockIdx.x;
+  for (int e = blockIdx.x; e < a.n; e += gridDim.x) {                  // sequences without rows; bad ones
+    const int s = __ldg(a.seqs + e);
+    if (s < 0 || s >= a.c.seqs) {
+      if (s != -1 && tid == 0) atomicOr(a.c.status, ST_BADINDEX);
+    } else if (__ldg(a.c.len + s) <= 0) {
+      T* out = static_cast<T*>(a.out.p) + e * a.out.row;
+      for (int x = tid; x < a.out.heads * DH; x += kThreads) out[x / DH * a.out.head + x % DH] = from_f32<T>(0.f);
+    }
+  }
   if (t0 >= total) return;
   const int run = static_cast<int>(t0 + per <= total ? per : total - t0);
-  {
-    // entry of tile t0: a thread's entries are a run of the list, found by the prefix of the threads' sums
-    const int each = (a.n + kThreads - 1) / kThreads, e0 = tid * each;
-    long long mine = 0;
-    for (int e = e0; e < min(a.n, e0 + each); ++e) mine += static_cast<long long>((seq_len(a, e) + kTile - 1) / kTile) * items;
-    long long incl = mine;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const long long u = __shfl_up_sync(0xffffffffu, incl, o);
-      if (lane >= o) incl += u;
-    }
-    __syncthreads();
-    if (lane == 31) red[warp] = incl;
-    __syncthreads();
-    for (int w = 0; w < warp; ++w) incl += red[w];
-    long long at = incl - mine;
-    if (at <= t0 && t0 < incl) {
-      int e = e0;
-      for (;; ++e) {
-        const long long k = static_cast<long long>((seq_len(a, e) + kTile - 1) / kTile) * items;
-        if (t0 < at + k) break;
-        at += k;
+  if (at0 <= t0 && t0 < at0 + mine) {
+    for (int e = e0;; ++e) {
+      const long long k = static_cast<long long>(seq_tiles(a, e)) * items;
+      if (t0 < at0 + k) {
+        first_entry = e;
+        first_tile = t0 - at0;
+        break;
       }
-      first_entry = e;
-      first_tile = t0 - at;
+      at0 += k;
     }
-    __syncthreads();
   }
+  __syncthreads();
   Place ld;
   ld.enter(a, first_entry);
   ld.item = static_cast<int>(first_tile / ld.tiles);
   ld.t = static_cast<int>(first_tile % ld.tiles);
   Place cp = ld;
 
-  unsigned char* ring = sh + warp * STAGES * kStage;
-  unsigned char* qbuf = sh + kWarps * STAGES * kStage;                 // [3][rows][RS]
-  float* join = reinterpret_cast<float*>(qbuf + 3 * rows * RS);        // [2][rows][64]
+  const uint32_t ring = smem_u32(sh) + warp * STAGES * R::kStage;
+  const uint32_t qbuf = smem_u32(sh) + kWarps * STAGES * R::kStage;                        // [STAGES][rows] tile rows
+  float* join = reinterpret_cast<float*>(sh + kWarps * STAGES * R::kStage + STAGES * rows * R::kRow);   // [2][rows][64]
   const T* pk = static_cast<const T*>(a.pk);
+  const T* pv = pk + a.plane;
   const bool whole = a.c.page % kTok == 0;     // a warp's 16 rows lie in one page
+  const auto page_at = [&](int tok) { return a.page_shift >= 0 ? tok >> a.page_shift : tok / a.c.page; };
+  const auto row_in_page = [&](int tok) { return a.page_shift >= 0 ? tok & (a.c.page - 1) : tok % a.c.page; };
 
   // ---- loads.  pid: page of the warp's first row (whole), else of row lane & 15, read a tile ahead.
-  auto page_of = [&](const Place& p) -> int {
+  const auto page_of = [&](const Place& p) -> int {
     if (p.i >= a.n) return 0;
     const int tok = p.t * kTile + warp * kTok + (whole ? 0 : lane & 15);
-    return tok < p.len ? __ldg(a.c.table + static_cast<long long>(p.s) * a.c.max_pages + tok / a.c.page) : 0;
+    return tok < p.len ? __ldg(a.c.table + static_cast<long long>(p.s) * a.c.max_pages + page_at(tok)) : 0;
   };
   int pid = page_of(ld), ld_seg = 0;
   bool ld_new = true;
-  auto load = [&](int slot) {
+  const auto load = [&](int slot) {
     const int kh = ld.item / a.subs;
     if (ld_new) {                              // the item's queries: a quarter a warp
       const int g0 = (ld.item % a.subs) * kRows, have = min(kRows, a.group - g0);
       const T* q = static_cast<const T*>(a.q.p) + ld.i * a.q.row + (kh * a.group + g0) * a.q.head;
       for (int e = tid; e < rows * VPR; e += kThreads) {
         const int r = e / VPR, x = e % VPR;
-        cp_async16_or_zero(smem_u32(qbuf + ((ld_seg % 3) * rows + r) * RS + x * 16), q + (r < have ? r : 0) * a.q.head + x * 8, r < have);
+        cp_async16_or_zero(qbuf + (ld_seg % STAGES) * rows * R::kRow + R::at(r, x), q + (r < have ? r : 0) * a.q.head + x * 8, r < have);
       }
     }
     const int tok0 = ld.t * kTile + warp * kTok, valid = ld.len - tok0;
     if (valid > 0) {
-      const uint32_t dst = smem_u32(ring + slot * kStage);
+      const uint32_t dst = ring + slot * R::kStage;
       if (whole) {
-        const T* src = pk + ((static_cast<long long>(pid) * a.c.heads + kh) * a.c.page + tok0 % a.c.page) * DH;
+        const long long first = ((static_cast<long long>(pid) * a.c.heads + kh) * a.c.page + row_in_page(tok0)) * DH;
+        const T* k = pk + first + lane * 8;
+        const T* v = pv + first + lane * 8;
+        if (valid >= kTok) {
 #pragma unroll
-        for (int j = 0; j < VPR / 2; ++j) {
-          const int e = lane + 32 * j, r = e / VPR, x = e % VPR;
-          cp_async16_or_zero(dst + r * RS + x * 16, src + e * 8, r < valid);
-          cp_async16_or_zero(dst + (kTok + r) * RS + x * 16, src + a.plane + e * 8, r < valid);
+          for (int j = 0; j < VPR / 2; ++j) {
+            const int e = lane + 32 * j;
+            cp_async16_at(dst + R::at(e / VPR, e % VPR), k + 256 * j);
+            cp_async16_at(dst + R::at(kTok + e / VPR, e % VPR), v + 256 * j);
+          }
+        } else {
+#pragma unroll
+          for (int j = 0; j < VPR / 2; ++j) {
+            const int e = lane + 32 * j;
+            cp_async16_or_zero(dst + R::at(e / VPR, e % VPR), k + 256 * j, e / VPR < valid);
+            cp_async16_or_zero(dst + R::at(kTok + e / VPR, e % VPR), v + 256 * j, e / VPR < valid);
+          }
         }
       } else {
-        const long long mine = ((static_cast<long long>(pid) * a.c.heads + kh) * a.c.page + (tok0 + (lane & 15)) % a.c.page) * DH;
+        const long long mine = ((static_cast<long long>(pid) * a.c.heads + kh) * a.c.page + row_in_page(tok0 + (lane & 15))) * DH;
 #pragma unroll
         for (int j = 0; j < VPR / 2; ++j) {
           const int e = lane + 32 * j, r = e / VPR, x = e % VPR;
-          const T* src = pk + __shfl_sync(0xffffffffu, mine, r) + x * 8;
-          cp_async16_or_zero(dst + r * RS + x * 16, src, r < valid);
-          cp_async16_or_zero(dst + (kTok + r) * RS + x * 16, src + a.plane, r < valid);
+          const long long from = __shfl_sync(0xffffffffu, mine, r) + x * 8;
+          cp_async16_or_zero(dst + R::at(r, x), pk + from, r < valid);
+          cp_async16_or_zero(dst + R::at(kTok + r, x), pv + from, r < valid);
         }
       }
     }
@@ -239,9 +356,7 @@ __global__ void __launch_bounds__(kThreads) attend_kernel(const __grid_constant_
   };
   reset();
   // ldmatrix rows: queries and values by (lane & 15, lane / 16), keys by ((lane & 7) + 8 (lane / 16), lane / 8 % 2)
-  const uint32_t q_at = min(lane & 15, rows - 1) * RS + (lane >> 4) * 16;
-  const uint32_t k_at = ((lane & 7) + ((lane >> 4) << 3)) * RS + ((lane >> 3) & 1) * 16;
-  const uint32_t v_at = (kTok + (lane & 15)) * RS + (lane >> 4) * 16;
+  const int q_row = min(lane & 15, rows - 1), k_row = (lane & 7) + ((lane >> 4) << 3), k_vec = (lane >> 3) & 1;
   const bool two = rows > 8;                   // rows 8 .. 15 hold heads too
 
   int loaded = 0;
@@ -255,59 +370,62 @@ __global__ void __launch_bounds__(kThreads) attend_kernel(const __grid_constant_
   for (int n = 0; n < run; ++n) {
     cp_async_wait_group<STAGES - 2>();
     if (begins) __syncthreads(); else __syncwarp();
-    const uint32_t qa = smem_u32(qbuf + (seg % 3) * rows * RS) + q_at;
+    const uint32_t qa = qbuf + (seg % STAGES) * rows * R::kRow;
     if (QREG && begins) {
 #pragma unroll
-      for (int k = 0; k < KSTEPS; ++k) ldsm4(qf[QREG ? k : 0], qa + k * 32);
+      for (int k = 0; k < KSTEPS; ++k) ldsm4(qf[QREG ? k : 0], qa + R::at(q_row, 2 * k + (lane >> 4)));
     }
     if (n + STAGES - 1 < run) load((n + STAGES - 1) % STAGES);
     cp_async_commit();
 
     const int valid = cp.len - cp.t * kTile - warp * kTok;
     if (valid > 0) {
-      const uint32_t st = smem_u32(ring + (n % STAGES) * kStage);
+      const uint32_t st = ring + (n % STAGES) * R::kStage;
       float z[2][4] = {};
 #pragma unroll
       for (int k = 0; k < KSTEPS; ++k) {
         uint32_t b[4];
-        ldsm4(b, st + k_at + k * 32);
+        ldsm4(b, st + R::at(k_row, 2 * k + k_vec));
         if (QREG) {
           mma16<T>(z[0], qf[QREG ? k : 0], b[0], b[1]);
           mma16<T>(z[1], qf[QREG ? k : 0], b[2], b[3]);
         } else {
           uint32_t f[4];
-          ldsm4(f, qa + k * 32);
+          ldsm4(f, qa + R::at(q_row, 2 * k + (lane >> 4)));
           mma16<T>(z[0], f, b[0], b[1]);
           mma16<T>(z[1], f, b[2], b[3]);
         }
       }
-      float f[2];
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        if (h == 1 && !two) { f[1] = 1.f; z[0][2] = z[0][3] = z[1][2] = z[1][3] = 0.f; continue; }
-        float mx = -INFINITY;
+      for (int j = 0; j < 2; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) z[j][e] *= a.scale2;
+      if (valid < kTok) {
 #pragma unroll
         for (int j = 0; j < 2; ++j)
 #pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            float& x = z[j][2 * h + e];
-            x = j * 8 + 2 * (lane & 3) + e < valid ? x * a.scale2 : -INFINITY;
-            mx = fmaxf(mx, x);
-          }
+          for (int e = 0; e < 4; ++e)
+            if (j * 8 + 2 * (lane & 3) + (e & 1) >= valid) z[j][e] = -INFINITY;
+      }
+      float f[2] = {1.f, 1.f};
+      uint32_t hi[4] = {}, lo[4] = {};
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        if (h == 1 && !two) break;
+        float mx = fmaxf(fmaxf(z[0][2 * h], z[0][2 * h + 1]), fmaxf(z[1][2 * h], z[1][2 * h + 1]));
         mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
         mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
         mx = fmaxf(mx, m[h]);
         const float at = mx == -INFINITY ? 0.f : mx;
-        f[h] = exp2f(m[h] - at);
+        f[h] = exp2_fast(m[h] - at);
         m[h] = mx;
         float sum = 0.f;
 #pragma unroll
-        for (int j = 0; j < 2; ++j)
-#pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            z[j][2 * h + e] = exp2f(z[j][2 * h + e] - (at - kLift<T>));
-            sum += z[j][2 * h + e];
-          }
+        for (int j = 0; j < 2; ++j) {
+          const float x = exp2_fast(z[j][2 * h] - (at - kLift<T>)), y = exp2_fast(z[j][2 * h + 1] - (at - kLift<T>));
+          sum += x + y;
+          split_weights(x, y, hi[2 * j + h], lo[2 * j + h], T());
+        }
         l[h] = l[h] * f[h] + sum;
       }
       if (__any_sync(0xffffffffu, f[0] != 1.f || f[1] != 1.f)) {
@@ -319,13 +437,10 @@ __global__ void __launch_bounds__(kThreads) attend_kernel(const __grid_constant_
           o[j][3] *= f[1];
         }
       }
-      uint32_t hi[4], lo[4];
-#pragma unroll
-      for (int e = 0; e < 4; ++e) split_weights(z[e >> 1][2 * (e & 1)], z[e >> 1][2 * (e & 1) + 1], hi[e], lo[e], T());
 #pragma unroll
       for (int j = 0; j < DH / 16; ++j) {
         uint32_t b[4];
-        ldsm4_t(b, st + v_at + j * 32);
+        ldsm4_t(b, st + R::at(kTok + (lane & 15), 2 * j + (lane >> 4)));
         mma16<T>(o[2 * j], hi, b[0], b[1]);
         mma16<T>(o[2 * j + 1], hi, b[2], b[3]);
         mma16<T>(o[2 * j], lo, b[0], b[1]);
@@ -351,7 +466,7 @@ __global__ void __launch_bounds__(kThreads) attend_kernel(const __grid_constant_
       for (int h = 0; h < 2; ++h) {
         const int r = (lane >> 2) + 8 * h;
         top[h] = fmaxf(fmaxf(sm[0][r], sm[1][r]), fmaxf(sm[2][r], sm[3][r]));
-        const float f = exp2f(m[h] - (top[h] == -INFINITY ? 0.f : top[h]));
+        const float f = exp2_fast(m[h] - (top[h] == -INFINITY ? 0.f : top[h]));
 #pragma unroll
         for (int j = 0; j < DH / 8; ++j) {
           o[j][2 * h] *= f;
@@ -390,8 +505,8 @@ __global__ void __launch_bounds__(kThreads) attend_kernel(const __grid_constant_
           const float v = join[r * 64 + x] + join[(rows + r) * 64 + x];
           if (done) {
             const float mr = fmaxf(fmaxf(sm[0][r], sm[1][r]), fmaxf(sm[2][r], sm[3][r])), at = mr == -INFINITY ? 0.f : mr;
-            const float lr = sl[0][r] * exp2f(sm[0][r] - at) + sl[1][r] * exp2f(sm[1][r] - at) +
-                             sl[2][r] * exp2f(sm[2][r] - at) + sl[3][r] * exp2f(sm[3][r] - at);
+            const float lr = sl[0][r] * exp2_fast(sm[0][r] - at) + sl[1][r] * exp2_fast(sm[1][r] - at) +
+                             sl[2][r] * exp2_fast(sm[2][r] - at) + sl[3][r] * exp2_fast(sm[3][r] - at);
             out[r * a.out.head + c0 + x] = from_f32<T>(v / lr);
           } else {
             part[2 * kRows + r * DH + c0 + x] = v;
@@ -399,11 +514,27 @@ __global__ void __launch_bounds__(kThreads) attend_kernel(const __grid_constant_
         }
         __syncthreads();
       }
-      if (!done && tid < have) {
-        const float mr = fmaxf(fmaxf(sm[0][tid], sm[1][tid]), fmaxf(sm[2][tid], sm[3][tid])), at = mr == -INFINITY ? 0.f : mr;
-        part[tid] = mr;
-        part[kRows + tid] = sl[0][tid] * exp2f(sm[0][tid] - at) + sl[1][tid] * exp2f(sm[1][tid] - at) +
-                            sl[2][tid] * exp2f(sm[2][tid] - at) + sl[3][tid] * exp2f(sm[3][tid] - at);
+      if (!done) {
+        if (tid < have) {
+          const float mr = fmaxf(fmaxf(sm[0][tid], sm[1][tid]), fmaxf(sm[2][tid], sm[3][tid])), at = mr == -INFINITY ? 0.f : mr;
+          part[tid] = mr;
+          part[kRows + tid] = sl[0][tid] * exp2_fast(sm[0][tid] - at) + sl[1][tid] * exp2_fast(sm[1][tid] - at) +
+                              sl[2][tid] * exp2_fast(sm[2][tid] - at) + sl[3][tid] * exp2_fast(sm[3][tid] - at);
+        }
+        // the item's parts: CTAs c0 (whose run begins it) to c0 + parts - 1, in groups of kGroup.  The last CTA of a
+        // group joins the group, the last group's the groups.  Counters: a group's at its first CTA, the groups' at c0;
+        // a group of one needs none, so the next item's first group may begin where this one's last does.
+        const long long tile = t0 + n - cp.t;
+        const int c0 = static_cast<int>(tile / per), parts = static_cast<int>((tile + cp.tiles - 1) / per) - c0 + 1;
+        const int g = (static_cast<int>(blockIdx.x) - c0) / kGroup, groups = (parts + kGroup - 1) / kGroup;
+        const int first = c0 + g * kGroup, count = min(kGroup, parts - g * kGroup);
+        float* sums = reinterpret_cast<float*>(red + kWarps);
+        if (is_last(a.c.status + 2 + first, count, &last_part)) {
+          if (groups == 1 || count > 1) join_parts<T, DH>(a, first, 1, g == 0, count, have, groups == 1 ? out : nullptr, sm[0], sums);
+          if (groups > 1 && is_last(a.c.status + 2 + kMaxGrid + c0, groups, &last_part))
+            join_parts<T, DH>(a, c0, kGroup, 1, groups, have, out, sm[0], sums);
+        }
+        __syncthreads();
       }
       reset();
     }
@@ -414,95 +545,31 @@ __global__ void __launch_bounds__(kThreads) attend_kernel(const __grid_constant_
   }
 }
 
-// Joins the parts of the items that several CTAs' runs share; zeros for sequences without rows.  A CTA a query head:
-// its warps take every fourth part, a lane the columns 4 lane .. (and 128 on).
-template <typename T>
-__global__ void __launch_bounds__(kThreads) attend_join_kernel(const __grid_constant__ AttendArgs a, int grid) {
-  __shared__ long long red[kWarps];
-  __shared__ float w[kMaxGrid], stat[2][kWarps];
-  __shared__ float4 acc[kWarps][kMaxHead / 4];
-  pdl_enter();
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, i = blockIdx.y, h = blockIdx.x, dh = a.c.dh;
-  const int s = __ldg(a.seqs + i);
-  if (s < 0 || s >= a.c.seqs) {
-    if (s != -1 && tid == 0) atomicOr(a.c.status, ST_BADINDEX);
-    return;
-  }
-  const int kh = h / a.group, g = h % a.group, items = a.c.heads * a.subs, item = kh * a.subs + g / kRows, r = g % kRows;
-  T* out = static_cast<T*>(a.out.p) + i * a.out.row + h * a.out.head;
-  const int tiles = (seq_len(a, i) + kTile - 1) / kTile;
-  if (tiles == 0) {
-    for (int d = tid; d < dh; d += kThreads) out[d] = from_f32<T>(0.f);
-    return;
-  }
-  const long long total = tiles_before(a, a.n, red) * items, per = (total + grid - 1) / grid;
-  const long long first = tiles_before(a, i, red) * items + static_cast<long long>(item) * tiles;
-  const int c0 = static_cast<int>(first / per), c1 = static_cast<int>((first + tiles - 1) / per), parts = c1 - c0 + 1;
-  if (parts == 1) return;
-  // part p: CTA c0 + p; the first is that CTA's second slot (its run begins the item)
-  const auto part = [&](int p) { return a.ws + (2 * static_cast<long long>(c0 + p) + (p == 0)) * part_floats(dh); };
-  float top = -INFINITY;
-  for (int p = tid; p < parts; p += kThreads) top = fmaxf(top, part(p)[r]);
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-  if (lane == 0) stat[0][warp] = top;
-  __syncthreads();
-  top = fmaxf(fmaxf(stat[0][0], stat[0][1]), fmaxf(stat[0][2], stat[0][3]));
-  const float at = top == -INFINITY ? 0.f : top;
-  float l = 0.f;
-  for (int p = tid; p < parts; p += kThreads) {
-    w[p] = exp2f(part(p)[r] - at);
-    l = fmaf(w[p], part(p)[kRows + r], l);
-  }
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
-  if (lane == 0) stat[1][warp] = l;
-  __syncthreads();
-  l = (stat[1][0] + stat[1][1]) + (stat[1][2] + stat[1][3]);
-  for (int v = lane; v < dh / 4; v += 32) {
-    float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
-    for (int p = warp; p < parts; p += kWarps) {
-      const float4 y = *reinterpret_cast<const float4*>(part(p) + 2 * kRows + r * dh + 4 * v);
-      x.x = fmaf(w[p], y.x, x.x);
-      x.y = fmaf(w[p], y.y, x.y);
-      x.z = fmaf(w[p], y.z, x.z);
-      x.w = fmaf(w[p], y.w, x.w);
-    }
-    acc[warp][v] = x;
-  }
-  __syncthreads();
-  const float* f = reinterpret_cast<const float*>(acc);
-  for (int d = tid; d < dh; d += kThreads)
-    out[d] = from_f32<T>(((f[d] + f[kMaxHead + d]) + (f[2 * kMaxHead + d] + f[3 * kMaxHead + d])) / l);
-}
-
-size_t attend_smem(int dh, int stages, int rows) {
-  return static_cast<size_t>(kWarps) * stages * 2 * kTok * (dh * 2 + 16) + 3 * rows * (dh * 2 + 16) + 2 * rows * 64 * 4;
-}
-
 template <typename T, int DH, int STAGES>
 cudaError_t launch_run(const AttendArgs& a, size_t smem, int grid, cudaStream_t st) {
-  cudaError_t e = cudaFuncSetAttribute(attend_kernel<T, DH, STAGES>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
-  if (e == cudaSuccess) e = launch_k(attend_kernel<T, DH, STAGES>, dim3(grid), dim3(kThreads), smem, st, a);
-  if (e == cudaSuccess) e = launch_k(attend_join_kernel<T>, dim3(a.q.heads, a.n), dim3(kThreads), 0, st, a, grid);
-  return e;
+  const cudaError_t e = cudaFuncSetAttribute(attend_kernel<T, DH, STAGES>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
+  return e != cudaSuccess ? e : launch_k(attend_kernel<T, DH, STAGES>, dim3(grid), dim3(kThreads), smem, st, a);
 }
 
-// Two CTAs an SM where two stages of both fit its 227 KB, else one; three stages where they fit then.
+template <int DH>
+constexpr size_t smem_of(int stages, int rows) {
+  return static_cast<size_t>(kWarps) * stages * Tile<DH>::kStage + stages * rows * Tile<DH>::kRow + 2 * rows * 64 * 4;
+}
+
+// Tiles in a ring and CTAs an SM: two tiles ahead and two CTAs where they fit (dh = 128: one sequence of 120001 rows 45
+// against 53 us with one ahead and three CTAs, 64 of 200 to 1600 rows 53 against 58), three CTAs up to 80 columns.
 template <typename T, int DH>
 cudaError_t launch_width(const AttendArgs& a, int sms, cudaStream_t st) {
-  constexpr size_t kHalf = 113 * 1024, kWhole = 226 * 1024;
+  constexpr size_t kSm = 228 * 1024, kOwn = 1024 + 768;      // an SM's shared memory; what a CTA takes beside its dynamic part
   const int rows = a.group < kRows ? a.group : kRows;
-  const size_t three = attend_smem(DH, 3, rows), two = attend_smem(DH, 2, rows);
-  const int ctas = two <= kHalf ? 2 : 1;
+  constexpr int kWant = DH <= 80 ? 3 : DH <= 192 ? 2 : 1;
+  const int deep = static_cast<int>(kSm / (smem_of<DH>(3, rows) + kOwn)), flat = static_cast<int>(kSm / (smem_of<DH>(2, rows) + kOwn));
+  const bool three = deep >= kWant || deep >= flat;
+  const int ctas = std::min(kWant, three ? deep : flat);
   const long long most = static_cast<long long>(a.n) * a.c.heads * a.subs *
                          ((static_cast<long long>(a.c.max_pages) * a.c.page + kTile - 1) / kTile);
-  int grid = ctas * sms < kMaxGrid ? ctas * sms : kMaxGrid;
-  if (most < grid) grid = static_cast<int>(most);
-  if constexpr (DH > 96)                       // up to 96 columns three stages always fit
-    if (three > (ctas == 2 ? kHalf : kWhole)) return launch_run<T, DH, 2>(a, two, grid, st);
-  return launch_run<T, DH, 3>(a, three, grid, st);
+  const int grid = static_cast<int>(std::min<long long>(most, std::min(ctas * sms, kMaxGrid)));
+  return three ? launch_run<T, DH, 3>(a, smem_of<DH>(3, rows), grid, st) : launch_run<T, DH, 2>(a, smem_of<DH>(2, rows), grid, st);
 }
 
 template <typename T>
@@ -552,6 +619,9 @@ int map_cache_attend(const map_cache* c, int layer, const map_heads* q, const in
   a.n = n;
   a.group = q->heads / c->heads;
   a.subs = (a.group + kRows - 1) / kRows;
+  a.page_shift = -1;
+  for (int k = 0; k < 11; ++k)
+    if (c->page == 1 << k) a.page_shift = k;
   a.scale2 = scale * 1.4426950408889634f;
   a.ws = static_cast<float*>(ws);
   int dev = 0, sms = 0;
