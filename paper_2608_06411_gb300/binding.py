@@ -427,7 +427,7 @@ def _type(dtype) -> int:
 def _heads(t, rows: int, dh: int, dtype, device):
     """map_heads of a [rows, heads, dh] tensor with any strides but dh's."""
     n, h, d = t.shape
-    if n != rows or d != dh or t.dtype != dtype or t.device != device:
+    if n != rows or d != dh or t.dtype is not dtype or t.device != device:
         raise ValueError(f"heads must be [{rows}, heads, {dh}] {dtype} on {device}: got {tuple(t.shape)} {t.dtype} on {t.device}")
     sr, sh, sd = t.stride()
     if sd != 1 and d > 1:
@@ -435,11 +435,21 @@ def _heads(t, rows: int, dh: int, dtype, device):
     return _pack_heads(t.data_ptr(), sr, sh, h)
 
 
+_CONTIGUOUS = torch.contiguous_format
+
+
+def _like(t, dh: int):
+    """A new contiguous tensor of t's shape and type, and its map_heads."""
+    out = torch.empty_like(t, memory_format=_CONTIGUOUS)
+    h = t.shape[1]
+    return out, _pack_heads(out.data_ptr(), h * dh, dh, h)
+
+
 def _dense(t, dtype, device, shape=None, what="tensor"):
     """Pointer of a contiguous tensor of the wanted type, place and shape (None: NULL)."""
     if t is None:
         return None
-    if t.dtype != dtype or t.device != device or not t.is_contiguous() or (shape is not None and tuple(t.shape) != shape):
+    if t.dtype is not dtype or t.device != device or not t.is_contiguous() or (shape is not None and t.shape != shape):
         raise ValueError(f"{what} must be a contiguous {dtype} tensor on {device}" + (f" of shape {shape}" if shape else ""))
     return t.data_ptr()
 
@@ -483,13 +493,17 @@ class Rope:
         dt, dh, rows = x.dtype, self.dh, x.shape[0]
         a = b = oa = ob = None
         if q is not None:
+            a = _heads(q, rows, dh, dt, dev)
             if q_out is None:
-                q_out = torch.empty(q.shape, dtype=dt, device=dev)
-            a, oa = _heads(q, rows, dh, dt, dev), _heads(q_out, rows, dh, dt, dev)
+                q_out, oa = _like(q, dh)
+            else:
+                oa = _heads(q_out, rows, dh, dt, dev)
         if k is not None:
+            b = _heads(k, rows, dh, dt, dev)
             if k_out is None:
-                k_out = torch.empty(k.shape, dtype=dt, device=dev)
-            b, ob = _heads(k, rows, dh, dt, dev), _heads(k_out, rows, dh, dt, dev)
+                k_out, ob = _like(k, dh)
+            else:
+                ob = _heads(k_out, rows, dh, dt, dev)
         _check(lib.map_qk_rotate(self.h, _type(dt), rows, _dense(pos, torch.int32, dev, (self.n_axes, rows), "pos"), a, b,
                                  _dense(wq, dt, dev, (dh,), "wq"), _dense(wk, dt, dev, (dh,), "wk"), oa, ob,
                                  _current_stream(dev.index)), "map_qk_rotate")
@@ -507,9 +521,11 @@ class Rope:
         dt, dh, rows, f32 = x.dtype, self.dh, x.shape[0], torch.float32
         a = b = xa = xb = oa = ob = ws = None
         if dq_out is not None:
+            a = _heads(dq_out, rows, dh, dt, dev)
             if dq is None:
-                dq = torch.empty(dq_out.shape, dtype=dt, device=dev)
-            a, oa = _heads(dq_out, rows, dh, dt, dev), _heads(dq, rows, dh, dt, dev)
+                dq, oa = _like(dq_out, dh)
+            else:
+                oa = _heads(dq, rows, dh, dt, dev)
             if wq is not None:
                 if q is None:
                     raise ValueError("q is needed with wq")
@@ -517,9 +533,11 @@ class Rope:
                 if dwq is None:
                     dwq = torch.empty(dh, dtype=f32, device=dev)
         if dk_out is not None:
+            b = _heads(dk_out, rows, dh, dt, dev)
             if dk is None:
-                dk = torch.empty(dk_out.shape, dtype=dt, device=dev)
-            b, ob = _heads(dk_out, rows, dh, dt, dev), _heads(dk, rows, dh, dt, dev)
+                dk, ob = _like(dk_out, dh)
+            else:
+                ob = _heads(dk, rows, dh, dt, dev)
             if wk is not None:
                 if k is None:
                     raise ValueError("k is needed with wk")
@@ -546,9 +564,11 @@ class Rope:
             raise ValueError("k has the cache's type and device")
         a = oa = None
         if q is not None:
+            a = _heads(q, rows, dh, dt, dev)
             if q_out is None:
-                q_out = torch.empty(q.shape, dtype=dt, device=dev)
-            a, oa = _heads(q, rows, dh, dt, dev), _heads(q_out, rows, dh, dt, dev)
+                q_out, oa = _like(q, dh)
+            else:
+                oa = _heads(q_out, rows, dh, dt, dev)
         _check(lib.map_qk_rotate_append(self.h, cache.desc, layer, rows, _dense(pos, torch.int32, dev, (self.n_axes, rows), "pos"),
                                         _dense(slots, torch.int32, dev, (rows,), "slots"), a, _heads(k, rows, dh, dt, dev),
                                         _heads(v, rows, dh, dt, dev), _dense(wq, dt, dev, (dh,), "wq"),
@@ -644,11 +664,14 @@ class Cache:
             with _on(dev, stream):
                 return self.attend(q, seqs, layer, scale, out)
         dt, n, dh = self.pool.dtype, seqs.shape[0], self.dh
+        a = _heads(q, n, dh, dt, dev)
         if out is None:
-            out = torch.empty(q.shape, dtype=dt, device=dev)
+            out, oa = _like(q, dh)
+        else:
+            oa = _heads(out, n, dh, dt, dev)
         ws = torch.empty(self._attend_ws, dtype=torch.uint8, device=dev)
-        _check(lib.map_cache_attend(self.desc, layer, _heads(q, n, dh, dt, dev), _dense(seqs, torch.int32, dev, (n,), "seqs"),
-                                    n, dh ** -0.5 if scale is None else scale, _heads(out, n, dh, dt, dev), ws.data_ptr(),
+        _check(lib.map_cache_attend(self.desc, layer, a, _dense(seqs, torch.int32, dev, (n,), "seqs"), n,
+                                    dh ** -0.5 if scale is None else scale, oa, ws.data_ptr(),
                                     _current_stream(dev.index)), "map_cache_attend")
         return out
 

@@ -5,7 +5,10 @@
 // every call can be captured.  One CTA does it for a whole call: the entries' needs are added up in shared memory, the
 // free pages are those with a reference count of zero, and the r-th lowest of them goes to the r-th need.  Nothing but
 // the counts says what is free, so results follow from the state alone, and a fork that is freed leaves it as it was.
-// A call is checked whole before it changes a length or a count; until then it writes only table entries past a length.
+// A call is checked whole before it changes a length; until then it writes only table entries past a length, and counts
+// that it puts back where the pages do not suffice.
+// A bookkeeping call is a chain of loads that depend on one another (entries, lengths, counts, table: about 0.7 us each),
+// so entries are read once, all together, and nothing that is known is read back.
 #include "handoff.h"
 
 namespace mapk {
@@ -67,24 +70,46 @@ __device__ __forceinline__ int entry_of(const int* start, int n, int x) {
   return lo;
 }
 
-// The total lowest free pages into the table: need r of entry i (start[i] <= r < start[i + 1]) is column
-// col[i] + r - start[i] of row seq[i].  False if there are fewer.  Counts are left as they are.
+// The total lowest free pages into the table, each with one holder: need r of entry i (start[i] <= r < start[i + 1]) is
+// column col[i] + r - start[i] of row seq[i].  False, and all counts as they were, if there are fewer.
+// The first pages' counts are read ahead of the entries (HeadCounts): most calls need no others.
+constexpr int kPagesEach = 4;              // neighbouring pages a thread looks at
+struct HeadCounts {
+  int v[kPagesEach];
+  __device__ __forceinline__ void load(const map_cache& c, int p) {
+#pragma unroll
+    for (int k = 0; k < kPagesEach; ++k) v[k] = p + k < c.pages ? c.refs[p + k] : 1;
+  }
+};
 __device__ bool take_pages(const map_cache& c, const int* start, const int* col, const int* seq, int n, int total,
-                           int* warp_sums) {
+                           HeadCounts& counts, int* warp_sums) {
+  const auto entry = [&](int r) {
+    const int i = entry_of(start, n, r);
+    return c.table + static_cast<long long>(seq[i]) * c.max_pages + col[i] + r - start[i];
+  };
   int found = 0;
-  for (int p0 = 0; p0 < c.pages && found < total; p0 += kPlanThreads) {
-    const int p = p0 + threadIdx.x;
-    const bool free_page = p < c.pages && c.refs[p] == 0;
-    int got;
-    const int r = found + block_scan(free_page, warp_sums, &got);
-    if (free_page && r < total) {
-      const int i = entry_of(start, n, r);
-      c.table[static_cast<long long>(seq[i]) * c.max_pages + col[i] + r - start[i]] = p;
-    }
+  for (int p0 = 0; p0 < c.pages && found < total; p0 += kPlanThreads * kPagesEach) {
+    const int p = p0 + threadIdx.x * kPagesEach;
+    int mine = 0, got;
+    if (p0 > 0) counts.load(c, p);
+#pragma unroll
+    for (int k = 0; k < kPagesEach; ++k) mine += counts.v[k] == 0;
+    int r = found + block_scan(mine, warp_sums, &got);
+#pragma unroll
+    for (int k = 0; k < kPagesEach; ++k)
+      if (counts.v[k] == 0) {
+        if (r < total) {
+          *entry(r) = p + k;
+          c.refs[p + k] = 1;
+        }
+        ++r;
+      }
     found += got;
   }
   __syncthreads();
-  return found >= total;
+  if (found >= total) return true;
+  for (int r = threadIdx.x; r < found; r += kPlanThreads) c.refs[*entry(r)] = 0;
+  return false;
 }
 
 // counts[i] more rows for sequence seqs[i], and their slots.  Without counts entry i has row i, padding or not.
@@ -103,6 +128,8 @@ __global__ void __launch_bounds__(kPlanThreads) extend_kernel(const map_cache c,
   pdl_enter();
   for (int i = threadIdx.x; i < (c.seqs + 31) / 32; i += kPlanThreads) seen[i] = 0;
   if (threadIdx.x == 0) error = 0;
+  HeadCounts head;
+  head.load(c, threadIdx.x * kPagesEach);
   __syncthreads();
   int pages0 = 0, rows0 = 0;
   for (int i0 = 0; i0 < n; i0 += kPlanThreads) {
@@ -148,25 +175,30 @@ __global__ void __launch_bounds__(kPlanThreads) extend_kernel(const map_cache c,
   if (threadIdx.x == 0) { start[n] = pages0; row0[n] = rows0; }
   __syncthreads();
   const bool ok = error == 0;
-  const bool enough = ok && take_pages(c, start, col, seq, n, pages0, warp_sums);
+  const bool enough = ok && take_pages(c, start, col, seq, n, pages0, head, warp_sums);
   if (!enough) {
     if (threadIdx.x == 0) atomicOr(c.status, ok ? ST_NOPAGES : error);
     for (int r = threadIdx.x; r < rows; r += kPlanThreads) slots[r] = -1;
     return;
   }
-  for (int r = threadIdx.x; r < pages0; r += kPlanThreads) {
-    const int i = entry_of(start, n, r);
-    c.refs[c.table[static_cast<long long>(seq[i]) * c.max_pages + col[i] + r - start[i]]] = 1;
-  }
   for (int i = threadIdx.x; i < n; i += kPlanThreads)
     if (old[i] >= 0) c.len[seq[i]] = old[i] + row0[i + 1] - row0[i];
-  for (int r = threadIdx.x; r < rows; r += kPlanThreads) {
-    int slot = -1;
-    if (r < rows0) {
-      const int i = entry_of(row0, n, r), t = old[i] + r - row0[i];
-      if (old[i] >= 0) slot = c.table[static_cast<long long>(seq[i]) * c.max_pages + t / c.page] * c.page + t % c.page;
+  constexpr int kEach = 4;                 // table entries a thread reads at once
+  for (int r0 = threadIdx.x; r0 < rows; r0 += kEach * kPlanThreads) {
+    int page[kEach], in_page[kEach];
+#pragma unroll
+    for (int k = 0; k < kEach; ++k) {
+      const int r = r0 + k * kPlanThreads;
+      page[k] = -1;
+      if (r < rows0) {
+        const int i = entry_of(row0, n, r), t = old[i] + r - row0[i];
+        in_page[k] = t % c.page;
+        if (old[i] >= 0) page[k] = c.table[static_cast<long long>(seq[i]) * c.max_pages + t / c.page];
+      }
     }
-    slots[r] = slot;
+#pragma unroll
+    for (int k = 0; k < kEach; ++k)
+      if (r0 + k * kPlanThreads < rows) slots[r0 + k * kPlanThreads] = page[k] < 0 ? -1 : page[k] * c.page + in_page[k];
   }
 }
 
@@ -187,6 +219,8 @@ __global__ void __launch_bounds__(kPlanThreads) fork_plan_kernel(const map_cache
   pdl_enter();
   for (int i = threadIdx.x; i < (c.seqs + 31) / 32; i += kPlanThreads) seen[i] = 0;
   if (threadIdx.x == 0) error = 0;
+  HeadCounts head;
+  head.load(c, threadIdx.x * kPagesEach);
   __syncthreads();
   int pages0 = 0;
   for (int i0 = 0; i0 < n; i0 += kPlanThreads) {
@@ -233,62 +267,89 @@ __global__ void __launch_bounds__(kPlanThreads) fork_plan_kernel(const map_cache
     if (seen[par[i] >> 5] >> (par[i] & 31) & 1u && error == 0) atomicOr(&error, ST_BADINDEX);
   __syncthreads();
   const bool ok = error == 0;
-  const bool enough = ok && take_pages(c, start, col, seq, n, pages0, warp_sums);
+  const bool enough = ok && take_pages(c, start, col, seq, n, pages0, head, warp_sums);
   if (threadIdx.x == 0) {
     c.status[1] = enough;
     if (!enough) atomicOr(c.status, ok ? ST_NOPAGES : error);
   }
   if (!enough) return;
-  for (int r = threadIdx.x; r < pages0; r += kPlanThreads) {
-    const int i = entry_of(start, n, r);
-    c.refs[c.table[static_cast<long long>(seq[i]) * c.max_pages + col[i] + r - start[i]]] = 1;
-  }
   for (int i = threadIdx.x >> 5; i < n; i += kPlanThreads / 32) {        // a warp an entry
     const int32_t* from = c.table + static_cast<long long>(par[i]) * c.max_pages;
     int32_t* to = c.table + static_cast<long long>(seq[i]) * c.max_pages;
     for (int j = threadIdx.x & 31; j < col[i]; j += 32) {
-      to[j] = from[j];
-      atomicAdd(&c.refs[from[j]], 1);
+      const int page = from[j];
+      to[j] = page;
+      atomicAdd(&c.refs[page], 1);
     }
     if ((threadIdx.x & 31) == 0) c.len[seq[i]] = len[i];
   }
 }
 
-// The rows of the children's own pages: a unit is one new page of one plane (K or V of a layer).
-constexpr int kCopyThreads = 256;
-__global__ void __launch_bounds__(kCopyThreads) fork_copy_kernel(const map_cache c, const int32_t* __restrict__ parents,
-                                                                 const int32_t* __restrict__ children, int n,
-                                                                 const int32_t* __restrict__ keep, int k,
-                                                                 const int32_t* __restrict__ base,
-                                                                 const int32_t* __restrict__ span) {
+// The rows of the children's own pages, HBM-bound (each row read once and written once, in every plane: K or V of a
+// layer).  A unit is one head of one new page in one plane, a slab of page * dh elements; a block takes an equal run of
+// the units, page by page, so that it looks a page's source rows up once.  Full occupancy with one vector a thread in
+// flight reads and writes at 6.4 TB/s (53 us for 8 questions on an image in 32 layers, 342 MB; two in flight 56, four with
+// six CTAs an SM 60).
+// What comes before griddepcontrol.wait (shapes, the parents' tables) fork_plan_kernel only reads, and so runs beside it.
+constexpr int kCopyThreads = 256, kCopyGrid = 152 * 8;
+__global__ void __launch_bounds__(kCopyThreads, 8) fork_copy_kernel(const map_cache c, const int32_t* __restrict__ parents,
+                                                                    const int32_t* __restrict__ children, int n,
+                                                                    const int32_t* __restrict__ keep, int k,
+                                                                    const int32_t* __restrict__ base,
+                                                                    const int32_t* __restrict__ span) {
   extern __shared__ int sh[];
   int* start = sh;                         // [n + 1] new pages before entry i
   int* from = sh + n + 1;                  // [page] source slot of each row: -1 none, -2 a bad index
-  pdl_enter();
-  if (c.status[1] == 0) return;
-  if (threadIdx.x == 0) {
-    int s = 0;
-    for (int i = 0; i < n; ++i) {
-      start[i] = s;
-      const ForkShape f = fork_shape(c.len[parents[i]], c.page, base != nullptr, base ? base[i] : 0, span ? span[i] : 0, k);
-      s += (f.len + c.page - 1) / c.page - f.shared;
-    }
-    start[n] = s;
+  __shared__ int warp_sums[kCopyThreads / 32];
+  const bool kept = base != nullptr;
+  const auto shape = [&](int i) {
+    const int p = parents[i], plen = p >= 0 && p < c.seqs ? c.len[p] : 0;
+    return fork_shape(plen, c.page, kept, kept ? base[i] : 0, kept ? span[i] : 0, k);
+  };
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  // a thread counts a run of the entries (a refused call may have any numbers here: nothing is copied for it)
+  const int each = (n + kCopyThreads - 1) / kCopyThreads, e0 = threadIdx.x * each, e1 = min(n, e0 + each);
+  int mine = 0;
+  for (int i = e0; i < e1; ++i) {
+    const ForkShape f = shape(i);
+    start[i] = mine;
+    mine += max(0, (f.len + c.page - 1) / c.page - f.shared);
   }
+  int incl = mine;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int u = __shfl_up_sync(0xffffffffu, incl, o);
+    if ((threadIdx.x & 31) >= o) incl += u;
+  }
+  if ((threadIdx.x & 31) == 31) warp_sums[threadIdx.x >> 5] = incl;
   __syncthreads();
-  const int planes = 2 * c.layers, vec = c.dh / 8, per_plane = c.heads * c.page * vec;
-  const long long units = static_cast<long long>(start[n]) * planes;
-  for (long long u = blockIdx.x; u < units; u += gridDim.x) {
-    const int r = static_cast<int>(u / planes), plane = static_cast<int>(u % planes), i = entry_of(start, n, r);
+  int before = incl - mine;
+  for (int w = 0; w < static_cast<int>(threadIdx.x >> 5); ++w) before += warp_sums[w];
+  for (int i = e0; i < e1; ++i) start[i] += before;
+  if (threadIdx.x == kCopyThreads - 1) start[n] = before + mine;
+  __syncthreads();
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  if (c.status[1] == 0) return;
+
+  const int vec = c.dh / 8, slab = c.page * vec, of_page = 2 * c.layers * c.heads;
+  const long long units = static_cast<long long>(start[n]) * of_page, plane = static_cast<long long>(c.pages) * c.heads * slab;
+  const long long u1 = units * (blockIdx.x + 1) / gridDim.x;
+  uint4* pool = static_cast<uint4*>(c.pool);
+  // threads beyond a slab take further units
+  const int lanes = min(slab, kCopyThreads), subs = kCopyThreads / lanes, sub = threadIdx.x / lanes;
+  for (long long u = units * blockIdx.x / gridDim.x; u < u1;) {
+    const int r = static_cast<int>(u / of_page), a0 = static_cast<int>(u % of_page);
+    const int a1 = static_cast<int>(min(static_cast<long long>(of_page), a0 + u1 - u)), i = entry_of(start, n, r);
     const int32_t* ptab = c.table + static_cast<long long>(parents[i]) * c.max_pages;
-    const ForkShape f = fork_shape(c.len[parents[i]], c.page, base != nullptr, base ? base[i] : 0, span ? span[i] : 0, k);
+    const ForkShape f = shape(i);
     const int colm = f.shared + r - start[i];
+    const int to_page = c.table[static_cast<long long>(children[i]) * c.max_pages + colm];
     __syncthreads();
     for (int t = threadIdx.x; t < c.page; t += kCopyThreads) {
       const int j = colm * c.page + t;
       int src = j;
       bool bad = false;
-      if (j >= f.base && base) {
+      if (j >= f.base && kept) {
         if (j < f.base + k) {
           const int x = keep[static_cast<long long>(i) * k + j - f.base];
           bad = x < 0 || x >= f.span;
@@ -298,18 +359,27 @@ __global__ void __launch_bounds__(kCopyThreads) fork_copy_kernel(const map_cache
         }
       }
       if (j >= f.len) from[t] = -1;
-      else if (bad) { from[t] = -2; if (plane == 0) atomicOr(c.status, ST_BADINDEX); }
+      else if (bad) { from[t] = -2; atomicOr(c.status, ST_BADINDEX); }
       else from[t] = ptab[src / c.page] * c.page + src % c.page;
     }
     __syncthreads();
-    uint4* pool = static_cast<uint4*>(c.pool) + static_cast<long long>(plane) * c.pages * per_plane;
-    uint4* to = pool + static_cast<long long>(c.table[static_cast<long long>(children[i]) * c.max_pages + colm]) * per_plane;
-    for (int v = threadIdx.x; v < per_plane; v += kCopyThreads) {
-      const int x = v % vec, t = v / vec % c.page, h = v / vec / c.page, s = from[t];
-      if (s == -1) continue;
-      to[v] = s < 0 ? make_uint4(0, 0, 0, 0)
-                    : pool[static_cast<long long>(s / c.page) * per_plane + (h * c.page + s % c.page) * vec + x];
+    if (sub < subs) {
+      for (int e = threadIdx.x % lanes; e < slab; e += lanes) {
+        const int t = e / vec, s = from[t];
+        if (s == -1) continue;
+        const uint4* src = pool + static_cast<long long>(s < 0 ? 0 : s / c.page) * c.heads * slab + (s < 0 ? 0 : s % c.page * vec + e % vec);
+        uint4* dst = pool + static_cast<long long>(to_page) * c.heads * slab + e;
+        // unit b = (plane b / heads, head b % heads) lies `at` past the first
+        int h = (a0 + sub) % c.heads;
+        long long at = (a0 + sub) / c.heads * plane + h * slab;
+        for (int b = a0 + sub; b < a1; b += subs) {
+          dst[at] = s < 0 ? make_uint4(0, 0, 0, 0) : src[at];
+          at += subs * slab;
+          for (h += subs; h >= c.heads; h -= c.heads) at += plane - c.heads * slab;
+        }
+      }
     }
+    u += a1 - a0;
   }
 }
 
@@ -378,7 +448,7 @@ int map_cache_fork(const map_cache* c, const int32_t* parents, const int32_t* ch
     e = launch_k(fork_plan_kernel, dim3(1), dim3(kPlanThreads), smem, st, *c, parents, children, n,
                  base != nullptr ? 1 : 0, k, base, span);
   if (e == cudaSuccess)
-    e = launch_k(fork_copy_kernel, dim3(1216), dim3(kCopyThreads), (n + 1 + static_cast<size_t>(c->page)) * 4, st, *c,
+    e = launch_k(fork_copy_kernel, dim3(kCopyGrid), dim3(kCopyThreads), (n + 1 + static_cast<size_t>(c->page)) * 4, st, *c,
                  parents, children, n, keep, k, base, span);
   return launch_err(e);
 }

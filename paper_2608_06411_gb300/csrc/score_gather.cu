@@ -206,18 +206,21 @@ __global__ void assemble_kernel(const __grid_constant__ AssembleChunk m, const u
   for (int v = threadIdx.x; v < vec_per_row; v += blockDim.x) d[v] = __ldg(src + v);
 }
 
+// (A launch copies its parameters: a table of 512 images, 18 KB, costs it 2 us more than one of 32.)
+template <int IMAGES>
 struct AxesChunk {
   int b0, count, N, k, pos_offset;
   long long rows;                   // of all images: distance of the axes in pos
-  int32_t lens[kAsmImages];
-  int32_t frames[kAsmImages], height[kAsmImages], width[kAsmImages], t_step[kAsmImages];
-  long long text_row[kAsmImages];
-  long long seq_row[kAsmImages];
+  int32_t lens[IMAGES];
+  int32_t frames[IMAGES], height[IMAGES], width[IMAGES], t_step[IMAGES];
+  long long text_row[IMAGES];
+  long long seq_row[IMAGES];
 };
 
 // The same with positions on three axes: kept token n of a frames x height x width grid at
 // (n / (height width) t_step, n / width % height, n % width), the question after the grid's largest position.
-__global__ void assemble_axes_kernel(const __grid_constant__ AxesChunk m, const uint4* __restrict__ V,
+template <int IMAGES>
+__global__ void assemble_axes_kernel(const __grid_constant__ AxesChunk<IMAGES> m, const uint4* __restrict__ V,
                                      const int32_t* __restrict__ idx, const uint4* __restrict__ T, int vec_per_row,
                                      uint4* __restrict__ seq, int32_t* __restrict__ pos, int* status) {
   pdl_enter();
@@ -319,16 +322,17 @@ cudaError_t launch_assemble(const void* V, const int32_t* idx, const void* T, co
   return cudaSuccess;
 }
 
-cudaError_t launch_assemble_axes(const void* V, const int32_t* idx, const void* T, const int32_t* lens,
-                                 const int32_t* grids, const int32_t* t_step, int B, int N, int k, int D,
-                                 int pos_offset, void* seq, int32_t* pos, int* status, cudaStream_t st) {
-  if (D % 8 != 0) return cudaErrorInvalidValue;
+namespace {
+template <int IMAGES>
+cudaError_t assemble_axes(const void* V, const int32_t* idx, const void* T, const int32_t* lens, const int32_t* grids,
+                          const int32_t* t_step, int B, int N, int k, int D, int pos_offset, void* seq, int32_t* pos,
+                          int* status, cudaStream_t st) {
   long long trow = 0, srow = 0, rows = 0;
   for (int b = 0; b < B; ++b) rows += k + lens[b];
-  for (int b0 = 0; b0 < B; b0 += kAsmImages) {
-    AxesChunk m;
+  for (int b0 = 0; b0 < B; b0 += IMAGES) {
+    AxesChunk<IMAGES> m;
     m.b0 = b0;
-    m.count = B - b0 < kAsmImages ? B - b0 : kAsmImages;
+    m.count = B - b0 < IMAGES ? B - b0 : IMAGES;
     m.N = N;
     m.k = k;
     m.pos_offset = pos_offset;
@@ -348,12 +352,21 @@ cudaError_t launch_assemble_axes(const void* V, const int32_t* idx, const void* 
       max_rows = std::max(max_rows, k + lens[b]);
     }
     if (max_rows == 0) continue;
-    const cudaError_t e = launch_k(assemble_axes_kernel, dim3(max_rows, m.count), dim3(128), 0, st, m,
+    const cudaError_t e = launch_k(assemble_axes_kernel<IMAGES>, dim3(max_rows, m.count), dim3(128), 0, st, m,
                                    static_cast<const uint4*>(V), idx, static_cast<const uint4*>(T), D / 8,
                                    static_cast<uint4*>(seq), pos, status);
     if (e != cudaSuccess) return e;
   }
   return cudaSuccess;
+}
+}  // namespace
+
+cudaError_t launch_assemble_axes(const void* V, const int32_t* idx, const void* T, const int32_t* lens,
+                                 const int32_t* grids, const int32_t* t_step, int B, int N, int k, int D,
+                                 int pos_offset, void* seq, int32_t* pos, int* status, cudaStream_t st) {
+  if (D % 8 != 0) return cudaErrorInvalidValue;
+  return B <= 32 ? assemble_axes<32>(V, idx, T, lens, grids, t_step, B, N, k, D, pos_offset, seq, pos, status, st)
+                 : assemble_axes<kAsmImages>(V, idx, T, lens, grids, t_step, B, N, k, D, pos_offset, seq, pos, status, st);
 }
 
 cudaError_t launch_flags_to_host(const int32_t* a, const int* b, int32_t* a_host_dev, int* b_host_dev, cudaStream_t st) {
