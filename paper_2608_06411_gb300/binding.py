@@ -144,6 +144,25 @@ def _lens(lens) -> tuple:
     return arr, arr.ctypes.data_as(POINTER(c_int32))
 
 
+def _host_ints(x, rows: int, cols: int, what: str) -> bytes:
+    """int32 [rows] or [rows, cols] as bytes, from an array, or a sequence (of sequences) of whole numbers."""
+    if isinstance(x, (np.ndarray, torch.Tensor)):
+        x = np.asarray(x)
+        if x.dtype.kind not in "iu" or x.shape != ((rows,) if cols == 1 else (rows, cols)):
+            raise ValueError(f"{what} must be {rows} x {cols} whole numbers")
+        x = x.reshape(-1).tolist()
+    elif cols > 1:
+        if any(len(r) != cols for r in x):
+            raise ValueError(f"{what} must be {rows} x {cols} whole numbers")
+        x = [v for r in x for v in r]
+    if len(x) != rows * cols:
+        raise ValueError(f"{what} must be {rows} x {cols} whole numbers")
+    try:
+        return struct.pack(f"{rows * cols}i", *x)
+    except struct.error as e:
+        raise ValueError(f"{what} must be {rows} x {cols} whole numbers: {e}") from None
+
+
 def default_config() -> MapConfig:
     cfg = MapConfig()
     _check(lib.map_config_default(ctypes.byref(cfg)), "map_config_default")
@@ -239,19 +258,18 @@ class Context:
         that are grids of grids[b] = (T, H, W) tokens, t_step[b] positions from frame to frame (default 1)."""
         B, N, D = vis.shape
         k = keep.shape[1]
-        m = np.array(lens, np.int32)
-        g = np.array(grids, np.int32)
-        t = None if t_step is None else np.array(t_step, np.int32)
-        if m.shape != (B,) or g.shape != (B, 3) or (t is not None and t.shape != (B,)) or keep.shape[0] != B:
-            raise ValueError("lens and t_step have one entry an image, grids three, keep one row")
-        rows = B * k + int(m.sum())
+        if keep.shape[0] != B:
+            raise ValueError("keep has one row an image")
+        m = _host_ints(lens, B, 1, "lens")
+        g = _host_ints(grids, B, 3, "grids")
+        t = None if t_step is None else _host_ints(t_step, B, 1, "t_step")
+        rows = B * k + int(sum(lens))
         if seq is None:
             seq = torch.empty((rows, D), dtype=vis.dtype, device=vis.device)
         if pos is None:
             pos = torch.empty((3, rows), dtype=torch.int32, device=vis.device)
         s = _current_stream(vis.device.index) if stream is None else stream.cuda_stream
-        _check(lib.map_assemble_axes(self.h, _ptr(vis), _ptr(keep), _ptr(text), m.tobytes(), g.tobytes(),
-                                     None if t is None else t.tobytes(), B, N, k, pos_offset, _ptr(seq), _ptr(pos), s),
+        _check(lib.map_assemble_axes(self.h, _ptr(vis), _ptr(keep), _ptr(text), m, g, t, B, N, k, pos_offset, _ptr(seq), _ptr(pos), s),
                "map_assemble_axes")
         return seq, pos
 
@@ -435,12 +453,9 @@ def _heads(t, rows: int, dh: int, dtype, device):
     return _pack_heads(t.data_ptr(), sr, sh, h)
 
 
-_CONTIGUOUS = torch.contiguous_format
-
-
 def _like(t, dh: int):
     """A new contiguous tensor of t's shape and type, and its map_heads."""
-    out = torch.empty_like(t, memory_format=_CONTIGUOUS)
+    out = torch.empty(t.shape, dtype=t.dtype, device=t.device)
     h = t.shape[1]
     return out, _pack_heads(out.data_ptr(), h * dh, dh, h)
 
@@ -596,7 +611,8 @@ class Cache:
         self.pool, self.table, self.length, self.refs, self.status_word = pool, table, length, refs, status
         self.device, self.heads, self.page, self.dh = dev, heads, page, dh
         self.desc = _pack_cache(pool.data_ptr(), *ptrs, TYPES[pool.dtype], layers, pages, heads, page, dh, seqs, max_pages)
-        self._attend_ws = int(lib.map_cache_attend_workspace(self.desc))
+        # attend's scratch: calls on one cache are ordered by the caller, so they can share it
+        self._ws = torch.empty(int(lib.map_cache_attend_workspace(self.desc)), dtype=torch.uint8, device=dev)
 
     @classmethod
     def empty(cls, layers: int, pages: int, heads: int, page: int, dh: int, seqs: int, max_pages: int,
@@ -669,9 +685,8 @@ class Cache:
             out, oa = _like(q, dh)
         else:
             oa = _heads(out, n, dh, dt, dev)
-        ws = torch.empty(self._attend_ws, dtype=torch.uint8, device=dev)
         _check(lib.map_cache_attend(self.desc, layer, a, _dense(seqs, torch.int32, dev, (n,), "seqs"), n,
-                                    dh ** -0.5 if scale is None else scale, oa, ws.data_ptr(),
+                                    dh ** -0.5 if scale is None else scale, oa, self._ws.data_ptr(),
                                     _current_stream(dev.index)), "map_cache_attend")
         return out
 

@@ -55,13 +55,30 @@ __device__ __forceinline__ int side_of_block(const Job& job) {
   return (blockIdx.x >= job.first[1] ? 1 : 0) + (blockIdx.x >= job.first[2] ? 1 : 0);
 }
 
+// cos and sin of a 32-bit fraction of a turn: the nearest quarter turn off, the rest x (|x| <= pi / 4) by the Taylor
+// series of both to x^9 and x^10, whose next terms are below 2e-9 and 2e-10; fp32 roundings add up to 2^-23.
+__device__ __forceinline__ float2 cos_sin(uint32_t turn) {
+  const uint32_t quarter = (turn + 0x20000000u) >> 30;
+  const float x = static_cast<float>(static_cast<int>(turn - (quarter << 30))) * 1.46291807926715968e-9f;   // 2 pi 2^-32
+  const float y = x * x;
+  float s = fmaf(y, 2.75573192e-6f, -1.98412698e-4f);
+  s = fmaf(s, y, 8.33333333e-3f);
+  s = fmaf(s, y, -1.66666667e-1f);
+  s = fmaf(s * y, x, x);
+  float c = fmaf(y, -2.75573192e-7f, 2.48015873e-5f);
+  c = fmaf(c, y, -1.38888889e-3f);
+  c = fmaf(c, y, 4.16666667e-2f);
+  c = fmaf(c, y, -0.5f);
+  c = fmaf(c, y, 1.f);
+  const float co = quarter & 1 ? s : c, si = quarter & 1 ? c : s;
+  return make_float2((quarter + 1) & 2 ? -co : co, quarter & 2 ? -si : si);
+}
+
 __device__ __forceinline__ float2 turn_of(const RopeTab& t, int pair, const int32_t* __restrict__ pos, long long rows,
                                           long long row) {
   const unsigned long long ph =
       t.turn[pair] * static_cast<unsigned long long>(static_cast<long long>(__ldg(pos + t.axis[pair] * rows + row)));
-  float s, c;
-  sincospif(static_cast<float>(static_cast<int>(ph >> 32)) * 0x1p-31f, &s, &c);
-  return make_float2(c, s);
+  return cos_sin(static_cast<uint32_t>(ph >> 32));
 }
 
 // Whether a row is written: not for slot -1 (padding), nor for one outside the pool, which is reported.
@@ -331,12 +348,11 @@ struct Turns {
     for (int p0 = 0; p0 < half; p0 += 32) {
       const int p = p0 + lane;
       const int x = __shfl_sync(0xffffffffu, at, p < half ? f.axis[p] : 0);
-      if (p >= half) break;
+      if (p >= half) break;                            // (in the last round only)
       const unsigned long long ph = f.turn[p] * static_cast<unsigned long long>(static_cast<long long>(x));
-      float si, co;
-      sincospif(static_cast<float>(static_cast<int>(ph >> 32)) * 0x1p-31f, &si, &co);
-      buf[(p >> 1) * 4 + (p & 1)] = co;                // (c, c, s, s) of two pairs
-      buf[(p >> 1) * 4 + 2 + (p & 1)] = si;
+      const float2 cs = cos_sin(static_cast<uint32_t>(ph >> 32));
+      buf[(p >> 1) * 4 + (p & 1)] = cs.x;              // (c, c, s, s) of two pairs
+      buf[(p >> 1) * 4 + 2 + (p & 1)] = cs.y;
     }
     __syncwarp();
 #pragma unroll
@@ -824,15 +840,21 @@ int shift_of(const RopeTab& t, int v) {
   return s;
 }
 
-// Blocks of the sides: `limit` in proportion to their passes of `per` heads, at most one for kWarps passes.
+// Blocks of the sides: `limit` in proportion to what a row of them costs, at most one for kWarps passes of `per` heads.
+// In thirds of a pass: a pass 3 (of values, which are copied, 2), a row's turns 2.  (By passes alone the keys of grouped
+// heads, with a pass a row, were the last to end: the gradient of 16171 rows of 28 and 4 heads took 100 us, not 82.)
 void spread_blocks(Job& job, int sides, int per, int limit) {
-  long long passes[3] = {}, all = 0;
-  for (int i = 0; i < sides; ++i) all += passes[i] = job.rows * ((job.s[i].heads + per - 1) / per);
+  long long passes[3] = {}, cost[3] = {}, all = 0;
+  for (int i = 0; i < sides; ++i) {
+    const long long of_row = (job.s[i].heads + per - 1) / per;
+    passes[i] = job.rows * of_row;
+    all += cost[i] = job.rows * (job.s[i].kind == kValues ? 2 * of_row : 3 * of_row + 2);
+  }
   unsigned at = 0;
   for (int i = 0; i < 4; ++i) {
     job.first[i] = at;
     if (i >= sides) continue;
-    const long long share = std::max(1ll, limit * passes[i] / all), most = (passes[i] + kWarps - 1) / kWarps;
+    const long long share = std::max(1ll, limit * cost[i] / all), most = (passes[i] + kWarps - 1) / kWarps;
     at += static_cast<unsigned>(std::min(share, most));
   }
 }
