@@ -63,7 +63,7 @@ SIGNATURES = {
                                  c_int, c_void_p, c_void_p, c_void_p, c_void_p]),
     "map_assemble_ragged": (c_int, [c_void_p, c_void_p, c_void_p, c_void_p, POINTER(c_int32), POINTER(c_int32),
                                     c_int, c_int, c_int, c_int, c_void_p, c_void_p, c_void_p]),
-    "map_assemble_axes": (c_int, [c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_int, c_int, c_int, c_int, c_void_p, c_void_p, c_void_p]),
+    "map_assemble_axes": (c_int, [c_void_p] * 7 + [c_int] * 4 + [c_void_p] * 3),
     "map_rope_init": (c_int, [c_int, c_int, c_int, c_int, POINTER(c_double), POINTER(c_int32), c_double,
                               POINTER(c_void_p)]),
     "map_rope_destroy": (None, [c_void_p]),
@@ -258,19 +258,28 @@ class Context:
         that are grids of grids[b] = (T, H, W) tokens, t_step[b] positions from frame to frame (default 1)."""
         B, N, D = vis.shape
         k = keep.shape[1]
-        if keep.shape[0] != B:
-            raise ValueError("keep has one row an image")
+        if vis.device.type != "cuda" or D != self.cfg.D or vis.element_size() != 2:
+            raise ValueError(f"vis must be [B, N, {self.cfg.D}] of a 2-byte type on a CUDA device")
+        if keep.shape[0] != B or keep.dtype is not torch.int32:
+            raise ValueError("keep must be int32 [B, k]")
         m = _host_ints(lens, B, 1, "lens")
         g = _host_ints(grids, B, 3, "grids")
         t = None if t_step is None else _host_ints(t_step, B, 1, "t_step")
-        rows = B * k + int(sum(lens))
+        questions = int(sum(lens))
+        rows = B * k + questions
+        if text.shape[0] < questions or text.shape[1] != D:
+            raise ValueError(f"text must be [sum(lens), {D}]")
         if seq is None:
             seq = torch.empty((rows, D), dtype=vis.dtype, device=vis.device)
+        elif seq.shape != (rows, D):
+            raise ValueError(f"seq must be [{rows}, {D}]")
         if pos is None:
             pos = torch.empty((3, rows), dtype=torch.int32, device=vis.device)
+        elif pos.shape != (3, rows) or pos.dtype is not torch.int32:
+            raise ValueError(f"pos must be int32 [3, {rows}]")
         s = _current_stream(vis.device.index) if stream is None else stream.cuda_stream
-        _check(lib.map_assemble_axes(self.h, _ptr(vis), _ptr(keep), _ptr(text), m, g, t, B, N, k, pos_offset, _ptr(seq), _ptr(pos), s),
-               "map_assemble_axes")
+        _check(lib.map_assemble_axes(self.h, _ptr(vis), _ptr(keep), _ptr(text), m, g, t, B, N, k, pos_offset, _ptr(seq),
+                                     _ptr(pos), s), "map_assemble_axes")
         return seq, pos
 
     # -- ragged batches (padded layout, n_valid tokens per image) ---------------------------

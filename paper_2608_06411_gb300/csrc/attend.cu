@@ -45,7 +45,8 @@ struct AttendArgs {
 
 __device__ __forceinline__ int seq_len(const AttendArgs& a, int i) {
   const int s = __ldg(a.seqs + i);
-  return s >= 0 && s < a.c.seqs ? max(0, __ldg(a.c.len + s)) : 0;
+  const int len = s >= 0 && s < a.c.seqs ? __ldg(a.c.len + s) : 0;
+  return good_len(a.c, len) ? len : 0;
 }
 
 __device__ __forceinline__ int seq_tiles(const AttendArgs& a, int i) { return (seq_len(a, i) + kTile - 1) / kTile; }
@@ -252,7 +253,8 @@ __global__ void __launch_bounds__(kThreads, DH <= 80 ? 3 : DH <= 192 ? 2 : 1) at
     const int s = __ldg(a.seqs + e);
     if (s < 0 || s >= a.c.seqs) {
       if (s != -1 && tid == 0) atomicOr(a.c.status, ST_BADINDEX);
-    } else if (__ldg(a.c.len + s) <= 0) {
+    } else if (const int len = __ldg(a.c.len + s); len == 0 || !good_len(a.c, len)) {
+      if (len != 0 && tid == 0) atomicOr(a.c.status, ST_BADINDEX);
       T* out = static_cast<T*>(a.out.p) + e * a.out.row;
       for (int x = tid; x < a.out.heads * DH; x += kThreads) out[x / DH * a.out.head + x % DH] = from_f32<T>(0.f);
     }
@@ -306,6 +308,10 @@ __global__ void __launch_bounds__(kThreads, DH <= 80 ? 3 : DH <= 192 ? 2 : 1) at
     }
     const int tok0 = ld.t * kTile + warp * kTok, valid = ld.len - tok0;
     if (valid > 0) {
+      if (!good_page(a.c, pid)) {              // (here, a tile after it was asked for: a check there would wait for it)
+        atomicOr(a.c.status, ST_BADINDEX);
+        pid = 0;
+      }
       const uint32_t dst = ring + slot * R::kStage;
       if (whole) {
         const long long first = ((static_cast<long long>(pid) * a.c.heads + kh) * a.c.page + row_in_page(tok0)) * DH;

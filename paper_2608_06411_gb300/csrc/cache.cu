@@ -148,7 +148,10 @@ __global__ void __launch_bounds__(kPlanThreads) extend_kernel(const map_cache c,
         } else {
           const int len = c.len[s];
           const long long pages = (static_cast<long long>(len) + add + c.page - 1) / c.page;
-          if (pages > c.max_pages) {
+          if (!good_len(c, len)) {
+            atomicOr(&error, ST_BADINDEX);
+            add = 0;
+          } else if (pages > c.max_pages) {
             atomicOr(&error, ST_NOPAGES);
             add = 0;
           } else {
@@ -194,6 +197,10 @@ __global__ void __launch_bounds__(kPlanThreads) extend_kernel(const map_cache c,
         const int i = entry_of(row0, n, r), t = old[i] + r - row0[i];
         in_page[k] = t % c.page;
         if (old[i] >= 0) page[k] = c.table[static_cast<long long>(seq[i]) * c.max_pages + t / c.page];
+        if (old[i] >= 0 && !good_page(c, page[k])) {
+          atomicOr(c.status, ST_BADINDEX);
+          page[k] = -1;
+        }
       }
     }
 #pragma unroll
@@ -234,7 +241,7 @@ __global__ void __launch_bounds__(kPlanThreads) fork_plan_kernel(const map_cache
         atomicOr(&error, ST_BADINDEX);
       } else {
         const int plen = c.len[p], b = kept ? base[i] : 0, sp = kept ? span[i] : 0;
-        if (b < 0 || sp < 0 || static_cast<long long>(b) + sp > plen) {
+        if (!good_len(c, plen) || b < 0 || sp < 0 || static_cast<long long>(b) + sp > plen) {
           atomicOr(&error, ST_BADINDEX);
         } else {
           // a child longer than its parent (keep may repeat rows) can pass its table row, or 2^31
@@ -279,7 +286,8 @@ __global__ void __launch_bounds__(kPlanThreads) fork_plan_kernel(const map_cache
     for (int j = threadIdx.x & 31; j < col[i]; j += 32) {
       const int page = from[j];
       to[j] = page;
-      atomicAdd(&c.refs[page], 1);
+      if (good_page(c, page)) atomicAdd(&c.refs[page], 1);
+      else atomicOr(c.status, ST_BADINDEX);
     }
     if ((threadIdx.x & 31) == 0) c.len[seq[i]] = len[i];
   }
@@ -303,7 +311,7 @@ __global__ void __launch_bounds__(kCopyThreads, 8) fork_copy_kernel(const map_ca
   __shared__ int warp_sums[kCopyThreads / 32];
   const bool kept = base != nullptr;
   const auto shape = [&](int i) {
-    const int p = parents[i], plen = p >= 0 && p < c.seqs ? c.len[p] : 0;
+    const int p = parents[i], plen = p >= 0 && p < c.seqs && good_len(c, c.len[p]) ? c.len[p] : 0;
     return fork_shape(plen, c.page, kept, kept ? base[i] : 0, kept ? span[i] : 0, k);
   };
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
@@ -358,9 +366,11 @@ __global__ void __launch_bounds__(kCopyThreads, 8) fork_copy_kernel(const map_ca
           src = j - k + f.span;
         }
       }
+      const int page = j < f.len && !bad ? ptab[src / c.page] : 0;
+      bad = bad || !good_page(c, page);
       if (j >= f.len) from[t] = -1;
       else if (bad) { from[t] = -2; atomicOr(c.status, ST_BADINDEX); }
-      else from[t] = ptab[src / c.page] * c.page + src % c.page;
+      else from[t] = page * c.page + src % c.page;
     }
     __syncthreads();
     if (sub < subs) {
@@ -395,8 +405,16 @@ __global__ void __launch_bounds__(256) free_kernel(const map_cache c, const int3
   }
   int len = lane == 0 ? atomicExch(&c.len[s], 0) : 0;
   len = __shfl_sync(0xffffffffu, len, 0);
+  if (!good_len(c, len)) {
+    if (lane == 0) atomicOr(c.status, ST_BADINDEX);
+    return;
+  }
   const int32_t* row = c.table + static_cast<long long>(s) * c.max_pages;
-  for (int j = lane; j < (len + c.page - 1) / c.page; j += 32) atomicSub(&c.refs[row[j]], 1);
+  for (int j = lane; j < (len + c.page - 1) / c.page; j += 32) {
+    const int page = row[j];
+    if (good_page(c, page)) atomicSub(&c.refs[page], 1);
+    else atomicOr(c.status, ST_BADINDEX);
+  }
 }
 
 cudaError_t allow_smem(const void* kern, size_t bytes) {

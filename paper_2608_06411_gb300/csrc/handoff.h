@@ -38,6 +38,13 @@ inline bool distinct_vectors(long long row, long long rows, long long head, long
   return (head >= dh && row >= (heads - 1) * head + dh) || (row >= dh && head >= (rows - 1) * row + dh);
 }
 
+// Whether a table entry is a page of the pool, and a length one that a table row can hold: what a call finds in the
+// caller's arrays is checked before it becomes an address.
+__device__ __forceinline__ bool good_page(const map_cache& c, int page) {
+  return static_cast<unsigned>(page) < static_cast<unsigned>(c.pages);
+}
+__device__ __forceinline__ bool good_len(const map_cache& c, int len) { return len >= 0 && len <= c.max_pages * c.page; }
+
 // MAP_OK, MAP_EINVAL or MAP_EUNSUPPORTED for a cache's description (host values only).
 int check_cache(const map_cache* c);
 

@@ -940,8 +940,9 @@ int map_rope_init(int dh, int rot, int adjacent, int n_axes, const double* inv_f
   t.eps = static_cast<float>(eps);
   t.inv_dh = 1.f / static_cast<float>(dh);
   for (int i = 0; i < rot / 2; ++i) {
-    const double turns = inv_freq[i] * 0.15915494309189533577;     // 1 / 2 pi
-    t.turn[i] = static_cast<unsigned long long>(std::ldexp(turns - std::floor(turns), 64));
+    const double turns = std::fabs(inv_freq[i]) * 0.15915494309189533577;     // 1 / 2 pi
+    const unsigned long long turn = static_cast<unsigned long long>(std::ldexp(turns - std::floor(turns), 64));
+    t.turn[i] = inv_freq[i] < 0 ? 0 - turn : turn;
     t.axis[i] = static_cast<uint8_t>(axis ? axis[i] : 0);
   }
   *out = r;

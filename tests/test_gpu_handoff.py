@@ -169,6 +169,12 @@ def test_rotate_edges(mb):
             y = wide.grad(x, None, ints([[3, 4]]))[0]
             assert int(torch.isfinite(y).sum()) == 127 and bool(torch.isinf(y[0, 0, 40]))
     x = torch.randn(3, 2, 8, device=DEV)
+    back = mb.Rope(64, [-0.5, 0.0, -1e-30, 1e-30], axis=[0, 0, 0, 0])     # turned the other way, not, and hardly
+    x = torch.randn(2, 1, 64, device=DEV)
+    y, z = H.rotate(f64(x), None, [[3, 2 ** 31 - 1]], [-0.5, 0.0, -1e-30, 1e-30], [0] * 4, False, 0.0)
+    got, _ = back.rotate(x, None, ints([[3, 2 ** 31 - 1]]))
+    assert np.abs(f64(got) - y).max() < 1e-5
+    x = torch.randn(3, 2, 8, device=DEV)
     for rows in (0,):
         q, k = plan.rotate(x[:rows], x[:rows], pos[:, :rows].contiguous())
         assert q.shape == (0, 2, 8) and k.shape == (0, 2, 8)
@@ -436,6 +442,47 @@ def test_many_entries_and_a_large_pool(mb):
     assert got == model.extend(list(range(0, n, 2)), [1] * (n // 2), n // 2)
     same_state(cache, model)
     cache.check()
+
+
+def test_bad_tables_and_lengths_are_reported_and_not_followed(mb):
+    """Entries outside the pool and lengths outside a table row, in the caller's own arrays."""
+    def fresh():
+        c = mb.Cache.empty(1, 12, 2, 4, 64, 5, 3)
+        c.pool.fill_(1.0)
+        c.extend(ints([0, 1]), ints([10, 5]), rows=15)
+        c.check()
+        return c
+
+    q = torch.ones(2, 2, 64, dtype=torch.bfloat16, device=DEV)
+    for page in (12, -1, 2 ** 31 - 1, -2 ** 31):
+        c = fresh()
+        c.table[0, 1] = page
+        out = c.attend(q, ints([0, 1]), 0)
+        assert c.status() == mb.MAP_EINTERNAL and bool((out == 1).all())
+        c.fork(ints([0]), ints([2]), ints([[0]]), ints([0]), ints([1]))             # a copied row of the page
+        assert c.status() == mb.MAP_EINTERNAL
+        c.free(ints([2]))
+        c.check()
+        c.fork(ints([0]), ints([3]))                                                # the page shared
+        assert c.status() == mb.MAP_EINTERNAL
+        c.free(ints([0, 3]))
+        assert c.status() == mb.MAP_EINTERNAL
+        c = fresh()
+        c.table[1, 1] = page                                                        # the part page that grows
+        assert c.extend(ints([1])).cpu().tolist() == [-1]
+        assert c.status() == mb.MAP_EINTERNAL
+    for length in (-1, 13, 2 ** 31 - 1, -2 ** 31):
+        c = fresh()
+        c.length[0] = length
+        before = c.refs.clone()
+        assert c.extend(ints([0])).cpu().tolist() == [-1] and c.status() == mb.MAP_EINTERNAL
+        c.fork(ints([0]), ints([2]))
+        assert c.status() == mb.MAP_EINTERNAL and int(c.length[2]) == 0
+        out = c.attend(q, ints([0, 1]), 0)
+        assert c.status() == mb.MAP_EINTERNAL and bool((out[0] == 0).all()) and bool((out[1] == 1).all())
+        assert torch.equal(c.refs, before)
+        c.free(ints([0]))
+        assert c.status() == mb.MAP_EINTERNAL and torch.equal(c.refs, before)
 
 
 def test_append_reports_bad_slots_and_skips_them(mb):
