@@ -273,8 +273,7 @@ __device__ __forceinline__ float2 unpack2(uint32_t w, __nv_bfloat16) {
   return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
 }
 __device__ __forceinline__ float2 unpack2(uint32_t w, __half) {
-  const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w));
-  return make_float2(f.x, f.y);
+  return __half22float2(*reinterpret_cast<const __half2*>(&w));
 }
 __device__ __forceinline__ uint32_t pack2(float2 v, __nv_bfloat16) {
   const __nv_bfloat162 h = __float22bfloat162_rn(v);
@@ -378,8 +377,7 @@ struct Turns {
 #pragma unroll
       for (int q = 0; q < V; ++q) {
         if (q >= turned) continue;
-        const float2 cc = c[q / 2], ss = s[q / 2];
-        const float co = q & 1 ? cc.y : cc.x, si = SIGN * (q & 1 ? ss.y : ss.x);
+        const float co = q & 1 ? c[q / 2].y : c[q / 2].x, si = SIGN * (q & 1 ? s[q / 2].y : s[q / 2].x);
         float2& v = q < V / 2 ? a[q] : b[q - V / 2];
         const float2 x = v;
         v = make_float2(x.x * co - x.y * si, x.y * co + x.x * si);
@@ -393,8 +391,7 @@ __device__ __forceinline__ float dot2(const float2 (&a)[N], const float2 (&b)[N]
   float2 s = make_float2(add, 0.f);
 #pragma unroll
   for (int i = 0; i < N; ++i) s = fma2(a[i], b[i], s);
-  const float2 f = s;
-  return f.x + f.y;
+  return s.x + s.y;
 }
 // Sum over the lanes of a head times 2^(5 - shift): steps past the head's lanes add a lane's sum to itself, which is
 // exact and costs less than branches around them.
@@ -429,10 +426,15 @@ __device__ __forceinline__ void weight_at(const float* w, float2 (&v)[V / 2]) {
 
 // Loads in flight, without registers: a lane copies its vectors to places of its own in shared memory (no other lane
 // reads them, so no barrier is needed), kAhead passes ahead.  Places that a lane never fills hold zeros.
+// (Predicated: with branches around the copies the gradient took 82 us, not 80.)
 template <int BYTES>
-__device__ __forceinline__ void copy_vec(uint32_t dst, const char* src) {
-  if (BYTES == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
-  else asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(dst), "l"(src) : "memory");
+__device__ __forceinline__ void copy_vec(uint32_t dst, const char* src, bool on) {
+  if (BYTES == 16)
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %2, 0;\n\t@p cp.async.cg.shared.global [%0], [%1], 16;\n\t}"
+                 ::"r"(dst), "l"(src), "r"(static_cast<int>(on)) : "memory");
+  else
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %2, 0;\n\t@p cp.async.ca.shared.global [%0], [%1], 8;\n\t}"
+                 ::"r"(dst), "l"(src), "r"(static_cast<int>(on)) : "memory");
 }
 __device__ __forceinline__ void copy_int(uint32_t dst, const int32_t* src) {
   asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst), "l"(src) : "memory");
@@ -520,19 +522,17 @@ __global__ void __launch_bounds__(kThreads, kRotateCtas) rotate_kernel(const __g
   char* cy = nullptr;
   bool enter = true;
   const auto load = [&](int stage) {
-    {
-      if (enter && !ld.left()) { enter = false; lh = 1 << 30; }
-      if (enter) {
-        lh = ld.k * per + (lane >> shift);
-        lx = in.at(ld.row, lh);
-        if (lane < tab.axes && tab.rot > 0 && !values) copy_int(row_at + (stage * 8 + lane) * 4, job.pos + lane * job.rows + ld.row);
-        if (APPEND && lane == 4) copy_int(row_at + (stage * 8 + 4) * 4, job.slots + ld.row);
-      }
-      if (lh < heads) copy_vec<VB>(mine_at + stage * 1024, lx);
-      if (lh < heads2) copy_vec<VB>(mine_at + stage * 1024 + 512, lx + gap);
-      lh += per;
-      lx += in_step;
+    if (enter && !ld.left()) { enter = false; lh = 1 << 30; }          // no passes left: no heads either
+    if (enter) {
+      lh = ld.k * per + (lane >> shift);
+      lx = in.at(ld.row, lh);
+      if (lane < tab.axes && tab.rot > 0 && !values) copy_int(row_at + (stage * 8 + lane) * 4, job.pos + lane * job.rows + ld.row);
+      if (APPEND && lane == 4) copy_int(row_at + (stage * 8 + 4) * 4, job.slots + ld.row);
     }
+    copy_vec<VB>(mine_at + stage * 1024, lx, lh < heads);
+    copy_vec<VB>(mine_at + stage * 1024 + 512, lx + gap, lh < heads2);
+    lh += per;
+    lx += in_step;
     if (ld.left()) enter = ld.next();
     cp_async_commit();
   };
@@ -628,27 +628,21 @@ __global__ void __launch_bounds__(kThreads, kGradCtas) grad_kernel(const __grid_
   char* cy = nullptr;
   bool enter = true;
   const auto load = [&](int stage) {
-    {
-      if (enter && !ld.left()) { enter = false; lh = 1 << 30; }
-      if (enter) {
-        lh = ld.k * per + (lane >> shift);
-        lg = ing.at(ld.row, lh);
-        lx = inx.at(ld.row, lh);
-        if (lane < tab.axes && tab.rot > 0) copy_int(row_at + (stage * 4 + lane) * 4, job.pos + lane * job.rows + ld.row);
-      }
-      const uint32_t to = mine_at + stage * 2048;
-      if (lh < heads) {
-        copy_vec<VB>(to, lg);
-        if (norm) copy_vec<VB>(to + 1024, lx);
-      }
-      if (lh < heads2) {
-        copy_vec<VB>(to + 512, lg + gap);
-        if (norm) copy_vec<VB>(to + 1536, lx + gap);
-      }
-      lh += per;
-      lg += g_step;
-      lx += x_step;
+    if (enter && !ld.left()) { enter = false; lh = 1 << 30; }          // no passes left: no heads either
+    if (enter) {
+      lh = ld.k * per + (lane >> shift);
+      lg = ing.at(ld.row, lh);
+      lx = inx.at(ld.row, lh);
+      if (lane < tab.axes && tab.rot > 0) copy_int(row_at + (stage * 4 + lane) * 4, job.pos + lane * job.rows + ld.row);
     }
+    const uint32_t to = mine_at + stage * 2048;
+    copy_vec<VB>(to, lg, lh < heads);
+    copy_vec<VB>(to + 512, lg + gap, lh < heads2);
+    copy_vec<VB>(to + 1024, lx, lh < heads && norm);
+    copy_vec<VB>(to + 1536, lx + gap, lh < heads2 && norm);
+    lh += per;
+    lg += g_step;
+    lx += x_step;
     if (ld.left()) enter = ld.next();
     cp_async_commit();
   };
@@ -864,8 +858,7 @@ cudaError_t run_rotate(const RopeTab& t, Job& job, int sides, cudaStream_t st) {
   const int shift = shift_of(t, V);
   spread_blocks(job, sides, 32 >> shift, 152 * kRotateCtas);
   constexpr size_t smem = kWarps * kStages * 64 * sizeof(uint4);
-  const cudaError_t e = cudaFuncSetAttribute(rotate_kernel<T, V, ADJ, APPEND>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
-  if (e != cudaSuccess) return e;
+  static_assert(smem <= 34 * 1024, "with 12 KB of fixed arrays within what a kernel has without asking");
   return launch_k(rotate_kernel<T, V, ADJ, APPEND>, dim3(job.first[3]), dim3(kThreads), smem, st, t, job, shift);
 }
 
