@@ -743,25 +743,25 @@ __global__ void __launch_bounds__(kThreads, kGradCtas) grad_kernel(const __grid_
   }
 }
 
-// dw[c] = sum over a side's blocks of part[b][c], in a fixed order: 32 columns a CTA, every 8th block a warp.
+// dw[c] = sum over a side's blocks of part[b][c], in a fixed order: 32 columns a CTA, every 32nd block a warp.
+constexpr int kSumWarps = 32;         // as many as columns
 struct Sums { const float* part[2]; float* dw[2]; int blocks[2]; };
-__global__ void __launch_bounds__(kThreads) grad_sum_kernel(const __grid_constant__ Sums g, int dh) {
-  __shared__ float red[kWarps][32];
+__global__ void __launch_bounds__(32 * kSumWarps) grad_sum_kernel(const __grid_constant__ Sums g, int dh) {
+  __shared__ float red[kSumWarps][33];
   pdl_enter();
-  const int c = blockIdx.x * 32 + (threadIdx.x & 31), warp = threadIdx.x >> 5, side = blockIdx.y;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, c = blockIdx.x * 32 + lane, side = blockIdx.y;
   float s = 0.f;
   if (c < dh) {
-#pragma unroll 8
-    for (int b = warp; b < g.blocks[side]; b += kWarps) s += g.part[side][static_cast<long long>(b) * dh + c];
+#pragma unroll 10
+    for (int b = warp; b < g.blocks[side]; b += kSumWarps) s += g.part[side][static_cast<long long>(b) * dh + c];
   }
-  red[warp][threadIdx.x & 31] = s;
+  red[warp][lane] = s;
   __syncthreads();
-  if (warp == 0 && c < dh && g.dw[side]) {
-    s = red[0][threadIdx.x];
+  // warp w adds the warps' sums of column w
+  s = red[lane][warp];
 #pragma unroll
-    for (int k = 1; k < kWarps; ++k) s += red[k][threadIdx.x];
-    g.dw[side][c] = s;
-  }
+  for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+  if (lane == 0 && blockIdx.x * 32 + warp < dh && g.dw[side]) g.dw[side][blockIdx.x * 32 + warp] = s;
 }
 
 int elem_size(int type) { return type == MAP_F32 ? 4 : 2; }
@@ -1018,7 +1018,7 @@ int map_qk_rotate_grad(const map_rope* rope, int type, long long rows, const int
         : type == MAP_F16 ? grad_job<__half>(t, job, sides, st)
                           : grad_job<__nv_bfloat16>(t, job, sides, st);
   for (int i = 0; i < 2; ++i) sums.blocks[i] = i < sides && sums.part[i] ? static_cast<int>(job.first[i + 1] - job.first[i]) : 0;
-  if (e == cudaSuccess && norm) e = launch_k(grad_sum_kernel, dim3((t.dh + 31) / 32, 2), dim3(kThreads), 0, st, sums, t.dh);
+  if (e == cudaSuccess && norm) e = launch_k(grad_sum_kernel, dim3((t.dh + 31) / 32, 2), dim3(32 * kSumWarps), 0, st, sums, t.dh);
   return launch_err(e);
 }
 
