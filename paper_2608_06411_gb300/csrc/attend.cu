@@ -25,7 +25,7 @@ constexpr int kTok = 16;                       // rows a warp takes of a tile
 constexpr int kTile = kWarps * kTok;
 constexpr int kRows = 16;                      // query heads of an item: the M of an mma.m16n8k16
 constexpr int kMaxGrid = 456;                  // three CTAs for each of 152 SMs
-constexpr int kGroup = 16;                     // parts that one CTA joins
+constexpr int kGroup = 10;                     // parts that one CTA joins
 static_assert(2 + 2 * kMaxGrid <= MAP_CACHE_STATUS_WORDS, "counters of an item's groups and of their parts");
 
 // A partial result: m [16], l [16], o [16][dh].
@@ -151,54 +151,67 @@ struct Tile {
   static __device__ __forceinline__ uint32_t at(int row, int x) { return row * kRow + x * 16; }
 };
 // Joins `count` parts, of CTAs c, c + stride, ... (the first one's slot `slot0`, the others' slot 0), in order: into out,
-// or into the first part where out is nullptr.  All of the block's threads, one for four columns of a row, with kGroup
-// parts in flight, for all that a join takes is latency.
+// or into the first part where out is nullptr.  All of the block's threads, two pieces of four columns of a row each, with
+// kGroup parts of both in flight, for all that a join takes is latency.
 template <typename T, int DH>
 __device__ __noinline__ void join_parts(const AttendArgs& a, int c, int stride, int slot0, int count, int have, T* out,
                                         float* tops, float* sums) {
   const auto part = [&](int p) { return a.ws + (2 * static_cast<long long>(c + p * stride) + (p == 0 ? slot0 : 0)) * part_floats(DH); };
-  for (int e = threadIdx.x; e < have * (DH / 4); e += kThreads) {
-    const int r = e / (DH / 4), x = 4 * (e % (DH / 4));
-    float top = -INFINITY, sum = 0.f;
-    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+  const int pieces = have * (DH / 4);
+  for (int e0 = threadIdx.x; e0 < pieces; e0 += 2 * kThreads) {
+    float top[2] = {-INFINITY, -INFINITY}, sum[2] = {0.f, 0.f};
+    float4 v[2] = {make_float4(0.f, 0.f, 0.f, 0.f), make_float4(0.f, 0.f, 0.f, 0.f)};
     for (int p0 = 0; p0 < count; p0 += kGroup) {
-      float4 y[kGroup];
-      float m[kGroup], l[kGroup], next = top;
+      float4 y[2][kGroup];
+      float m[2][kGroup], l[2][kGroup];
 #pragma unroll
-      for (int k = 0; k < kGroup; ++k) {
-        const bool on = p0 + k < count;
-        const float* q = part(on ? p0 + k : 0);
-        m[k] = on ? __ldcg(q + r) : -INFINITY;
-        l[k] = on ? __ldcg(q + kRows + r) : 0.f;
-        y[k] = on ? __ldcg(reinterpret_cast<const float4*>(q + 2 * kRows + r * DH + x)) : make_float4(0.f, 0.f, 0.f, 0.f);
+      for (int d = 0; d < 2; ++d) {
+        const int e = e0 + d * kThreads, r = e / (DH / 4), x = 4 * (e % (DH / 4));
+#pragma unroll
+        for (int k = 0; k < kGroup; ++k) {
+          const bool on = p0 + k < count && e < pieces;
+          const float* q = part(p0 + k < count ? p0 + k : 0);
+          m[d][k] = on ? __ldcg(q + r) : -INFINITY;
+          l[d][k] = on ? __ldcg(q + kRows + r) : 0.f;
+          y[d][k] = on ? __ldcg(reinterpret_cast<const float4*>(q + 2 * kRows + r * DH + x)) : make_float4(0.f, 0.f, 0.f, 0.f);
+        }
       }
 #pragma unroll
-      for (int k = 0; k < kGroup; ++k) next = fmaxf(next, m[k]);
-      const float at = next == -INFINITY ? 0.f : next, f0 = exp2_fast(top - at);
-      top = next;
-      sum *= f0;
-      v = make_float4(v.x * f0, v.y * f0, v.z * f0, v.w * f0);
+      for (int d = 0; d < 2; ++d) {
+        float next = top[d];
 #pragma unroll
-      for (int k = 0; k < kGroup; ++k) {
-        const float f = exp2_fast(m[k] - at);
-        sum = fmaf(f, l[k], sum);
-        v.x = fmaf(f, y[k].x, v.x);
-        v.y = fmaf(f, y[k].y, v.y);
-        v.z = fmaf(f, y[k].z, v.z);
-        v.w = fmaf(f, y[k].w, v.w);
+        for (int k = 0; k < kGroup; ++k) next = fmaxf(next, m[d][k]);
+        const float at = next == -INFINITY ? 0.f : next, f0 = exp2_fast(top[d] - at);
+        top[d] = next;
+        sum[d] *= f0;
+        v[d] = make_float4(v[d].x * f0, v[d].y * f0, v[d].z * f0, v[d].w * f0);
+#pragma unroll
+        for (int k = 0; k < kGroup; ++k) {
+          const float f = exp2_fast(m[d][k] - at);
+          sum[d] = fmaf(f, l[d][k], sum[d]);
+          v[d].x = fmaf(f, y[d][k].x, v[d].x);
+          v[d].y = fmaf(f, y[d][k].y, v[d].y);
+          v[d].z = fmaf(f, y[d][k].z, v[d].z);
+          v[d].w = fmaf(f, y[d][k].w, v[d].w);
+        }
       }
     }
-    if (out) {
-      T* o = out + r * a.out.head + x;
-      o[0] = from_f32<T>(v.x / sum);
-      o[1] = from_f32<T>(v.y / sum);
-      o[2] = from_f32<T>(v.z / sum);
-      o[3] = from_f32<T>(v.w / sum);
-    } else {
-      *reinterpret_cast<float4*>(part(0) + 2 * kRows + r * DH + x) = v;
-      if (x == 0) {
-        tops[r] = top;
-        sums[r] = sum;
+#pragma unroll
+    for (int d = 0; d < 2; ++d) {
+      const int e = e0 + d * kThreads, r = e / (DH / 4), x = 4 * (e % (DH / 4));
+      if (e >= pieces) break;
+      if (out) {
+        T* o = out + r * a.out.head + x;
+        o[0] = from_f32<T>(v[d].x / sum[d]);
+        o[1] = from_f32<T>(v[d].y / sum[d]);
+        o[2] = from_f32<T>(v[d].z / sum[d]);
+        o[3] = from_f32<T>(v[d].w / sum[d]);
+      } else {
+        *reinterpret_cast<float4*>(part(0) + 2 * kRows + r * DH + x) = v[d];
+        if (x == 0) {
+          tops[r] = top[d];
+          sums[r] = sum[d];
+        }
       }
     }
   }
@@ -210,16 +223,18 @@ __device__ __noinline__ void join_parts(const AttendArgs& a, int c, int stride, 
   }
 }
 
-// Whether this block is the last of `count` to come here after writing a part (its writes are then visible to the last,
-// and theirs to it).  The counter is zero between uses.
+// Whether this block is the last of `count` to come here after writing a part.  The barriers order every thread's writes
+// before, and reads after, thread 0's add, which releases them to the last block and acquires theirs.  The counter is zero
+// between uses.
 __device__ __forceinline__ bool is_last(int* counter, int count, int* flag) {
   __syncthreads();
   if (threadIdx.x == 0) {
-    __threadfence();
-    const bool last = count == 1 || atomicAdd(counter, 1) == count - 1;
-    if (last && count > 1) {
-      *counter = 0;
-      __threadfence();
+    bool last = true;
+    if (count > 1) {
+      int old;
+      asm volatile("atom.acq_rel.gpu.global.add.s32 %0, [%1], 1;" : "=r"(old) : "l"(counter) : "memory");
+      last = old == count - 1;
+      if (last) *counter = 0;
     }
     *flag = last;
   }
