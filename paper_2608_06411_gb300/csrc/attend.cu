@@ -28,6 +28,10 @@ constexpr int kMaxGrid = 456;                  // three CTAs for each of 152 SMs
 constexpr int kGroup = 10;                     // parts that one CTA joins
 static_assert(2 + 2 * kMaxGrid <= MAP_CACHE_STATUS_WORDS, "counters of an item's groups and of their parts");
 
+// CTAs that an SM is to hold, by the registers and the ring that a head's width takes, and the largest grid.
+__host__ __device__ constexpr int ctas_of(int dh) { return dh <= 80 ? 3 : dh <= 192 ? 2 : 1; }
+constexpr int max_grid(int dh) { return kMaxGrid / 3 * ctas_of(dh); }
+
 // A partial result: m [16], l [16], o [16][dh].
 __host__ __device__ constexpr int part_floats(int dh) { return kRows * (dh + 2); }
 
@@ -243,7 +247,7 @@ __device__ __forceinline__ bool is_last(int* counter, int count, int* flag) {
 }
 
 template <typename T, int DH, int STAGES>
-__global__ void __launch_bounds__(kThreads, DH <= 80 ? 3 : DH <= 192 ? 2 : 1) attend_kernel(const __grid_constant__ AttendArgs a) {
+__global__ void __launch_bounds__(kThreads, ctas_of(DH)) attend_kernel(const __grid_constant__ AttendArgs a) {
   using R = Tile<DH>;
   constexpr int VPR = R::kVecs, KSTEPS = DH / 16;
   constexpr bool QREG = DH <= 128;             // query fragments stay in registers
@@ -583,13 +587,13 @@ template <typename T, int DH>
 cudaError_t launch_width(const AttendArgs& a, int sms, cudaStream_t st) {
   constexpr size_t kSm = 228 * 1024, kOwn = 1024 + 768;      // an SM's shared memory; what a CTA takes beside its dynamic part
   const int rows = a.group < kRows ? a.group : kRows;
-  constexpr int kWant = DH <= 80 ? 3 : DH <= 192 ? 2 : 1;
+  constexpr int kWant = ctas_of(DH);
   const int deep = static_cast<int>(kSm / (smem_of<DH>(3, rows) + kOwn)), flat = static_cast<int>(kSm / (smem_of<DH>(2, rows) + kOwn));
   const bool three = deep >= kWant || deep >= flat;
   const int ctas = std::min(kWant, three ? deep : flat);
   const long long most = static_cast<long long>(a.n) * a.c.heads * a.subs *
                          ((static_cast<long long>(a.c.max_pages) * a.c.page + kTile - 1) / kTile);
-  const int grid = static_cast<int>(std::min<long long>(most, std::min(ctas * sms, kMaxGrid)));
+  const int grid = static_cast<int>(std::min<long long>(most, std::min(ctas * sms, max_grid(DH))));
   return three ? launch_run<T, DH, 3>(a, smem_of<DH>(3, rows), grid, st) : launch_run<T, DH, 2>(a, smem_of<DH>(2, rows), grid, st);
 }
 
@@ -613,7 +617,7 @@ using namespace mapk;
 extern "C" {
 
 size_t map_cache_attend_workspace(const map_cache* c) { 
-  return check_cache(c) == MAP_OK ? static_cast<size_t>(2) * kMaxGrid * part_floats(c->dh) * sizeof(float) : 0;
+  return check_cache(c) == MAP_OK ? static_cast<size_t>(2) * max_grid(c->dh) * part_floats(c->dh) * sizeof(float) : 0;
 }
 
 int map_cache_attend(const map_cache* c, int layer, const map_heads* q, const int32_t* seqs, int n, float scale,
