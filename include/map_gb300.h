@@ -389,8 +389,9 @@ int map_qk_rotate_grad(const map_rope *rope, int type, long long rows, const int
  *   refs    int32 [pages]: sequences that hold the page; 0: free.
  *   status  int32 [MAP_CACHE_STATUS_WORDS]: error bits for map_cache_status; the calls' own counters.
  * type MAP_BF16 or MAP_F16; dh a multiple of 8 up to 256; page 1 .. 1024; pages <= 1048576;
- * seqs <= 262144; max_pages * page < 2^31 (MAP_EUNSUPPORTED beyond these).  New pages are the free ones with the lowest numbers, in the order of the
- * call's entries: results do not depend on timing.
+ * seqs <= 262144; max_pages * page < 2^31; heads <= 65535, layers * heads <= 2^23
+ * (MAP_EUNSUPPORTED beyond these).  New pages are the free ones with the lowest numbers, in the
+ * order of the call's entries: results do not depend on timing.
  * A call that names a bad sequence, names one twice where that is not allowed, or needs more
  * pages than are free or than a table row holds, changes no length and no page: map_cache_status
  * then reports it.  Table entries outside the pool and lengths that no row holds are reported
@@ -429,12 +430,13 @@ int map_qk_rotate_append(const map_rope *rope, const map_cache *cache, int layer
 
 /*
  * Forks sequences: the empty sequence children[i] gets the rows of parents[i] in all layers.
- *   keep = NULL  all rows.
+ *   keep, base and span NULL, k = 0: all rows.
  *   keep int32 [n, k] (device), base, span int32 [n] (device): rows base .. base + span - 1 of
  *        the parent (its visual tokens) are replaced by its rows base + keep[i, 0 .. k); the rows
  *        before and after stay.  keep is map_select's keep_idx: a question's own pruned view of
  *        an image that stays cached whole.  base, span >= 0, base + span <= the parent's
- *        length.  An index outside [0, span) gives a row of zeros and is reported.
+ *        length.  An index outside [0, span) gives a row of zeros and is reported.  With k = 0
+ *        (keep may be NULL) the rows of the span are left out.
  * Pages that are full and end before the first replaced row are shared (not copied); the other
  * rows are copied to new pages.  parents may repeat, children may not, and no child may be a
  * parent.  Compaction in place is a fork of the kept rows followed by map_cache_free of the

@@ -258,28 +258,31 @@ class Context:
         that are grids of grids[b] = (T, H, W) tokens, t_step[b] positions from frame to frame (default 1)."""
         B, N, D = vis.shape
         k = keep.shape[1]
-        if vis.device.type != "cuda" or D != self.cfg.D or vis.element_size() != 2:
+        dev, dt = vis.device, vis.dtype
+        if dev.type != "cuda" or D != self.cfg.D or vis.element_size() != 2:
             raise ValueError(f"vis must be [B, N, {self.cfg.D}] of a 2-byte type on a CUDA device")
-        if keep.shape[0] != B or keep.dtype is not torch.int32:
-            raise ValueError("keep must be int32 [B, k]")
+        if stream is not None:               # outputs are allocated on the stream that writes them
+            with _on(dev, stream):
+                return self.assemble_axes(vis, keep, text, lens, grids, t_step, pos_offset, seq, pos)
+        if keep.shape[0] != B or keep.dtype is not torch.int32 or keep.device != dev:
+            raise ValueError(f"keep must be int32 [B, k] on {dev}")
         m = _host_ints(lens, B, 1, "lens")
         g = _host_ints(grids, B, 3, "grids")
         t = None if t_step is None else _host_ints(t_step, B, 1, "t_step")
         questions = int(sum(lens))
         rows = B * k + questions
-        if text.shape[0] < questions or text.shape[1] != D:
-            raise ValueError(f"text must be [sum(lens), {D}]")
+        if text.shape[0] < questions or text.shape[1] != D or text.dtype is not dt or text.device != dev:
+            raise ValueError(f"text must be {dt} [sum(lens), {D}] on {dev}")
         if seq is None:
-            seq = torch.empty((rows, D), dtype=vis.dtype, device=vis.device)
-        elif seq.shape != (rows, D):
-            raise ValueError(f"seq must be [{rows}, {D}]")
+            seq = torch.empty((rows, D), dtype=dt, device=dev)
+        elif seq.shape != (rows, D) or seq.dtype is not dt or seq.device != dev:
+            raise ValueError(f"seq must be {dt} [{rows}, {D}] on {dev}")
         if pos is None:
-            pos = torch.empty((3, rows), dtype=torch.int32, device=vis.device)
-        elif pos.shape != (3, rows) or pos.dtype is not torch.int32:
-            raise ValueError(f"pos must be int32 [3, {rows}]")
-        s = _current_stream(vis.device.index) if stream is None else stream.cuda_stream
+            pos = torch.empty((3, rows), dtype=torch.int32, device=dev)
+        elif pos.shape != (3, rows) or pos.dtype is not torch.int32 or pos.device != dev:
+            raise ValueError(f"pos must be int32 [3, {rows}] on {dev}")
         _check(lib.map_assemble_axes(self.h, _ptr(vis), _ptr(keep), _ptr(text), m, g, t, B, N, k, pos_offset, _ptr(seq),
-                                     _ptr(pos), s), "map_assemble_axes")
+                                     _ptr(pos), _current_stream(dev.index)), "map_assemble_axes")
         return seq, pos
 
     # -- ragged batches (padded layout, n_valid tokens per image) ---------------------------
@@ -510,6 +513,8 @@ class Rope:
         """map_qk_rotate: (q_out, k_out) of q [rows, heads, dh] and k (either may be None), pos int32 [n_axes, rows],
         norm weights wq, wk [dh] or None (no norm of that side).  Outputs not given are new, contiguous tensors."""
         x = q if q is not None else k
+        if x is None:
+            raise ValueError("q or k is needed")
         dev = x.device
         if stream is not None or dev.index != _current_device():
             with _on(dev, stream):
@@ -538,6 +543,8 @@ class Rope:
         """map_qk_rotate_grad: (dq, dk, dwq, dwk) from the gradients of rotate's outputs; q and k (rotate's inputs) are
         needed where wq and wk are given, dwq and dwk are float32 (None without a norm)."""
         x = dq_out if dq_out is not None else dk_out
+        if x is None:
+            raise ValueError("dq_out or dk_out is needed")
         dev = x.device
         if stream is not None or dev.index != _current_device():
             with _on(dev, stream):
@@ -603,7 +610,8 @@ class Rope:
 class Cache:
     """Pages of a key/value cache (map_cache) over the caller's tensors: pool [layers, 2, pages, heads, page, dh] bf16 or
     fp16, table int32 [seqs, max_pages], length int32 [seqs], refs int32 [pages], status int32 [CACHE_STATUS_WORDS], the last
-    four initially zero (`Cache.empty` makes all of them)."""
+    four initially zero (`Cache.empty` makes all of them).  Calls on one cache, replays of captured ones included, are
+    ordered by the caller; a graph that holds such calls needs the Cache as long as it is replayed."""
 
     def __init__(self, pool, table, length, refs, status=None):
         dev = pool.device
@@ -622,6 +630,7 @@ class Cache:
         self.desc = _pack_cache(pool.data_ptr(), *ptrs, TYPES[pool.dtype], layers, pages, heads, page, dh, seqs, max_pages)
         # attend's scratch: calls on one cache are ordered by the caller, so they can share it
         self._ws = torch.empty(int(lib.map_cache_attend_workspace(self.desc)), dtype=torch.uint8, device=dev)
+        self._ws_streams = {_current_stream(dev.index)} if dev.type == "cuda" else set()     # that the allocator knows of
 
     @classmethod
     def empty(cls, layers: int, pages: int, heads: int, page: int, dh: int, seqs: int, max_pages: int,
@@ -663,7 +672,7 @@ class Cache:
             with _on(dev, stream):
                 return self.fork(parents, children, keep, base, span)
         n, i32 = parents.shape[0], torch.int32
-        if keep is not None and (keep.dim() != 2 or base is None or span is None):
+        if (keep is None) != (base is None) or (base is None) != (span is None) or (keep is not None and keep.dim() != 2):
             raise ValueError("keep is [n, k] and comes with base and span")
         k = 0 if keep is None else keep.shape[1]
         _check(lib.map_cache_fork(self.desc, _dense(parents, i32, dev, (n,), "parents"),
@@ -694,9 +703,12 @@ class Cache:
             out, oa = _like(q, dh)
         else:
             oa = _heads(out, n, dh, dt, dev)
+        st = _current_stream(dev.index)
+        if st not in self._ws_streams:
+            self._ws.record_stream(torch.cuda.current_stream(dev))
+            self._ws_streams.add(st)
         _check(lib.map_cache_attend(self.desc, layer, a, _dense(seqs, torch.int32, dev, (n,), "seqs"), n,
-                                    dh ** -0.5 if scale is None else scale, oa, self._ws.data_ptr(),
-                                    _current_stream(dev.index)), "map_cache_attend")
+                                    dh ** -0.5 if scale is None else scale, oa, self._ws.data_ptr(), st), "map_cache_attend")
         return out
 
     def status(self, stream=None) -> int:

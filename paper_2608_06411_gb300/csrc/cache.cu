@@ -22,6 +22,7 @@ int check_cache(const map_cache* c) {
   if (c->dh % 8 || c->dh > kMaxHead || c->page > 1024 || c->seqs > 262144) return MAP_EUNSUPPORTED;
   if (c->pages > (1 << 20)) return MAP_EUNSUPPORTED;            // block_scan adds 1024 needs of at most so many pages
   if (static_cast<long long>(c->max_pages) * c->page >= (1ll << 31)) return MAP_EUNSUPPORTED;
+  if (c->heads > 65535 || 2ll * c->layers * c->heads > (1 << 24)) return MAP_EUNSUPPORTED;      // units of a page: 32 bits
   return MAP_OK;
 }
 
@@ -246,7 +247,8 @@ __global__ void __launch_bounds__(kPlanThreads) fork_plan_kernel(const map_cache
         } else {
           // a child longer than its parent (keep may repeat rows) can pass its table row, or 2^31
           const long long pages = (static_cast<long long>(plen) - sp + (kept ? k : 0) + c.page - 1) / c.page;
-          if (pages > c.max_pages) {
+          // (needs beyond the pool are refused here: 1024 of them could pass 2^31 in their sum)
+          if (pages > c.max_pages || pages - (kept ? b : plen) / c.page > c.pages) {
             atomicOr(&error, ST_NOPAGES);
           } else {
             const ForkShape f = fork_shape(plen, c.page, kept, b, sp, k);

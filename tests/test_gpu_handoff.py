@@ -485,6 +485,25 @@ def test_bad_tables_and_lengths_are_reported_and_not_followed(mb):
         assert c.status() == mb.MAP_EINTERNAL and torch.equal(c.refs, before)
 
 
+def test_forks_whose_pages_add_up_past_32_bits(mb):
+    """A length that a very wide table row holds: 16 children of 2^27 pages each, of a pool of 64, are refused."""
+    c = mb.Cache(torch.ones(1, 2, 64, 1, 1, 8, dtype=torch.float16, device=DEV),
+                 torch.zeros(17, 1 << 27, dtype=torch.int32, device=DEV), ints([1 << 27] + [0] * 16), ints([0] * 64))
+    children = ints(list(range(1, 17)))
+    for n, code in ((16, mb.MAP_ENOMEM), (1, mb.MAP_ENOMEM)):
+        c.fork(ints([0] * n), children[:n], torch.zeros(n, 0, dtype=torch.int32, device=DEV), ints([0] * n), ints([0] * n))
+        assert c.status() == code
+        assert int(c.length[1:].abs().sum()) == 0 and int(c.refs.abs().sum()) == 0 and int(c.table[1].abs().sum()) == 0
+
+
+def test_a_fork_takes_its_window_whole_or_not_at_all(mb):
+    c = mb.Cache.empty(1, 4, 1, 4, 8, 2, 2)
+    one, keep = ints([0]), ints([[0]])
+    for args in ((keep,), (keep, one), (keep, None, one), (None, one, one), (one, one, one)):
+        with pytest.raises(ValueError):
+            c.fork(one, ints([1]), *args)
+
+
 def test_append_reports_bad_slots_and_skips_them(mb):
     cache = mb.Cache.empty(1, 2, 1, 4, 8, 2, 2)
     cache.pool.fill_(5.0)
@@ -652,6 +671,43 @@ def test_calls_on_a_stream_of_the_callers(mb):
     gatt = cache.attend(q.expand(2, -1, -1), ints([0, 1]), 0, stream=s)
     s.synchronize()
     assert all(torch.equal(a, b) for a, b in zip((*want, *wgrad, watt), (*got, *ggrad, gatt)))
+
+
+def test_a_cache_dropped_while_another_stream_attends(mb):
+    """Attention's scratch is not handed out again before the stream that uses it is done."""
+    cache = filled(mb, torch.float16, 64, 2, 16, [300, 20], 3)
+    q = randn(gen(5), 2, 8, 64, typ=torch.float16)
+    seqs = ints([0, 1])
+    want = cache.attend(q, seqs, 0)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        torch.cuda._sleep(100_000_000)                               # some 50 ms
+        got = cache.attend(q, seqs, 0)
+    place, size, keep = cache._ws.data_ptr(), cache._ws.numel(), (cache.pool, cache.table, cache.length, cache.refs, cache.status_word)
+    del cache
+    other = torch.full((size,), 255, dtype=torch.uint8, device=DEV)
+    assert other.data_ptr() != place
+    torch.cuda.synchronize()
+    assert torch.equal(got, want) and len(keep) == 5
+
+
+def test_assemble_axes_on_a_stream_and_its_refusals(mb):
+    ctx = handoff_context(mb, 512)
+    vis, text = torch.ones((1, 8, 512), dtype=torch.int16, device=DEV), torch.full((2, 512), 2, dtype=torch.int16, device=DEV)
+    keep, grid = ints([[1, 7]]), [(2, 2, 2)]
+    want = ctx.assemble_axes(vis, keep, text, [2], grid)
+    torch.cuda.synchronize()
+    s = torch.cuda.Stream()
+    got = ctx.assemble_axes(vis, keep, text, [2], grid, stream=s)
+    held = ctx.assemble_axes(vis, keep, text, [2], grid, seq=torch.zeros_like(want[0]), stream=s)
+    s.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(want + want, got + held))
+    for bad in (dict(keep=keep.cpu()), dict(keep=keep.long()), dict(text=text.cpu()), dict(text=text.to(torch.uint8)),
+                dict(seq=torch.zeros(4, 512, dtype=torch.uint8, device=DEV)), dict(seq=torch.zeros(4, 512, dtype=torch.int16)),
+                dict(pos=torch.zeros(3, 4, dtype=torch.int32))):
+        with pytest.raises(ValueError):
+            ctx.assemble_axes(**{**dict(vis=vis, keep=keep, text=text, lens=[2], grids=grid), **bad})
 
 
 def test_a_decoding_step_captured_and_replayed(mb):

@@ -135,6 +135,22 @@ def test_cache_refusals(mb, rope):
     assert T(c, 0, h, None, 0, 1.0, h, None, None) == mb.MAP_OK
 
 
+def test_cache_limits_of_a_page(mb):
+    """heads, and the units (planes times heads) that a page is copied in, are counted in 32 bits."""
+    free, E = mb.lib.map_cache_free, mb.MAP_EUNSUPPORTED
+    assert free(cache(mb, hk=65535, layers=128), None, 0, None) == mb.MAP_OK
+    assert free(cache(mb, hk=1, layers=1 << 23), None, 0, None) == mb.MAP_OK
+    for bad in (dict(hk=65536), dict(hk=65535, layers=129), dict(hk=1, layers=(1 << 23) + 1), dict(hk=65535, layers=1 << 30)):
+        assert free(cache(mb, **bad), None, 0, None) == E, bad
+
+
+def test_calls_without_any_heads(mb, rope):
+    with pytest.raises(ValueError):
+        rope.rotate(None, None, None)
+    with pytest.raises(ValueError):
+        rope.grad(None, None, None)
+
+
 def test_assemble_axes_refusals(mb):
     lib, E = mb.lib, mb.MAP_EINVAL
     lens = (ctypes.c_int32 * 1)(3)
