@@ -93,6 +93,10 @@ ROTATIONS = [
     ("bf16", 2500, 32, 32, 128, 128, 3, False, True, "packed", 8192),
     ("f32", 1027, 4, 4, 128, 96, 2, False, False, "packed", 8192),
     ("f32", 3, 1, 2, 254, 254, 1, False, True, "dense", 8192),
+    ("bf16", 1601, 56, 8, 36, 36, 3, False, True, "dense", 8192),
+    ("f16", 801, 9, 2, 72, 36, 2, False, True, "packed", 8192),
+    ("bf16", 300, 13, 4, 256, 256, 2, False, True, "odd", 8192),
+    ("bf16", 301, 70, 5, 9, 8, 1, True, True, "odd", 8192),
 ]
 IDS = ["-".join(str(v) for v in c) for c in ROTATIONS]
 
@@ -671,6 +675,31 @@ def test_calls_on_a_stream_of_the_callers(mb):
     gatt = cache.attend(q.expand(2, -1, -1), ints([0, 1]), 0, stream=s)
     s.synchronize()
     assert all(torch.equal(a, b) for a, b in zip((*want, *wgrad, watt), (*got, *ggrad, gatt)))
+
+
+def test_append_of_rows_at_any_alignment(mb):
+    """Half of 72 columns turned, 18 pairs, and heads that begin on odd elements: keys and values reach their slots."""
+    rows, hq, hk, dh = 45, 6, 3, 72
+    case = ("bf16", rows, hq, hk, dh, 36, 2, False, True, "odd", 5000)
+    typ, q, k, wq, wk, pos, inv, ax, plan = rotation(mb, case)
+    v = randn(gen(8), rows, hk, dh, typ=typ)
+    cache = mb.Cache.empty(1, 4, hk, 16, dh, 2, 3)
+    cache.pool.fill_(5.0)
+    slots = cache.extend(ints([1]), ints([rows]), rows=rows)
+    slots[7] = -1
+    (qv, _), (kv, _), (vv, _) = (place(t, "odd") for t in (q, k, v))
+    qo = torch.full_like(q, 7.0)
+    plan.append(qv, kv, vv, pos, cache, 0, slots, wq, wk, q_out=qo)
+    cache.check()
+    got = cache.pool[0].transpose(2, 3).reshape(2, 64, hk, dh)        # by slot
+    on = [r for r in range(rows) if r != 7]
+    at = slots[on].long()
+    check_rotated(qo[on], q[on], wq, pos[:, on], inv, ax, False, typ)
+    check_rotated(got[0][at], k[on], wk, pos[:, on], inv, ax, False, typ)
+    assert torch.equal(got[1][at], v[on])
+    rest = torch.ones(64, dtype=torch.bool, device=DEV)
+    rest[at] = False
+    assert bool((got[:, rest] == 5).all()) and bool((qo[7] == 7).all())
 
 
 def test_a_cache_dropped_while_another_stream_attends(mb):
