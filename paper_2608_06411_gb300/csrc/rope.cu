@@ -40,10 +40,10 @@ struct Side {                        // one tensor's heads: input, output, norm 
 };
 enum Kind { kRowsOut = 0, kKeys = 1, kValues = 2 };
 
-// Up to three tensors of one launch; side i takes blocks first[i] .. first[i + 1] - 1.
+// Up to three tensors of one launch; side i takes blocks first[i] .. first[i + 1] - 1, its warps runs of run[i] passes.
 struct Job {
   Side s[3];
-  unsigned first[4];
+  unsigned first[4], run[3];
   const int32_t* pos;
   long long rows;
   const int32_t* slots;              // append: a row's slot
@@ -271,14 +271,10 @@ constexpr int kStages = 4, kAhead = kStages - 1;
 
 // A pass is 32 >> shift heads of one row.  A warp takes runs of `run` passes of a row, the runs first, first + stride,
 // ...: it makes the row's turns once a run, and from pass to pass only adds to its addresses.
-constexpr int kRuns = 4;             // runs a warp, at least, where a row has several (the last ones leave warps idle)
 struct Passes {
   unsigned row, k, end, at, rows, of_row, run, of_run, drow, dat;
-  __device__ __forceinline__ Passes(unsigned first, unsigned stride, long long rows_, unsigned of_row_)
-      : rows(static_cast<unsigned>(rows_)), of_row(of_row_) {
-    const unsigned long long most = static_cast<unsigned long long>(rows) * of_row / (stride * kRuns);
-    const unsigned cap = most < 1 ? 1 : most < of_row ? static_cast<unsigned>(most) : of_row, runs = (of_row + cap - 1) / cap;
-    run = (of_row + runs - 1) / runs;
+  __device__ __forceinline__ Passes(unsigned first, unsigned stride, long long rows_, unsigned of_row_, unsigned run_)
+      : rows(static_cast<unsigned>(rows_)), of_row(of_row_), run(run_) {
     of_run = (of_row + run - 1) / run;
     row = first / of_run;
     at = first % of_run;
@@ -321,7 +317,7 @@ __device__ __forceinline__ void store_vec(const char* y, const float2 (&v)[V / 2
 }
 
 // A block's warps take the passes of one side.  HBM-bound (q and k once in, once out): 18944 rows of 32 and 32 heads of
-// 128 in bf16 take 102 us, 6.1 TB/s where a copy reaches 6.8, with issue slots 76 % busy; 3 CTAs an SM, for 80 registers hold
+// 128 in bf16 take 101 us, 6.1 TB/s where a copy reaches 6.8, with issue slots 76 % busy; 3 CTAs an SM, for 80 registers hold
 // a lane's 16 columns and their turns, and the loads in flight need none.
 template <typename T, int V, bool ADJ, bool APPEND>
 __global__ void __launch_bounds__(kThreads, kRotateCtas) rotate_kernel(const __grid_constant__ RopeTab tab,
@@ -350,7 +346,7 @@ __global__ void __launch_bounds__(kThreads, kRotateCtas) rotate_kernel(const __g
   const Heads in(sd.x, sd.xrow, sd.xhead, ln.a, T());
   const Heads out(sd.y, paged ? 0 : sd.yrow, paged ? static_cast<long long>(job.page) * tab.dh : sd.yhead, ln.a, T());
   const long long in_step = per * in.head, out_step = per * out.head;
-  Passes ld(warp * blocks + blk, blocks * kWarps, job.rows, (sd.heads + per - 1) / per), cp = ld;
+  Passes ld(warp * blocks + blk, blocks * kWarps, job.rows, (sd.heads + per - 1) / per, job.run[si]), cp = ld;
   int lh = 0, ch = 0;                          // head of the lane in the pass loaded and in the one computed
   const char* lx = nullptr;
   char* cy = nullptr;
@@ -458,7 +454,7 @@ __global__ void __launch_bounds__(kThreads, kGradCtas) grad_kernel(const __grid_
   const uint32_t mine_at = smem_u32(mine), row_at = smem_u32(row_buf[warp][0]);
   const Heads ing(sd.g, sd.grow, sd.ghead, ln.a, T()), inx(sd.x, sd.xrow, sd.xhead, ln.a, T()), out(sd.y, sd.yrow, sd.yhead, ln.a, T());
   const long long g_step = per * ing.head, x_step = per * inx.head, out_step = per * out.head;
-  Passes ld(warp * blocks + blk, blocks * kWarps, job.rows, (sd.heads + per - 1) / per), cp = ld;
+  Passes ld(warp * blocks + blk, blocks * kWarps, job.rows, (sd.heads + per - 1) / per, job.run[si]), cp = ld;
   int lh = 0, ch = 0;
   const char *lg = nullptr, *lx = nullptr;
   char* cy = nullptr;
@@ -683,7 +679,7 @@ __global__ void __launch_bounds__(kThreads, kAnyCtas<S>) rotate_any_kernel(const
   Pairs<T, S> pairs(tab, job, static_cast<const T*>(sd.w), lane & ((1 << shift) - 1), shift);
   const LaneSum lane_sum(shift);
   const float inv = tab.inv_dh * static_cast<float>(1 << shift) * 0.03125f;
-  for (Passes at((threadIdx.x >> 5) * blocks + blk, blocks * kWarps, job.rows, (sd.heads + per - 1) / per); at.left(); at.next_run()) {
+  for (Passes at((threadIdx.x >> 5) * blocks + blk, blocks * kWarps, job.rows, (sd.heads + per - 1) / per, job.run[si]); at.left(); at.next_run()) {
     const T* x = static_cast<const T*>(sd.x) + at.row * sd.xrow;
     T* y = static_cast<T*>(sd.y) + (paged ? 0 : at.row * sd.yrow);
     if (APPEND) {
@@ -737,7 +733,7 @@ __global__ void __launch_bounds__(kThreads, kGradCtas) grad_any_kernel(const __g
   const LaneSum lane_sum(shift);
   const float inv = tab.inv_dh * static_cast<float>(1 << shift) * 0.03125f;
   float da[S] = {}, db[S] = {};
-  for (Passes at(warp * blocks + blk, blocks * kWarps, job.rows, (sd.heads + per - 1) / per); at.left(); at.next_run()) {
+  for (Passes at(warp * blocks + blk, blocks * kWarps, job.rows, (sd.heads + per - 1) / per, job.run[si]); at.left(); at.next_run()) {
     const T* g = static_cast<const T*>(sd.g) + at.row * sd.grow;
     const T* x = static_cast<const T*>(sd.x) + at.row * sd.xrow;
     T* y = static_cast<T*>(sd.y) + at.row * sd.yrow;
@@ -894,22 +890,39 @@ int shift_of(const RopeTab& t, int v) {
   return s;
 }
 
+// Passes of a run: the split of a row that ends first where its runs are dealt to `warps` warps and the row's turns cost
+// as much as a pass.  (At least four runs a warp instead: a prompt's append 33.7 us, not 31.8.)
+unsigned run_of(long long rows, long long of_row, long long warps) {
+  long long best = 0;
+  unsigned run = 1;
+  for (long long parts = 1; parts <= std::min(of_row, 64ll); ++parts) {
+    const long long r = (of_row + parts - 1) / parts, runs = rows * ((of_row + r - 1) / r);
+    const long long end = (runs + warps - 1) / warps * (r + 1);
+    if (parts == 1 || end < best) {
+      best = end;
+      run = static_cast<unsigned>(r);
+    }
+  }
+  return run;
+}
+
 // Blocks of the sides: `limit` in proportion to what a row of them costs, at most one for kWarps passes of `per` heads.
 // In thirds of a pass: a pass 3 (of values, which are copied, 2), a row's turns 2.  (By passes alone the keys of grouped
 // heads, with a pass a row, were the last to end: the gradient of 16171 rows of 28 and 4 heads took 100 us, not 82.)
 void spread_blocks(Job& job, int sides, int per, int limit) {
-  long long passes[3] = {}, cost[3] = {}, all = 0;
+  long long of_row[3] = {}, cost[3] = {}, all = 0;
   for (int i = 0; i < sides; ++i) {
-    const long long of_row = (job.s[i].heads + per - 1) / per;
-    passes[i] = job.rows * of_row;
-    all += cost[i] = job.rows * (job.s[i].kind == kValues ? 2 * of_row : 3 * of_row + 2);
+    of_row[i] = (job.s[i].heads + per - 1) / per;
+    all += cost[i] = job.rows * (job.s[i].kind == kValues ? 2 * of_row[i] : 3 * of_row[i] + 2);
   }
   unsigned at = 0;
   for (int i = 0; i < 4; ++i) {
     job.first[i] = at;
     if (i >= sides) continue;
-    const long long share = std::max(1ll, limit * cost[i] / all), most = (passes[i] + kWarps - 1) / kWarps;
-    at += static_cast<unsigned>(std::min(share, most));
+    const long long share = std::max(1ll, limit * cost[i] / all), most = (job.rows * of_row[i] + kWarps - 1) / kWarps;
+    const long long blocks = std::min(share, most);
+    job.run[i] = run_of(job.rows, of_row[i], blocks * kWarps);
+    at += static_cast<unsigned>(blocks);
   }
 }
 

@@ -218,7 +218,9 @@ struct AxesChunk {
 };
 
 // The same with positions on three axes: kept token n of a frames x height x width grid at
-// (n / (height width) t_step, n / width % height, n % width), the question after the grid's largest position.
+// (n / (height width) t_step, n / width % height, n % width), the question after the grid's largest position.  A CTA a row
+// of the sequence, 128 threads of 16 bytes, so that a row's index, loads and stores are all that it waits for; HBM's work is
+// each row once in and once out: 3200 rows of 7 KB take 8 us, 10.6 with cold caches (6.7 at the copy rate).
 template <int IMAGES>
 __global__ void assemble_axes_kernel(const __grid_constant__ AxesChunk<IMAGES> m, const uint4* __restrict__ V,
                                      const int32_t* __restrict__ idx, const uint4* __restrict__ T, int vec_per_row,
