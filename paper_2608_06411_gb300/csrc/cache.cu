@@ -50,15 +50,16 @@ __device__ __forceinline__ int block_scan(int v, int* warp_sums, int* total) {
   }
   if (lane == 31) warp_sums[warp] = s;
   __syncthreads();
-  int before = 0, all = 0;
-  for (int w = 0; w < kPlanThreads / 32; ++w) {
-    const int x = warp_sums[w];
-    before += w < warp ? x : 0;
-    all += x;
+  int w = warp_sums[lane];                 // every warp scans the 32 sums for itself
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int u = __shfl_up_sync(0xffffffffu, w, o);
+    if (lane >= o) w += u;
   }
   __syncthreads();
-  *total = all;
-  return before + s - v;
+  *total = __shfl_sync(0xffffffffu, w, 31);
+  const int before = __shfl_sync(0xffffffffu, w, max(warp - 1, 0));
+  return (warp > 0 ? before : 0) + s - v;
 }
 
 // Last i in [0, n) with start[i] <= x (start ascending, start[0] = 0).
@@ -150,11 +151,11 @@ __global__ void __launch_bounds__(kPlanThreads) extend_kernel(const map_cache c,
           add = 0;
         } else {
           const int len = c.len[s];
-          const long long pages = (static_cast<long long>(len) + add + c.page - 1) / c.page;
+          const unsigned pages = (static_cast<unsigned>(len) + add + c.page - 1) / c.page;     // below 2^31 + 2^20 + 2^10 rows
           if (!good_len(c, len)) {
             atomicOr(&error, ST_BADINDEX);
             add = 0;
-          } else if (pages > c.max_pages) {
+          } else if (pages > static_cast<unsigned>(c.max_pages)) {
             atomicOr(&error, ST_NOPAGES);
             add = 0;
           } else {
@@ -249,12 +250,12 @@ __global__ void __launch_bounds__(kPlanThreads) fork_plan_kernel(const map_cache
           atomicOr(&error, ST_BADINDEX);
         } else {
           // a child longer than its parent (keep may repeat rows) can pass its table row, or 2^31
-          const long long pages = (static_cast<long long>(plen) - sp + (kept ? k : 0) + c.page - 1) / c.page;
           // (needs beyond the pool are refused here: 1024 of them could pass 2^31 in their sum)
-          if (pages > c.max_pages || pages - (kept ? b : plen) / c.page > c.pages) {
+          const unsigned pages = (static_cast<unsigned>(plen) - sp + (kept ? k : 0) + c.page - 1) / c.page;   // below 2^32 rows
+          const ForkShape f = fork_shape(plen, c.page, kept, b, sp, k);
+          if (pages > static_cast<unsigned>(c.max_pages) || static_cast<int>(pages) - f.shared > c.pages) {
             atomicOr(&error, ST_NOPAGES);
           } else {
-            const ForkShape f = fork_shape(plen, c.page, kept, b, sp, k);
             par[i] = p;
             seq[i] = s;
             col[i] = f.shared;
