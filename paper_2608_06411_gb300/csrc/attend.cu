@@ -596,7 +596,10 @@ cudaError_t launch_width(const AttendArgs& a, int sms, cudaStream_t st) {
   const long long most = static_cast<long long>(a.n) * a.c.heads * a.subs *
                          ((static_cast<long long>(a.c.max_pages) * a.c.page + kTile - 1) / kTile);
   const int grid = static_cast<int>(std::min<long long>(most, std::min(ctas * sms, max_grid(DH))));
-  return three ? launch_run<T, DH, 3>(a, smem_of<DH>(3, rows), grid, st) : launch_run<T, DH, 2>(a, smem_of<DH>(2, rows), grid, st);
+  // (64 and 96 columns have room for three with any number of rows)
+  if constexpr (kSm / (smem_of<DH>(3, kRows) + kOwn) < kWant)
+    if (!three) return launch_run<T, DH, 2>(a, smem_of<DH>(2, rows), grid, st);
+  return launch_run<T, DH, 3>(a, smem_of<DH>(3, rows), grid, st);
 }
 
 template <typename T>

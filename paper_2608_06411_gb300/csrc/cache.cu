@@ -116,7 +116,7 @@ __device__ bool take_pages(const map_cache& c, const int* start, const int* col,
 
 // counts[i] more rows for sequence seqs[i], and their slots.  Without counts entry i has row i, padding or not.  Latency-bound
 // (a few KB): one CTA, since every entry's pages depend on the needs of those before it.  16 entries of 200 rows and the call
-// that frees them take 10.8 us one after the other, 64 decoding rows and theirs 9.2.
+// that frees them take 8.5 us one after the other, 64 decoding rows and theirs 7.0 (with 512 threads 10.2 and 8.1).
 __global__ void __launch_bounds__(kPlanThreads) extend_kernel(const map_cache c, const int32_t* __restrict__ seqs,
                                                               const int32_t* __restrict__ counts, int n, int rows,
                                                               int32_t* __restrict__ slots) {
@@ -214,7 +214,8 @@ __global__ void __launch_bounds__(kPlanThreads) extend_kernel(const map_cache c,
 }
 
 // Tables, counts and lengths of the children.  status[1]: whether fork_copy_kernel is to copy.  Latency-bound like
-// extend_kernel, and one CTA for the same reason; beside the copy of 8 questions on a cached image it adds 6 us to 53.
+// extend_kernel, and one CTA for the same reason: of the 64 us of 8 questions' forks on a cached image and their free call the
+// copy takes 53 to 55.
 __global__ void __launch_bounds__(kPlanThreads) fork_plan_kernel(const map_cache c, const int32_t* __restrict__ parents,
                                                                  const int32_t* __restrict__ children, int n, int kept,
                                                                  int k, const int32_t* __restrict__ base,
@@ -400,7 +401,7 @@ __global__ void __launch_bounds__(kCopyThreads, 8) fork_copy_kernel(const map_ca
 }
 
 // A warp a sequence; the first to take its length frees its pages.  Latency-bound: three loads that depend on one another,
-// 5 us by itself with cold caches, 1 to 3 behind another call.
+// 5 us by itself with cold caches, 1.2 behind another call.
 __global__ void __launch_bounds__(256) free_kernel(const map_cache c, const int32_t* __restrict__ seqs, int n) {
   pdl_enter();
   const int i = (blockIdx.x * 256 + threadIdx.x) >> 5, lane = threadIdx.x & 31;
