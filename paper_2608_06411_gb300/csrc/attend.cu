@@ -8,12 +8,14 @@
 // that is below the loads for any G up to 16).  Split: an item is a sequence and up to 16 query heads of one key
 // head; the 64-row tiles of all items form one list, and every CTA takes an equal run of it (the lengths are read on the
 // device, so one long sequence and many short ones fill the chip alike).  A CTA's four warps take 16 rows of a tile
-// each, with a ring of tiles of their own filled by cp.async, and join once an item ends: no barrier in the loop over
+// each, with a ring of tiles of their own filled by cp.async, and join once an item ends (one barrier; 64 columns at a time
+// through a smaller buffer took eight, and 53 us where 50 are taken now): no barrier in the loop over
 // tiles.  Runs that begin or end inside an item leave (m, l, o) in the workspace; the last CTA of an item to do so
 // (counted in the cache's status words) joins them in list order, so results do not depend on timing.  (A second
 // kernel for that took 7 to 8 us; this way the join takes 3 to 4.)
-// Measured, dh = 128 in bf16: 64 sequences of 200 to 1600 rows, 32 heads over 8: 52.5 us, 4.8 TB/s, where the loads alone,
-// in this order and without any use, take 45.7; one sequence of 120001 rows, 28 heads over 4: 51.6 us, loads alone 42.5.
+// Measured, dh = 128 in bf16: 64 sequences of 200 to 1600 rows, 32 heads over 8: 50.2 us, 5.0 TB/s, where the loads alone,
+// in this order and without any use, take 45.7; one sequence of 120001 rows, 28 heads over 4: 50.8 us, loads alone 42.5.
+// Short sequences are bound by an item's own latency, about 2 us on a CTA: 1024 of 64 rows 76 us, 4000 of one row 217.
 #include <algorithm>
 #include <cmath>
 
@@ -127,6 +129,12 @@ __device__ __forceinline__ void split_weights(float x, float y, uint32_t& hi, ui
   lo = *reinterpret_cast<const uint32_t*>(&r);
 }
 
+template <typename T>
+__device__ __forceinline__ void store4(T* p, float4 v) {      // 8-byte aligned: strides are multiples of 8, columns of 4
+  alignas(8) const T x[4] = {from_f32<T>(v.x), from_f32<T>(v.y), from_f32<T>(v.z), from_f32<T>(v.w)};
+  *reinterpret_cast<uint2*>(p) = *reinterpret_cast<const uint2*>(x);
+}
+
 // Place in the list: tile t of item `item` (key head * subs + sub) of entry i.
 struct Place {
   int i, s, len, tiles, item, t;
@@ -154,6 +162,8 @@ struct Tile {
   static constexpr int kVecs = DH / 8;
   static constexpr int kRow = DH * 2 + 16;
   static constexpr int kStage = 2 * kTok * kRow;             // K and V rows of one warp's part of a tile
+  static constexpr int kSum = DH + 8;                        // floats of a row of sums: four rows' halves meet distinct banks
+  static_assert(kRows * kSum * 4 <= kStage, "sums take the place of a tile");
   static __device__ __forceinline__ uint32_t at(int row, int x) { return row * kRow + x * 16; }
 };
 // Joins `count` parts, of CTAs c, c + stride, ... (the first one's slot `slot0`, the others' slot 0), in order: into out,
@@ -208,10 +218,7 @@ __device__ __noinline__ void join_parts(const AttendArgs& a, int c, int stride, 
       if (e >= pieces) break;
       if (out) {
         T* o = out + r * a.out.head + x;
-        o[0] = from_f32<T>(v[d].x / sum[d]);
-        o[1] = from_f32<T>(v[d].y / sum[d]);
-        o[2] = from_f32<T>(v[d].z / sum[d]);
-        o[3] = from_f32<T>(v[d].w / sum[d]);
+        store4(o, make_float4(v[d].x / sum[d], v[d].y / sum[d], v[d].z / sum[d], v[d].w / sum[d]));
       } else {
         *reinterpret_cast<float4*>(part(0) + 2 * kRows + r * DH + x) = v[d];
         if (x == 0) {
@@ -302,7 +309,6 @@ __global__ void __launch_bounds__(kThreads, ctas_of(DH)) attend_kernel(const __g
 
   const uint32_t ring = smem_u32(sh) + warp * STAGES * R::kStage;
   const uint32_t qbuf = smem_u32(sh) + kWarps * STAGES * R::kStage;                        // [STAGES][rows] tile rows
-  float* join = reinterpret_cast<float*>(sh + kWarps * STAGES * R::kStage + STAGES * rows * R::kRow);   // [2][rows][64]
   const T* pk = static_cast<const T*>(a.pk);
   const T* pv = pk + a.plane;
   const bool whole = a.c.page % kTok == 0;     // a warp's 16 rows lie in one page
@@ -477,7 +483,8 @@ __global__ void __launch_bounds__(kThreads, ctas_of(DH)) attend_kernel(const __g
 
     const bool ends = cp.t + 1 == cp.tiles;
     if (ends || n + 1 == run) {
-      // join the warps
+      // join the warps: each lays its sums down where its rows of this tile were, which nothing but itself has read and
+      // the next load to write there is behind the next barrier
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         l[h] += __shfl_xor_sync(0xffffffffu, l[h], 1);
@@ -487,67 +494,43 @@ __global__ void __launch_bounds__(kThreads, ctas_of(DH)) attend_kernel(const __g
           sl[warp][(lane >> 2) + 8 * h] = l[h];
         }
       }
+      __syncwarp();
+      float* sums = reinterpret_cast<float*>(sh + (n % STAGES) * R::kStage);     // of warp 0
+      float* own = sums + warp * (STAGES * R::kStage / 4) + (lane >> 2) * R::kSum + 2 * (lane & 3);
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+        if ((lane >> 2) + 8 * h < rows)
+#pragma unroll
+          for (int j = 0; j < DH / 8; ++j)
+            *reinterpret_cast<float2*>(own + 8 * h * R::kSum + 8 * j) = make_float2(o[j][2 * h], o[j][2 * h + 1]);
       __syncthreads();
-      float top[2];
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const int r = (lane >> 2) + 8 * h;
-        top[h] = fmaxf(fmaxf(sm[0][r], sm[1][r]), fmaxf(sm[2][r], sm[3][r]));
-        const float f = exp2_fast(m[h] - (top[h] == -INFINITY ? 0.f : top[h]));
-#pragma unroll
-        for (int j = 0; j < DH / 8; ++j) {
-          o[j][2 * h] *= f;
-          o[j][2 * h + 1] *= f;
-        }
-      }
       const int kh = cp.item / a.subs, g0 = (cp.item % a.subs) * kRows, have = min(kRows, a.group - g0);
       const bool done = ends && from_start;
       float* part = a.ws + static_cast<long long>(2 * blockIdx.x + (from_start ? 1 : 0)) * part_floats(DH);
       T* out = static_cast<T*>(a.out.p) + cp.i * a.out.row + (kh * a.group + g0) * a.out.head;
+      for (int e = tid; e < have * (DH / 4); e += kThreads) {                    // four columns of a row
+        const int r = e / (DH / 4), x = 4 * (e % (DH / 4));
+        const float top = fmaxf(fmaxf(sm[0][r], sm[1][r]), fmaxf(sm[2][r], sm[3][r])), at = top == -INFINITY ? 0.f : top;
+        float lr = 0.f;
+        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-      for (int c0 = 0; c0 < DH; c0 += 64) {
-        // warps 0 and 2 lay down 64 columns, 1 and 3 add theirs, all threads add the two
-        float* buf = join + (warp >> 1) * rows * 64;
-#pragma unroll
-        for (int turn = 0; turn < 2; ++turn) {
-          if ((warp & 1) == turn) {
-#pragma unroll
-            for (int jj = 0; jj < 8; ++jj)
-#pragma unroll
-              for (int h = 0; h < 2; ++h) {
-                const int r = (lane >> 2) + 8 * h, j = c0 / 8 + jj;
-                if (j >= DH / 8 || r >= rows) continue;
-                float2* x = reinterpret_cast<float2*>(buf + r * 64 + jj * 8 + 2 * (lane & 3));
-                float2 v = make_float2(o[j][2 * h], o[j][2 * h + 1]);
-                if (turn) { v.x += x->x; v.y += x->y; }
-                *x = v;
-              }
-          }
-          __syncthreads();
+        for (int w = 0; w < kWarps; ++w) {
+          const float f = exp2_fast(sm[w][r] - at);
+          const float4 y = *reinterpret_cast<const float4*>(sums + w * (STAGES * R::kStage / 4) + r * R::kSum + x);
+          lr = fmaf(f, sl[w][r], lr);
+          v = make_float4(fmaf(f, y.x, v.x), fmaf(f, y.y, v.y), fmaf(f, y.z, v.z), fmaf(f, y.w, v.w));
         }
-        const int width = DH - c0 < 64 ? DH - c0 : 64;
-        for (int e = tid; e < have * 64; e += kThreads) {
-          const int r = e >> 6, x = e & 63;
-          if (x >= width) continue;
-          const float v = join[r * 64 + x] + join[(rows + r) * 64 + x];
-          if (done) {
-            const float mr = fmaxf(fmaxf(sm[0][r], sm[1][r]), fmaxf(sm[2][r], sm[3][r])), at = mr == -INFINITY ? 0.f : mr;
-            const float lr = sl[0][r] * exp2_fast(sm[0][r] - at) + sl[1][r] * exp2_fast(sm[1][r] - at) +
-                             sl[2][r] * exp2_fast(sm[2][r] - at) + sl[3][r] * exp2_fast(sm[3][r] - at);
-            out[r * a.out.head + c0 + x] = from_f32<T>(v / lr);
-          } else {
-            part[2 * kRows + r * DH + c0 + x] = v;
+        if (done) {
+          store4(out + r * a.out.head + x, make_float4(v.x / lr, v.y / lr, v.z / lr, v.w / lr));
+        } else {
+          *reinterpret_cast<float4*>(part + 2 * kRows + r * DH + x) = v;
+          if (x == 0) {
+            part[r] = top;
+            part[kRows + r] = lr;
           }
         }
-        __syncthreads();
       }
       if (!done) {
-        if (tid < have) {
-          const float mr = fmaxf(fmaxf(sm[0][tid], sm[1][tid]), fmaxf(sm[2][tid], sm[3][tid])), at = mr == -INFINITY ? 0.f : mr;
-          part[tid] = mr;
-          part[kRows + tid] = sl[0][tid] * exp2_fast(sm[0][tid] - at) + sl[1][tid] * exp2_fast(sm[1][tid] - at) +
-                              sl[2][tid] * exp2_fast(sm[2][tid] - at) + sl[3][tid] * exp2_fast(sm[3][tid] - at);
-        }
         // the item's parts: CTAs c0 (whose run begins it) to c0 + parts - 1, in groups of kGroup.  The last CTA of a
         // group joins the group, the last group's the groups.  Counters: a group's at its first CTA, the groups' at c0;
         // a group of one needs none, so the next item's first group may begin where this one's last does.
@@ -555,11 +538,11 @@ __global__ void __launch_bounds__(kThreads, ctas_of(DH)) attend_kernel(const __g
         const int c0 = static_cast<int>(tile / per), parts = static_cast<int>((tile + cp.tiles - 1) / per) - c0 + 1;
         const int g = (static_cast<int>(blockIdx.x) - c0) / kGroup, groups = (parts + kGroup - 1) / kGroup;
         const int first = c0 + g * kGroup, count = min(kGroup, parts - g * kGroup);
-        float* sums = reinterpret_cast<float*>(red + kWarps);
+        float* scratch = reinterpret_cast<float*>(red + kWarps);
         if (is_last(a.c.status + 2 + first, count, &last_part)) {
-          if (groups == 1 || count > 1) join_parts<T, DH>(a, first, 1, g == 0, count, have, groups == 1 ? out : nullptr, sm[0], sums);
+          if (groups == 1 || count > 1) join_parts<T, DH>(a, first, 1, g == 0, count, have, groups == 1 ? out : nullptr, sm[0], scratch);
           if (groups > 1 && is_last(a.c.status + 2 + kMaxGrid + c0, groups, &last_part))
-            join_parts<T, DH>(a, c0, kGroup, 1, groups, have, out, sm[0], sums);
+            join_parts<T, DH>(a, c0, kGroup, 1, groups, have, out, sm[0], scratch);
         }
         __syncthreads();
       }
@@ -580,7 +563,7 @@ cudaError_t launch_run(const AttendArgs& a, size_t smem, int grid, cudaStream_t 
 
 template <int DH>
 constexpr size_t smem_of(int stages, int rows) {
-  return static_cast<size_t>(kWarps) * stages * Tile<DH>::kStage + stages * rows * Tile<DH>::kRow + 2 * rows * 64 * 4;
+  return static_cast<size_t>(kWarps) * stages * Tile<DH>::kStage + stages * rows * Tile<DH>::kRow;
 }
 
 // Tiles in a ring and CTAs an SM: two tiles ahead and two CTAs where they fit (dh = 128, without the join: one sequence of
