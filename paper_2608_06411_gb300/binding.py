@@ -603,7 +603,7 @@ class Rope:
         _check(lib.map_qk_rotate_append(self.h, cache.desc, layer, rows, _dense(pos, torch.int32, dev, (self.n_axes, rows), "pos"),
                                         _dense(slots, torch.int32, dev, (rows,), "slots"), a, _heads(k, rows, dh, dt, dev),
                                         _heads(v, rows, dh, dt, dev), _dense(wq, dt, dev, (dh,), "wq"),
-                                        _dense(wk, dt, dev, (dh,), "wk"), oa, _current_stream(dev.index)), "map_qk_rotate_append")
+                                        _dense(wk, dt, dev, (dh,), "wk"), oa, cache._stream()), "map_qk_rotate_append")
         return q_out
 
 
@@ -630,7 +630,17 @@ class Cache:
         self.desc = _pack_cache(pool.data_ptr(), *ptrs, TYPES[pool.dtype], layers, pages, heads, page, dh, seqs, max_pages)
         # attend's scratch: calls on one cache are ordered by the caller, so they can share it
         self._ws = torch.empty(int(lib.map_cache_attend_workspace(self.desc)), dtype=torch.uint8, device=dev)
-        self._ws_streams = {_current_stream(dev.index)} if dev.type == "cuda" else set()     # that the allocator knows of
+        self._streams = set()                # that the allocator knows of
+        self._tensors = (pool, table, length, refs, status, self._ws)
+
+    def _stream(self) -> int:
+        """The current stream.  The allocator hears of it once, so that the memory of a Cache that is dropped waits for it."""
+        st = _current_stream(self.device.index)
+        if st not in self._streams:
+            for t in self._tensors:
+                t.record_stream(torch.cuda.current_stream(self.device))
+            self._streams.add(st)
+        return st
 
     @classmethod
     def empty(cls, layers: int, pages: int, heads: int, page: int, dh: int, seqs: int, max_pages: int,
@@ -660,7 +670,7 @@ class Cache:
             slots = torch.empty(rows, dtype=torch.int32, device=dev)
         _check(lib.map_cache_extend(self.desc, _dense(seqs, torch.int32, dev, (n,), "seqs"),
                                     _dense(counts, torch.int32, dev, (n,), "counts"), n, rows,
-                                    _dense(slots, torch.int32, dev, (rows,), "slots"), _current_stream(dev.index)),
+                                    _dense(slots, torch.int32, dev, (rows,), "slots"), self._stream()),
                "map_cache_extend")
         return slots
 
@@ -678,7 +688,7 @@ class Cache:
         _check(lib.map_cache_fork(self.desc, _dense(parents, i32, dev, (n,), "parents"),
                                   _dense(children, i32, dev, (n,), "children"), n, _dense(keep, i32, dev, (n, k), "keep"), k,
                                   _dense(base, i32, dev, (n,), "base"), _dense(span, i32, dev, (n,), "span"),
-                                  _current_stream(dev.index)), "map_cache_fork")
+                                  self._stream()), "map_cache_fork")
 
     def free(self, seqs, stream=None) -> None:
         """map_cache_free: the pages of seqs (int32 [n] on the device) lose a holder, the lengths become 0."""
@@ -687,7 +697,7 @@ class Cache:
             with _on(dev, stream):
                 return self.free(seqs)
         n = seqs.shape[0]
-        _check(lib.map_cache_free(self.desc, _dense(seqs, torch.int32, dev, (n,), "seqs"), n, _current_stream(dev.index)),
+        _check(lib.map_cache_free(self.desc, _dense(seqs, torch.int32, dev, (n,), "seqs"), n, self._stream()),
                "map_cache_free")
 
     def attend(self, q, seqs, layer: int, scale: float | None = None, out=None, stream=None):
@@ -703,12 +713,9 @@ class Cache:
             out, oa = _like(q, dh)
         else:
             oa = _heads(out, n, dh, dt, dev)
-        st = _current_stream(dev.index)
-        if st not in self._ws_streams:
-            self._ws.record_stream(torch.cuda.current_stream(dev))
-            self._ws_streams.add(st)
         _check(lib.map_cache_attend(self.desc, layer, a, _dense(seqs, torch.int32, dev, (n,), "seqs"), n,
-                                    dh ** -0.5 if scale is None else scale, oa, self._ws.data_ptr(), st), "map_cache_attend")
+                                    dh ** -0.5 if scale is None else scale, oa, self._ws.data_ptr(), self._stream()),
+               "map_cache_attend")
         return out
 
     def status(self, stream=None) -> int:

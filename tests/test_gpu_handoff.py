@@ -677,6 +677,24 @@ def test_calls_on_a_stream_of_the_callers(mb):
     assert all(torch.equal(a, b) for a, b in zip((*want, *wgrad, watt), (*got, *ggrad, gatt)))
 
 
+def test_a_dropped_cache_waits_for_every_stream(mb):
+    """The same of the pages that Cache.empty made: rows appended on another stream land before they are handed out."""
+    cache = mb.Cache.empty(1, 64, 2, 16, 64, 2, 32, dtype=torch.float16)
+    plan, x = mb.Rope(64, [1.0]), torch.ones(300, 2, 64, dtype=torch.float16, device=DEV)
+    pos, slots = torch.zeros(1, 300, dtype=torch.int32, device=DEV), cache.extend(ints([0]), ints([300]), rows=300)
+    torch.cuda.synchronize()
+    s = torch.cuda.Stream()
+    with torch.cuda.stream(s):
+        torch.cuda._sleep(100_000_000)
+        plan.append(None, x, x, pos, cache, 0, slots)
+    place, size = cache.pool.data_ptr(), cache.pool.numel()
+    del cache
+    other = torch.full((size,), 7.0, dtype=torch.float16, device=DEV)
+    assert other.data_ptr() != place
+    torch.cuda.synchronize()
+    assert bool((other == 7).all())
+
+
 def test_append_of_rows_at_any_alignment(mb):
     """Half of 72 columns turned, 18 pairs, and heads that begin on odd elements: keys and values reach their slots."""
     rows, hq, hk, dh = 45, 6, 3, 72
