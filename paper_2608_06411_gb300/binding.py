@@ -11,6 +11,7 @@ import ctypes
 import os
 import struct
 from ctypes import POINTER, c_double, c_float, c_int, c_int32, c_longlong, c_size_t, c_void_p
+from itertools import chain
 
 import numpy as np
 import torch
@@ -152,9 +153,9 @@ def _host_ints(x, rows: int, cols: int, what: str) -> bytes:
             raise ValueError(f"{what} must be {rows} x {cols} whole numbers")
         x = x.reshape(-1).tolist()
     elif cols > 1:
-        if any(len(r) != cols for r in x):
+        if set(map(len, x)) != {cols}:
             raise ValueError(f"{what} must be {rows} x {cols} whole numbers")
-        x = [v for r in x for v in r]
+        x = list(chain.from_iterable(x))
     if len(x) != rows * cols:
         raise ValueError(f"{what} must be {rows} x {cols} whole numbers")
     try:
@@ -264,25 +265,21 @@ class Context:
         if stream is not None:               # outputs are allocated on the stream that writes them
             with _on(dev, stream):
                 return self.assemble_axes(vis, keep, text, lens, grids, t_step, pos_offset, seq, pos)
-        if keep.shape[0] != B or keep.dtype is not torch.int32 or keep.device != dev:
-            raise ValueError(f"keep must be int32 [B, k] on {dev}")
         m = _host_ints(lens, B, 1, "lens")
         g = _host_ints(grids, B, 3, "grids")
         t = None if t_step is None else _host_ints(t_step, B, 1, "t_step")
         questions = int(sum(lens))
         rows = B * k + questions
-        if text.shape[0] < questions or text.shape[1] != D or text.dtype is not dt or text.device != dev:
-            raise ValueError(f"text must be {dt} [sum(lens), {D}] on {dev}")
+        if text.shape[0] < questions or text.shape[1] != D:
+            raise ValueError(f"text must be [sum(lens), {D}]")
         if seq is None:
             seq = torch.empty((rows, D), dtype=dt, device=dev)
-        elif seq.shape != (rows, D) or seq.dtype is not dt or seq.device != dev:
-            raise ValueError(f"seq must be {dt} [{rows}, {D}] on {dev}")
         if pos is None:
             pos = torch.empty((3, rows), dtype=torch.int32, device=dev)
-        elif pos.shape != (3, rows) or pos.dtype is not torch.int32 or pos.device != dev:
-            raise ValueError(f"pos must be int32 [3, {rows}] on {dev}")
-        _check(lib.map_assemble_axes(self.h, _ptr(vis), _ptr(keep), _ptr(text), m, g, t, B, N, k, pos_offset, _ptr(seq),
-                                     _ptr(pos), _current_stream(dev.index)), "map_assemble_axes")
+        _check(lib.map_assemble_axes(self.h, _dense(vis, dt, dev, None, "vis"), _dense(keep, torch.int32, dev, (B, k), "keep"),
+                                     _dense(text, dt, dev, None, "text"), m, g, t, B, N, k, pos_offset,
+                                     _dense(seq, dt, dev, (rows, D), "seq"), _dense(pos, torch.int32, dev, (3, rows), "pos"),
+                                     _current_stream(dev.index)), "map_assemble_axes")
         return seq, pos
 
     # -- ragged batches (padded layout, n_valid tokens per image) ---------------------------
