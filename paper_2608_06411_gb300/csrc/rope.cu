@@ -450,6 +450,9 @@ __global__ void __launch_bounds__(kThreads, kGradCtas) grad_kernel(const __grid_
   uint4* mine = stages + warp * (kStages * 128) + lane;
 #pragma unroll
   for (int n = 0; n < 4 * kStages; ++n) mine[n * 32] = make_uint4(0, 0, 0, 0);
+  // behind a row's turns too: a lane without columns turns its zeros by what stands there and adds them to its head's sums,
+  // which an earlier kernel's words could make NaN
+  for (int c = tab.rot + lane; c < kMaxHead; c += 32) turns_buf[warp][c] = 0.f;
   __syncthreads();                             // before the copies to the same places
   const uint32_t mine_at = smem_u32(mine), row_at = smem_u32(row_buf[warp][0]);
   const Heads ing(sd.g, sd.grow, sd.ghead, ln.a, T()), inx(sd.x, sd.xrow, sd.xhead, ln.a, T()), out(sd.y, sd.yrow, sd.yhead, ln.a, T());

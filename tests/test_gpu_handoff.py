@@ -283,6 +283,24 @@ def test_rotate_grad_of_no_rows_and_one_side(mb):
     assert dk is None and dwk is None and dq.shape == z.shape and bool((dwq == 0).all())
 
 
+@pytest.mark.parametrize("typ,dh,adjacent", [("bf16", 80, False), ("bf16", 96, False), ("f16", 192, False), ("f16", 48, False),
+                                             ("f32", 80, False), ("f32", 72, False), ("f16", 20, False), ("bf16", 80, True),
+                                             ("f32", 12, True)])
+def test_rotate_grad_after_sums_of_nan(mb, typ, dh, adjacent):
+    """Heads whose vectors are no power of two leave lanes without columns.  What an earlier kernel left in shared memory
+    must not reach their heads' sums: a gradient of NaN, 256 columns wide, leaves sums of NaN there."""
+    typ, g, rows, heads = TYPES[typ], gen(3), 1200, 4
+    inv = [0.9 ** i for i in range(dh // 2)]
+    x, dy = (randn(g, rows, heads, dh, typ=typ) for _ in range(2))
+    w = (1 + 0.3 * torch.randn(dh, generator=g, device=DEV)).to(typ)
+    pos = torch.randint(0, 5000, (1, rows), generator=g, device=DEV, dtype=torch.int32)
+    wide = torch.full((rows, heads, 256), float("nan"), dtype=typ, device=DEV)
+    bad, plan = (mb.Rope(d, f, adjacent=adjacent) for d, f in ((256, [1.0] * 128), (dh, inv)))
+    assert bool(torch.isnan(bad.grad(wide, None, pos, wide, None, wide[0, 0])[2]).all())
+    dx, _, dw, _ = plan.grad(dy, None, pos, x, None, w)
+    check_grad(dx, dw, dy, x, w, pos, inv, [0] * len(inv), adjacent, typ)
+
+
 # ----------------------------------------------------------------------------- positions
 
 @pytest.mark.parametrize("grids,lens,k,step,off,N", [
