@@ -221,11 +221,13 @@ __device__ __forceinline__ float dot2(const float2 (&a)[N], const float2 (&b)[N]
   for (int i = 0; i < N; ++i) s = fma2(a[i], b[i], s);
   return s.x + s.y;
 }
-// Sum over the lanes of a head times 2^(5 - shift): steps past the head's lanes add a lane's sum to itself, which is
-// exact and costs less than branches around them.
+// Sum over the lanes of a head, of what a lane gives times `part` = 2^(shift - 5): always five steps, for those past the
+// head's lanes, which add a lane's sum to itself, cost less than branches around them.  What they double is taken out
+// before: squares that add up to less than 2^128 do not pass it on the way.
 struct LaneSum {
   int m[5];
-  __device__ __forceinline__ explicit LaneSum(int shift) {
+  float part;
+  __device__ __forceinline__ explicit LaneSum(int shift) : part(static_cast<float>(1 << shift) * 0.03125f) {
 #pragma unroll
     for (int i = 0; i < 5; ++i) m[i] = i < shift ? 1 << i : 0;
   }
@@ -373,7 +375,7 @@ __global__ void __launch_bounds__(kThreads, kRotateCtas) rotate_kernel(const __g
   const float* w_a = weight + (ln.on ? ln.a : 0);
   const float* w_b = weight + (ln.two ? ln.b : 0);
   const LaneSum lane_sum(shift);
-  const float inv = tab.inv_dh * static_cast<float>(1 << shift) * 0.03125f;
+  const float inv = tab.inv_dh;
   Turns<V> turns;
   unsigned turned_row = 0xffffffffu;
   bool begins = true, write = true;
@@ -403,7 +405,7 @@ __global__ void __launch_bounds__(kThreads, kRotateCtas) rotate_kernel(const __g
       va.get(a);
       vb.get(b);
       if (norm) {
-        const float ss = lane_sum(dot2(a, a, dot2(b, b, 0.f)));
+        const float ss = lane_sum(dot2(a, a, dot2(b, b, 0.f)) * lane_sum.part);
         const float r = rsqrtf(fmaf(ss, inv, tab.eps));
         const float2 r2 = make_float2(r, r);
         float2 wa[V / 2], wb[V / 2];
@@ -491,7 +493,7 @@ __global__ void __launch_bounds__(kThreads, kGradCtas) grad_kernel(const __grid_
 #pragma unroll
   for (int i = 0; i < V / 2; ++i) da[i] = db[i] = make_float2(0.f, 0.f);
   const LaneSum lane_sum(shift);
-  const float inv = tab.inv_dh * static_cast<float>(1 << shift) * 0.03125f;
+  const float inv = tab.inv_dh, minus = -inv * lane_sum.part;
   Turns<V> turns;
   unsigned turned_row = 0xffffffffu;
   bool begins = true;
@@ -527,9 +529,9 @@ __global__ void __launch_bounds__(kThreads, kGradCtas) grad_kernel(const __grid_
         ha[i] = mul2(a[i], ha[i]);
         hb[i] = mul2(b[i], hb[i]);
       }
-      const float ss = lane_sum(dot2(na, na, dot2(nb, nb, 0.f)));
+      const float ss = lane_sum(dot2(na, na, dot2(nb, nb, 0.f)) * lane_sum.part);
       const float r = rsqrtf(fmaf(ss, inv, tab.eps));
-      const float m = lane_sum(dot2(ha, na, dot2(hb, nb, 0.f))) * r * -inv;        // -mean(g w n)
+      const float m = lane_sum(dot2(ha, na, dot2(hb, nb, 0.f)) * minus) * r;       // -mean(g w n)
       const float2 r2 = make_float2(r, r), m2 = make_float2(m, m);
 #pragma unroll
       for (int i = 0; i < V / 2; ++i) {
@@ -681,7 +683,7 @@ __global__ void __launch_bounds__(kThreads, kAnyCtas<S>) rotate_any_kernel(const
   const long long yhead = paged ? static_cast<long long>(job.page) * tab.dh : sd.yhead;
   Pairs<T, S> pairs(tab, job, static_cast<const T*>(sd.w), lane & ((1 << shift) - 1), shift);
   const LaneSum lane_sum(shift);
-  const float inv = tab.inv_dh * static_cast<float>(1 << shift) * 0.03125f;
+  const float inv = tab.inv_dh;
   for (Passes at((threadIdx.x >> 5) * blocks + blk, blocks * kWarps, job.rows, (sd.heads + per - 1) / per, job.run[si]); at.left(); at.next_run()) {
     const T* x = static_cast<const T*>(sd.x) + at.row * sd.xrow;
     T* y = static_cast<T*>(sd.y) + (paged ? 0 : at.row * sd.yrow);
@@ -705,7 +707,7 @@ __global__ void __launch_bounds__(kThreads, kAnyCtas<S>) rotate_any_kernel(const
           float ss = 0.f;
 #pragma unroll
           for (int i = 0; i < S; ++i) ss = fmaf(a[i], a[i], fmaf(b[i], b[i], ss));
-          const float r = rsqrtf(fmaf(lane_sum(ss), inv, tab.eps));
+          const float r = rsqrtf(fmaf(lane_sum(ss * lane_sum.part), inv, tab.eps));
 #pragma unroll
           for (int i = 0; i < S; ++i) {
             a[i] *= r * pairs.wa[i];
@@ -734,7 +736,7 @@ __global__ void __launch_bounds__(kThreads, kGradCtas) grad_any_kernel(const __g
   const bool norm = sd.w != nullptr;
   Pairs<T, S> pairs(tab, job, static_cast<const T*>(sd.w), lane & ((1 << shift) - 1), shift);
   const LaneSum lane_sum(shift);
-  const float inv = tab.inv_dh * static_cast<float>(1 << shift) * 0.03125f;
+  const float inv = tab.inv_dh;
   float da[S] = {}, db[S] = {};
   for (Passes at(warp * blocks + blk, blocks * kWarps, job.rows, (sd.heads + per - 1) / per, job.run[si]); at.left(); at.next_run()) {
     const T* g = static_cast<const T*>(sd.g) + at.row * sd.grow;
@@ -764,8 +766,8 @@ __global__ void __launch_bounds__(kThreads, kGradCtas) grad_any_kernel(const __g
             ss = fmaf(na[i], na[i], fmaf(nb[i], nb[i], ss));
             dot = fmaf(a[i] * pairs.wa[i], na[i], fmaf(b[i] * pairs.wb[i], nb[i], dot));
           }
-          const float r = rsqrtf(fmaf(lane_sum(ss), inv, tab.eps));
-          const float m = lane_sum(dot) * r * inv;             // mean(g w n)
+          const float r = rsqrtf(fmaf(lane_sum(ss * lane_sum.part), inv, tab.eps));
+          const float m = lane_sum(dot * lane_sum.part) * r * inv;             // mean(g w n)
 #pragma unroll
           for (int i = 0; i < S; ++i) {
             na[i] *= r;

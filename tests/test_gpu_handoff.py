@@ -250,6 +250,26 @@ def test_rotate_grad_matches_the_formula(mb, case):
     assert torch.equal(dqv, a) and torch.equal(dkv, b)
 
 
+@pytest.mark.parametrize("typ,dh,layout,top", [("bf16", 128, "dense", 1.4e18), ("f32", 128, "dense", 1.4e18),
+                                               ("bf16", 64, "dense", 2e18), ("f32", 256, "dense", 1e18), ("bf16", 8, "dense", 6e18),
+                                               ("f32", 128, "odd", 1.4e18), ("bf16", 36, "odd", 2.9e18), ("bf16", 6, "dense", 6e18)])
+def test_norms_of_heads_whose_squares_almost_overflow(mb, typ, dh, layout, top):
+    """The sum of a head's squares is below 2^128, 32 / lanes times it is not."""
+    typ, g, rows, heads = TYPES[typ], gen(3), 33, 3
+    inv = [0.9 ** i for i in range(dh // 2)]
+    x = (randn(g, rows, heads, dh, typ=torch.float32).sign() * top * (1 - 0.2 * torch.rand(rows, heads, dh, generator=g, device=DEV))).to(typ)
+    assert float(x.double().square().sum(-1).max()) < 3.3e38
+    dy = randn(g, rows, heads, dh, typ=typ)
+    w = (1 + 0.3 * torch.randn(dh, generator=g, device=DEV)).to(typ)
+    pos = torch.randint(0, 5000, (1, rows), generator=g, device=DEV, dtype=torch.int32)
+    plan = mb.Rope(dh, inv)
+    (xv, _), (dyv, _) = place(x, layout), place(dy, layout)
+    y, _ = plan.rotate(xv, None, pos, w)
+    check_rotated(y, x, w, pos, inv, [0] * len(inv), False, typ)
+    dx, _, dw, _ = plan.grad(dyv, None, pos, xv, None, w)
+    check_grad(dx, dw, dy, x, w, pos, inv, [0] * len(inv), False, typ)
+
+
 def test_rotate_grad_against_differences(mb):
     """<grad, d> = (loss(x + h d) - loss(x - h d)) / 2h in fp32: the difference is off by h^2 / 6 of the third derivative
     (of order 10 for heads of unit norm: 2e-4 at h = 1e-2 times the sum's size) and by fp32 roundings over h (a sum of
