@@ -111,21 +111,26 @@ template <> __device__ __forceinline__ void mma16<__half>(float (&d)[4], const u
                : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 // Weights as two halves of T, 16 bits of them and more: one half alone would add an error as large as the output's own
-// rounding.  The first is cut, so that the second is not negative, and the second is never zero: an infinite v stays
-// infinite.  kLift: weights are taken 2^kLift times too large, l and o with them, where T's range needs it.
+// rounding.  The first is cut, so that the second is not negative.  Both halves of a weight above zero are kept above zero, and
+// those of a weight of zero are zero: an infinite v is infinite in the sum as far as fp32 knows its weight, and scores that
+// are all minus infinity add up to nothing.  (A half that is raised adds its type's smallest number at most: 2^-39 of the
+// largest weight.)  kLift: weights are taken 2^kLift times too large, l and o with them, where T's range needs it.
 template <typename T> constexpr float kLift = 0.f;
 template <> constexpr float kLift<__half> = 15.f;            // 2^15 down to 2^-24
+__device__ __forceinline__ float at_least(float least, float x) { return x > 0.f ? least : 0.f; }
 __device__ __forceinline__ void split_weights(float x, float y, uint32_t& hi, uint32_t& lo, __nv_bfloat16) {
   const uint32_t a = __float_as_uint(x), b = __float_as_uint(y);
-  hi = __byte_perm(a, b, 0x7632);
+  hi = __byte_perm(a, b, 0x7632);              // above zero where x is: ex2 gives no subnormal numbers
   const __nv_bfloat162 r = __hmax2(__floats2bfloat162_rn(x - __uint_as_float(a & 0xffff0000u), y - __uint_as_float(b & 0xffff0000u)),
-                                   __floats2bfloat162_rn(0x1p-126f, 0x1p-126f));
+                                   __floats2bfloat162_rn(at_least(0x1p-126f, x), at_least(0x1p-126f, y)));
   lo = *reinterpret_cast<const uint32_t*>(&r);
 }
 __device__ __forceinline__ void split_weights(float x, float y, uint32_t& hi, uint32_t& lo, __half) {
   asm("cvt.rz.f16x2.f32 %0, %1, %2;" : "=r"(hi) : "f"(y), "f"(x));
-  const __half2 h = *reinterpret_cast<const __half2*>(&hi);
-  const __half2 r = __hmax2(__floats2half2_rn(x - __low2float(h), y - __high2float(h)), __floats2half2_rn(0x1p-24f, 0x1p-24f));
+  const __half2 cut = *reinterpret_cast<const __half2*>(&hi), least = __floats2half2_rn(at_least(0x1p-24f, x), at_least(0x1p-24f, y));
+  const __half2 h = __hmax2_nan(cut, least);                 // (not a number where x is none)
+  const __half2 r = __hmax2(__floats2half2_rn(x - __low2float(cut), y - __high2float(cut)), least);
+  hi = *reinterpret_cast<const uint32_t*>(&h);
   lo = *reinterpret_cast<const uint32_t*>(&r);
 }
 

@@ -672,6 +672,29 @@ def test_attend_values_at_the_edges(mb):
     assert cache.attend(q[:0], ints([]), 0).shape == (0, 2, 64)
 
 
+@pytest.mark.parametrize("typ", ["f16", "bf16"])
+def test_attend_infinite_values_of_small_weights(mb, typ):
+    """Weights from 1 down to 2^-110 (scores 8 k, in 1 / ln 2 steps): an infinite value of any of them is infinite in the
+    sum.  Scores of minus infinity alone give no weights: NaN."""
+    typ = TYPES[typ]
+    for gap in (1.0, 3.0, 5.0, 9.5):                                  # 11, 34, 57 and 109 powers of two
+        for sign, row in ((1.0, 5), (-1.0, 69)):                      # of the first warp in both tiles
+            cache = filled(mb, typ, 64, 1, 16, [100, 40], 2)
+            page = cache.table[0, row // 16].long()
+            keys, values = cache.pool[0, 0, :, 0], cache.pool[0, 1, :, 0]
+            keys[cache.table[0, :7].long()] = 0.0
+            keys[cache.table[0, 0].long(), 3] = gap
+            values[page, 5, 7] = sign * float("inf")
+            q = torch.ones(2, 2, 64, dtype=typ, device=DEV)
+            out = cache.attend(q, ints([0, 1]), 0)
+            assert bool((out[0, :, 7] == sign * float("inf")).all()), (gap, out[0, :, 7])
+            out[0, :, 7] = 0.0
+            assert bool(torch.isfinite(out).all())
+    keys[cache.table[0, :7].long(), :, 0] = float("-inf")
+    out = cache.attend(q, ints([0, 1]), 0)
+    assert bool(torch.isnan(out[0]).all()) and bool(torch.isfinite(out[1]).all())
+
+
 def test_pool_offsets_past_32_bits(mb):
     """The last pages of a pool of 2^33 bytes: appended, attended, forked and freed."""
     dh, hk, page = 128, 8, 64
