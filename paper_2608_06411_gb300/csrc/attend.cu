@@ -560,15 +560,18 @@ __global__ void __launch_bounds__(kThreads, ctas_of(DH)) attend_kernel(const __g
   }
 }
 
-template <typename T, int DH, int STAGES>
-cudaError_t launch_run(const AttendArgs& a, size_t smem, int grid, cudaStream_t st) {
-  const cudaError_t e = cudaFuncSetAttribute(attend_kernel<T, DH, STAGES>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
-  return e != cudaSuccess ? e : launch_k(attend_kernel<T, DH, STAGES>, dim3(grid), dim3(kThreads), smem, st, a);
-}
-
 template <int DH>
 constexpr size_t smem_of(int stages, int rows) {
   return static_cast<size_t>(kWarps) * stages * Tile<DH>::kStage + stages * rows * Tile<DH>::kRow;
+}
+
+// The kernel's limit of shared memory belongs to all threads of the process: every call sets the same one, the largest, so that
+// none lowers it between another's setting and its launch.
+template <typename T, int DH, int STAGES>
+cudaError_t launch_run(const AttendArgs& a, size_t smem, int grid, cudaStream_t st) {
+  constexpr int most = static_cast<int>(smem_of<DH>(STAGES, kRows));
+  const cudaError_t e = cudaFuncSetAttribute(attend_kernel<T, DH, STAGES>, cudaFuncAttributeMaxDynamicSharedMemorySize, most);
+  return e != cudaSuccess ? e : launch_k(attend_kernel<T, DH, STAGES>, dim3(grid), dim3(kThreads), smem, st, a);
 }
 
 // Tiles in a ring and CTAs an SM: two tiles ahead and two CTAs where they fit (dh = 128, without the join: one sequence of

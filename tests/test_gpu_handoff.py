@@ -5,6 +5,8 @@ Tolerances.  u = eps / 2 of the output's type is its one rounding.  Rotation: z 
 products; cos and sin carry their argument's rounding, pi 2^-24, and 2 ulp; the turn adds 3 roundings: under 32 * 2^-24
 of |z_a| + |z_b|.  fp16 results below 2^-14 are rounded to multiples of 2^-24.
 """
+import threading
+
 import numpy as np
 import pytest
 import torch
@@ -947,3 +949,41 @@ def test_an_image_answered_twice_from_one_cache(mb):
     cache.free(ints([0, 1, 3]))
     assert int(cache.refs.sum()) == 0
     ctx.close()
+
+
+# ----------------------------------------------------------------------------- calls from several host threads
+
+def together(calls, times=30000):
+    """Codes other than 0 that the calls returned, each made over and over by a host thread of its own."""
+    codes = []
+
+    def work(call):
+        for _ in range(times):
+            rc = call()
+            if rc:
+                codes.append(rc)
+
+    threads = [threading.Thread(target=work, args=(c,)) for c in calls]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    torch.cuda.synchronize()
+    return codes
+
+
+@pytest.mark.parametrize("dh,groups", [(64, (16, 1)), (128, (8, 1)), (256, (16, 1))])
+def test_attend_of_two_caches_from_two_threads(mb, dh, groups):
+    """Groups of more and of fewer query heads, and so launches of one kernel with more and with less shared memory."""
+    seqs, calls, held = ints([0, 1]), [], []
+    for g in groups * 2:
+        c, st = filled(mb, torch.float16, dh, 1, 16, [40, 20], 3), torch.cuda.Stream()
+        q = randn(gen(4), 2, g, dh, typ=torch.float16)
+        out = torch.empty_like(q)
+        held.append((c, q, out, c.attend(q, seqs, 0)))
+        args = (c.desc, 0, mb._heads(q, 2, dh, q.dtype, q.device), seqs.data_ptr(), 2, dh ** -0.5,
+                mb._heads(out, 2, dh, q.dtype, q.device), c._ws.data_ptr(), st.cuda_stream)
+        calls.append(lambda args=args, st=st: mb.lib.map_cache_attend(*args))
+    torch.cuda.synchronize()
+    assert together(calls) == []
+    assert all(torch.equal(out, want) for _, _, out, want in held)
