@@ -13,13 +13,15 @@
 
 namespace mapk {
 
+static constexpr int kMaxSeqs = 262144;
+
 int check_cache(const map_cache* c) {
   if (!c || !c->pool || !c->table || !c->len || !c->refs || !c->status) return MAP_EINVAL;
   if (c->type != MAP_BF16 && c->type != MAP_F16) return MAP_EINVAL;
   if (c->layers < 1 || c->pages < 1 || c->heads < 1 || c->page < 1 || c->dh < 1 || c->seqs < 1 || c->max_pages < 1)
     return MAP_EINVAL;
   if (!aligned16(c->pool)) return MAP_EINVAL;
-  if (c->dh % 8 || c->dh > kMaxHead || c->page > 1024 || c->seqs > 262144) return MAP_EUNSUPPORTED;
+  if (c->dh % 8 || c->dh > kMaxHead || c->page > 1024 || c->seqs > kMaxSeqs) return MAP_EUNSUPPORTED;
   if (c->pages > (1 << 20)) return MAP_EUNSUPPORTED;            // block_scan adds 1024 needs of at most so many pages
   if (static_cast<long long>(c->max_pages) * c->page >= (1ll << 31)) return MAP_EUNSUPPORTED;
   if (c->heads > 65535 || 2ll * c->layers * c->heads > (1 << 24)) return MAP_EUNSUPPORTED;      // units of a page: 32 bits
@@ -425,9 +427,15 @@ __global__ void __launch_bounds__(256) free_kernel(const map_cache c, const int3
   }
 }
 
+// Shared memory of a bookkeeping call (extend_kernel's; fork_plan_kernel takes a word less): five words an entry, a bit a
+// sequence.
+constexpr size_t plan_smem(size_t n, size_t seqs) { return (5 * n + 2 + (seqs + 31) / 32) * 4; }
+
+// The limit belongs to all threads of the process: every call that needs one sets the same, the largest, so that none lowers it
+// between another's setting and its launch.
 cudaError_t allow_smem(const void* kern, size_t bytes) {
   if (bytes <= 48 * 1024) return cudaSuccess;
-  return cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(bytes));
+  return cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(plan_smem(kMaxEntries, kMaxSeqs)));
 }
 
 int launch_err(cudaError_t e) {
@@ -450,7 +458,7 @@ int map_cache_extend(const map_cache* c, const int32_t* seqs, const int32_t* cou
   if (n < 0 || rows < 0 || (n > 0 && !seqs) || (rows > 0 && !slots)) return MAP_EINVAL;
   if (n > kMaxEntries || rows > (1 << 20)) return MAP_EUNSUPPORTED;
   if (n == 0 && rows == 0) return MAP_OK;
-  const size_t smem = (2 * (n + 1) + 3 * static_cast<size_t>(n) + (c->seqs + 31) / 32) * 4;
+  const size_t smem = plan_smem(n, c->seqs);
   cudaError_t e = allow_smem(reinterpret_cast<const void*>(extend_kernel), smem);
   if (e == cudaSuccess)
     e = launch_k(extend_kernel, dim3(1), dim3(kPlanThreads), smem, static_cast<cudaStream_t>(stream), *c, seqs, counts,
@@ -467,7 +475,7 @@ int map_cache_fork(const map_cache* c, const int32_t* parents, const int32_t* ch
   if (!parents || !children) return MAP_EINVAL;
   if ((base == nullptr) != (span == nullptr) || (keep && !base) || (k > 0 && !keep)) return MAP_EINVAL;
   if (n > kMaxEntries || k > (1 << 24)) return MAP_EUNSUPPORTED;
-  const size_t smem = (n + 1 + 4 * static_cast<size_t>(n) + (c->seqs + 31) / 32) * 4;
+  const size_t smem = plan_smem(n, c->seqs);
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   cudaError_t e = allow_smem(reinterpret_cast<const void*>(fork_plan_kernel), smem);
   if (e == cudaSuccess)

@@ -987,3 +987,23 @@ def test_attend_of_two_caches_from_two_threads(mb, dh, groups):
     torch.cuda.synchronize()
     assert together(calls) == []
     assert all(torch.equal(out, want) for _, _, out, want in held)
+
+
+@pytest.mark.parametrize("call", ["extend", "fork"])
+def test_page_calls_of_two_caches_from_two_threads(mb, call):
+    """4096 and 2500 entries at the same time, each on caches of their own.  (Children stay empty: their parents are.)"""
+    calls, held = [], []
+    for n in (4096, 2500) * 2:
+        c, st = mb.Cache.empty(1, 16, 1, 4, 8, 2 * n, 1), torch.cuda.Stream()
+        who, kids, slots, none = ints(list(range(n))), ints(list(range(n, 2 * n))), ints([0] * n), ints([0] * n)
+        held.append((c, who, kids, slots, none, st))
+        if call == "extend":
+            args = (c.desc, who.data_ptr(), none.data_ptr(), n, n, slots.data_ptr(), st.cuda_stream)
+            calls.append(lambda args=args: mb.lib.map_cache_extend(*args))
+        else:
+            args = (c.desc, who.data_ptr(), kids.data_ptr(), n, None, 0, None, None, st.cuda_stream)
+            calls.append(lambda args=args: mb.lib.map_cache_fork(*args))
+    torch.cuda.synchronize()
+    assert together(calls, 10000) == []
+    for c, *_ in held:
+        c.check()
