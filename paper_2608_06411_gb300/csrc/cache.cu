@@ -432,9 +432,10 @@ __global__ void __launch_bounds__(256) free_kernel(const map_cache c, const int3
 constexpr size_t plan_smem(size_t n, size_t seqs) { return (5 * n + 2 + (seqs + 31) / 32) * 4; }
 
 // The limit belongs to all threads of the process: every call that needs one sets the same, the largest, so that none lowers it
-// between another's setting and its launch.
+// between another's setting and its launch.  What a kernel has without asking, 48 KB, holds its fixed words too.
 cudaError_t allow_smem(const void* kern, size_t bytes) {
-  if (bytes <= 48 * 1024) return cudaSuccess;
+  constexpr size_t fixed = 256;            // warp_sums and error are 132
+  if (bytes + fixed <= 48 * 1024) return cudaSuccess;
   return cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(plan_smem(kMaxEntries, kMaxSeqs)));
 }
 

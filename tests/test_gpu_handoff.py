@@ -5,6 +5,9 @@ Tolerances.  u = eps / 2 of the output's type is its one rounding.  Rotation: z 
 products; cos and sin carry their argument's rounding, pi 2^-24, and 2 ulp; the turn adds 3 roundings: under 32 * 2^-24
 of |z_a| + |z_b|.  fp16 results below 2^-14 are rounded to multiples of 2^-24.
 """
+import os
+import subprocess
+import sys
 import threading
 
 import numpy as np
@@ -562,6 +565,29 @@ def test_append_reports_bad_slots_and_skips_them(mb):
     assert int((cache.pool != 5).any(-1).sum()) == 4
     plan.append(None, x, x, pos, cache, 0, ints([0, 1, 2, 3, 4]))           # keys and values alone
     assert torch.equal(cache.pool[0, 1, 0, 0], x[:4, 0])
+
+
+def test_page_calls_whose_shared_memory_is_48_kb(mb):
+    """Entries and sequences that take just under 48 KB beside the kernels' fixed words, in a new process, where no larger
+    call came before."""
+    prog = """
+import torch
+from paper_2608_06411_gb300 import binding as mb
+i32 = dict(dtype=torch.int32, device="cuda")
+for seqs in (72192, 73152, 73184):
+    c = mb.Cache.empty(1, 2000, 1, 4, 8, seqs, 1)
+    who = torch.arange(2000, **i32)
+    assert c.extend(who).tolist() == [4 * i for i in range(2000)]
+    c.free(who)
+    c.extend(who[:1000])
+    c.fork(torch.arange(2000, **i32) % 1000, torch.arange(3000, 5000, **i32), torch.zeros(2000, 0, **i32),
+           torch.zeros(2000, **i32), torch.ones(2000, **i32))
+    c.check()
+    assert c.length[:5000].sum().item() == 1000
+"""
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    r = subprocess.run([sys.executable, "-c", prog], cwd=root, capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0, r.stderr[-2000:]
 
 
 # ----------------------------------------------------------------------------- attention
