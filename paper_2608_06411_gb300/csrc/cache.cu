@@ -415,8 +415,11 @@ __global__ void __launch_bounds__(256) free_kernel(const map_cache c, const int3
   }
   int len = lane == 0 ? atomicExch(&c.len[s], 0) : 0;
   len = __shfl_sync(0xffffffffu, len, 0);
-  if (!good_len(c, len)) {
-    if (lane == 0) atomicOr(c.status, ST_BADINDEX);
+  if (!good_len(c, len)) {                 // as it was: the sequence is not empty (another entry that names it finds the same, or 0)
+    if (lane == 0) {
+      atomicExch(&c.len[s], len);
+      atomicOr(c.status, ST_BADINDEX);
+    }
     return;
   }
   const int32_t* row = c.table + static_cast<long long>(s) * c.max_pages;

@@ -532,6 +532,16 @@ def test_bad_tables_and_lengths_are_reported_and_not_followed(mb):
         assert c.status() == mb.MAP_EINTERNAL and torch.equal(c.refs, before)
 
 
+def test_free_leaves_a_bad_length_as_it_is(mb):
+    for length in (-1, 13, 2 ** 31 - 1, -2 ** 31):
+        c = mb.Cache.empty(1, 12, 2, 4, 64, 5, 3)
+        c.extend(ints([0, 1]), ints([10, 5]), rows=15)
+        c.length[0] = length
+        c.free(ints([0, 1, 0, 1]))
+        assert c.status() == mb.MAP_EINTERNAL
+        assert c.length.cpu().tolist() == [length, 0, 0, 0, 0] and int(c.refs.sum()) == 3
+
+
 def test_forks_whose_pages_add_up_past_32_bits(mb):
     """A length that a very wide table row holds: 16 children of 2^27 pages each, of a pool of 64, are refused."""
     c = mb.Cache(torch.ones(1, 2, 64, 1, 1, 8, dtype=torch.float16, device=DEV),
