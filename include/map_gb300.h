@@ -393,8 +393,8 @@ int map_qk_rotate_grad(const map_rope *rope, int type, long long rows, const int
  * (MAP_EUNSUPPORTED beyond these).  New pages are the free ones with the lowest numbers, in the
  * order of the call's entries: results do not depend on timing.
  * A call that names a bad sequence, names one twice where that is not allowed, or needs more
- * pages than are free or than a table row holds, changes no length and no page: map_cache_status
- * then reports it.  Table entries outside the pool and lengths that no row holds are reported
+ * pages than are free or than a table row holds, changes no length and no page (map_cache_free
+ * apart): map_cache_status then reports it.  Table entries outside the pool and lengths that no row holds are reported
  * too and never followed: such rows read as zeros or as page 0, get slot -1, are not freed.
  */
 #define MAP_CACHE_STATUS_WORDS 1024
@@ -447,7 +447,8 @@ int map_cache_fork(const map_cache *cache, const int32_t *parents, const int32_t
 
 /* Frees sequences: each page loses one holder, the length becomes 0.  seqs int32 [n] (device);
  * -1 is padding, a sequence that is empty or appears again is left alone.  n <= 1048576
- * (MAP_EUNSUPPORTED beyond). */
+ * (MAP_EUNSUPPORTED beyond).  Alone of these calls it goes entry by entry: a bad sequence, or one
+ * whose length no row can hold, is reported and left as it is, the others are freed. */
 int map_cache_free(const map_cache *cache, const int32_t *seqs, int n, void *stream);
 
 /*

@@ -542,6 +542,15 @@ def test_free_leaves_a_bad_length_as_it_is(mb):
         assert c.length.cpu().tolist() == [length, 0, 0, 0, 0] and int(c.refs.sum()) == 3
 
 
+def test_free_takes_the_good_entries_of_a_call(mb):
+    """Free is the one page call that goes entry by entry: a bad sequence is reported, the others are freed."""
+    c = mb.Cache.empty(1, 12, 2, 4, 64, 5, 3)
+    c.extend(ints([0, 1, 4]), ints([10, 5, 1]), rows=16)
+    c.free(ints([5, 0, -1, -7, 0, 4, 2]))
+    assert c.status() == mb.MAP_EINTERNAL
+    assert c.length.cpu().tolist() == [0, 5, 0, 0, 0] and c.refs.cpu().tolist() == [0, 0, 0, 1, 1] + [0] * 7
+
+
 def test_forks_whose_pages_add_up_past_32_bits(mb):
     """A length that a very wide table row holds: 16 children of 2^27 pages each, of a pool of 64, are refused."""
     c = mb.Cache(torch.ones(1, 2, 64, 1, 1, 8, dtype=torch.float16, device=DEV),
