@@ -334,8 +334,8 @@ typedef struct {
  *   axis      int32 [rot / 2] HOST: the axis whose position turns the pair, 0 .. n_axes - 1
  *             (time, height and width in runs, by turns, or any other way); NULL: axis 0.
  *   eps       added to the mean square of a head before its root, >= 0.
- * The angle pos * inv_freq is reduced modulo 2 pi exactly (64-bit fixed point), for any int32
- * position.  Returns MAP_EINVAL for arguments outside these ranges.
+ * The angle pos * inv_freq is taken modulo 2 pi in 64-bit fixed point: within 2^-29 radians for
+ * any int32 position and frequencies up to 2^40.  Returns MAP_EINVAL for arguments outside these ranges.
  */
 typedef struct map_rope map_rope;
 int map_rope_init(int dh, int rot, int adjacent, int n_axes, const double *inv_freq, const int32_t *axis,

@@ -6,9 +6,10 @@
 // t = pos[axis] inv_freq:  y_a = z_a cos t - z_b sin t, y_b = z_b cos t + z_a sin t.  Backward, with g the
 // pair turned back (t -> -t) and n = x r:  dx = r (g w - n mean(g w n)),  dw = sum over rows and heads of g n.
 //
-// Angles.  inv_freq / 2 pi is held as a 64-bit binary fraction of a turn; its product with a position is taken
-// modulo 2^64, which drops whole turns exactly, so an angle is as exact at position 2^31 as at 1 (2^-33 turns from
-// the 32 bits kept, plus 2^-53 of the frequency).  cos and sin come from the fraction's upper 32 bits in fp32.
+// Angles.  inv_freq / 2 pi is held as a 64-bit binary fraction of a turn, the nearest one; that times a position is taken
+// modulo 2^64, which drops whole turns exactly.  The fraction is off by 2^-65 turns (frequencies up to 2^40), its multiple by
+// |pos| times as much, at most 2^-34; the 32 bits that are kept of it are cut, 2^-32 at most: together under 2^-29 radians at
+// any position.  cos and sin come from those bits in fp32.
 #include <algorithm>
 #include <cmath>
 #include <cstdint>
@@ -825,6 +826,18 @@ __global__ void __launch_bounds__(32 * kSumWarps) grad_sum_kernel(const __grid_c
   if (lane == 0 && blockIdx.x * 32 + warp < dh && g.dw[side]) g.dw[side][blockIdx.x * 32 + warp] = s;
 }
 
+// f / 2 pi modulo 1 in units of 2^-64, rounded: f times 1 / 2 pi as a double p and the rest of it (1 / 2 pi in two doubles,
+// the product's own rest exact by fma), whole turns dropped from both before they are added.  (fmod: a compiler that
+// contracts p - floor(p) to one fma would take p's rest in twice.)
+unsigned long long turn_of(double f) {
+  constexpr double hi = 0.15915494309189535, lo = -9.839338337591243e-18;
+  const double p = f * hi, rest = std::fma(f, hi, -p) + f * lo;
+  const double a = std::ldexp(std::fmod(p, 1.0), 64), whole = std::floor(a);     // below 2^64
+  double b = std::ldexp(rest - std::nearbyint(rest), 64);                        // half a turn at most
+  if (b >= 0x1p63) b -= 0x1p64;
+  return static_cast<unsigned long long>(whole) + static_cast<unsigned long long>(std::llrint(a - whole + b));
+}
+
 int elem_size(int type) { return type == MAP_F32 ? 4 : 2; }
 bool good_type(int type) { return type == MAP_BF16 || type == MAP_F16 || type == MAP_F32; }
 bool absent(const map_heads* h) { return !h || h->heads == 0; }
@@ -1014,8 +1027,7 @@ int map_rope_init(int dh, int rot, int adjacent, int n_axes, const double* inv_f
   t.eps = static_cast<float>(eps);
   t.inv_dh = 1.f / static_cast<float>(dh);
   for (int i = 0; i < rot / 2; ++i) {
-    const double turns = std::fabs(inv_freq[i]) * 0.15915494309189533577;     // 1 / 2 pi
-    const unsigned long long turn = static_cast<unsigned long long>(std::ldexp(turns - std::floor(turns), 64));
+    const unsigned long long turn = turn_of(std::fabs(inv_freq[i]));
     t.turn[i] = inv_freq[i] < 0 ? 0 - turn : turn;
     t.axis[i] = static_cast<uint8_t>(axis ? axis[i] : 0);
   }

@@ -9,6 +9,7 @@ import os
 import subprocess
 import sys
 import threading
+from fractions import Fraction
 
 import numpy as np
 import pytest
@@ -202,6 +203,26 @@ def test_rotate_edges(mb):
         plan.rotate(x.transpose(1, 2), None, pos)
     with pytest.raises(ValueError):
         plan.rotate(x.double(), None, pos)
+
+
+def test_rotation_angles_at_far_positions(mb):
+    """Angles from rational arithmetic with 50 digits of 2 pi: cut to 32 bits they are off by 2^-32 turns, and by |pos| 2^-65 of
+    the stored fraction's rounding, together under 2^-29 radians; the rest as above."""
+    two_pi = Fraction("6.28318530717958647692528676655900576839433879875021")
+    inv = [1000.0, 37.5, 1.0, 123456.789, 0.1, 3e9, -777.25, 1e-3, 2.0 ** 40 + 0.125, 6.283185307179586, 0.5, -2.5]
+    at = [2 ** 31 - 1, -2 ** 31, 2 ** 31 - 12345, 1999999999, -1234567891, 7]
+    plan = mb.Rope(32, inv)
+    x = randn(gen(1), len(at), 2, 32, typ=torch.float32)
+    for v in (x, place(x, "odd")[0]):
+        got = f64(plan.rotate(v, None, ints([at]))[0])
+        for r, p in enumerate(at):
+            for i, f in enumerate(inv):
+                t = p * Fraction(f) / two_pi
+                t = float((t - int(t)) * two_pi)
+                a, b = f64(x[r, :, i]), f64(x[r, :, len(inv) + i])
+                size = (32 * E24 + 2.0 ** -29) * (np.abs(a) + np.abs(b))
+                assert (np.abs(got[r, :, i] - (a * np.cos(t) - b * np.sin(t))) <= size).all(), (p, f)
+                assert (np.abs(got[r, :, len(inv) + i] - (b * np.cos(t) + a * np.sin(t))) <= size).all(), (p, f)
 
 
 def check_grad(dx, dw, dy, x, w, pos, inv, ax, adjacent, typ):
