@@ -367,7 +367,7 @@ int map_qk_rotate(const map_rope *rope, int type, long long rows, const int32_t 
  * sums over all rows and heads in fp32, in a fixed order.  ws: device scratch of
  * map_qk_rotate_grad_workspace(rope) bytes, 16-byte aligned, the caller's until the call's work
  * completes (may be NULL without norms).  Other arguments as for map_qk_rotate.  rows = 0 zeroes
- * dwq and dwk.
+ * dwq and dwk, a dq_out or dk_out of 0 heads that of its side (NULL leaves it alone).
  */
 size_t map_qk_rotate_grad_workspace(const map_rope *rope);
 int map_qk_rotate_grad(const map_rope *rope, int type, long long rows, const int32_t *pos,

@@ -1084,7 +1084,13 @@ int map_qk_rotate_grad(const map_rope* rope, int type, long long rows, const int
   int sides = 0;
   bool norm = false;
   for (int i = 0; i < 2; ++i) {
-    if (absent(g[i])) continue;
+    if (absent(g[i])) {
+      if (g[i] && w[i] && dw[i]) {             // no heads: a sum of nothing, in the place behind the one side that has some
+        sums.dw[1] = dw[i];
+        norm = true;
+      }
+      continue;
+    }
     if (!good_in(g[i], type, rows) || !good_out(out[i], type, rows, t.dh, g[i]->heads)) return MAP_EINVAL;
     if (w[i] && (absent(x[i]) || !good_in(x[i], type, rows) || x[i]->heads != g[i]->heads || !dw[i] || !ws ||
                  !aligned16(ws)))

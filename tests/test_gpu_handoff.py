@@ -347,6 +347,18 @@ def test_rotate_grad_after_sums_of_nan(mb, typ, dh, adjacent):
     check_grad(dx, dw, dy, x, w, pos, inv, [0] * len(inv), adjacent, typ)
 
 
+def test_rotate_grad_of_a_side_without_heads(mb):
+    plan, pos = mb.Rope(64, [1.0] * 32), ints([[1, 2, 3, 4, 5]])
+    none, x, dy = torch.zeros(5, 0, 64, device=DEV), *(randn(gen(s), 5, 2, 64, typ=torch.float32) for s in (1, 2))
+    w = torch.ones(64, device=DEV)
+    alone = plan.grad(None, dy, pos, None, x, None, w)
+    for sides in (0, 1):
+        d = torch.full((64,), 3.0, device=DEV)
+        got = plan.grad(none, dy, pos, none, x, w, w, dwq=d) if sides == 0 else plan.grad(dy, none, pos, x, none, w, w, dwk=d)
+        assert bool((d == 0).all())
+        assert torch.equal(got[2 + (1 - sides)], alone[3])
+
+
 # ----------------------------------------------------------------------------- positions
 
 @pytest.mark.parametrize("grids,lens,k,step,off,N", [
