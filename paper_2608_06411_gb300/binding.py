@@ -263,7 +263,7 @@ class Context:
         if dev.type != "cuda" or D != self.cfg.D or vis.element_size() != 2:
             raise ValueError(f"vis must be [B, N, {self.cfg.D}] of a 2-byte type on a CUDA device")
         if stream is not None:               # outputs are allocated on the stream that writes them
-            with _on(dev, stream):
+            with _on(dev, stream, vis, keep, text, seq, pos):
                 return self.assemble_axes(vis, keep, text, lens, grids, t_step, pos_offset, seq, pos)
         m = _host_ints(lens, B, 1, "lens")
         g = _host_ints(grids, B, 3, "grids")
@@ -416,6 +416,7 @@ def qcts(attn, lens, attn_ref, L: int, H: int, N: int, p=None, p_ref=None, js=No
 # ------------------------------------------------------------------ queries, keys and a cache's pages
 # These calls run on the device of the tensors they are given, whichever is current, and on that device's current
 # stream unless `stream` is given; scratch and outputs that are not given are allocated on the stream that uses them.
+# With `stream` given, inputs have to be ready there (an event, or wait_stream), and may be dropped once the call has returned.
 
 TYPES = {torch.bfloat16: 0, torch.float16: 1, torch.float32: 2}      # MAP_BF16, MAP_F16, MAP_F32
 CACHE_STATUS_WORDS = 1024                                            # MAP_CACHE_STATUS_WORDS
@@ -428,13 +429,19 @@ _current_stream = torch._C._cuda_getCurrentRawStream    # Python objects: 1.5 us
 
 
 class _on:
-    """A device made current, and with a stream of the caller's that one for torch's allocations too."""
+    """A device made current, and with a stream of the caller's that one for torch's allocations too.  `tensors` (any of them
+    may be None) are what the call reads and writes there: the allocator hears of it, so that the memory of one that the
+    caller drops before the stream is done is not handed out before that."""
 
-    def __init__(self, device, stream):
+    def __init__(self, device, stream, *tensors):
         if device.type != "cuda":
             raise ValueError("tensors passed to libmap_gb300 must be on a CUDA device")
-        if stream is not None and stream.device != device:
-            raise ValueError("the stream is not on the tensors' device")
+        if stream is not None:
+            if stream.device != device:
+                raise ValueError("the stream is not on the tensors' device")
+            for t in tensors:
+                if t is not None and t.device == device:        # (others are refused by the call)
+                    t.record_stream(stream)
         self.guard = torch.cuda.stream(stream) if stream is not None else torch.cuda.device(device)
 
     def __enter__(self):
@@ -514,7 +521,7 @@ class Rope:
             raise ValueError("q or k is needed")
         dev = x.device
         if stream is not None or dev.index != _current_device():
-            with _on(dev, stream):
+            with _on(dev, stream, q, k, pos, wq, wk, q_out, k_out):
                 return self.rotate(q, k, pos, wq, wk, q_out, k_out)
         dt, dh, rows = x.dtype, self.dh, x.shape[0]
         a = b = oa = ob = None
@@ -544,7 +551,7 @@ class Rope:
             raise ValueError("dq_out or dk_out is needed")
         dev = x.device
         if stream is not None or dev.index != _current_device():
-            with _on(dev, stream):
+            with _on(dev, stream, dq_out, dk_out, pos, q, k, wq, wk, dq, dk, dwq, dwk):
                 return self.grad(dq_out, dk_out, pos, q, k, wq, wk, dq, dk, dwq, dwk)
         dt, dh, rows, f32 = x.dtype, self.dh, x.shape[0], torch.float32
         a = b = xa = xb = oa = ob = ws = None
@@ -585,7 +592,7 @@ class Rope:
         without q)."""
         dev = k.device
         if stream is not None or dev.index != _current_device():
-            with _on(dev, stream):
+            with _on(dev, stream, q, k, v, pos, slots, wq, wk, q_out):
                 return self.append(q, k, v, pos, cache, layer, slots, wq, wk, q_out)
         dt, dh, rows = k.dtype, self.dh, k.shape[0]
         if dt != cache.pool.dtype or dev != cache.pool.device:
@@ -653,7 +660,7 @@ class Cache:
         be given with counts."""
         dev = self.device
         if stream is not None or dev.index != _current_device():
-            with _on(dev, stream):
+            with _on(dev, stream, seqs, counts, slots):
                 return self.extend(seqs, counts, rows, slots)
         n = seqs.shape[0]
         if rows is None:
@@ -676,7 +683,7 @@ class Cache:
         base[i] .. base[i] + span[i] that keep[i] names (all int32 on the device)."""
         dev = self.device
         if stream is not None or dev.index != _current_device():
-            with _on(dev, stream):
+            with _on(dev, stream, parents, children, keep, base, span):
                 return self.fork(parents, children, keep, base, span)
         n, i32 = parents.shape[0], torch.int32
         if (keep is None) != (base is None) or (base is None) != (span is None) or (keep is not None and keep.dim() != 2):
@@ -691,7 +698,7 @@ class Cache:
         """map_cache_free: the pages of seqs (int32 [n] on the device) lose a holder, the lengths become 0."""
         dev = self.device
         if stream is not None or dev.index != _current_device():
-            with _on(dev, stream):
+            with _on(dev, stream, seqs):
                 return self.free(seqs)
         n = seqs.shape[0]
         _check(lib.map_cache_free(self.desc, _dense(seqs, torch.int32, dev, (n,), "seqs"), n, self._stream()),
@@ -702,7 +709,7 @@ class Cache:
         scale defaults to dh ** -0.5."""
         dev = self.device
         if stream is not None or dev.index != _current_device():
-            with _on(dev, stream):
+            with _on(dev, stream, q, seqs, out):
                 return self.attend(q, seqs, layer, scale, out)
         dt, n, dh = self.pool.dtype, seqs.shape[0], self.dh
         a = _heads(q, n, dh, dt, dev)

@@ -880,6 +880,55 @@ def test_a_cache_dropped_while_another_stream_attends(mb):
     assert torch.equal(got, want) and len(keep) == 5
 
 
+def test_inputs_dropped_while_the_given_stream_reads_them(mb):
+    """`stream=` calls on temporaries: their memory is not handed out before that stream is done with it."""
+    s, g = torch.cuda.Stream(), gen(7)
+    plan, ctx = mb.Rope(64, [0.5 ** i for i in range(32)]), handoff_context(mb, 512)
+    q, k, dy = (randn(g, 3000, h, 64, typ=torch.bfloat16) for h in (4, 2, 4))
+    pos = torch.randint(0, 900, (1, 3000), generator=g, device=DEV, dtype=torch.int32)
+    w = torch.ones(64, device=DEV, dtype=torch.bfloat16)
+    vis = torch.randint(0, 999, (1, 2000, 512), generator=g, device=DEV, dtype=torch.int16)
+    text, keep = vis[0, :100].clone(), torch.arange(0, 2000, 2, dtype=torch.int32, device=DEV)[None]
+
+    def fresh():
+        c = filled(mb, torch.bfloat16, 64, 2, 16, [40, 0, 0], 3, spare=400)
+        wide = torch.zeros(3, 200, dtype=torch.int32, device=DEV)
+        wide[:, : c.table.shape[1]] = c.table
+        return mb.Cache(c.pool, wide, c.length, c.refs)
+
+    def calls(c, x, stream):
+        """Every call, on tensors of the dict x."""
+        out = list(plan.rotate(x["q"], x["k"], x["pos"], x["w"], x["w"], stream=stream))
+        out += plan.grad(x["dy"], None, x["pos"], x["q"], None, x["w"], stream=stream)[::2]
+        out += ctx.assemble_axes(x["vis"], x["keep"], x["text"], [100], [(1, 40, 50)], stream=stream)
+        slots = c.extend(x["seqs"], x["counts"], rows=3000, stream=stream)
+        out.append(plan.append(x["q"], x["k"], x["k"], x["pos"], c, 0, slots, x["w"], x["w"], stream=stream))
+        c.fork(x["one"], x["two"], x["kept"], x["base"], x["span"], stream=stream)
+        out.append(c.attend(x["q"][:2], x["both"], 0, stream=stream))
+        c.free(x["one"], stream=stream)
+        return out
+
+    values = dict(q=q, k=k, dy=dy, pos=pos, w=w, vis=vis, text=text, keep=keep, seqs=ints([1]), counts=ints([3000]), one=ints([1]),
+                  two=ints([2]), kept=ints([[7, 9, 2000]]), base=ints([3]), span=ints([2990]), both=ints([0, 2]))
+    a, b = fresh(), fresh()
+    want = calls(a, values, None)
+    torch.cuda.synchronize()
+    temps = {n: t.clone() for n, t in values.items()}
+    at, sizes = {t.data_ptr() for t in temps.values()}, [(t.shape, t.dtype) for t in temps.values()]
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        torch.cuda._sleep(100_000_000)                               # some 50 ms
+    got = calls(b, temps, s)
+    del temps
+    others = [torch.full(shape, 1, dtype=typ, device=DEV) for shape, typ in sizes]
+    assert not at & {t.data_ptr() for t in others}
+    s.synchronize()
+    assert all(torch.equal(x, y) for x, y in zip(got, want, strict=True))
+    for c in (a, b):
+        c.check()
+    assert all(torch.equal(x, y) for x, y in ((a.table, b.table), (a.length, b.length), (a.refs, b.refs)))
+
+
 def test_assemble_axes_on_a_stream_and_its_refusals(mb):
     ctx = handoff_context(mb, 512)
     vis, text = torch.ones((1, 8, 512), dtype=torch.int16, device=DEV), torch.full((2, 512), 2, dtype=torch.int16, device=DEV)
