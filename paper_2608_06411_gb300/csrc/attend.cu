@@ -57,7 +57,7 @@ __device__ __forceinline__ int seq_len(const AttendArgs& a, int i) {
   return good_len(a.c, len) ? len : 0;
 }
 
-__device__ __forceinline__ int seq_tiles(const AttendArgs& a, int i) { return (seq_len(a, i) + kTile - 1) / kTile; }
+__device__ __forceinline__ int seq_tiles(const AttendArgs& a, int i) { return pieces_of(seq_len(a, i), kTile); }
 
 // Sum over the block's threads before this one, and over all (red: kWarps words).
 __device__ __forceinline__ long long block_prefix(long long v, long long* red, long long* total) {
@@ -149,7 +149,7 @@ struct Place {
       if (len > 0) break;
     }
     if (i < a.n) s = __ldg(a.seqs + i);
-    tiles = (len + kTile - 1) / kTile;
+    tiles = pieces_of(len, kTile);
   }
   __device__ __forceinline__ void next(const AttendArgs& a, int items) {
     if (++t < tiles) return;

@@ -163,7 +163,7 @@ __global__ void __launch_bounds__(kPlanThreads) extend_kernel(const map_cache c,
           } else {
             seq[i] = s;
             old[i] = len;
-            col[i] = (len + c.page - 1) / c.page;
+            col[i] = pieces_of(len, c.page);
             need = static_cast<int>(pages) - col[i];
           }
         }
@@ -330,7 +330,7 @@ __global__ void __launch_bounds__(kCopyThreads, 8) fork_copy_kernel(const map_ca
   for (int i = e0; i < e1; ++i) {
     const ForkShape f = shape(i);
     start[i] = mine;
-    mine += max(0, (f.len + c.page - 1) / c.page - f.shared);
+    mine += max(0, pieces_of(f.len, c.page) - f.shared);
   }
   int incl = mine;
 #pragma unroll
@@ -423,7 +423,7 @@ __global__ void __launch_bounds__(256) free_kernel(const map_cache c, const int3
     return;
   }
   const int32_t* row = c.table + static_cast<long long>(s) * c.max_pages;
-  for (int j = lane; j < (len + c.page - 1) / c.page; j += 32) {
+  for (int j = lane; j < pieces_of(len, c.page); j += 32) {
     const int page = row[j];
     if (good_page(c, page)) atomicSub(&c.refs[page], 1);
     else atomicOr(c.status, ST_BADINDEX);

@@ -44,6 +44,8 @@ __device__ __forceinline__ bool good_page(const map_cache& c, int page) {
   return static_cast<unsigned>(page) < static_cast<unsigned>(c.pages);
 }
 __device__ __forceinline__ bool good_len(const map_cache& c, int len) { return len >= 0 && len <= c.max_pages * c.page; }
+// Pieces of `size` rows that hold `len` (a good length; it and a piece can add up past 2^31).
+__device__ __forceinline__ int pieces_of(int len, int size) { return static_cast<int>((static_cast<unsigned>(len) + size - 1) / size); }
 
 // MAP_OK, MAP_EINVAL or MAP_EUNSUPPORTED for a cache's description (host values only).
 int check_cache(const map_cache* c);

@@ -595,6 +595,35 @@ def test_forks_whose_pages_add_up_past_32_bits(mb):
         assert int(c.length[1:].abs().sum()) == 0 and int(c.refs.abs().sum()) == 0 and int(c.table[1].abs().sum()) == 0
 
 
+def test_lengths_just_below_32_bits(mb):
+    """Lengths that a row of the table holds, where a page or a tile more passes 2^31: rows added, forked, freed, attended.
+    (Every page of the long rows is page 0; its count says so.)"""
+    long, cols = 2147482900, 2147483                                 # 2147483 pages of 1000
+    pool = randn(gen(3), 1, 2, 4, 1, 1000, 8, typ=torch.float16)
+    before = pool.clone()
+    c = mb.Cache(pool, torch.zeros(3, cols, dtype=torch.int32, device=DEV), ints([long, 0, 0]), ints([cols, 0, 0, 0]))
+    assert c.extend(ints([0])).cpu().tolist() == [900]
+    assert c.length.cpu().tolist() == [long + 1, 0, 0] and c.refs.cpu().tolist() == [cols, 0, 0, 0]
+    c.fork(ints([0]), ints([2]))
+    c.check()
+    assert c.length.cpu().tolist() == [long + 1, 0, long + 1] and c.refs.cpu().tolist() == [2 * cols - 1, 1, 0, 0]
+    assert int(c.table[2, :-1].abs().max()) == 0 and int(c.table[2, -1]) == 1
+    before[:, :, 1, :, :901] = before[:, :, 0, :, :901]
+    assert torch.equal(pool, before)
+    c.free(ints([2, 0]))
+    c.check()
+    assert c.length.cpu().tolist() == [0, 0, 0] and c.refs.cpu().tolist() == [0, 0, 0, 0]
+    cols = 2 ** 27 - 1
+    pool = torch.zeros(1, 2, 2, 1, 16, 64, dtype=torch.float16, device=DEV)
+    pool[:, 1, 0], pool[:, 1, 1] = 1.0, 2.0
+    c = mb.Cache(pool, torch.zeros(2, cols, dtype=torch.int32, device=DEV), ints([2 ** 31 - 20, 5]), ints([cols, 1]))
+    c.table[1, 0] = 1
+    q = randn(gen(4), 2, 1, 64, typ=torch.float16)
+    out = c.attend(q, ints([0, 1]), 0)
+    c.check()
+    assert bool((out[0] == 1).all()) and bool((out[1] == 2).all())
+
+
 def test_a_fork_takes_its_window_whole_or_not_at_all(mb):
     c = mb.Cache.empty(1, 4, 1, 4, 8, 2, 2)
     one, keep = ints([0]), ints([[0]])
