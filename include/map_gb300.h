@@ -394,8 +394,9 @@ int map_qk_rotate_grad(const map_rope *rope, int type, long long rows, const int
  * order of the call's entries: results do not depend on timing.
  * A call that names a bad sequence, names one twice where that is not allowed, or needs more
  * pages than are free or than a table row holds, changes no length and no page (map_cache_free
- * apart): map_cache_status then reports it.  Table entries outside the pool and lengths that no row holds are reported
- * too and never followed: such rows read as zeros or as page 0, get slot -1, are not freed.
+ * apart): map_cache_status then reports it.  Table entries outside the pool and lengths that no
+ * row holds are reported too and never followed: such rows read as zeros or as page 0, get slot
+ * -1, are not freed.
  */
 #define MAP_CACHE_STATUS_WORDS 1024
 typedef struct {

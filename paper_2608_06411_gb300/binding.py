@@ -417,6 +417,7 @@ def qcts(attn, lens, attn_ref, L: int, H: int, N: int, p=None, p_ref=None, js=No
 # These calls run on the device of the tensors they are given, whichever is current, and on that device's current
 # stream unless `stream` is given; scratch and outputs that are not given are allocated on the stream that uses them.
 # With `stream` given, inputs have to be ready there (an event, or wait_stream), and may be dropped once the call has returned.
+# Autograd does not see these calls: their outputs require no gradient, whatever the inputs do (Rope.grad is rotate's).
 
 TYPES = {torch.bfloat16: 0, torch.float16: 1, torch.float32: 2}      # MAP_BF16, MAP_F16, MAP_F32
 CACHE_STATUS_WORDS = 1024                                            # MAP_CACHE_STATUS_WORDS
@@ -515,7 +516,8 @@ class Rope:
 
     def rotate(self, q, k, pos, wq=None, wk=None, q_out=None, k_out=None, stream=None):
         """map_qk_rotate: (q_out, k_out) of q [rows, heads, dh] and k (either may be None), pos int32 [n_axes, rows],
-        norm weights wq, wk [dh] or None (no norm of that side).  Outputs not given are new, contiguous tensors."""
+        norm weights wq, wk [dh] or None (no norm of that side).  Outputs not given are new, contiguous tensors.  Not recorded
+        by autograd: a torch.autograd.Function around rotate and grad carries gradients."""
         x = q if q is not None else k
         if x is None:
             raise ValueError("q or k is needed")
@@ -705,8 +707,8 @@ class Cache:
                "map_cache_free")
 
     def attend(self, q, seqs, layer: int, scale: float | None = None, out=None, stream=None):
-        """map_cache_attend: attention of q [n, heads, dh], row i over sequence seqs[i] (int32 on the device);
-        scale defaults to dh ** -0.5."""
+        """map_cache_attend: attention of q [n, heads, dh], row i over all rows of sequence seqs[i] (int32 on the device);
+        scale defaults to dh ** -0.5.  Forward only, and without a causal mask: single tokens."""
         dev = self.device
         if stream is not None or dev.index != _current_device():
             with _on(dev, stream, q, seqs, out):

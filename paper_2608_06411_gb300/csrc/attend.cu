@@ -14,7 +14,7 @@
 // (counted in the cache's status words) joins them in list order, so results do not depend on timing.  (A second
 // kernel for that took 7 to 8 us; this way the join takes 3 to 4.)
 // Measured, dh = 128 in bf16: 64 sequences of 200 to 1600 rows, 32 heads over 8: 50.2 us, 5.0 TB/s, where the loads alone,
-// in this order and without any use, take 45.7; one sequence of 120001 rows, 28 heads over 4: 50.8 us, loads alone 42.5.
+// in this order and without any use, take 45.7; one sequence of 120001 rows, 28 heads over 4: 51.0 us, loads alone 42.5.
 // Short sequences are bound by an item's own latency, about 2 us on a CTA: 1024 of 64 rows 76 us, 4000 of one row 217.
 #include <algorithm>
 #include <cmath>
@@ -576,6 +576,8 @@ cudaError_t launch_run(const AttendArgs& a, size_t smem, int grid, cudaStream_t 
 
 // Tiles in a ring and CTAs an SM: two tiles ahead and two CTAs where they fit (dh = 128, without the join: one sequence of
 // 120001 rows 45 us, with one ahead and three CTAs 53; 64 of 200 to 1600 rows 53 and 58), three CTAs up to 80 columns.
+// At 192 columns two rings of two tiles fit with up to 15 query heads a key head; with 16 they are 512 bytes too large, and an
+// SM holds one CTA of three tiles.
 template <typename T, int DH>
 cudaError_t launch_width(const AttendArgs& a, int sms, cudaStream_t st) {
   constexpr size_t kSm = 228 * 1024, kOwn = 1024 + 768;      // an SM's shared memory; what a CTA takes beside its dynamic part

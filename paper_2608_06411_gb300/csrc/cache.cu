@@ -302,11 +302,12 @@ __global__ void __launch_bounds__(kPlanThreads) fork_plan_kernel(const map_cache
   }
 }
 
-// The rows of the children's own pages, HBM-bound (each row read once and written once, in every plane: K or V of a
-// layer).  A unit is one head of one new page in one plane, a slab of page * dh elements; a block takes an equal run of
-// the units, page by page, so that it looks a page's source rows up once.  Full occupancy with one vector a thread in
-// flight reads and writes at 6.4 TB/s (53 us for 8 questions on an image in 32 layers, 342 MB; two in flight 56, four with
-// six CTAs an SM 60).
+// The rows of the children's own pages, each read once and written once in every plane (K or V of a layer).  A unit is one
+// head of one new page in one plane, a slab of page * dh elements; a block takes an equal run of the units, page by page, so
+// that it looks a page's source rows up once.  Full occupancy with one vector a thread in flight: 53 us for 8 questions on an
+// image in 32 layers, 171 MB copied (two in flight 56, four with six CTAs an SM 60).  Of those 342 MB DRAM sees 261 in that
+// time, 4.7 TB/s, 0.7 of what a copy reaches: each row is 256 bytes at a place of its own, and rows that several children keep
+// (32 of the 171 MB) are read by each, page by page of one child, mostly from L2.
 // What comes before griddepcontrol.wait (shapes, the parents' tables) fork_plan_kernel only reads, and so runs beside it.
 constexpr int kCopyThreads = 256, kCopyGrid = 152 * 8;
 __global__ void __launch_bounds__(kCopyThreads, 8) fork_copy_kernel(const map_cache c, const int32_t* __restrict__ parents,

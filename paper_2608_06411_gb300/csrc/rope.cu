@@ -430,7 +430,7 @@ __global__ void __launch_bounds__(kThreads, kRotateCtas) rotate_kernel(const __g
 
 // The same passes; the lanes' sums of g n stay in registers until the end (two CTAs an SM, 128 registers).  HBM's work is q, k
 // and the gradients of both once in, their gradients once out; bound by instructions and by the warps that hide their
-// latency: 16171 rows of 28 and 4 heads of 128 in bf16 take 79 us with the sums of dw, 5.0 TB/s, issue slots 65 % busy.
+// latency: 16171 rows of 28 and 4 heads of 128 in bf16 take 80 us with the sums of dw, 5.0 TB/s, issue slots 65 % busy.
 // (8-byte vectors and three CTAs 128 us; x, w and turns read again from shared memory, three CTAs, 134.)
 template <typename T, int V, bool ADJ>
 __global__ void __launch_bounds__(kThreads, kGradCtas) grad_kernel(const __grid_constant__ RopeTab tab,
