@@ -18,12 +18,13 @@ using mapk::GemmDesc;
 
 namespace {
 
-constexpr int kMaxKDiverse = 768;   // k limit when the diversity term is on (the coordinate update
-                                    // stages slot rows and 32 basis rows of k floats in shared memory)
+// k limit when the diversity term is on (the coordinate update stages slot rows and 32 basis rows of k floats in
+// shared memory)
+constexpr int kMaxKDiverse = mapk::kSelMaxKDiverse;
 constexpr int kProjMaxBasis = 128;  // basis vectors one projection pass takes
-constexpr int kMaxK = 4096;
+constexpr int kMaxK = mapk::kSelMaxK;
 constexpr int kCombineInTile = 28;  // most softmax statistics a thread combines in Eq. 3's second pass itself
-constexpr int kMaxN = 16384;
+constexpr int kMaxN = mapk::kSelMaxN;
 
 struct DevBuf {
   void* p = nullptr;

@@ -48,9 +48,9 @@ namespace {
 constexpr size_t kNoAllocScratchBytes = MAP_NOALLOC_SCRATCH_BYTES;
 constexpr int kSelS = mapk::kActiveSlots;
 constexpr int kMaxDevices = 64;
-constexpr int kMaxN = 16384;
-constexpr int kMaxK = 4096;          // plain top-k
-constexpr int kMaxKDiverse = 768;    // with the diversity term (as map_select)
+constexpr int kMaxN = mapk::kSelMaxN;
+constexpr int kMaxK = mapk::kSelMaxK;                  // plain top-k
+constexpr int kMaxKDiverse = mapk::kSelMaxKDiverse;    // with the diversity term (as map_select)
 
 static __device__ __align__(256) unsigned char g_scratch[kNoAllocScratchBytes];
 

@@ -1225,16 +1225,23 @@ size_t sel_update_smem(int KP) {
   return static_cast<size_t>(kUpdSlots + kChunk) * coord_pitch(KP) * 4;
 }
 
+// The limit of a kernel's shared memory belongs to all threads of the process: every call sets the same one, what the largest
+// selection takes, so that no context's call lowers it between another's setting and its launch.
+template <typename K>
+static cudaError_t allow_smem(K* kern, size_t most) {
+  return cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(most));
+}
+
 cudaError_t launch_sel_init(const SelState& s, cudaStream_t st) {
   const size_t sm = sel_init_smem(s.N, s.K0);
-  cudaError_t e = cudaFuncSetAttribute(sel_init_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(sm));
+  cudaError_t e = allow_smem(sel_init_kernel, sel_init_smem(kSelMaxN, kSelMaxK));
   if (e != cudaSuccess) return e;
   return launch_k(sel_init_kernel, dim3(s.B), dim3(kKthThreads), sm, st, s);
 }
 
 cudaError_t launch_sel_choose(const SelState& s, cudaStream_t st) {
   const size_t sm = sel_choose_smem(s.N);
-  cudaError_t e = cudaFuncSetAttribute(sel_choose_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(sm));
+  cudaError_t e = allow_smem(sel_choose_kernel, sel_choose_smem(kSelMaxN));
   if (e != cudaSuccess) return e;
   return launch_k(sel_choose_kernel, dim3(s.B), dim3(kKthThreads), sm, st, s);
 }
@@ -1244,7 +1251,7 @@ cudaError_t launch_sel_greedy(const SelState& s, bool update, cudaStream_t st) {
   cudaError_t e = cudaSuccess;
   if (update) {
     const size_t um = sel_update_smem(s.KP);
-    e = cudaFuncSetAttribute(sel_update_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(um));
+    e = allow_smem(sel_update_kernel, sel_update_smem(kSelMaxKDiverse));
     if (e != cudaSuccess) return e;
     e = launch_k(sel_update_kernel, dim3((s.S + kUpdSlots - 1) / kUpdSlots, s.B), dim3(32 * kUpdWarps), um, st, s);
     if (e != cudaSuccess) return e;
@@ -1253,7 +1260,7 @@ cudaError_t launch_sel_greedy(const SelState& s, bool update, cudaStream_t st) {
   e = launch_k(sel_resgram_kernel, dim3(T * (T + 1) / 2, s.B), dim3(kRgThreads), 0, st, s);
   if (e != cudaSuccess) return e;
   const size_t sm = sel_greedy_smem(s.S);
-  e = cudaFuncSetAttribute(sel_greedy_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(sm));
+  e = allow_smem(sel_greedy_kernel, sm);
   if (e != cudaSuccess) return e;
   return launch_k(sel_greedy_kernel, dim3(s.B), dim3(s.S), sm, st, s);
 }
@@ -1261,7 +1268,7 @@ cudaError_t launch_sel_greedy(const SelState& s, bool update, cudaStream_t st) {
 cudaError_t launch_sel_chol(const SelState& s, cudaStream_t st) {
   if (s.K0 < 1 || s.K0 > kCholMax || s.K0 > s.S) return cudaErrorInvalidValue;
   const size_t sm = sel_chol_smem(s.K0);
-  cudaError_t e = cudaFuncSetAttribute(sel_chol_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(sm));
+  cudaError_t e = allow_smem(sel_chol_kernel, sel_chol_smem(kCholMax));
   if (e != cudaSuccess) return e;
   return launch_k(sel_chol_kernel, dim3(s.B), dim3(kCholThreads), sm, st, s);
 }

@@ -6,6 +6,8 @@
 
 namespace mapk {
 
+// Limits of a selection: tokens an image, k, k with the diversity term.
+constexpr int kSelMaxN = 16384, kSelMaxK = 4096, kSelMaxKDiverse = 768;
 constexpr int kCholMax = 256;     // largest R0 factored by sel_chol_kernel (a thread per token)
 
 struct SelState {

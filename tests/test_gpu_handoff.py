@@ -1163,3 +1163,22 @@ def test_page_calls_of_two_caches_from_two_threads(mb, call):
     assert together(calls, 10000) == []
     for c, *_ in held:
         c.check()
+
+
+def test_select_of_two_contexts_from_two_threads(mb):
+    """A context a thread, images of 2880 and of 300 tokens: the selection's launches differ in shared memory too."""
+    from paper_2608_06411_gb300 import workloads as W
+    w = {n: torch.from_numpy(v.view(np.int16)).to(DEV) for n, v in W.make_weights(W.PredictorDims(D=512, Dh=256, dp=64), seed=7).items()}
+    calls, held = [], []
+    for N, k in ((2880, 160), (300, 24)) * 2:
+        ctx, st = mb.Context(w, 512, 256, 64), torch.cuda.Stream()
+        vis, scores = randn(gen(N), 1, N, 512, typ=torch.bfloat16), torch.rand(1, N, generator=gen(1), device=DEV)
+        keep = torch.zeros(1, k, dtype=torch.int32, device=DEV)
+        held.append((ctx, vis, scores, keep, st, ctx.select(scores, vis, k)[0]))
+        args = (ctx.h, scores.data_ptr(), vis.data_ptr(), 1, N, k, keep.data_ptr(), None, st.cuda_stream)
+        calls.append(lambda args=args: mb.lib.map_select(*args))
+    torch.cuda.synchronize()
+    assert together(calls, 4000) == []
+    for ctx, _, _, keep, _, want in held:
+        assert ctx.status() == mb.MAP_OK and torch.equal(keep, want)
+        ctx.close()
