@@ -468,6 +468,54 @@ size_t map_cache_attend_workspace(const map_cache *cache);
 int map_cache_attend(const map_cache *cache, int layer, const map_heads *q, const int32_t *seqs, int n, float scale,
                      const map_heads *out, void *ws, void *stream);
 
+/*
+ * map_cache_attend for groups of sequences that begin with the same pages (questions and samples on one cached image): the rows
+ * that all of a group's sequences share are read once for the group.  The same result as map_cache_attend's, but for the order
+ * of its sums; what is shared is found in the page table, so that any groups are right.
+ *   starts    int32 [groups + 1] (device): entries starts[g] .. starts[g + 1] - 1 of seqs form group g; ascending from 0 to n
+ *             (else it is reported, and nothing is shared).  Shared are the whole pages that the sequences of a group (those with
+ *             rows) have in common in front; a group whose sequences have none is attended as by map_cache_attend.
+ *   ws        device scratch of map_cache_attend_shared_workspace(cache, q heads, n, groups) bytes, 16-byte aligned, the
+ *             caller's until the call's work completes.
+ * groups 1 .. 65535 (MAP_EUNSUPPORTED beyond); everything else as for map_cache_attend.
+ */
+size_t map_cache_attend_shared_workspace(const map_cache *cache, int heads, int n, int groups);
+int map_cache_attend_shared(const map_cache *cache, int layer, const map_heads *q, const int32_t *seqs, int n,
+                            const int32_t *starts, int groups, float scale, const map_heads *out, void *ws, void *stream);
+
+/*
+ * map_cache_attend that also keeps count of who is looked at: for each query row i of sequence s = seqs[i], key head h and t < len[s]
+ *   weights[layer, s, h, t] += sum over the G query heads of h of softmax_t(scale <q, K[t, h]>).
+ *   weights   float32 [layers, seqs, heads, max_pages * page] (device).  The caller zeroes a sequence's when it begins, is forked
+ *             or freed; a row that is appended must find its weight as the caller wants it to begin.  What lies at or behind a
+ *             sequence's length is not read or written.
+ *   ws        device scratch of map_cache_attend_weigh_workspace(cache, q heads, n) bytes, 16-byte aligned, the caller's until
+ *             the call's work completes; 4 bytes for each row that a sequence can have and query head.
+ * A sequence that appears in several rows gets the weights of all, added up in their order.  Everything else as for
+ * map_cache_attend.
+ */
+size_t map_cache_attend_weigh_workspace(const map_cache *cache, int heads, int n);
+int map_cache_attend_weigh(const map_cache *cache, int layer, const map_heads *q, const int32_t *seqs, int n, float scale,
+                           const map_heads *out, float *weights, void *ws, void *stream);
+
+/*
+ * Takes the rows of least weight out of sequences, for each layer and key head by itself: of sequence seqs[i]'s rows first[i] ..
+ * len - last[i] - 1 the k of greatest weights[layer, seqs[i], h, .] stay (of equal ones those in front; NaN is the greatest), in
+ * their order; the rows before and after stay.  Rows behind one that leaves move up, their weights with them, and len shrinks by
+ * as many rows as leave, which is the same in all layers and heads.  A sequence with k candidates or fewer is left as it is.
+ *   seqs         int32 [n] (device); -1: padding.  A sequence may appear once.
+ *   first, last  int32 [n] (device), >= 0; NULL: 0.
+ *   weights      as map_cache_attend_weigh's; those behind the new length, up to the old one, become 0.
+ *   ws           device scratch of map_cache_evict_workspace(cache, n) bytes, 16-byte aligned, the caller's until the call's work
+ *                completes.
+ * Pages that other sequences hold as well keep their rows: where rows move (or stay beside ones that do) the sequence gets new
+ * pages instead, taken before any is given up.  Pages behind the new length lose a holder.  n <= 4096, n * max_pages < 2^31
+ * (MAP_EUNSUPPORTED beyond).
+ */
+size_t map_cache_evict_workspace(const map_cache *cache, int n);
+int map_cache_evict(const map_cache *cache, float *weights, const int32_t *seqs, int n, const int32_t *first,
+                    const int32_t *last, int k, void *ws, void *stream);
+
 /* Synchronises `stream` and returns the error recorded by calls on this cache since the last
  * call (MAP_ENOMEM: no free page or a full table row; MAP_EINTERNAL: a bad sequence, slot, count or index),
  * clearing it; else a CUDA error as MAP_ECUDA; else MAP_OK. */

@@ -137,6 +137,48 @@ class Pages:
                 self.refs[p] -= 1
             self.table[s], self.length[s] = [], 0
 
+    def evict(self, seqs, first, last, k, weights):
+        """weights [layers, seqs, heads, rows] float32, changed in place.  [(layer, head, slots, source slots)] of the rows that
+        move, or None if the call is refused."""
+        named = [s for s in seqs if s != -1]
+        if len(set(named)) < len(named) or any(s < 0 or s >= len(self.table) for s in named):
+            return None
+        plan, free, holders = [], self._free(), list(self.refs)
+        for s, f, l in zip(seqs, first, last):
+            if s == -1:
+                continue
+            if f < 0 or l < 0:
+                return None
+            t = self.length[s]
+            window = t - f - l
+            if window <= k:
+                continue
+            left, new = t - window + k, list(self.table[s])
+            for j in range(f // self.page, -(-left // self.page)):
+                if holders[new[j]] > 1:
+                    if not free:
+                        return None
+                    new[j] = free.pop(0)
+            plan.append((s, f, window, t, left, new[: -(-left // self.page)]))
+        moves = []
+        for s, f, window, t, left, new in plan:
+            old = self.table[s]
+            at = [[pages[r // self.page] * self.page + r % self.page for r in range(n)] for pages, n in ((old, t), (new, left))]
+            for layer in range(weights.shape[0]):
+                for head in range(weights.shape[2]):
+                    w = weights[layer, s, head]
+                    order = sorted(range(f, f + window), key=lambda r: (0, 0, r) if np.isnan(w[r]) else (1, -float(w[r]), r))
+                    src = list(range(f)) + sorted(order[:k]) + list(range(f + window, t))
+                    pairs = [(to, at[0][r]) for to, r in zip(at[1], src) if to != at[0][r]]
+                    moves.append((layer, head, [a for a, _ in pairs], [b for _, b in pairs]))
+                    w[:left], w[left:t] = w[src].copy(), 0.0
+            for p in old:
+                self.refs[p] -= 1
+            for p in new:
+                self.refs[p] += 1
+            self.table[s], self.length[s] = new, left
+        return moves
+
 
 def attend(q, k, v, scale):
     """q [heads, dh], k and v [rows, kv heads, dh] float64 -> (out, sum p |v|, largest sum |q k| scale)."""
@@ -151,3 +193,14 @@ def attend(q, k, v, scale):
         out[h], mag[h] = p @ v[:, h // g], p @ np.abs(v[:, h // g])
         dz = max(dz, float((np.abs(k[:, h // g]) @ np.abs(q[h])).max() * abs(scale)))
     return out, mag, dz
+
+
+def attend_weights(q, k, scale):
+    """The weights that `attend` gives the rows, summed over the query heads of a key head: [kv heads, rows]."""
+    g = q.shape[0] // k.shape[1]
+    w = np.zeros((k.shape[1], k.shape[0]))
+    for h in range(q.shape[0]):
+        z = k[:, h // g] @ q[h] * scale
+        p = np.exp(z - z.max())
+        w[h // g] += p / p.sum()
+    return w

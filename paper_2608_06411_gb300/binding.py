@@ -78,6 +78,13 @@ SIGNATURES = {
     "map_cache_free": (c_int, [c_void_p, c_void_p, c_int, c_void_p]),
     "map_cache_attend_workspace": (c_size_t, [c_void_p]),
     "map_cache_attend": (c_int, [c_void_p, c_int, c_void_p, c_void_p, c_int, c_float, c_void_p, c_void_p, c_void_p]),
+    "map_cache_attend_shared_workspace": (c_size_t, [c_void_p, c_int, c_int, c_int]),
+    "map_cache_attend_shared": (c_int, [c_void_p, c_int, c_void_p, c_void_p, c_int, c_void_p, c_int, c_float, c_void_p,
+                                        c_void_p, c_void_p]),
+    "map_cache_attend_weigh_workspace": (c_size_t, [c_void_p, c_int, c_int]),
+    "map_cache_attend_weigh": (c_int, [c_void_p, c_int, c_void_p, c_void_p, c_int, c_float] + [c_void_p] * 4),
+    "map_cache_evict_workspace": (c_size_t, [c_void_p, c_int]),
+    "map_cache_evict": (c_int, [c_void_p, c_void_p, c_void_p, c_int, c_void_p, c_void_p, c_int, c_void_p, c_void_p]),
     "map_cache_status": (c_int, [c_void_p, c_void_p]),
     "map_distill_grad": (c_int, [c_void_p, c_void_p, c_void_p, POINTER(c_int32), c_void_p, c_int, c_int, c_void_p,
                                  POINTER(MapGrads), c_void_p]),
@@ -633,6 +640,7 @@ class Cache:
                 _dense(refs, torch.int32, dev, (pages,), "refs"), _dense(status, torch.int32, dev, (CACHE_STATUS_WORDS,), "status"))
         self.pool, self.table, self.length, self.refs, self.status_word = pool, table, length, refs, status
         self.device, self.heads, self.page, self.dh = dev, heads, page, dh
+        self._weights_shape = (layers, seqs, heads, max_pages * page)
         self.desc = _pack_cache(pool.data_ptr(), *ptrs, TYPES[pool.dtype], layers, pages, heads, page, dh, seqs, max_pages)
         # attend's scratch: calls on one cache are ordered by the caller, so they can share it
         self._ws = torch.empty(int(lib.map_cache_attend_workspace(self.desc)), dtype=torch.uint8, device=dev)
@@ -723,6 +731,64 @@ class Cache:
                                     dh ** -0.5 if scale is None else scale, oa, self._ws.data_ptr(), self._stream()),
                "map_cache_attend")
         return out
+
+    def _scratch(self, size: int):
+        """A call's workspace: torch's allocator keeps it for the current stream (and a graph's capture for the graph)."""
+        return torch.empty(size, dtype=torch.uint8, device=self.device)
+
+    def attend_shared(self, q, seqs, layer: int, starts, scale: float | None = None, out=None, stream=None):
+        """map_cache_attend_shared: attend, for groups of entries starts[g] .. starts[g + 1] - 1 (int32 [groups + 1] on the
+        device, from 0 to n) whose sequences begin with the same pages: those rows are read once for a group."""
+        dev = self.device
+        if stream is not None or dev.index != _current_device():
+            with _on(dev, stream, q, seqs, starts, out):
+                return self.attend_shared(q, seqs, layer, starts, scale, out)
+        dt, n, dh, groups = self.pool.dtype, seqs.shape[0], self.dh, starts.shape[0] - 1
+        a = _heads(q, n, dh, dt, dev)
+        if out is None:
+            out, oa = _like(q, dh)
+        else:
+            oa = _heads(out, n, dh, dt, dev)
+        ws = self._scratch(lib.map_cache_attend_shared_workspace(self.desc, q.shape[1], n, groups))
+        _check(lib.map_cache_attend_shared(self.desc, layer, a, _dense(seqs, torch.int32, dev, (n,), "seqs"), n,
+                                           _dense(starts, torch.int32, dev, (groups + 1,), "starts"), groups,
+                                           dh ** -0.5 if scale is None else scale, oa, ws.data_ptr(), self._stream()),
+               "map_cache_attend_shared")
+        return out
+
+    def attend_weigh(self, q, seqs, layer: int, weights, scale: float | None = None, out=None, stream=None):
+        """map_cache_attend_weigh: attend, and each row's attention weight, summed over a key head's query heads, is added to
+        weights float32 [layers, seqs, heads, max_pages * page].  Zero a sequence's weights when it begins or is freed."""
+        dev = self.device
+        if stream is not None or dev.index != _current_device():
+            with _on(dev, stream, q, seqs, weights, out):
+                return self.attend_weigh(q, seqs, layer, weights, scale, out)
+        dt, n, dh = self.pool.dtype, seqs.shape[0], self.dh
+        a = _heads(q, n, dh, dt, dev)
+        if out is None:
+            out, oa = _like(q, dh)
+        else:
+            oa = _heads(out, n, dh, dt, dev)
+        ws = self._scratch(lib.map_cache_attend_weigh_workspace(self.desc, q.shape[1], n))
+        _check(lib.map_cache_attend_weigh(self.desc, layer, a, _dense(seqs, torch.int32, dev, (n,), "seqs"), n,
+                                          dh ** -0.5 if scale is None else scale, oa,
+                                          _dense(weights, torch.float32, dev, self._weights_shape, "weights"), ws.data_ptr(),
+                                          self._stream()), "map_cache_attend_weigh")
+        return out
+
+    def evict(self, weights, seqs, first, last, k: int, stream=None) -> None:
+        """map_cache_evict: of rows first[i] .. length - last[i] - 1 of sequence seqs[i] the k with the greatest weights stay,
+        for each layer and head by itself; the rows behind move up, their weights with them (all int32 on the device, first
+        and last None for 0)."""
+        dev = self.device
+        if stream is not None or dev.index != _current_device():
+            with _on(dev, stream, weights, seqs, first, last):
+                return self.evict(weights, seqs, first, last, k)
+        n, i32 = seqs.shape[0], torch.int32
+        ws = self._scratch(lib.map_cache_evict_workspace(self.desc, n))
+        _check(lib.map_cache_evict(self.desc, _dense(weights, torch.float32, dev, self._weights_shape, "weights"),
+                                   _dense(seqs, i32, dev, (n,), "seqs"), n, _dense(first, i32, dev, (n,), "first"),
+                                   _dense(last, i32, dev, (n,), "last"), k, ws.data_ptr(), self._stream()), "map_cache_evict")
 
     def status(self, stream=None) -> int:
         dev = self.device

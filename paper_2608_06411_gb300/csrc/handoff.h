@@ -1,4 +1,4 @@
-// Shared by the language-model hand-off (rope.cu, cache.cu, attend.cu): element types, checks.
+// Shared by the language-model hand-off (rope.cu, cache.cu, evict.cu, attend*.cu): element types, checks.
 #pragma once
 #include <cstdint>
 #include <cuda_bf16.h>
@@ -45,9 +45,16 @@ __device__ __forceinline__ bool good_page(const map_cache& c, int page) {
 }
 __device__ __forceinline__ bool good_len(const map_cache& c, int len) { return len >= 0 && len <= c.max_pages * c.page; }
 // Pieces of `size` rows that hold `len` (a good length; it and a piece can add up past 2^31).
-__device__ __forceinline__ int pieces_of(int len, int size) { return static_cast<int>((static_cast<unsigned>(len) + size - 1) / size); }
+__host__ __device__ __forceinline__ int pieces_of(int len, int size) { return static_cast<int>((static_cast<unsigned>(len) + size - 1) / size); }
 
 // MAP_OK, MAP_EINVAL or MAP_EUNSUPPORTED for a cache's description (host values only).
 int check_cache(const map_cache* c);
+
+// A launch's status as a call's, the runtime's sticky copy of it cleared.
+inline int launch_err(cudaError_t e) {
+  if (e == cudaSuccess) return MAP_OK;
+  cudaGetLastError();
+  return MAP_ECUDA;
+}
 
 }  // namespace mapk

@@ -860,12 +860,6 @@ int check_rotation(const map_rope* r, int type, long long rows, const int32_t* p
   return MAP_OK;
 }
 
-int launch_err(cudaError_t e) {
-  if (e == cudaSuccess) return MAP_OK;
-  cudaGetLastError();
-  return MAP_ECUDA;
-}
-
 Side side_of(const map_heads* in, const map_heads* out, const void* w) {
   Side s{};
   s.x = in->p;
