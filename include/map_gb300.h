@@ -506,13 +506,13 @@ int map_cache_attend_weigh(const map_cache *cache, int layer, const map_heads *q
  *   seqs         int32 [n] (device); -1: padding.  A sequence may appear once.
  *   first, last  int32 [n] (device), >= 0; NULL: 0.
  *   weights      as map_cache_attend_weigh's; those behind the new length, up to the old one, become 0.
- *   ws           device scratch of map_cache_evict_workspace(cache, n) bytes, 16-byte aligned, the caller's until the call's work
+ *   ws           device scratch of map_cache_evict_workspace(cache, n, k) bytes, 16-byte aligned, the caller's until the call's work
  *                completes.
  * Pages that other sequences hold as well keep their rows: where rows move (or stay beside ones that do) the sequence gets new
- * pages instead, taken before any is given up.  Pages behind the new length lose a holder.  n <= 4096, n * max_pages < 2^31
- * (MAP_EUNSUPPORTED beyond).
+ * pages instead, taken before any is given up.  Pages behind the new length lose a holder.  n <= 4096, n * max_pages < 2^31,
+ * n * layers * heads <= 2^24 (MAP_EUNSUPPORTED beyond).
  */
-size_t map_cache_evict_workspace(const map_cache *cache, int n);
+size_t map_cache_evict_workspace(const map_cache *cache, int n, int k);
 int map_cache_evict(const map_cache *cache, float *weights, const int32_t *seqs, int n, const int32_t *first,
                     const int32_t *last, int k, void *ws, void *stream);
 

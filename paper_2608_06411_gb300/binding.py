@@ -83,7 +83,7 @@ SIGNATURES = {
                                         c_void_p, c_void_p]),
     "map_cache_attend_weigh_workspace": (c_size_t, [c_void_p, c_int, c_int]),
     "map_cache_attend_weigh": (c_int, [c_void_p, c_int, c_void_p, c_void_p, c_int, c_float] + [c_void_p] * 4),
-    "map_cache_evict_workspace": (c_size_t, [c_void_p, c_int]),
+    "map_cache_evict_workspace": (c_size_t, [c_void_p, c_int, c_int]),
     "map_cache_evict": (c_int, [c_void_p, c_void_p, c_void_p, c_int, c_void_p, c_void_p, c_int, c_void_p, c_void_p]),
     "map_cache_status": (c_int, [c_void_p, c_void_p]),
     "map_distill_grad": (c_int, [c_void_p, c_void_p, c_void_p, POINTER(c_int32), c_void_p, c_int, c_int, c_void_p,
@@ -785,7 +785,7 @@ class Cache:
             with _on(dev, stream, weights, seqs, first, last):
                 return self.evict(weights, seqs, first, last, k)
         n, i32 = seqs.shape[0], torch.int32
-        ws = self._scratch(lib.map_cache_evict_workspace(self.desc, n))
+        ws = self._scratch(lib.map_cache_evict_workspace(self.desc, n, k))
         _check(lib.map_cache_evict(self.desc, _dense(weights, torch.float32, dev, self._weights_shape, "weights"),
                                    _dense(seqs, i32, dev, (n,), "seqs"), n, _dense(first, i32, dev, (n,), "first"),
                                    _dense(last, i32, dev, (n,), "last"), k, ws.data_ptr(), self._stream()), "map_cache_evict")

@@ -27,6 +27,7 @@ struct EvictArgs {
   Eviction* entries;                       // [n]
   int32_t* was;                            // [n, max_pages]: pages before the call, of the columns that rows move to
   int32_t* taken;                          // [pages]
+  int32_t* kept;                           // [n][layers][heads][k]: rows that stay of those that may leave
 };
 
 // Checks, lengths, pages.  Latency-bound, one CTA (see extend_kernel); the columns of all entries form one list.
@@ -133,8 +134,7 @@ __global__ void __launch_bounds__(kPlanThreads) evict_plan_kernel(const EvictArg
 
 constexpr int kThreads = 256, kWarps = kThreads / 32;
 constexpr int kEach = 4, kChunk = kThreads * kEach;      // candidates looked at together
-constexpr int kList = 2 * kChunk;                        // rows that move, at most so many at a time
-constexpr int kBins = 2048;
+constexpr int kBins = 2048, kBinsEach = kBins / kThreads;
 
 // Weights in ascending order as unsigned numbers; NaN of either sign is the greatest, zeros are equal.
 __device__ __forceinline__ uint32_t key_of(float w) {
@@ -165,182 +165,260 @@ __device__ __forceinline__ uint32_t scan_block(uint32_t v, uint32_t* sums, uint3
   return before + s - v;
 }
 
-__global__ void __launch_bounds__(kThreads, 3) evict_kernel(const EvictArgs a) {
-  __shared__ union {
-    int hist[kBins];
-    struct { long long from[kList], to[kList]; } list;   // vectors of a plane
-  } sh;
+__device__ __forceinline__ int4 ld_peer(uint32_t at) {
+  int4 v;
+  asm volatile("ld.shared::cluster.v4.s32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at) : "memory");
+  return v;
+}
+__device__ __forceinline__ int cluster_size() {
+  int n;
+  asm("mov.u32 %0, %%cluster_nctaid.x;" : "=r"(n));
+  return n;
+}
+
+struct Unit { Eviction e; int layer, head; long long id; };
+__device__ __forceinline__ Unit unit_of(const EvictArgs& a, long long u) {
+  Unit x;
+  x.id = u;
+  x.head = static_cast<int>(u % a.c.heads);
+  x.layer = static_cast<int>(u / a.c.heads % a.c.layers);
+  const int4 e = __ldcg(reinterpret_cast<const int4*>(a.entries + u / a.c.heads / a.c.layers));
+  x.e = Eviction{e.x, e.y, e.z, e.w};
+  return x;
+}
+__device__ __forceinline__ float* weights_of(const EvictArgs& a, const Unit& x) {
+  return a.weights + ((static_cast<long long>(x.layer) * a.c.seqs + x.e.seq) * a.c.heads + x.head) * (static_cast<long long>(a.c.max_pages) * a.c.page);
+}
+
+// The rows that stay, in order, into kept [units][k]: a cluster a unit, an equal run of the candidates a CTA.
+__global__ void __launch_bounds__(kThreads) evict_select_kernel(const EvictArgs a) {
+  __shared__ __align__(16) int hist[2][kBins];
   __shared__ uint32_t sums[kWarps];
   __shared__ uint32_t pick_bin;
   __shared__ int pick_want, pick_size;
+  __shared__ __align__(16) int4 mine;          // candidates of this CTA above the least key, and with it
+  pdl_enter();
+  const int tid = threadIdx.x, ranks = cluster_size(), rank = blockIdx.x % ranks;
+  const Unit x = unit_of(a, blockIdx.x / ranks);
+  if (x.e.seq < 0 || a.k == 0) return;         // (one decision a cluster)
+  const int window = x.e.len - x.e.left + a.k, each = (window + ranks - 1) / ranks;
+  const int t0 = min(window, rank * each), t1 = min(window, t0 + each);
+  const float* w = weights_of(a, x) + x.e.first;
+  const auto all_here = [&]() { if (ranks > 1) cluster_sync(); else __syncthreads(); };
+
+  // the least key that stays, and how many rows with it: a digit a pass, of the keys with the digits found so far
+  for (int b = tid; b < kBins; b += kThreads) hist[0][b] = 0;
+  if (tid == 0) mine = make_int4(0, 0, 0, 0);
+  __syncthreads();
+  uint32_t prefix = 0;
+  int want = a.k, shift = 32, pass = 0;
+#pragma unroll 1
+  for (; shift > 0; pass ^= 1) {
+    const int bits = shift > 10 ? 11 : 10, down = shift - bits;
+    for (int t = t0 + tid; t < t1; t += kThreads * kEach) {
+      float v[kEach];
+#pragma unroll
+      for (int j = 0; j < kEach; ++j) v[j] = t + j * kThreads < t1 ? w[t + j * kThreads] : 0.f;
+#pragma unroll
+      for (int j = 0; j < kEach; ++j) {
+        const uint32_t key = key_of(v[j]);
+        if (t + j * kThreads < t1 && (shift == 32 || key >> shift == prefix)) atomicAdd(&hist[pass][key >> down & ((1 << bits) - 1)], 1);
+      }
+    }
+    all_here();
+    for (int b = tid; b < kBins; b += kThreads) hist[pass ^ 1][b] = 0;       // (the others have read it: they are here)
+    // from the greatest digit on: a thread counts eight, over all of the cluster's CTAs
+    const int bin0 = kBins - (tid + 1) * kBinsEach;
+    int count[kBinsEach] = {}, own[kBinsEach];
+    for (int r = 0; r < ranks; ++r) {
+#pragma unroll
+      for (int b = 0; b < kBinsEach; b += 4) {
+        const int4 v = ranks > 1 ? ld_peer(mapa_u32(&hist[pass][bin0 + b], r)) : *reinterpret_cast<const int4*>(&hist[pass][bin0 + b]);
+        count[b] += v.x;
+        count[b + 1] += v.y;
+        count[b + 2] += v.z;
+        count[b + 3] += v.w;
+        if (r == rank) {
+          own[b] = v.x;
+          own[b + 1] = v.y;
+          own[b + 2] = v.z;
+          own[b + 3] = v.w;
+        }
+      }
+    }
+    int sum = 0;
+#pragma unroll
+    for (int b = 0; b < kBinsEach; ++b) sum += count[b];
+    uint32_t all;
+    int above = static_cast<int>(scan_block(sum, sums, &all));
+    if (above < want && want <= above + sum) {
+#pragma unroll
+      for (int b = kBinsEach - 1; b >= 0; --b) {
+        if (above < want && want <= above + count[b]) {
+          pick_bin = bin0 + b;
+          pick_want = want - above;
+          pick_size = count[b];
+        }
+        above += count[b];
+      }
+    }
+    __syncthreads();
+    const int pick = static_cast<int>(pick_bin);
+    const bool done = pick_size == pick_want || down == 0;
+    int greater = 0, equal = 0;
+#pragma unroll
+    for (int b = 0; b < kBinsEach; ++b) {
+      greater += bin0 + b > pick ? own[b] : 0;
+      equal += bin0 + b == pick ? own[b] : 0;
+    }
+    if (greater) atomicAdd(&mine.x, greater);
+    if (equal && done) mine.y = equal;
+    prefix = shift == 32 ? pick_bin : prefix << bits | pick_bin;
+    want = pick_want;
+    shift = down;
+    if (pick_size == want) break;              // all of the digit's rows stay
+  }
+  const uint32_t least = prefix << shift;      // (all of the digit's, where they all stay)
+  const uint32_t above = shift > 0 ? prefix << shift | ((1u << shift) - 1) : prefix;
+
+  all_here();
+  int kept = 0, equals = 0;                    // rows so far above, and with the digits found
+  for (int r = 0; r < rank; ++r) {
+    const int4 v = ld_peer(mapa_u32(&mine, r));
+    kept += v.x;
+    equals += v.y;
+  }
+  kept += min(equals, want);
+  int32_t* out = a.kept + x.id * a.k;
+  for (int c0 = t0; c0 < t1; c0 += kChunk) {
+    uint32_t key[kEach], counts = 0;
+#pragma unroll
+    for (int j = 0; j < kEach; ++j) {
+      const int t = c0 + tid * kEach + j;
+      key[j] = t < t1 ? key_of(w[t]) : 0u;
+      counts += key[j] > above ? 1u : key[j] >= least ? 0x10000u : 0u;
+    }
+    uint32_t all;
+    const uint32_t at = scan_block(counts, sums, &all);
+    int greater = at & 0xffff, eq = equals + (at >> 16);
+    const int eq0 = min(equals, want);
+#pragma unroll
+    for (int j = 0; j < kEach; ++j) {
+      const bool more = key[j] > above, same = !more && key[j] >= least;
+      if (more || (same && eq < want)) out[kept + greater + min(eq, want) - eq0] = x.e.first + c0 + tid * kEach + j;
+      greater += more;
+      eq += same;
+    }
+    equals += all >> 16;
+    kept += (all & 0xffff) + min(equals, want) - eq0;
+  }
+  if (ranks > 1) cluster_sync();               // no CTA leaves while another may read its counts
+}
+
+// The rows that move, a slice of a unit's columns (or its weights) a CTA.
+constexpr int kMoveThreads = 256, kMoveEach = 8;
+constexpr int kMoveRows = 1024;                // of a batch, at most
+__global__ void __launch_bounds__(kMoveThreads, 4) evict_move_kernel(const EvictArgs a, int slices) {
+  __shared__ long long from[kMoveRows], to[kMoveRows];       // vectors of a plane; -1: the row is where it shall be
   pdl_enter();
   const map_cache& c = a.c;
-  const int tid = threadIdx.x, vec = c.dh / 8, max_rows = c.max_pages * c.page;
+  const int tid = threadIdx.x, parts = 2 * slices + 1, part = blockIdx.x % parts;
+  const Unit x = unit_of(a, blockIdx.x / parts);
+  if (x.e.seq < 0) return;
+  const Eviction& e = x.e;
+  const int tail = e.left - e.first - a.k;
+  const int32_t* kept = a.kept + x.id * a.k;
+  // row r of those from e.first on: where it comes from
+  const auto source = [&](int r) { return r < a.k ? __ldcg(kept + r) : e.len - tail + r - a.k; };
+
+  if (part == parts - 1) {                     // the weights, and zeros behind them
+    float* w = weights_of(a, x);
+    constexpr int kBatch = kMoveThreads * kMoveEach;
+    for (int r0 = 0; r0 < a.k + tail; r0 += kBatch) {
+      float v[kMoveEach];
+#pragma unroll
+      for (int j = 0; j < kMoveEach; ++j) {
+        const int r = r0 + tid + j * kMoveThreads;
+        v[j] = r < a.k + tail ? w[source(r)] : 0.f;
+      }
+      __syncthreads();                         // the batch has been read
+#pragma unroll
+      for (int j = 0; j < kMoveEach; ++j) {
+        const int r = r0 + tid + j * kMoveThreads;
+        if (r < a.k + tail) w[e.first + r] = v[j];
+      }
+    }
+    __syncthreads();                           // the last rows' sources lie where the zeros go
+    for (int t = e.left + tid; t < e.len; t += kMoveThreads) w[t] = 0.f;
+    return;
+  }
+
+  const int vec = c.dh / 8, slice = part % slices, v0 = vec * slice / slices, wide = vec * (slice + 1) / slices - v0;
   const long long plane = static_cast<long long>(c.pages) * c.heads * c.page * vec;
-  const long long units = static_cast<long long>(a.n) * c.layers * c.heads;
-  for (long long u = blockIdx.x; u < units; u += gridDim.x) {
-    const int head = static_cast<int>(u % c.heads), layer = static_cast<int>(u / c.heads % c.layers);
-    const int i = static_cast<int>(u / c.heads / c.layers);
-    const int4 en = __ldcg(reinterpret_cast<const int4*>(a.entries + i));
-    const int seq = en.x, len = en.y, first = en.z, left = en.w;
-    if (seq < 0) continue;
-    const int window = len - left + a.k, tail = left - first - a.k;
-    float* w = a.weights + ((static_cast<long long>(layer) * c.seqs + seq) * c.heads + head) * max_rows;
-
-    // the least key that stays, and how many rows with it
-    uint32_t least = 0xffffffffu;
-    int want = 0;
-    if (a.k > 0) {
-      uint32_t prefix = 0;                     // of the keys' bits above `shift`
-      want = a.k;
-      int shift = 32;
-#pragma unroll 1
-      while (shift > 0) {
-        const int bits = shift > 10 ? 11 : 10, down = shift - bits;
-        __syncthreads();
-        for (int b = tid; b < kBins; b += kThreads) sh.hist[b] = 0;
-        __syncthreads();
-        for (int t = tid; t < window; t += kThreads) {
-          const uint32_t key = key_of(w[first + t]);
-          if (shift == 32 || key >> shift == prefix) atomicAdd(&sh.hist[key >> down & ((1 << bits) - 1)], 1);
-        }
-        __syncthreads();
-        // from the greatest digit on: a thread counts eight
-        constexpr int kOwn = kBins / kThreads;
-        int mine = 0;
-#pragma unroll
-        for (int b = 0; b < kOwn; ++b) mine += sh.hist[kBins - 1 - tid * kOwn - b];
-        uint32_t all;
-        int above = static_cast<int>(scan_block(mine, sums, &all));
-        if (above < want && want <= above + mine)
-          for (int b = kBins - 1 - tid * kOwn;; --b) {
-            if (want <= above + sh.hist[b]) {
-              pick_bin = b;
-              pick_want = want - above;
-              pick_size = sh.hist[b];
-              break;
-            }
-            above += sh.hist[b];
-          }
-        __syncthreads();
-        prefix = shift == 32 ? pick_bin : prefix << bits | pick_bin;
-        want = pick_want;
-        shift = down;
-        if (pick_size == want) break;          // all of the digit's rows stay
-      }
-      least = prefix << shift;
-      if (pick_size == want) { --least; want = 0; }        // (no weight has a key of zero)
+  uint4* pool = static_cast<uint4*>(c.pool) + (2 * x.layer + part / slices) * plane + v0;
+  const int32_t* row = c.table + static_cast<long long>(e.seq) * c.max_pages;
+  const int32_t* was = a.was + x.id / c.heads / c.layers * c.max_pages;
+  const int moved_to = pieces_of(e.left, c.page);
+  const auto place = [&](int page, int in_page) { return ((static_cast<long long>(page) * c.heads + x.head) * c.page + in_page) * vec; };
+  // rows before e.first in its page move too, where the page is replaced
+  const int head = e.first % c.page, rows = head + a.k + tail, batch = min(kMoveRows, kMoveThreads * kMoveEach / wide);
+  for (int r0 = 0; r0 < rows; r0 += batch) {
+    const int n = min(batch, rows - r0);
+    for (int i = tid; i < n; i += kMoveThreads) {
+      const int r = r0 + i - head, t = e.first + r, s = r < 0 ? t : source(r);
+      const int cf = s / c.page, ct = t / c.page;
+      const int old = cf < moved_to ? __ldcg(was + cf) & ~kReplaced : __ldcg(row + cf), now = __ldcg(row + ct);
+      const bool stays = s == t && old == now;
+      from[i] = stays ? -1 : place(old, s - cf * c.page);
+      to[i] = place(now, t - ct * c.page);
     }
-
-    const int32_t* row = c.table + static_cast<long long>(seq) * c.max_pages;
-    const int32_t* was = a.was + static_cast<long long>(i) * c.max_pages;
-    const int moved_to = pieces_of(left, c.page);
-    const auto place = [&](int page, int t) { return ((static_cast<long long>(page) * c.heads + head) * c.page + t % c.page) * vec; };
-    const auto push = [&](int at, int from, int to) {
-      const int cf = from / c.page;
-      sh.list.from[at] = place(cf < moved_to ? was[cf] & ~kReplaced : row[cf], from);
-      sh.list.to[at] = place(row[to / c.page], to);
-    };
-    uint4* pk = static_cast<uint4*>(c.pool) + 2 * layer * plane;
-    uint4* pv = pk + plane;
-    int listed = 0;
-    const auto flush = [&]() {
-      __syncthreads();
-      const int vecs = listed * vec;
-      for (int e0 = tid; e0 - tid < vecs; e0 += kThreads * kEach) {
-        uint4 kx[kEach], vx[kEach];
-        long long to[kEach];
-#pragma unroll
-        for (int j = 0; j < kEach; ++j) {
-          const int e = e0 + j * kThreads, r = e / vec, x = e % vec;
-          to[j] = -1;
-          if (e < vecs && sh.list.from[r] != sh.list.to[r]) {
-            const long long from = sh.list.from[r] + x;
-            to[j] = sh.list.to[r] + x;
-            kx[j] = pk[from];
-            vx[j] = pv[from];
-          }
-        }
-        __syncthreads();                       // the batch has been read
-#pragma unroll
-        for (int j = 0; j < kEach; ++j)
-          if (to[j] >= 0) {
-            pk[to[j]] = kx[j];
-            pv[to[j]] = vx[j];
-          }
-      }
-      listed = 0;
-      __syncthreads();
-    };
-
-    // rows before the first that may leave, in its page: they move where the page is replaced
     __syncthreads();
-    const int at0 = first / c.page * c.page;
-    for (int t = at0 + tid; t < first; t += kThreads) push(t - at0, t, t);
-    listed = first - at0;
-    int kept = 0, equals = 0;                  // rows so far that stay, and with the least key
-    for (int t0 = 0; t0 < window; t0 += kChunk) {
-      float x[kEach];
-      uint32_t key[kEach], mine = 0;
+    uint4 v[kMoveEach];
+    const int vecs = n * wide;
 #pragma unroll
-      for (int j = 0; j < kEach; ++j) {
-        const int t = t0 + tid * kEach + j;
-        x[j] = t < window ? w[first + t] : 0.f;
-        key[j] = t < window ? key_of(x[j]) : 0u;
-        mine += key[j] > least ? 1u : key[j] == least ? 0x10000u : 0u;
-      }
-      uint32_t all, at = scan_block(mine, sums, &all);       // (the chunk has been read behind it)
-      int greater = at & 0xffff, eq = equals + (at >> 16);
-      const int eq0 = min(equals, want);
-#pragma unroll
-      for (int j = 0; j < kEach; ++j) {
-        const int here = greater + min(eq, want) - eq0;
-        const bool same = key[j] == least && t0 + tid * kEach + j < window;
-        if (key[j] > least || (same && eq < want)) {
-          push(listed + here, first + t0 + tid * kEach + j, first + kept + here);
-          w[first + kept + here] = x[j];
-        }
-        greater += key[j] > least;
-        eq += same;
-      }
-      equals += all >> 16;
-      const int stay = (all & 0xffff) + min(equals, want) - eq0;
-      kept += stay;
-      listed += stay;
-      if (listed > kList - kChunk) flush();
+    for (int j = 0; j < kMoveEach; ++j) {
+      const int i = tid + j * kMoveThreads, r = i / wide;
+      if (i < vecs && from[r] >= 0) v[j] = pool[from[r] + i - r * wide];
     }
-    for (int t0 = 0; t0 < tail; t0 += kChunk) {
-      const int from = len - tail + t0, to = left - tail + t0, rows = min(kChunk, tail - t0);
-      float x[kEach];
+    __syncthreads();                           // the batch has been read
 #pragma unroll
-      for (int j = 0; j < kEach; ++j)
-        if (tid + j * kThreads < rows) x[j] = w[from + tid + j * kThreads];
-      __syncthreads();
-#pragma unroll
-      for (int j = 0; j < kEach; ++j) {
-        const int r = tid + j * kThreads;
-        if (r < rows) {
-          w[to + r] = x[j];
-          push(listed + r, from + r, to + r);
-        }
-      }
-      listed += rows;
-      if (listed > kList - kChunk) flush();
+    for (int j = 0; j < kMoveEach; ++j) {
+      const int i = tid + j * kMoveThreads, r = i / wide;
+      if (i < vecs && from[r] >= 0) pool[to[r] + i - r * wide] = v[j];
     }
-    flush();
-    for (int t = left + tid; t < len; t += kThreads) w[t] = 0.f;
+    __syncthreads();                           // the lists have been read
   }
 }
 
-struct EvictSpace { size_t was, taken, bytes; };
-EvictSpace evict_space(const map_cache* c, long long n) {
+template <typename... P, typename... Args>
+cudaError_t launch_cluster(void (*kern)(P...), unsigned grid, unsigned threads, int ranks, cudaStream_t st, const Args&... args) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(grid);
+  cfg.blockDim = dim3(threads);
+  cfg.stream = st;
+  cudaLaunchAttribute at[2];
+  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at[0].val.programmaticStreamSerializationAllowed = pdl_disabled() ? 0 : 1;
+  at[1].id = cudaLaunchAttributeClusterDimension;
+  at[1].val.clusterDim.x = ranks;
+  at[1].val.clusterDim.y = at[1].val.clusterDim.z = 1;
+  cfg.attrs = at;
+  cfg.numAttrs = 2;
+  return cudaLaunchKernelEx(&cfg, kern, args...);
+}
+
+struct EvictSpace { size_t was, taken, kept, bytes; };
+EvictSpace evict_space(const map_cache* c, long long n, long long k) {
   EvictSpace s;
   s.was = static_cast<size_t>(n) * sizeof(Eviction);
   s.taken = s.was + static_cast<size_t>(n) * c->max_pages * 4;
-  s.bytes = s.taken + static_cast<size_t>(c->pages) * 4;
+  s.kept = s.taken + static_cast<size_t>(c->pages) * 4;
+  s.bytes = s.kept + static_cast<size_t>(n) * c->layers * c->heads * std::min<long long>(k, static_cast<long long>(c->max_pages) * c->page) * 4;
   return s;
 }
-bool evict_fits(const map_cache* c, int n) { return n <= kMaxEntries && static_cast<long long>(n) * c->max_pages < (1ll << 31); }
+bool evict_fits(const map_cache* c, long long n) {            // units: 9 CTAs each, and 2^31 rows that stay, of 4 bytes
+  return n <= kMaxEntries && n * c->max_pages < (1ll << 31) && n * c->layers * c->heads <= (1 << 24);
+}
 
 }  // namespace
 }  // namespace mapk
@@ -349,8 +427,8 @@ using namespace mapk;
 
 extern "C" {
 
-size_t map_cache_evict_workspace(const map_cache* c, int n) {
-  return check_cache(c) == MAP_OK && n >= 0 && evict_fits(c, n) ? evict_space(c, n).bytes : 0;
+size_t map_cache_evict_workspace(const map_cache* c, int n, int k) {
+  return check_cache(c) == MAP_OK && n >= 0 && k >= 0 && evict_fits(c, n) ? evict_space(c, n, k).bytes : 0;
 }
 
 int map_cache_evict(const map_cache* c, float* weights, const int32_t* seqs, int n, const int32_t* first, const int32_t* last,
@@ -361,17 +439,22 @@ int map_cache_evict(const map_cache* c, float* weights, const int32_t* seqs, int
   if (!evict_fits(c, n)) return MAP_EUNSUPPORTED;
   if (n == 0) return MAP_OK;
   if (!seqs || !weights || (reinterpret_cast<uintptr_t>(weights) & 3) || !ws || !aligned16(ws)) return MAP_EINVAL;
-  const EvictSpace s = evict_space(c, n);
+  const EvictSpace s = evict_space(c, n, k);
   char* p = static_cast<char*>(ws);
   const EvictArgs a{*c, weights, seqs, first, last, n, k, reinterpret_cast<Eviction*>(p),
-                    reinterpret_cast<int32_t*>(p + s.was), reinterpret_cast<int32_t*>(p + s.taken)};
+                    reinterpret_cast<int32_t*>(p + s.was), reinterpret_cast<int32_t*>(p + s.taken), reinterpret_cast<int32_t*>(p + s.kept)};
   const size_t smem = plan_smem(n, c->seqs);
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   cudaError_t e = allow_smem(reinterpret_cast<const void*>(evict_plan_kernel), smem);
   if (e == cudaSuccess) e = launch_k(evict_plan_kernel, dim3(1), dim3(kPlanThreads), smem, st, a);
-  const long long units = static_cast<long long>(n) * c->layers * c->heads;
+  const long long units = static_cast<long long>(n) * c->layers * c->heads, max_rows = static_cast<long long>(c->max_pages) * c->page;
+  // CTAs that look for a unit's rows, and slices that its columns move in: as many as fill the chip where the units do not
+  int ranks = 1, slices = 1;
+  while (ranks < 8 && units * ranks < 2 * 152 && max_rows / ranks > 2 * kChunk) ranks *= 2;
+  while (slices < 4 && units * slices < 2 * 152 && c->dh / 8 / slices >= 8) slices *= 2;
+  if (e == cudaSuccess) e = launch_cluster(evict_select_kernel, static_cast<unsigned>(units * ranks), kThreads, ranks, st, a);
   if (e == cudaSuccess)
-    e = launch_k(evict_kernel, dim3(static_cast<unsigned>(std::min<long long>(units, 152 * 6))), dim3(kThreads), 0, st, a);
+    e = launch_k(evict_move_kernel, dim3(static_cast<unsigned>(units * (2 * slices + 1))), dim3(kMoveThreads), 0, st, a, slices);
   return launch_err(e);
 }
 

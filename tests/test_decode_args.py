@@ -63,15 +63,18 @@ def test_evict_refusals(mb):  # noqa: F811
     for kind, bad in BAD_CACHES:
         b = cache(mb, **bad)
         assert lib.map_cache_evict(b, F, F, 1, F, F, 1, F, None) == {"E": E, "U": U}[kind], bad
-        assert lib.map_cache_evict_workspace(b, 1) == 0
+        assert lib.map_cache_evict_workspace(b, 1, 1) == 0
     c = cache(mb)
     for args in ((None, F, 1, F, F, 1, F), (F + 2, F, 1, F, F, 1, F), (F, None, 1, F, F, 1, F), (F, F, -1, F, F, 1, F),
                  (F, F, 1, F, F, -1, F), (F, F, 1, F, F, 1, None), (F, F, 1, F, F, 1, F + 8)):
         assert lib.map_cache_evict(c, *args, None) == E, args
     assert lib.map_cache_evict(c, F, F, 4097, F, F, 1, F, None) == U
     many = cache(mb, page=1, max_pages=1 << 20)
-    assert lib.map_cache_evict(many, F, F, 2048, F, F, 1, F, None) == U and lib.map_cache_evict_workspace(many, 2048) == 0
-    assert lib.map_cache_evict_workspace(many, 2047) >= 2047 * 4 << 20
+    assert lib.map_cache_evict(many, F, F, 2048, F, F, 1, F, None) == U and lib.map_cache_evict_workspace(many, 2048, 1) == 0
+    heads_of_all = cache(mb, hk=8, layers=1024)                       # 4096 * 8192 units
+    assert lib.map_cache_evict(heads_of_all, F, F, 4096, F, F, 1, F, None) == U and lib.map_cache_evict_workspace(heads_of_all, 4096, 1) == 0
+    assert lib.map_cache_evict_workspace(heads_of_all, 2048, 1) > 0 == lib.map_cache_evict_workspace(heads_of_all, 2048, -1)
+    assert lib.map_cache_evict_workspace(many, 2047, 1) >= 2047 * 4 << 20
     assert lib.map_cache_evict(c, None, None, 0, None, None, 0, None, None) == mb.MAP_OK
 
 

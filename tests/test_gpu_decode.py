@@ -635,7 +635,7 @@ def test_decode_calls_of_two_caches_from_two_threads(mb, call):  # noqa: F811
             held.append((out, c.attend(q, seqs, 0), ws))
             fn = lib.map_cache_attend_weigh
         else:
-            ws = ws_of(lib.map_cache_evict_workspace(c.desc, 2))
+            ws = ws_of(lib.map_cache_evict_workspace(c.desc, 2, 1000))
             args = (c.desc, w.data_ptr(), seqs.data_ptr(), 2, None, None, 1000, ws.data_ptr(), st.cuda_stream)
             out.fill_(1.0)
             held.append((out, out.clone(), ws))
