@@ -132,37 +132,13 @@ __global__ void __launch_bounds__(kPlanThreads) evict_plan_kernel(const EvictArg
   }
 }
 
-constexpr int kThreads = 256, kWarps = kThreads / 32;
-constexpr int kEach = 4, kChunk = kThreads * kEach;      // candidates looked at together
-constexpr int kBins = 2048, kBinsEach = kBins / kThreads;
+constexpr int kHold = 16;                      // candidates of a thread that it keeps in registers
+constexpr int kBins = 2048;
 
 // Weights in ascending order as unsigned numbers; NaN of either sign is the greatest, zeros are equal.
 __device__ __forceinline__ uint32_t key_of(float w) {
   const uint32_t b = __float_as_uint(w + 0.f);
   return isnan(w) ? 0xffffffffu : b & 0x80000000u ? ~b : b | 0x80000000u;
-}
-
-// Exclusive prefix sums over the block's threads, and the total.
-__device__ __forceinline__ uint32_t scan_block(uint32_t v, uint32_t* sums, uint32_t* total) {
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  uint32_t s = v;
-#pragma unroll
-  for (int o = 1; o < 32; o <<= 1) {
-    const uint32_t u = __shfl_up_sync(0xffffffffu, s, o);
-    if (lane >= o) s += u;
-  }
-  __syncthreads();                             // the sums of the last call have been read
-  if (lane == 31) sums[warp] = s;
-  __syncthreads();
-  uint32_t before = 0, all = 0;
-#pragma unroll
-  for (int w = 0; w < kWarps; ++w) {
-    const uint32_t x = sums[w];
-    before += w < warp ? x : 0;
-    all += x;
-  }
-  *total = all;
-  return before + s - v;
 }
 
 __device__ __forceinline__ int4 ld_peer(uint32_t at) {
@@ -190,46 +166,60 @@ __device__ __forceinline__ float* weights_of(const EvictArgs& a, const Unit& x) 
   return a.weights + ((static_cast<long long>(x.layer) * a.c.seqs + x.e.seq) * a.c.heads + x.head) * (static_cast<long long>(a.c.max_pages) * a.c.page);
 }
 
-// The rows that stay, in order, into kept [units][k]: a cluster a unit, an equal run of the candidates a CTA.
-__global__ void __launch_bounds__(kThreads) evict_select_kernel(const EvictArgs a) {
+// The rows that stay, in order, into kept [units][k]: a cluster a unit, an equal run of the candidates a CTA, of which a warp holds
+// kHold times 32 in a row.  Runs of up to kHold * THREADS are read once.
+template <int THREADS>
+__global__ void __launch_bounds__(THREADS) evict_select_kernel(const EvictArgs a) {
+  constexpr int kWarps = THREADS / 32, kBinsEach = kBins / THREADS, kChunk = kHold * THREADS;
   __shared__ __align__(16) int hist[2][kBins];
-  __shared__ uint32_t sums[kWarps];
+  __shared__ int warp_sum[kWarps];
+  __shared__ int2 warp_kept[kWarps];
   __shared__ uint32_t pick_bin;
   __shared__ int pick_want, pick_size;
-  __shared__ __align__(16) int4 mine;          // candidates of this CTA above the least key, and with it
+  __shared__ __align__(16) int4 mine;          // candidates of this CTA above the digits found, and with them
   pdl_enter();
-  const int tid = threadIdx.x, ranks = cluster_size(), rank = blockIdx.x % ranks;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, ranks = cluster_size(), rank = blockIdx.x % ranks;
   const Unit x = unit_of(a, blockIdx.x / ranks);
   if (x.e.seq < 0 || a.k == 0) return;         // (one decision a cluster)
   const int window = x.e.len - x.e.left + a.k, each = (window + ranks - 1) / ranks;
   const int t0 = min(window, rank * each), t1 = min(window, t0 + each);
   const float* w = weights_of(a, x) + x.e.first;
   const auto all_here = [&]() { if (ranks > 1) cluster_sync(); else __syncthreads(); };
+  uint32_t key[kHold];                         // of candidates row0 + 32 j; 0, below all weights, where there is none
+  const auto load = [&](int c0) {
+    const int row0 = c0 + warp * (32 * kHold) + lane;
+    float v[kHold];
+#pragma unroll
+    for (int j = 0; j < kHold; ++j) v[j] = row0 + 32 * j < t1 ? __ldcg(w + row0 + 32 * j) : 0.f;
+#pragma unroll
+    for (int j = 0; j < kHold; ++j) key[j] = row0 + 32 * j < t1 ? key_of(v[j]) : 0u;
+  };
+  const bool once = t1 - t0 <= kChunk;
+  load(t0);
 
-  // the least key that stays, and how many rows with it: a digit a pass, of the keys with the digits found so far
-  for (int b = tid; b < kBins; b += kThreads) hist[0][b] = 0;
+  for (int b = tid; b < kBins; b += THREADS) hist[0][b] = 0;
   if (tid == 0) mine = make_int4(0, 0, 0, 0);
   __syncthreads();
+  // a digit a pass, of the keys with the digits found so far
   uint32_t prefix = 0;
   int want = a.k, shift = 32, pass = 0;
 #pragma unroll 1
   for (; shift > 0; pass ^= 1) {
     const int bits = shift > 10 ? 11 : 10, down = shift - bits;
-    for (int t = t0 + tid; t < t1; t += kThreads * kEach) {
-      float v[kEach];
+#pragma unroll 1
+    for (int c0 = t0; c0 < t1; c0 += kChunk) {
+      if (!once) load(c0);
 #pragma unroll
-      for (int j = 0; j < kEach; ++j) v[j] = t + j * kThreads < t1 ? w[t + j * kThreads] : 0.f;
-#pragma unroll
-      for (int j = 0; j < kEach; ++j) {
-        const uint32_t key = key_of(v[j]);
-        if (t + j * kThreads < t1 && (shift == 32 || key >> shift == prefix)) atomicAdd(&hist[pass][key >> down & ((1 << bits) - 1)], 1);
-      }
+      for (int j = 0; j < kHold; ++j)
+        if (key[j] != 0 && (shift == 32 || key[j] >> shift == prefix)) atomicAdd(&hist[pass][key[j] >> down & ((1 << bits) - 1)], 1);
     }
     all_here();
-    for (int b = tid; b < kBins; b += kThreads) hist[pass ^ 1][b] = 0;       // (the others have read it: they are here)
-    // from the greatest digit on: a thread counts eight, over all of the cluster's CTAs
+    // (the others have read the last pass's counts: they are here)
+    for (int b = tid; b < kBins; b += THREADS) hist[pass ^ 1][b] = 0;
+    // from the greatest digit on: a thread counts kBinsEach, over all of the cluster's CTAs
     const int bin0 = kBins - (tid + 1) * kBinsEach;
     int count[kBinsEach] = {}, own[kBinsEach];
+#pragma unroll 8
     for (int r = 0; r < ranks; ++r) {
 #pragma unroll
       for (int b = 0; b < kBinsEach; b += 4) {
@@ -238,19 +228,24 @@ __global__ void __launch_bounds__(kThreads) evict_select_kernel(const EvictArgs 
         count[b + 1] += v.y;
         count[b + 2] += v.z;
         count[b + 3] += v.w;
-        if (r == rank) {
-          own[b] = v.x;
-          own[b + 1] = v.y;
-          own[b + 2] = v.z;
-          own[b + 3] = v.w;
-        }
       }
     }
+#pragma unroll
+    for (int b = 0; b < kBinsEach; ++b) own[b] = hist[pass][bin0 + b];
     int sum = 0;
 #pragma unroll
     for (int b = 0; b < kBinsEach; ++b) sum += count[b];
-    uint32_t all;
-    int above = static_cast<int>(scan_block(sum, sums, &all));
+    int above = sum;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int u = __shfl_up_sync(0xffffffffu, above, o);
+      if (lane >= o) above += u;
+    }
+    if (lane == 31) warp_sum[warp] = above;
+    __syncthreads();
+    above -= sum;
+#pragma unroll
+    for (int i = 0; i < kWarps; ++i) above += i < warp ? warp_sum[i] : 0;
     if (above < want && want <= above + sum) {
 #pragma unroll
       for (int b = kBinsEach - 1; b >= 0; --b) {
@@ -271,55 +266,70 @@ __global__ void __launch_bounds__(kThreads) evict_select_kernel(const EvictArgs 
       greater += bin0 + b > pick ? own[b] : 0;
       equal += bin0 + b == pick ? own[b] : 0;
     }
-    if (greater) atomicAdd(&mine.x, greater);
+    greater = __reduce_add_sync(0xffffffffu, greater);
+    if (lane == 0 && greater) atomicAdd(&mine.x, greater);
     if (equal && done) mine.y = equal;
     prefix = shift == 32 ? pick_bin : prefix << bits | pick_bin;
     want = pick_want;
     shift = down;
     if (pick_size == want) break;              // all of the digit's rows stay
   }
-  const uint32_t least = prefix << shift;      // (all of the digit's, where they all stay)
-  const uint32_t above = shift > 0 ? prefix << shift | ((1u << shift) - 1) : prefix;
+  // keys from `least` on have the digits found, those past `most` greater ones
+  const uint32_t least = prefix << shift, most = shift > 0 ? least | ((1u << shift) - 1) : least;
 
   all_here();
-  int kept = 0, equals = 0;                    // rows so far above, and with the digits found
+  int kept = 0, equals = 0;                    // rows so far with greater digits, and with the digits found
+#pragma unroll 8
   for (int r = 0; r < rank; ++r) {
     const int4 v = ld_peer(mapa_u32(&mine, r));
     kept += v.x;
     equals += v.y;
   }
-  kept += min(equals, want);
   int32_t* out = a.kept + x.id * a.k;
+#pragma unroll 1
   for (int c0 = t0; c0 < t1; c0 += kChunk) {
-    uint32_t key[kEach], counts = 0;
+    if (!once) load(c0);
+    int2 n = make_int2(0, 0);
 #pragma unroll
-    for (int j = 0; j < kEach; ++j) {
-      const int t = c0 + tid * kEach + j;
-      key[j] = t < t1 ? key_of(w[t]) : 0u;
-      counts += key[j] > above ? 1u : key[j] >= least ? 0x10000u : 0u;
+    for (int j = 0; j < kHold; ++j) {
+      n.x += __popc(__ballot_sync(0xffffffffu, key[j] > most));
+      n.y += __popc(__ballot_sync(0xffffffffu, key[j] >= least && key[j] <= most));
     }
-    uint32_t all;
-    const uint32_t at = scan_block(counts, sums, &all);
-    int greater = at & 0xffff, eq = equals + (at >> 16);
-    const int eq0 = min(equals, want);
+    __syncthreads();                           // the last chunk's have been read
+    if (lane == 0) warp_kept[warp] = n;
+    __syncthreads();
+    int at = kept, eq = equals;
 #pragma unroll
-    for (int j = 0; j < kEach; ++j) {
-      const bool more = key[j] > above, same = !more && key[j] >= least;
-      if (more || (same && eq < want)) out[kept + greater + min(eq, want) - eq0] = x.e.first + c0 + tid * kEach + j;
-      greater += more;
-      eq += same;
+    for (int i = 0; i < kWarps; ++i) {
+      const int2 v = warp_kept[i];
+      if (i < warp) {
+        at += v.x;
+        eq += v.y;
+      }
+      kept += v.x;
+      equals += v.y;
     }
-    equals += all >> 16;
-    kept += (all & 0xffff) + min(equals, want) - eq0;
+    const uint32_t before = (1u << lane) - 1;
+    const int row0 = x.e.first + c0 + warp * (32 * kHold) + lane;
+#pragma unroll
+    for (int j = 0; j < kHold; ++j) {
+      const bool more = key[j] > most, same = !more && key[j] >= least;
+      const uint32_t m = __ballot_sync(0xffffffffu, more), s = __ballot_sync(0xffffffffu, same);
+      const int mine_eq = eq + __popc(s & before);
+      if (more || (same && mine_eq < want)) out[at + __popc(m & before) + min(mine_eq, want)] = row0 + 32 * j;
+      at += __popc(m);
+      eq += __popc(s);
+    }
   }
   if (ranks > 1) cluster_sync();               // no CTA leaves while another may read its counts
 }
 
 // The rows that move, a slice of a unit's columns (or its weights) a CTA.
 constexpr int kMoveThreads = 256, kMoveEach = 8;
-constexpr int kMoveRows = 1024;                // of a batch, at most
+constexpr int kMoveRowsEach = 2, kMoveRows = kMoveRowsEach * kMoveThreads;   // of a batch, at most
 __global__ void __launch_bounds__(kMoveThreads, 4) evict_move_kernel(const EvictArgs a, int slices) {
-  __shared__ long long from[kMoveRows], to[kMoveRows];       // vectors of a plane; -1: the row is where it shall be
+  struct Row { long long from, to; };          // vectors of a plane; from -1: the row is where it shall be
+  __shared__ Row list[3][kMoveRows];           // batches: being stored, loaded, looked up
   pdl_enter();
   const map_cache& c = a.c;
   const int tid = threadIdx.x, parts = 2 * slices + 1, part = blockIdx.x % parts;
@@ -362,31 +372,47 @@ __global__ void __launch_bounds__(kMoveThreads, 4) evict_move_kernel(const Evict
   const auto place = [&](int page, int in_page) { return ((static_cast<long long>(page) * c.heads + x.head) * c.page + in_page) * vec; };
   // rows before e.first in its page move too, where the page is replaced
   const int head = e.first % c.page, rows = head + a.k + tail, batch = min(kMoveRows, kMoveThreads * kMoveEach / wide);
-  for (int r0 = 0; r0 < rows; r0 += batch) {
-    const int n = min(batch, rows - r0);
-    for (int i = tid; i < n; i += kMoveThreads) {
-      const int r = r0 + i - head, t = e.first + r, s = r < 0 ? t : source(r);
+  int src[kMoveRowsEach];                      // of the batch to be looked up next
+  const auto sources = [&](int r0, int n) {
+#pragma unroll
+    for (int k = 0; k < kMoveRowsEach; ++k) {
+      const int i = tid + k * kMoveThreads;
+      src[k] = i < min(batch, n) ? (r0 + i < head ? e.first + r0 + i - head : source(r0 + i - head)) : -1;
+    }
+  };
+  const auto look_up = [&](int r0, Row* to) {
+#pragma unroll
+    for (int k = 0; k < kMoveRowsEach; ++k) {
+      const int s = src[k], t = e.first + r0 + tid + k * kMoveThreads - head;
+      if (s < 0) continue;
       const int cf = s / c.page, ct = t / c.page;
       const int old = cf < moved_to ? __ldcg(was + cf) & ~kReplaced : __ldcg(row + cf), now = __ldcg(row + ct);
-      const bool stays = s == t && old == now;
-      from[i] = stays ? -1 : place(old, s - cf * c.page);
-      to[i] = place(now, t - ct * c.page);
+      to[tid + k * kMoveThreads] = Row{s == t && old == now ? -1 : place(old, s - cf * c.page), place(now, t - ct * c.page)};
     }
-    __syncthreads();
+  };
+  sources(0, rows);
+  look_up(0, list[0]);
+  sources(batch, rows - batch);
+  __syncthreads();
+  int at = 0;
+  for (int r0 = 0, n = rows; n > 0; r0 += batch, n -= batch) {
+    const Row* here = list[at];
+    at = at == 2 ? 0 : at + 1;
+    const int vecs = min(batch, n) * wide;
     uint4 v[kMoveEach];
-    const int vecs = n * wide;
 #pragma unroll
     for (int j = 0; j < kMoveEach; ++j) {
       const int i = tid + j * kMoveThreads, r = i / wide;
-      if (i < vecs && from[r] >= 0) v[j] = pool[from[r] + i - r * wide];
+      if (i < vecs && here[r].from >= 0) v[j] = pool[here[r].from + i - r * wide];
     }
-    __syncthreads();                           // the batch has been read
+    look_up(r0 + batch, list[at]);
+    sources(r0 + 2 * batch, n - 2 * batch);    // (past 2^31 only where there is none)
+    __syncthreads();                           // the batch has been read, the next one looked up
 #pragma unroll
     for (int j = 0; j < kMoveEach; ++j) {
       const int i = tid + j * kMoveThreads, r = i / wide;
-      if (i < vecs && from[r] >= 0) pool[to[r] + i - r * wide] = v[j];
+      if (i < vecs && here[r].from >= 0) pool[here[r].to + i - r * wide] = v[j];
     }
-    __syncthreads();                           // the lists have been read
   }
 }
 
@@ -450,9 +476,12 @@ int map_cache_evict(const map_cache* c, float* weights, const int32_t* seqs, int
   const long long units = static_cast<long long>(n) * c->layers * c->heads, max_rows = static_cast<long long>(c->max_pages) * c->page;
   // CTAs that look for a unit's rows, and slices that its columns move in: as many as fill the chip where the units do not
   int ranks = 1, slices = 1;
-  while (ranks < 8 && units * ranks < 2 * 152 && max_rows / ranks > 2 * kChunk) ranks *= 2;
+  while (ranks < 8 && units * ranks < 2 * 152 && max_rows / ranks > 2048) ranks *= 2;
   while (slices < 4 && units * slices < 2 * 152 && c->dh / 8 / slices >= 8) slices *= 2;
-  if (e == cudaSuccess) e = launch_cluster(evict_select_kernel, static_cast<unsigned>(units * ranks), kThreads, ranks, st, a);
+  const unsigned select = static_cast<unsigned>(units * ranks);
+  if (e == cudaSuccess)
+    e = max_rows / ranks > kHold * 256 ? launch_cluster(evict_select_kernel<512>, select, 512, ranks, st, a)
+                                       : launch_cluster(evict_select_kernel<256>, select, 256, ranks, st, a);
   if (e == cudaSuccess)
     e = launch_k(evict_move_kernel, dim3(static_cast<unsigned>(units * (2 * slices + 1))), dim3(kMoveThreads), 0, st, a, slices);
   return launch_err(e);
