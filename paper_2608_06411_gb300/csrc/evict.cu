@@ -23,7 +23,7 @@ struct EvictArgs {
   map_cache c;
   float* weights;
   const int32_t *seqs, *first, *last;
-  int n, k;
+  int n, k, page_shift;                    // log2 of the page, -1: no power of two
   Eviction* entries;                       // [n]
   int32_t* was;                            // [n, max_pages]: pages before the call, of the columns that rows move to
   int32_t* taken;                          // [pages]
@@ -324,12 +324,13 @@ __global__ void __launch_bounds__(THREADS) evict_select_kernel(const EvictArgs a
   if (ranks > 1) cluster_sync();               // no CTA leaves while another may read its counts
 }
 
-// The rows that move, a slice of a unit's columns (or its weights) a CTA.
-constexpr int kMoveThreads = 256, kMoveEach = 8;
-constexpr int kMoveRowsEach = 2, kMoveRows = kMoveRowsEach * kMoveThreads;   // of a batch, at most
-__global__ void __launch_bounds__(kMoveThreads, 4) evict_move_kernel(const EvictArgs a, int slices) {
+// The rows that move, a slice of a unit's columns (or its weights) a CTA.  THREADS / wide rows are read together, a 16-byte vector a
+// thread, kMoveEach times before the first is written.
+constexpr int kMoveEach = 8, kMoveRowsEach = 2;
+template <int THREADS>
+__global__ void __launch_bounds__(THREADS, 1024 / THREADS) evict_move_kernel(const EvictArgs a, int slices) {
   struct Row { long long from, to; };          // vectors of a plane; from -1: the row is where it shall be
-  __shared__ Row list[3][kMoveRows];           // batches: being stored, loaded, looked up
+  __shared__ Row list[3][kMoveRowsEach * THREADS];           // batches: being stored, loaded, looked up
   pdl_enter();
   const map_cache& c = a.c;
   const int tid = threadIdx.x, parts = 2 * slices + 1, part = blockIdx.x % parts;
@@ -343,51 +344,53 @@ __global__ void __launch_bounds__(kMoveThreads, 4) evict_move_kernel(const Evict
 
   if (part == parts - 1) {                     // the weights, and zeros behind them
     float* w = weights_of(a, x);
-    constexpr int kBatch = kMoveThreads * kMoveEach;
+    constexpr int kBatch = THREADS * kMoveEach;
     for (int r0 = 0; r0 < a.k + tail; r0 += kBatch) {
       float v[kMoveEach];
 #pragma unroll
       for (int j = 0; j < kMoveEach; ++j) {
-        const int r = r0 + tid + j * kMoveThreads;
+        const int r = r0 + tid + j * THREADS;
         v[j] = r < a.k + tail ? w[source(r)] : 0.f;
       }
       __syncthreads();                         // the batch has been read
 #pragma unroll
       for (int j = 0; j < kMoveEach; ++j) {
-        const int r = r0 + tid + j * kMoveThreads;
+        const int r = r0 + tid + j * THREADS;
         if (r < a.k + tail) w[e.first + r] = v[j];
       }
     }
     __syncthreads();                           // the last rows' sources lie where the zeros go
-    for (int t = e.left + tid; t < e.len; t += kMoveThreads) w[t] = 0.f;
+    for (int t = e.left + tid; t < e.len; t += THREADS) w[t] = 0.f;
     return;
   }
 
   const int vec = c.dh / 8, slice = part % slices, v0 = vec * slice / slices, wide = vec * (slice + 1) / slices - v0;
+  const int together = min(THREADS / wide, kMoveRowsEach * THREADS / kMoveEach), mine = tid / wide;    // rows; this thread's
   const long long plane = static_cast<long long>(c.pages) * c.heads * c.page * vec;
-  uint4* pool = static_cast<uint4*>(c.pool) + (2 * x.layer + part / slices) * plane + v0;
+  uint4* pool = static_cast<uint4*>(c.pool) + (2 * x.layer + part / slices) * plane + v0 + tid % wide;
   const int32_t* row = c.table + static_cast<long long>(e.seq) * c.max_pages;
   const int32_t* was = a.was + x.id / c.heads / c.layers * c.max_pages;
   const int moved_to = pieces_of(e.left, c.page);
+  const auto page_of = [&](int t) { return a.page_shift >= 0 ? t >> a.page_shift : t / c.page; };
   const auto place = [&](int page, int in_page) { return ((static_cast<long long>(page) * c.heads + x.head) * c.page + in_page) * vec; };
   // rows before e.first in its page move too, where the page is replaced
-  const int head = e.first % c.page, rows = head + a.k + tail, batch = min(kMoveRows, kMoveThreads * kMoveEach / wide);
+  const int head = e.first - page_of(e.first) * c.page, rows = head + a.k + tail, batch = together * kMoveEach;
   int src[kMoveRowsEach];                      // of the batch to be looked up next
   const auto sources = [&](int r0, int n) {
 #pragma unroll
     for (int k = 0; k < kMoveRowsEach; ++k) {
-      const int i = tid + k * kMoveThreads;
+      const int i = tid + k * THREADS;
       src[k] = i < min(batch, n) ? (r0 + i < head ? e.first + r0 + i - head : source(r0 + i - head)) : -1;
     }
   };
   const auto look_up = [&](int r0, Row* to) {
 #pragma unroll
     for (int k = 0; k < kMoveRowsEach; ++k) {
-      const int s = src[k], t = e.first + r0 + tid + k * kMoveThreads - head;
+      const int s = src[k], t = e.first + r0 + tid + k * THREADS - head;
       if (s < 0) continue;
-      const int cf = s / c.page, ct = t / c.page;
+      const int cf = page_of(s), ct = page_of(t);
       const int old = cf < moved_to ? __ldcg(was + cf) & ~kReplaced : __ldcg(row + cf), now = __ldcg(row + ct);
-      to[tid + k * kMoveThreads] = Row{s == t && old == now ? -1 : place(old, s - cf * c.page), place(now, t - ct * c.page)};
+      to[tid + k * THREADS] = Row{s == t && old == now ? -1 : place(old, s - cf * c.page), place(now, t - ct * c.page)};
     }
   };
   sources(0, rows);
@@ -396,23 +399,19 @@ __global__ void __launch_bounds__(kMoveThreads, 4) evict_move_kernel(const Evict
   __syncthreads();
   int at = 0;
   for (int r0 = 0, n = rows; n > 0; r0 += batch, n -= batch) {
-    const Row* here = list[at];
+    const Row* here = list[at] + mine;
     at = at == 2 ? 0 : at + 1;
-    const int vecs = min(batch, n) * wide;
+    const int here_n = mine < together ? min(batch, n) - mine : 0;       // this thread's rows: 0, together, ... below it
     uint4 v[kMoveEach];
 #pragma unroll
-    for (int j = 0; j < kMoveEach; ++j) {
-      const int i = tid + j * kMoveThreads, r = i / wide;
-      if (i < vecs && here[r].from >= 0) v[j] = pool[here[r].from + i - r * wide];
-    }
+    for (int j = 0; j < kMoveEach; ++j)
+      if (j * together < here_n && here[j * together].from >= 0) v[j] = pool[here[j * together].from];
     look_up(r0 + batch, list[at]);
     sources(r0 + 2 * batch, n - 2 * batch);    // (past 2^31 only where there is none)
     __syncthreads();                           // the batch has been read, the next one looked up
 #pragma unroll
-    for (int j = 0; j < kMoveEach; ++j) {
-      const int i = tid + j * kMoveThreads, r = i / wide;
-      if (i < vecs && here[r].from >= 0) pool[here[r].to + i - r * wide] = v[j];
-    }
+    for (int j = 0; j < kMoveEach; ++j)
+      if (j * together < here_n && here[j * together].from >= 0) pool[here[j * together].to] = v[j];
   }
 }
 
@@ -467,7 +466,8 @@ int map_cache_evict(const map_cache* c, float* weights, const int32_t* seqs, int
   if (!seqs || !weights || (reinterpret_cast<uintptr_t>(weights) & 3) || !ws || !aligned16(ws)) return MAP_EINVAL;
   const EvictSpace s = evict_space(c, n, k);
   char* p = static_cast<char*>(ws);
-  const EvictArgs a{*c, weights, seqs, first, last, n, k, reinterpret_cast<Eviction*>(p),
+  const int shift = (c->page & (c->page - 1)) == 0 ? __builtin_ctz(c->page) : -1;
+  const EvictArgs a{*c, weights, seqs, first, last, n, k, shift, reinterpret_cast<Eviction*>(p),
                     reinterpret_cast<int32_t*>(p + s.was), reinterpret_cast<int32_t*>(p + s.taken), reinterpret_cast<int32_t*>(p + s.kept)};
   const size_t smem = plan_smem(n, c->seqs);
   cudaStream_t st = static_cast<cudaStream_t>(stream);
@@ -482,8 +482,10 @@ int map_cache_evict(const map_cache* c, float* weights, const int32_t* seqs, int
   if (e == cudaSuccess)
     e = max_rows / ranks > kHold * 256 ? launch_cluster(evict_select_kernel<512>, select, 512, ranks, st, a)
                                        : launch_cluster(evict_select_kernel<256>, select, 256, ranks, st, a);
+  const unsigned move = static_cast<unsigned>(units * (2 * slices + 1));
   if (e == cudaSuccess)
-    e = launch_k(evict_move_kernel, dim3(static_cast<unsigned>(units * (2 * slices + 1))), dim3(kMoveThreads), 0, st, a, slices);
+    e = move <= 2 * 152 ? launch_k(evict_move_kernel<512>, dim3(move), dim3(512), 0, st, a, slices)
+                        : launch_k(evict_move_kernel<256>, dim3(move), dim3(256), 0, st, a, slices);
   return launch_err(e);
 }
 
