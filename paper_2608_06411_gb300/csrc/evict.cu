@@ -152,13 +152,15 @@ __device__ __forceinline__ int cluster_size() {
   return n;
 }
 
-struct Unit { Eviction e; int layer, head; long long id; };
-__device__ __forceinline__ Unit unit_of(const EvictArgs& a, long long u) {
+struct Unit { Eviction e; int entry, layer, head; long long id; };
+__device__ __forceinline__ Unit unit_of(const EvictArgs& a, unsigned u) {       // (entry, layer, head)
+  const unsigned heads = a.c.heads, layers = a.c.layers, r = u / heads;
   Unit x;
   x.id = u;
-  x.head = static_cast<int>(u % a.c.heads);
-  x.layer = static_cast<int>(u / a.c.heads % a.c.layers);
-  const int4 e = __ldcg(reinterpret_cast<const int4*>(a.entries + u / a.c.heads / a.c.layers));
+  x.head = u - r * heads;
+  x.entry = r / layers;
+  x.layer = r - x.entry * layers;
+  const int4 e = __ldcg(reinterpret_cast<const int4*>(a.entries + x.entry));
   x.e = Eviction{e.x, e.y, e.z, e.w};
   return x;
 }
@@ -169,7 +171,7 @@ __device__ __forceinline__ float* weights_of(const EvictArgs& a, const Unit& x) 
 // The rows that stay, in order, into kept [units][k]: a cluster a unit, an equal run of the candidates a CTA, of which a warp holds
 // kHold times 32 in a row.  Runs of up to kHold * THREADS are read once.
 template <int THREADS>
-__global__ void __launch_bounds__(THREADS) evict_select_kernel(const EvictArgs a) {
+__global__ void __launch_bounds__(THREADS, 1280 / THREADS) evict_select_kernel(const EvictArgs a) {
   constexpr int kWarps = THREADS / 32, kBinsEach = kBins / THREADS, kChunk = kHold * THREADS;
   __shared__ __align__(16) int hist[2][kBins];
   __shared__ int warp_sum[kWarps];
@@ -197,7 +199,7 @@ __global__ void __launch_bounds__(THREADS) evict_select_kernel(const EvictArgs a
   const bool once = t1 - t0 <= kChunk;
   load(t0);
 
-  for (int b = tid; b < kBins; b += THREADS) hist[0][b] = 0;
+  for (int b = tid; b < kBins / 4; b += THREADS) reinterpret_cast<int4*>(hist[0])[b] = make_int4(0, 0, 0, 0);
   if (tid == 0) mine = make_int4(0, 0, 0, 0);
   __syncthreads();
   // a digit a pass, of the keys with the digits found so far
@@ -215,23 +217,29 @@ __global__ void __launch_bounds__(THREADS) evict_select_kernel(const EvictArgs a
     }
     all_here();
     // (the others have read the last pass's counts: they are here)
-    for (int b = tid; b < kBins; b += THREADS) hist[pass ^ 1][b] = 0;
+    for (int b = tid; b < kBins / 4; b += THREADS) reinterpret_cast<int4*>(hist[pass ^ 1])[b] = make_int4(0, 0, 0, 0);
     // from the greatest digit on: a thread counts kBinsEach, over all of the cluster's CTAs
     const int bin0 = kBins - (tid + 1) * kBinsEach;
-    int count[kBinsEach] = {}, own[kBinsEach];
-#pragma unroll 8
-    for (int r = 0; r < ranks; ++r) {
+    int count[kBinsEach], own[kBinsEach];
+#pragma unroll
+    for (int b = 0; b < kBinsEach; b += 4) {
+      const int4 v = *reinterpret_cast<const int4*>(&hist[pass][bin0 + b]);
+      count[b] = own[b] = v.x;
+      count[b + 1] = own[b + 1] = v.y;
+      count[b + 2] = own[b + 2] = v.z;
+      count[b + 3] = own[b + 3] = v.w;
+    }
+#pragma unroll 7
+    for (int r = 1; r < ranks; ++r) {
 #pragma unroll
       for (int b = 0; b < kBinsEach; b += 4) {
-        const int4 v = ranks > 1 ? ld_peer(mapa_u32(&hist[pass][bin0 + b], r)) : *reinterpret_cast<const int4*>(&hist[pass][bin0 + b]);
+        const int4 v = ld_peer(mapa_u32(&hist[pass][bin0 + b], rank + r < ranks ? rank + r : rank + r - ranks));
         count[b] += v.x;
         count[b + 1] += v.y;
         count[b + 2] += v.z;
         count[b + 3] += v.w;
       }
     }
-#pragma unroll
-    for (int b = 0; b < kBinsEach; ++b) own[b] = hist[pass][bin0 + b];
     int sum = 0;
 #pragma unroll
     for (int b = 0; b < kBinsEach; ++b) sum += count[b];
@@ -258,17 +266,18 @@ __global__ void __launch_bounds__(THREADS) evict_select_kernel(const EvictArgs a
       }
     }
     __syncthreads();
-    const int pick = static_cast<int>(pick_bin);
-    const bool done = pick_size == pick_want || down == 0;
-    int greater = 0, equal = 0;
+    if (ranks > 1) {                           // for the CTAs behind this one
+      const int pick = static_cast<int>(pick_bin);
+      int greater = 0, equal = 0;
 #pragma unroll
-    for (int b = 0; b < kBinsEach; ++b) {
-      greater += bin0 + b > pick ? own[b] : 0;
-      equal += bin0 + b == pick ? own[b] : 0;
+      for (int b = 0; b < kBinsEach; ++b) {
+        greater += bin0 + b > pick ? own[b] : 0;
+        equal += bin0 + b == pick ? own[b] : 0;
+      }
+      greater = __reduce_add_sync(0xffffffffu, greater);
+      if (lane == 0 && greater) atomicAdd(&mine.x, greater);
+      if (equal && (pick_size == pick_want || down == 0)) mine.y = equal;
     }
-    greater = __reduce_add_sync(0xffffffffu, greater);
-    if (lane == 0 && greater) atomicAdd(&mine.x, greater);
-    if (equal && done) mine.y = equal;
     prefix = shift == 32 ? pick_bin : prefix << bits | pick_bin;
     want = pick_want;
     shift = down;
@@ -292,9 +301,11 @@ __global__ void __launch_bounds__(THREADS) evict_select_kernel(const EvictArgs a
     int2 n = make_int2(0, 0);
 #pragma unroll
     for (int j = 0; j < kHold; ++j) {
-      n.x += __popc(__ballot_sync(0xffffffffu, key[j] > most));
-      n.y += __popc(__ballot_sync(0xffffffffu, key[j] >= least && key[j] <= most));
+      n.x += key[j] > most;
+      n.y += key[j] >= least;
     }
+    n.x = __reduce_add_sync(0xffffffffu, n.x);
+    n.y = __reduce_add_sync(0xffffffffu, n.y) - n.x;
     __syncthreads();                           // the last chunk's have been read
     if (lane == 0) warp_kept[warp] = n;
     __syncthreads();
@@ -369,7 +380,7 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) evict_move_kernel(con
   const long long plane = static_cast<long long>(c.pages) * c.heads * c.page * vec;
   uint4* pool = static_cast<uint4*>(c.pool) + (2 * x.layer + part / slices) * plane + v0 + tid % wide;
   const int32_t* row = c.table + static_cast<long long>(e.seq) * c.max_pages;
-  const int32_t* was = a.was + x.id / c.heads / c.layers * c.max_pages;
+  const int32_t* was = a.was + static_cast<long long>(x.entry) * c.max_pages;
   const int moved_to = pieces_of(e.left, c.page);
   const auto page_of = [&](int t) { return a.page_shift >= 0 ? t >> a.page_shift : t / c.page; };
   const auto place = [&](int page, int in_page) { return ((static_cast<long long>(page) * c.heads + x.head) * c.page + in_page) * vec; };
