@@ -28,15 +28,17 @@ struct SharedArgs {
   float* parts;                                // [grid][2] parts of items that several CTAs share
   float2* whole_stats;                         // the others': (m, l) [n][q.heads]
   float* whole;                                //         o [n][q.heads][dh]
-  int grid;                                    // of shared_kernel
+  int grid, m;                                 // of shared_kernel: its CTAs, query rows of an item
 };
 
-constexpr int kPlan = 512;
+constexpr int kPlan = 1024, kPlanEach = 8;
 
-// What a group shares: the pages that all its sequences with rows hold in front, as far as all are full.
+// What a group shares: the pages that all its sequences with rows hold in front, as far as all are full.  A CTA a group, latency:
+// a group's sequences are looked up together, then the pages of all of them.
 __global__ void __launch_bounds__(kPlan) shared_plan_kernel(const __grid_constant__ SharedArgs p) {
   const AttendArgs& a = p.a;
   __shared__ int least, lead, valid;
+  __shared__ int seq[kPlan];                   // of kPlan members; -1: without rows
   pdl_enter();
   const int g = blockIdx.x, tid = threadIdx.x;
   if (tid == 0) {
@@ -59,56 +61,83 @@ __global__ void __launch_bounds__(kPlan) shared_plan_kernel(const __grid_constan
     return;
   }
   const int first = __ldg(p.starts + g), last = __ldg(p.starts + g + 1);
-  int mine = 0;
+  int mine = 0, from = a.n, pages = a.c.max_pages;
   for (int i = first + tid; i < last; i += kPlan) {
     const int len = seq_len(a, i);
     if (len == 0) continue;
     ++mine;
-    atomicMin(&lead, i);
-    atomicMin(&least, len / a.c.page);
+    from = min(from, i);
+    pages = min(pages, len / a.c.page);
   }
-  if (mine) atomicAdd(&valid, mine);
+  mine = __reduce_add_sync(0xffffffffu, mine);
+  from = __reduce_min_sync(0xffffffffu, from);
+  pages = __reduce_min_sync(0xffffffffu, pages);
+  if (tid % 32 == 0 && mine) {
+    atomicAdd(&valid, mine);
+    atomicMin(&lead, from);
+    atomicMin(&least, pages);
+  }
   __syncthreads();
   const int of = lead, full = valid > 1 ? least : 0;
-  __syncthreads();
+  const int lead_seq = full > 0 ? __ldg(a.seqs + of) : 0;
   int same = full;
   if (full > 0) {
-    const int32_t* row = a.c.table + static_cast<long long>(__ldg(a.seqs + of)) * a.c.max_pages;
-    for (int i = first + tid / 32; i < last; i += kPlan / 32) {          // a warp a member
-      if (seq_len(a, i) == 0) continue;
-      const int32_t* other = a.c.table + static_cast<long long>(__ldg(a.seqs + i)) * a.c.max_pages;
-#pragma unroll 8
-      for (int j = tid % 32; j < full; j += 32)
-        if (__ldg(other + j) != __ldg(row + j)) same = min(same, j);
+    const int32_t* row = a.c.table + static_cast<long long>(lead_seq) * a.c.max_pages;
+    for (int i0 = first; i0 < last; i0 += kPlan) {
+      __syncthreads();
+      const int i = i0 + tid, count = min(kPlan, last - i0);
+      if (i < last) seq[tid] = seq_len(a, i) > 0 ? __ldg(a.seqs + i) : -1;
+      __syncthreads();
+      const long long all = static_cast<long long>(count) * full;
+      for (long long x0 = tid; x0 < all; x0 += kPlan * kPlanEach) {
+        int j[kPlanEach], page[kPlanEach], other[kPlanEach];
+#pragma unroll
+        for (int k = 0; k < kPlanEach; ++k) {
+          const long long x = x0 + k * kPlan;
+          const int m = x < all ? (all < (1ll << 31) ? static_cast<int>(x) / full : static_cast<int>(x / full)) : 0;
+          const int s = x < all ? seq[m] : -1;
+          j[k] = static_cast<int>(x - static_cast<long long>(m) * full);
+          page[k] = other[k] = 0;
+          if (s >= 0) {
+            page[k] = __ldg(a.c.table + static_cast<long long>(s) * a.c.max_pages + j[k]);
+            other[k] = __ldg(row + j[k]);
+          }
+        }
+#pragma unroll
+        for (int k = 0; k < kPlanEach; ++k)
+          if (page[k] != other[k]) same = min(same, j[k]);
+      }
     }
-    atomicMin(&least, same);
+    same = __reduce_min_sync(0xffffffffu, same);
+    if (tid % 32 == 0) atomicMin(&least, same);
   }
   __syncthreads();
   const int rows = full > 0 ? least * a.c.page : 0;
   for (int i = first + tid; i < last; i += kPlan) {
     p.of[i] = g;
-    p.skip[i] = seq_len(a, i) > 0 ? rows : 0;
+    p.skip[i] = rows > 0 && seq_len(a, i) > 0 ? rows : 0;
   }
-  if (tid == 0) p.group[g] = Group{first, last - first, rows, rows > 0 ? __ldg(a.seqs + of) : 0};
+  if (tid == 0) p.group[g] = Group{first, last - first, rows, lead_seq};
 }
 
-// ---- the shared rows.  An item is up to 128 rows of queries (member, head) of one key head and group: the M of a
+// ---- the shared rows.  An item is up to M = 128 MT rows of queries (member, head) of one key head and group, 128 the M of a
 // tcgen05.mma.  64 keys are the N of the scores' product and the K of the values', whose first operand, the weights as two halves
-// of T, lies in TMEM.  Warps 0-3 do the softmax, a row a thread; 4 and 5 load keys, 6 and 7 values, each with a ring of its own;
-// a thread of warp 8 issues the products: scores of a tile while the last one's weights are made.
+// of T, lies in TMEM.  Four warps for each 128 rows do the softmax, a row a thread; a warp loads keys and one values, each with a
+// ring of its own; a thread of a third issues the products: scores of a tile while the last one's weights are made.
 constexpr int kM = 128, kN = 64;
-constexpr int kSharedThreads = 288, kKeyRing = 3, kValueRing = 2;
 
-template <int DH>
+template <int DH, int MT>
 struct Shape {
+  static constexpr int kThreads = 128 * MT + 128;
   static constexpr int kBlocks = (DH + 63) / 64;             // boxes of 64 columns, 128 bytes a row, 16-byte units exchanged by the row's low bits
-  static constexpr int kTileBytes = kBlocks * kN * 128, kQBytes = kBlocks * kM * 128;
+  static constexpr int kTileBytes = kBlocks * kN * 128, kQBytes = kBlocks * MT * kM * 128;
+  static constexpr int kCtas = MT == 1 && DH <= 128 ? 2 : 1;
+  static constexpr int kRing = (227 * 1024 / kCtas - 1536 - kQBytes) / kTileBytes;           // tiles that fit
+  static constexpr int kKeyRing = kRing >= 8 ? 4 : (kRing + 1) / 2, kValueRing = kRing >= 8 ? 4 : kRing / 2;
   static constexpr int kTiles = kQBytes + (kKeyRing + kValueRing) * kTileBytes, kSmem = kTiles + 512;    // the barriers behind the tiles
-  static constexpr int kCtas = DH <= 128 ? 2 : 1;
-  static constexpr int kHi = kN, kLo = kN + kN / 2, kO = 2 * kN;       // TMEM columns: scores at 0
+  static constexpr int kHi = kN, kLo = kN + kN / 2, kO = 2 * kN;       // TMEM columns of 128 rows: scores at 0
   static constexpr int kCols = kO + DH <= 256 ? 256 : 512;
-  static constexpr int kPart = kM * (DH + 2);                // floats: m [128], l [128], o [DH / 4][128] float4
-  static_assert(kCtas * kCols <= 512 && kCtas * (kSmem + 1024) <= 228 * 1024, "TMEM and shared memory");
+  static_assert(kKeyRing <= 4 && kValueRing >= 2 && kCtas * (kSmem + 1024) <= 228 * 1024 && kCtas * MT * kCols <= 512, "an SM");
 };
 
 constexpr uint32_t kBf16Types = (1u << 7) | (1u << 10);      // of an instruction descriptor: A and B
@@ -126,6 +155,62 @@ __device__ __forceinline__ void umma_ts(uint32_t d, uint32_t a, uint64_t b, uint
       : "memory");
 }
 
+// 64 columns of the warp's 32 TMEM lanes; eight columns, completed by tmem_wait_st.
+__device__ __forceinline__ void tmem_ld64(uint32_t at, uint32_t (&r)[64]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x64.b32 "
+      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32, %33, %34, %35, %36, %37, %38, %39, %40, %41, %42, %43, %44, %45, %46, %47, %48, %49, %50, %51, %52, %53, %54, %55, %56, %57, %58, %59, %60, %61, %62, %63}, [%64];\n\t"
+      "tcgen05.wait::ld.sync.aligned;"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31]), "=r"(r[32]), "=r"(r[33]), "=r"(r[34]), "=r"(r[35]), "=r"(r[36]), "=r"(r[37]), "=r"(r[38]), "=r"(r[39]), "=r"(r[40]), "=r"(r[41]), "=r"(r[42]), "=r"(r[43]), "=r"(r[44]), "=r"(r[45]), "=r"(r[46]), "=r"(r[47]), "=r"(r[48]), "=r"(r[49]), "=r"(r[50]), "=r"(r[51]), "=r"(r[52]), "=r"(r[53]), "=r"(r[54]), "=r"(r[55]), "=r"(r[56]), "=r"(r[57]), "=r"(r[58]), "=r"(r[59]), "=r"(r[60]), "=r"(r[61]), "=r"(r[62]), "=r"(r[63])
+      : "r"(at)
+      : "memory");
+}
+__device__ __forceinline__ void tmem_st8(uint32_t at, const uint32_t (&r)[8]) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"r"(at), "r"(r[0]), "r"(r[1]),
+               "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]) : "memory");
+}
+__device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+
+// Two fp32 at once: half the instructions.
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+  float2 d;
+  asm("{\n\t.reg .b64 x, y, z;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\tmov.b64 z, {%6, %7};\n\t"
+      "fma.rn.f32x2 x, x, y, z;\n\tmov.b64 {%0, %1}, x;\n\t}"
+      : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+  return d;
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+  float2 d;
+  asm("{\n\t.reg .b64 x, y;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\t"
+      "add.rn.f32x2 x, x, y;\n\tmov.b64 {%0, %1}, x;\n\t}"
+      : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  return d;
+}
+
+// Weights as two halves like split_weights, with fewer instructions: every half is raised to its type's smallest number, not only
+// those of weights above zero.  (A weight of zero is a score of minus infinity, or a row past the last, whose value is 0 here.)
+// Weights are 2^lift times what they are to the row's base, which the largest score passes by kSlack at most: sums are scaled
+// only then, not whenever a tile has a greater score.  What is raised adds 2^-24 / 2^lift of the base's weight (f16: 2^-35).
+template <typename T> constexpr float kSlack = 8.f;
+template <> constexpr float kSlack<__half> = 4.f;
+template <typename T> constexpr float kLiftShared = 0.f;
+template <> constexpr float kLiftShared<__half> = 11.f;      // 2^(11 + 4) is below f16's largest
+__device__ __forceinline__ void halves(float2 x, uint32_t& hi, uint32_t& lo, __nv_bfloat16) {
+  const uint32_t a = __float_as_uint(x.x), b = __float_as_uint(x.y);
+  hi = __byte_perm(a, b, 0x7632);
+  const float2 rest = fma2(make_float2(__uint_as_float(a & 0xffff0000u), __uint_as_float(b & 0xffff0000u)), make_float2(-1.f, -1.f), x);
+  const __nv_bfloat162 r = __hmax2(__floats2bfloat162_rn(rest.x, rest.y), __float2bfloat162_rn(0x1p-126f));
+  lo = *reinterpret_cast<const uint32_t*>(&r);
+}
+__device__ __forceinline__ void halves(float2 x, uint32_t& hi, uint32_t& lo, __half) {
+  asm("cvt.rz.f16x2.f32 %0, %1, %2;" : "=r"(hi) : "f"(x.y), "f"(x.x));
+  const __half2 least = __float2half2_rn(0x1p-24f), h = __hmax2_nan(*reinterpret_cast<const __half2*>(&hi), least);
+  const float2 rest = fma2(__half22float2(h), make_float2(-1.f, -1.f), x);
+  const __half2 r = __hmax2(__floats2half2_rn(rest.x, rest.y), least);
+  hi = *reinterpret_cast<const uint32_t*>(&h);
+  lo = *reinterpret_cast<const uint32_t*>(&r);
+}
+
 // Where a run of the list (group, key head, rows of queries, tile) is.
 struct SharedPlace {
   Group gr;
@@ -141,7 +226,9 @@ struct SharedPlace {
     tiles = pieces_of(gr.rows, kN);
     items = p.a.c.heads * blocks(p);
   }
-  __device__ __forceinline__ int blocks(const SharedArgs& p) const { return (gr.count * p.a.group + kM - 1) / kM; }
+  __device__ __forceinline__ int blocks(const SharedArgs& p) const { return (gr.count * p.a.group + p.m - 1) / p.m; }
+  // query rows of the item
+  __device__ __forceinline__ int have(const SharedArgs& p) const { return min(p.m, gr.count * p.a.group - item % blocks(p) * p.m); }
   __device__ __forceinline__ bool next(const SharedArgs& p) {          // whether another item begins
     if (++t < tiles) return false;
     t = 0;
@@ -153,21 +240,23 @@ struct SharedPlace {
 };
 
 struct SharedBars {
-  uint64_t k_full[kKeyRing], k_empty[kKeyRing], v_full[kValueRing], v_empty[kValueRing], q_full, s_full, s_free, p_full, o_done, drain;
+  uint64_t k_full[4], k_empty[4], v_full[4], v_empty[4], q_full[2], s_full[2], s_free[2], p_full[2], o_done[2], drain;
   uint32_t tmem;
   int abort, group;
   long long tile;
-  long long red[kSharedThreads / 32];
+  long long red[12];
 };
 static_assert(sizeof(SharedBars) <= 512, "behind the tiles");
 
-template <typename T, int DH>
-__global__ void __launch_bounds__(kSharedThreads, Shape<DH>::kCtas) shared_kernel(const __grid_constant__ SharedArgs p) {
-  using S = Shape<DH>;
-  constexpr int VPR = DH / 8;
+template <typename T, int DH, int MT>
+__global__ void __launch_bounds__(Shape<DH, MT>::kThreads, Shape<DH, MT>::kCtas) shared_kernel(const __grid_constant__ SharedArgs p) {
+  using S = Shape<DH, MT>;
+  constexpr int VPR = DH / 8, kWarpsAll = S::kThreads / 32, kKeys = 4 * MT, kValues = kKeys + 1, kProducts = kKeys + 2;
   extern __shared__ __align__(1024) unsigned char sh[];
   SharedBars& b = *reinterpret_cast<SharedBars*>(sh + S::kTiles);
-  pdl_enter();
+  // The kernel launched before this one attends the sequences' own rows: it has waited for the plan, and so has this one when it
+  // starts.  Nothing of it is needed here; the wait at the end makes it end before the join begins.
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   const AttendArgs& a = p.a;
   const int tid = threadIdx.x, lane = tid & 31, warp = __shfl_sync(0xffffffffu, tid >> 5, 0);
 
@@ -178,10 +267,10 @@ __global__ void __launch_bounds__(kSharedThreads, Shape<DH>::kCtas) shared_kerne
     x.gr = Group{v.x, v.y, v.z, v.w};
     return x.gr.rows > 0 ? static_cast<long long>(pieces_of(x.gr.rows, kN)) * a.c.heads * x.blocks(p) : 0;
   };
-  const int each = (p.groups + kSharedThreads - 1) / kSharedThreads, g0 = min(p.groups, tid * each), g1 = min(p.groups, g0 + each);
+  const int each = (p.groups + S::kThreads - 1) / S::kThreads, g0 = min(p.groups, tid * each), g1 = min(p.groups, g0 + each);
   long long mine = 0, total;
   for (int g = g0; g < g1; ++g) mine += tiles_of(g);
-  long long at0 = block_prefix<kSharedThreads / 32>(mine, b.red, &total);
+  long long at0 = block_prefix<kWarpsAll>(mine, b.red, &total);
   const long long per = (total + gridDim.x - 1) / gridDim.x, t0 = per * blockIdx.x;
   if (blockIdx.x == 0) {
     long long at = at0;
@@ -191,9 +280,9 @@ __global__ void __launch_bounds__(kSharedThreads, Shape<DH>::kCtas) shared_kerne
     }
     if (tid == 0) p.tile0[p.groups] = total;
   }
-  if (t0 >= total) return;
-  if (smem_u32(sh) & 1023) {                   // (never: the alignment that its declaration asks for)
-    if (tid == 0) atomicOr(a.c.status, ST_INTERNAL);
+  if (t0 >= total || (smem_u32(sh) & 1023) != 0) {           // (the alignment is what its declaration asks for)
+    if (t0 < total && tid == 0) atomicOr(a.c.status, ST_INTERNAL);
+    asm volatile("griddepcontrol.wait;" ::: "memory");
     return;
   }
   const int run = static_cast<int>(t0 + per <= total ? per : total - t0);
@@ -209,32 +298,32 @@ __global__ void __launch_bounds__(kSharedThreads, Shape<DH>::kCtas) shared_kerne
     }
   }
   if (tid == 0) {
-    for (int i = 0; i < kKeyRing; ++i) {
-      mbar_init(&b.k_full[i], 64);
+    for (int i = 0; i < 4; ++i) {
+      mbar_init(&b.k_full[i], 32);
       mbar_init(&b.k_empty[i], 1);
-    }
-    for (int i = 0; i < kValueRing; ++i) {
-      mbar_init(&b.v_full[i], 64);
+      mbar_init(&b.v_full[i], 32);
       mbar_init(&b.v_empty[i], 1);
     }
-    mbar_init(&b.q_full, 128);
-    mbar_init(&b.s_full, 1);
-    mbar_init(&b.s_free, 4);
-    mbar_init(&b.p_full, 4);
-    mbar_init(&b.o_done, 1);
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(&b.q_full[i], 128);
+      mbar_init(&b.s_full[i], 1);
+      mbar_init(&b.s_free[i], 4);
+      mbar_init(&b.p_full[i], 4);
+      mbar_init(&b.o_done[i], 1);
+    }
     mbar_init(&b.drain, 1);
     b.abort = 0;
     fence_mbar_init();
   }
-  if (warp == 8) {
-    tmem_alloc(&b.tmem, S::kCols);
+  if (warp == kProducts) {
+    tmem_alloc(&b.tmem, MT * S::kCols);
     tmem_relinquish();
   }
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = b.tmem;
-  const uint32_t base = smem_u32(sh), keys = base + S::kQBytes, values = keys + kKeyRing * S::kTileBytes;
+  const uint32_t base = smem_u32(sh), keys = base + S::kQBytes, values = keys + S::kKeyRing * S::kTileBytes;
   volatile int* stop = &b.abort;
   const auto wait = [&](uint64_t* bar, uint32_t parity) { return mbar_wait(bar, parity & 1, a.c.status, stop); };
 
@@ -243,161 +332,199 @@ __global__ void __launch_bounds__(kSharedThreads, Shape<DH>::kCtas) shared_kerne
   pl.item = static_cast<int>(b.tile / pl.tiles);
   pl.t = static_cast<int>(b.tile % pl.tiles);
 
-  if (warp < 4) {
+  if (warp < 4 * MT) {
     // ---- softmax: row `tid` of the item's queries
-    const uint32_t mine_at = tmem + (static_cast<uint32_t>(warp * 32) << 16);
-    const float lift = kLift<T>;
+    const int mt = MT > 1 ? warp >> 2 : 0;
+    const uint32_t mine_at = tmem + mt * S::kCols + (static_cast<uint32_t>((warp & 3) * 32) << 16);
     float m = -INFINITY, l = 0.f;
     bool begins = true, from_start = pl.t == 0;
     int have = 0, q0 = 0, kh = 0;
+    uint32_t count = 0;                        // tiles of these 128 rows so far
     for (int n = 0; n < run; ++n) {
       if (begins) {
         const int mb = pl.blocks(p);
         kh = pl.item / mb;
-        q0 = pl.item % mb * kM;                // of the group's rows (member, head)
-        have = min(kM, pl.gr.count * a.group - q0);
-        // (the last item's scores are done with the queries)
-        const T* q = static_cast<const T*>(a.q.p) + kh * a.group * a.q.head;
-        for (int e = tid; e < kM * VPR; e += 128) {
-          const int r = e / VPR, x = e % VPR, i = (q0 + r) / a.group, h = (q0 + r) % a.group;
-          const bool on = r < have;
-          cp_async16_or_zero(base + (x >> 3) * (kM * 128) + r * 128 + (((x & 7) ^ (r & 7)) << 4),
-                             q + (on ? static_cast<long long>(pl.gr.first + i) * a.q.row + h * a.q.head : 0) + x * 8, on);
+        q0 = pl.item % mb * p.m;               // of the group's rows (member, head)
+        have = pl.have(p);
+        if (mt * kM < have) {                  // (these rows' last scores are done with the queries)
+          const T* q = static_cast<const T*>(a.q.p) + kh * a.group * a.q.head;
+          for (int e = tid & 127; e < kM * VPR; e += 128) {
+            const int r = mt * kM + e / VPR, x = e % VPR, i = (q0 + r) / a.group, h = (q0 + r) % a.group;
+            const bool on = r < have;
+            cp_async16_or_zero(base + mt * (S::kQBytes / MT) + (x >> 3) * (kM * 128) + (r % kM) * 128 + (((x & 7) ^ (r & 7)) << 4),
+                               q + (on ? static_cast<long long>(pl.gr.first + i) * a.q.row + h * a.q.head : 0) + x * 8, on);
+          }
+          cp_async_commit();
+          cp_async_wait_group<0>();
+          fence_proxy_async_smem();
+          mbar_arrive(&b.q_full[mt]);
         }
-        cp_async_commit();
-        cp_async_wait_group<0>();
-        fence_proxy_async_smem();
-        mbar_arrive(&b.q_full);
         m = -INFINITY;
         l = 0.f;
       }
-      if (!wait(&b.s_full, n)) break;
-      tc_fence_after();
-      const bool busy = warp * 32 < have;      // rows of this warp hold queries
-      uint32_t z[kN];
-      if (busy) {
-        tmem_ld32(mine_at, *reinterpret_cast<uint32_t(*)[32]>(z));
-        tmem_ld32(mine_at + 32, *reinterpret_cast<uint32_t(*)[32]>(z + 32));
-      }
-      tc_fence_before();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(&b.s_free);
-      float f = 1.f;
-      if (busy) {
-        const int valid = pl.gr.rows - pl.t * kN;
-        float top = m;
-#pragma unroll
-        for (int j = 0; j < kN; ++j) {
-          float x = __uint_as_float(z[j]) * a.scale2;
-          if (valid < kN && j >= valid) x = -INFINITY;
-          z[j] = __float_as_uint(x);
-          top = fmaxf(top, x);
-        }
-        const float at = top == -INFINITY ? 0.f : top;
-        f = exp2_fast(m - at);
-        m = top;
-        float sum = 0.f;
-#pragma unroll
-        for (int j = 0; j < kN; j += 2) {
-          const float x = exp2_fast(__uint_as_float(z[j]) - (at - lift)), y = exp2_fast(__uint_as_float(z[j + 1]) - (at - lift));
-          sum += x + y;
-          split_weights(x, y, z[j], z[j + 1], T());
-        }
-        l = l * f + sum;
-      }
-      // the last tile's product is done: its sums can be scaled, its weights overwritten
-      if (n > 0 && !wait(&b.o_done, n - 1)) break;
-      tc_fence_after();
-      if (busy) {
-        if (!begins && __any_sync(0xffffffffu, f != 1.f)) {
-#pragma unroll 1
-          for (int x = 0; x < DH; x += 16) {
-            uint32_t o[16];
-            tmem_ld16(mine_at + S::kO + x, o);
-#pragma unroll
-            for (int j = 0; j < 16; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * f);
-            tmem_st16(mine_at + S::kO + x, o);
-          }
-        }
-        uint32_t w[32];
-#pragma unroll
-        for (int j = 0; j < 32; ++j) w[j] = z[2 * j];
-        tmem_st32(mine_at + S::kHi, w);
-#pragma unroll
-        for (int j = 0; j < 32; ++j) w[j] = z[2 * j + 1];
-        tmem_st32(mine_at + S::kLo, w);
-      }
-      tc_fence_before();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(&b.p_full);
-
-      const bool ends = pl.t + 1 == pl.tiles;
-      if (ends || n + 1 == run) {
-        if (!wait(&b.o_done, n)) break;
+      if (mt * kM < have) {
+        const bool busy = warp * 32 < have;    // rows of this warp hold queries
+        if (!wait(&b.s_full[mt], count)) break;
         tc_fence_after();
-        const bool done = ends && from_start, on = tid < have;
-        const int i = pl.gr.first + (q0 + tid) / a.group, head = kh * a.group + (q0 + tid) % a.group;
-        const long long at = static_cast<long long>(i) * a.q.heads + head;
-        float* part = p.parts + static_cast<long long>(2 * blockIdx.x + (from_start ? 1 : 0)) * S::kPart;
+        uint32_t z[kN];
+        if (busy) tmem_ld64(mine_at, z);
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&b.s_free[mt]);
+        float f = 1.f;
+        bool grows = false;
         if (busy) {
-#pragma unroll 1
-          for (int x = 0; x < DH; x += 16) {
-            uint32_t o[16];
-            tmem_ld16(mine_at + S::kO + x, o);
+          const int valid = pl.gr.rows - pl.t * kN;
+          float mul = a.scale2;
+          if (valid < kN) {
 #pragma unroll
-            for (int j = 0; j < 16; j += 4) {
-              const float4 v = make_float4(__uint_as_float(o[j]), __uint_as_float(o[j + 1]), __uint_as_float(o[j + 2]), __uint_as_float(o[j + 3]));
-              if (!on) continue;
-              if (done) *reinterpret_cast<float4*>(p.whole + at * DH + x + j) = v;
-              else *reinterpret_cast<float4*>(part + 2 * kM + ((x + j) / 4 * kM + tid) * 4) = v;
+            for (int j = 0; j < kN; ++j) z[j] = __float_as_uint(j < valid ? __uint_as_float(z[j]) * mul : -INFINITY);
+            mul = 1.f;
+          }
+          float t[4];
+          const float sign = mul < 0.f ? -1.f : 1.f;
+          if (mul >= 0.f) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) t[i] = __uint_as_float(z[i]);
+#pragma unroll
+            for (int j = 4; j < kN; j += 8)
+#pragma unroll
+              for (int i = 0; i < 4; ++i) t[i] = j + 4 + i < kN ? fmaxf(fmaxf(t[i], __uint_as_float(z[j + i])), __uint_as_float(z[j + 4 + i])) : fmaxf(t[i], __uint_as_float(z[j + i]));
+          } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) t[i] = -__uint_as_float(z[i]);
+#pragma unroll
+            for (int j = 4; j < kN; ++j) t[j & 3] = fmaxf(t[j & 3], -__uint_as_float(z[j]));
+          }
+          const float top = fmaxf(fmaxf(t[0], t[1]), fmaxf(t[2], t[3])) * (sign * mul);
+          grows = __any_sync(0xffffffffu, top > m + kSlack<T>);
+          if (grows) {
+            const float next = fmaxf(m, top);
+            f = exp2_fast(m - (next == -INFINITY ? 0.f : next));
+            m = next;
+          }
+          const float c = kLiftShared<T> - (m == -INFINITY ? 0.f : m);
+          float2 sum = make_float2(0.f, 0.f);
+#pragma unroll
+          for (int j = 0; j < kN; j += 2) {
+            float2 x = fma2(make_float2(__uint_as_float(z[j]), __uint_as_float(z[j + 1])), make_float2(mul, mul), make_float2(c, c));
+            x = make_float2(exp2_fast(x.x), exp2_fast(x.y));
+            sum = add2(sum, x);
+            halves(x, z[j], z[j + 1], T());
+          }
+          l = l * f + (sum.x + sum.y);
+        }
+        // the last tile's product is done: its sums can be scaled, its weights overwritten
+        if (count > 0 && !wait(&b.o_done[mt], count - 1)) break;
+        tc_fence_after();
+        if (busy) {
+          if (!begins && grows) {
+#pragma unroll 1
+            for (int x = 0; x < DH; x += 16) {
+              uint32_t o[16];
+              tmem_ld16(mine_at + S::kO + x, o);
+#pragma unroll
+              for (int j = 0; j < 16; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * f);
+              tmem_st16(mine_at + S::kO + x, o);
             }
           }
-          if (on && done) p.whole_stats[at] = make_float2(m, l);
-          if (on && !done) {
-            part[tid] = m;
-            part[kM + tid] = l;
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            uint32_t w[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) w[i] = z[16 * j + 2 * i];
+            tmem_st8(mine_at + S::kHi + 8 * j, w);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) w[i] = z[16 * j + 2 * i + 1];
+            tmem_st8(mine_at + S::kLo + 8 * j, w);
           }
+          tmem_wait_st();
         }
         tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&b.p_full[mt]);
+
+        const bool ends = pl.t + 1 == pl.tiles;
+        if (ends || n + 1 == run) {
+          if (!wait(&b.o_done[mt], count)) break;
+          tc_fence_after();
+          const bool done = ends && from_start, on = tid < have;
+          const int i = pl.gr.first + (q0 + tid) / a.group, head = kh * a.group + (q0 + tid) % a.group;
+          const long long at = static_cast<long long>(i) * a.q.heads + head;
+          float* part = p.parts + static_cast<long long>(2 * blockIdx.x + (from_start ? 1 : 0)) * (MT * kM * (DH + 2));
+          constexpr float up = kLift<T> - kLiftShared<T>;    // as the sequences' own rows have it
+          if (busy) {
+#pragma unroll 1
+            for (int x = 0; x < DH; x += 16) {
+              uint32_t o[16];
+              tmem_ld16(mine_at + S::kO + x, o);
+#pragma unroll
+              for (int j = 0; j < 16; j += 4) {
+                const float4 v = make_float4(__uint_as_float(o[j]), __uint_as_float(o[j + 1]), __uint_as_float(o[j + 2]), __uint_as_float(o[j + 3]));
+                if (!on) continue;
+                if (done) *reinterpret_cast<float4*>(p.whole + at * DH + x + j) = v;
+                else *reinterpret_cast<float4*>(part + 2 * MT * kM + ((x + j) / 4 * (MT * kM) + tid) * 4) = v;
+              }
+            }
+            if (on && done) p.whole_stats[at] = make_float2(m + up, l);
+            if (on && !done) {
+              part[tid] = m + up;
+              part[MT * kM + tid] = l;
+            }
+          }
+          tc_fence_before();
+        }
+        ++count;
       }
       begins = pl.next(p);
       if (begins) from_start = true;
     }
-  } else if (warp < 8) {
-    // ---- loads: the rows 32 w .. 32 w + 31 of each tile a warp, a row's page by the lane of that number
-    const bool of_keys = warp < 6;
-    const int w = warp & 1, stages = of_keys ? kKeyRing : kValueRing;
+  } else if (warp <= kValues) {
+    // ---- loads: a row's page by the lane of its number, rows 32 .. 63 by the same lanes
+    const bool of_keys = warp == kKeys;
+    const int stages = of_keys ? S::kKeyRing : S::kValueRing;
     uint64_t *full = of_keys ? b.k_full : b.v_full, *empty = of_keys ? b.k_empty : b.v_empty;
     const uint32_t ring = of_keys ? keys : values;
     const T* from = static_cast<const T*>(a.pk) + (of_keys ? 0 : a.plane);
-    const auto page_of = [&]() -> int {
-      const int tok = pl.t * kN + w * 32 + lane;
-      if (pl.g >= p.groups || tok >= pl.gr.rows) return 0;
-      return __ldg(a.c.table + static_cast<long long>(pl.gr.seq) * a.c.max_pages + (a.page_shift >= 0 ? tok >> a.page_shift : tok / a.c.page));
+    int pid[2];
+    const auto pages_of = [&]() {
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const int tok = pl.t * kN + h * 32 + lane;
+        pid[h] = pl.g < p.groups && tok < pl.gr.rows
+                     ? __ldg(a.c.table + static_cast<long long>(pl.gr.seq) * a.c.max_pages + (a.page_shift >= 0 ? tok >> a.page_shift : tok / a.c.page))
+                     : 0;
+      }
     };
-    int pid = page_of(), slot = 0, last = 0;
+    pages_of();
+    int slot = 0, last = 0;
     uint32_t turn = 1;                         // parity of `empty`: the first pass finds the slots free
     bool ok = true;
     for (int n = 0; n < run; ++n) {
+      const int valid = pl.gr.rows - pl.t * kN, kh = pl.item / pl.blocks(p);
+      long long row[2];
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const int tok = pl.t * kN + h * 32 + lane, in_page = a.page_shift >= 0 ? tok & (a.c.page - 1) : tok % a.c.page;
+        if (h * 32 + lane < valid && !good_page(a.c, pid[h])) {
+          atomicOr(a.c.status, ST_BADINDEX);
+          pid[h] = 0;
+        }
+        row[h] = h * 32 + lane < valid ? ((static_cast<long long>(pid[h]) * a.c.heads + kh) * a.c.page + in_page) * DH : 0;
+      }
+      pl.next(p);
+      pages_of();
       ok = wait(&empty[slot], turn);
       if (!ok) break;
-      const int tok = pl.t * kN + w * 32 + lane, valid = pl.gr.rows - pl.t * kN - w * 32;
-      const int kh = pl.item / pl.blocks(p);
-      if (tok < pl.gr.rows && !good_page(a.c, pid)) {
-        atomicOr(a.c.status, ST_BADINDEX);
-        pid = 0;
-      }
-      const int in_page = a.page_shift >= 0 ? tok & (a.c.page - 1) : tok % a.c.page;
-      const long long row = lane < valid ? ((static_cast<long long>(pid) * a.c.heads + kh) * a.c.page + in_page) * DH : 0;
-      pl.next(p);
-      pid = page_of();
-      const uint32_t dst = ring + slot * S::kTileBytes + w * 32 * 128;
+      const uint32_t dst = ring + slot * S::kTileBytes;
 #pragma unroll
-      for (int j = 0; j < VPR; ++j) {
-        const int e = lane + 32 * j, r = e / VPR, x = e % VPR;
-        const long long src = __shfl_sync(0xffffffffu, row, r) + x * 8;
-        cp_async16_or_zero(dst + (x >> 3) * (kN * 128) + r * 128 + (((x & 7) ^ (r & 7)) << 4), from + src, r < valid);
-      }
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int j = 0; j < VPR; ++j) {
+          const int e = lane + 32 * j, r = e / VPR, x = e % VPR;
+          const long long src = __shfl_sync(0xffffffffu, row[h], r) + x * 8;
+          cp_async16_or_zero(dst + h * (32 * 128) + (x >> 3) * (kN * 128) + r * 128 + (((x & 7) ^ (r & 7)) << 4), from + src, h * 32 + r < valid);
+        }
       cp_async_commit();
       if (n > 0) {
         cp_async_wait_group<1>();
@@ -413,88 +540,97 @@ __global__ void __launch_bounds__(kSharedThreads, Shape<DH>::kCtas) shared_kerne
     cp_async_wait_group<0>();
     fence_proxy_async_smem();
     if (ok) mbar_arrive(&full[last]);
-  } else if (elect_one()) {
+  } else if (warp == kProducts && elect_one()) {
     // ---- products
     constexpr uint32_t kScores = idesc_of<T>(kM, kN), kSums = idesc_of<T>(kM, DH) | 1u << 16;
     const uint64_t qd = desc_sw128(base), kd = desc_sw128(0), vd = desc_sw128_mn(0);
     bool ok = true, first = true;              // of an item's tiles in this run
-    int vslot = 0;
-    uint32_t vturn = 0;
-    const auto weigh = [&](int n) {            // sums += weights of tile n * values
-      ok = ok && wait(&b.p_full, n) && wait(&b.v_full[vslot], vturn);
-      if (!ok) return;
-      tc_fence_after();
+    int vslot = 0, kslot = 0, active = 0;      // 128-row halves of the item
+    uint32_t vturn = 0, kturn = 0, asked[2] = {0, 0}, scored[2] = {0, 0}, weighed[2] = {0, 0};
+    const auto weigh = [&]() {                 // sums += weights of the last tile * values
+      ok = ok && wait(&b.v_full[vslot], vturn);
       const uint32_t at = values + vslot * S::kTileBytes;
 #pragma unroll
-      for (int k = 0; k < kN / 16; ++k) umma_ts(tmem + S::kO, tmem + S::kHi + 8 * k, vd + ((at + k * 2048) >> 4), kSums, !first || k != 0);
+      for (int mt = 0; mt < MT; ++mt) {
+        if (mt >= active) break;
+        ok = ok && wait(&b.p_full[mt], weighed[mt]);
+        if (!ok) return;
+        ++weighed[mt];
+        tc_fence_after();
+        const uint32_t tm = tmem + mt * S::kCols;
 #pragma unroll
-      for (int k = 0; k < kN / 16; ++k) umma_ts(tmem + S::kO, tmem + S::kLo + 8 * k, vd + ((at + k * 2048) >> 4), kSums, 1);
+        for (int k = 0; k < kN / 16; ++k) umma_ts(tm + S::kO, tm + S::kHi + 8 * k, vd + ((at + k * 2048) >> 4), kSums, !first || k != 0);
+#pragma unroll
+        for (int k = 0; k < kN / 16; ++k) umma_ts(tm + S::kO, tm + S::kLo + 8 * k, vd + ((at + k * 2048) >> 4), kSums, 1);
+        umma_commit(&b.o_done[mt]);
+      }
       first = false;
       umma_commit(&b.v_empty[vslot]);
-      umma_commit(&b.o_done);
-      if (++vslot == kValueRing) {
+      if (++vslot == S::kValueRing) {
         vslot = 0;
         vturn ^= 1;
       }
     };
-    int kslot = 0, item = 0;
-    uint32_t kturn = 0;
     bool begins = true;
     for (int n = 0; n < run && ok; ++n) {
       if (begins) {
-        if (n > 0) weigh(n - 1);
+        if (n > 0) weigh();
         first = true;
-        ok = ok && wait(&b.q_full, item++);
+        active = MT == 1 || pl.have(p) <= kM ? 1 : 2;
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt)
+          if (mt < active) ok = ok && wait(&b.q_full[mt], asked[mt]++);
       }
-      ok = ok && (n == 0 || wait(&b.s_free, n - 1)) && wait(&b.k_full[kslot], kturn);
-      if (!ok) break;
-      tc_fence_after();
+      ok = ok && wait(&b.k_full[kslot], kturn);
       const uint32_t at = keys + kslot * S::kTileBytes;
 #pragma unroll
-      for (int k = 0; k < DH / 16; ++k)
-        umma_bf16(tmem, qd + (((k >> 2) * (kM * 128) + (k & 3) * 32) >> 4), kd + ((at + (k >> 2) * (kN * 128) + (k & 3) * 32) >> 4), kScores, k != 0);
+      for (int mt = 0; mt < MT; ++mt) {
+        if (mt >= active) break;
+        ok = ok && (scored[mt] == 0 || wait(&b.s_free[mt], scored[mt] - 1));
+        if (!ok) break;
+        ++scored[mt];
+        tc_fence_after();
+#pragma unroll
+        for (int k = 0; k < DH / 16; ++k)
+          umma_bf16(tmem + mt * S::kCols, qd + ((mt * (S::kQBytes / MT) + (k >> 2) * (kM * 128) + (k & 3) * 32) >> 4),
+                    kd + ((at + (k >> 2) * (kN * 128) + (k & 3) * 32) >> 4), kScores, k != 0);
+        umma_commit(&b.s_full[mt]);
+      }
+      if (!ok) break;
       umma_commit(&b.k_empty[kslot]);
-      umma_commit(&b.s_full);
-      if (++kslot == kKeyRing) {
+      if (++kslot == S::kKeyRing) {
         kslot = 0;
         kturn ^= 1;
       }
-      if (!begins) weigh(n - 1);
+      if (!begins) weigh();
       begins = pl.next(p);
     }
-    if (ok) weigh(run - 1);
+    if (ok) weigh();
     umma_commit(&b.drain);                     // all products have ended, whatever came before
     mbar_wait(&b.drain, 0, a.c.status, nullptr);
   }
   tc_fence_before();
   __syncthreads();
-  if (warp == 8) {
+  if (warp == kProducts) {
     tc_fence_after();
-    tmem_dealloc(tmem, S::kCols);
+    tmem_dealloc(tmem, MT * S::kCols);
   }
+  asm volatile("griddepcontrol.wait;" ::: "memory");
 }
 
-// ---- the join: 8 rows (entry, head of a key head) by dh / 4 pieces of four columns a block.
+// ---- the join: 8 rows (entry, head of a key head) by dh / 4 pieces of four columns by kSplit runs of the parts a block.
+constexpr int kSplit = 4, kJoinEach = 5;
 template <typename T>
-__global__ void __launch_bounds__(512) shared_join_kernel(const __grid_constant__ SharedArgs p) {
+__global__ void __launch_bounds__(1024) shared_join_kernel(const __grid_constant__ SharedArgs p) {
+  extern __shared__ __align__(16) float js[];  // (m, l) and four sums of each run but the first
   pdl_enter();
   const AttendArgs& a = p.a;
-  const int dh = a.c.dh, kh = blockIdx.y, x = 4 * (threadIdx.x / 8);
-  const long long row = static_cast<long long>(blockIdx.x) * 8 + threadIdx.x % 8;
-  if (row >= static_cast<long long>(a.n) * a.group) return;
-  const int i = static_cast<int>(row / a.group), head = kh * a.group + static_cast<int>(row % a.group);
-  T* out = static_cast<T*>(a.out.p) + i * a.out.row + head * a.out.head + x;
-  const int s = __ldg(a.seqs + i);
-  if (s < 0 || s >= a.c.seqs) {
-    if (s != -1 && x == 0) atomicOr(a.c.status, ST_BADINDEX);
-    return;
-  }
-  const int len = seq_len(a, i), skip = __ldcg(p.skip + i);
-  if (len == 0) {
-    if (x == 0 && __ldg(a.c.len + s) != 0) atomicOr(a.c.status, ST_BADINDEX);
-    store4(out, make_float4(0.f, 0.f, 0.f, 0.f));
-    return;
-  }
+  const int dh = a.c.dh, kh = blockIdx.y, cells = 2 * dh, cell = threadIdx.x % cells, split = threadIdx.x / cells, x = 4 * (cell / 8);
+  const int splits = blockDim.x / cells;
+  const long long row = static_cast<long long>(blockIdx.x) * 8 + cell % 8;
+  const bool real = row < static_cast<long long>(a.n) * a.group;
+  const int i = real ? static_cast<int>(row / a.group) : 0, head = kh * a.group + static_cast<int>(row % a.group);
+  const int s = real ? __ldg(a.seqs + i) : -1, len = real ? seq_len(a, i) : 0, skip = len > 0 ? __ldcg(p.skip + i) : 0;
   const long long at = static_cast<long long>(i) * a.q.heads + head;
   float top = -INFINITY, l = 0.f;
   float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -507,36 +643,74 @@ __global__ void __launch_bounds__(512) shared_join_kernel(const __grid_constant_
   if (skip > 0) {
     const int g = __ldcg(p.of + i);
     const int4 gr = __ldcg(reinterpret_cast<const int4*>(p.group + g));
-    const int tiles = pieces_of(gr.z, kN), blocks = (gr.y * a.group + kM - 1) / kM;
-    const int q = (i - gr.x) * a.group + static_cast<int>(row % a.group), r = q % kM;
+    const int tiles = pieces_of(gr.z, kN), blocks = (gr.y * a.group + p.m - 1) / p.m;
+    const int q = (i - gr.x) * a.group + static_cast<int>(row % a.group), r = q % p.m;
     const long long total = __ldcg(p.tile0 + p.groups), per = (total + p.grid - 1) / p.grid;
-    const long long tile = __ldcg(p.tile0 + g) + static_cast<long long>(kh * blocks + q / kM) * tiles;
+    const long long tile = __ldcg(p.tile0 + g) + static_cast<long long>(kh * blocks + q / p.m) * tiles;
     const int c0 = static_cast<int>(tile / per), c1 = static_cast<int>((tile + tiles - 1) / per);
-    if (c0 == c1) {
+    if (c0 < c1) {
+      const long long size = static_cast<long long>(p.m) * (dh + 2);
+      for (int c = c0 + split; c <= c1; c += splits * kJoinEach) {
+        float m[kJoinEach], sum[kJoinEach];
+        float4 y[kJoinEach];
+#pragma unroll
+        for (int k = 0; k < kJoinEach; ++k) {
+          const int d = c + k * splits;
+          const float* part = p.parts + (2ll * d + (d == c0 ? 1 : 0)) * size;
+          const bool on = d <= c1;
+          m[k] = on ? __ldcg(part + r) : -INFINITY;
+          sum[k] = on ? __ldcg(part + p.m + r) : 0.f;
+          y[k] = on ? __ldcg(reinterpret_cast<const float4*>(part + 2 * p.m + (x / 4 * p.m + r) * 4)) : make_float4(0.f, 0.f, 0.f, 0.f);
+        }
+#pragma unroll
+        for (int k = 0; k < kJoinEach; ++k) add(m[k], sum[k], y[k]);
+      }
+    } else if (split == 0) {
       const float2 st = __ldcg(p.whole_stats + at);
       add(st.x, st.y, __ldcg(reinterpret_cast<const float4*>(p.whole + at * dh + x)));
-    } else {
-      const long long size = static_cast<long long>(kM) * (dh + 2);
-#pragma unroll 4
-      for (int c = c0; c <= c1; ++c) {
-        const float* part = p.parts + (2ll * c + (c == c0 ? 1 : 0)) * size;
-        add(__ldcg(part + r), __ldcg(part + kM + r), __ldcg(reinterpret_cast<const float4*>(part + 2 * kM + (x / 4 * kM + r) * 4)));
-      }
     }
   }
-  if (len > skip) {
+  if (len > skip && split == splits - 1) {
     const float2 st = __ldcg(a.stats + at);
     add(st.x, st.y, __ldcg(reinterpret_cast<const float4*>(a.own + at * dh + x)));
   }
-  store4(out, make_float4(v.x / l, v.y / l, v.z / l, v.w / l));
+  if (split > 0) {
+    float* mine = js + ((split - 1) * cells + cell) * 6;
+    reinterpret_cast<float2*>(mine)[0] = make_float2(top, l);
+    reinterpret_cast<float2*>(mine)[1] = make_float2(v.x, v.y);
+    reinterpret_cast<float2*>(mine)[2] = make_float2(v.z, v.w);
+  }
+  __syncthreads();
+  if (split > 0 || !real) return;
+  if (s < 0 || s >= a.c.seqs) {
+    if (s != -1 && x == 0) atomicOr(a.c.status, ST_BADINDEX);
+    return;
+  }
+  T* out = static_cast<T*>(a.out.p) + i * a.out.row + head * a.out.head + x;
+  if (len == 0) {
+    if (x == 0 && __ldg(a.c.len + s) != 0) atomicOr(a.c.status, ST_BADINDEX);
+    store4(out, make_float4(0.f, 0.f, 0.f, 0.f));
+    return;
+  }
+  for (int k = 1; k < splits; ++k) {
+    const float2* other = reinterpret_cast<const float2*>(js + ((k - 1) * cells + cell) * 6);
+    add(other[0].x, other[0].y, make_float4(other[1].x, other[1].y, other[2].x, other[2].y));
+  }
+  const float none = l == 0.f ? NAN : 1.f;     // scores of minus infinity alone: raised halves are no weights
+  store4(out, make_float4(v.x / l * none, v.y / l * none, v.z / l * none, v.w / l * none));
 }
 
+template <typename T, int DH, int MT>
+cudaError_t launch_shared_rows(const SharedArgs& p, cudaStream_t st) {
+  using S = Shape<DH, MT>;
+  const cudaError_t e = cudaFuncSetAttribute(shared_kernel<T, DH, MT>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kSmem);
+  return e != cudaSuccess ? e : launch_k(shared_kernel<T, DH, MT>, dim3(p.grid), dim3(S::kThreads), S::kSmem, st, p);
+}
 template <typename T, int DH>
 cudaError_t launch_shared_width(const SharedArgs& p, cudaStream_t st) {
-  using S = Shape<DH>;
-  cudaError_t e = cudaFuncSetAttribute(shared_kernel<T, DH>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kSmem);
-  if (e == cudaSuccess) e = launch_k(shared_kernel<T, DH>, dim3(p.grid), dim3(kSharedThreads), S::kSmem, st, p);
-  return e;
+  if constexpr (DH <= 128)
+    if (p.m > kM) return launch_shared_rows<T, DH, 2>(p, st);
+  return launch_shared_rows<T, DH, 1>(p, st);
 }
 template <typename T>
 cudaError_t launch_shared(const SharedArgs& p, cudaStream_t st) {
@@ -550,7 +724,11 @@ cudaError_t launch_shared(const SharedArgs& p, cudaStream_t st) {
   }
 }
 
-constexpr int shared_grid(int dh) { return 152 * (dh <= 128 ? 2 : 1); }
+// Rows of an item: 256, on an SM of its own, where groups have more than 128 on average.
+int shared_rows(const map_cache* c, long long heads, long long n, long long groups) {
+  return c->dh <= 128 && n * (heads / c->heads) > kM * groups ? 2 * kM : kM;
+}
+int shared_grid(const map_cache* c, int m) { return m == kM && c->dh <= 128 ? 2 * 152 : 152; }
 
 struct SharedSpace { size_t group, of, skip, tile0, stats, own, whole_stats, whole, parts, bytes; };
 SharedSpace shared_space(const map_cache* c, long long heads, long long n, long long groups) {
@@ -569,7 +747,7 @@ SharedSpace shared_space(const map_cache* c, long long heads, long long n, long 
   s.own = take(n * heads * c->dh * 4);
   s.whole_stats = take(n * heads * sizeof(float2));
   s.whole = take(n * heads * c->dh * 4);
-  s.parts = take(2ull * shared_grid(c->dh) * kM * (c->dh + 2) * 4);
+  s.parts = take(2ull * 2 * 152 * kM * (c->dh + 2) * 4);      // (152 CTAs of 256 rows or 304 of 128)
   s.bytes = at;
   return s;
 }
@@ -607,18 +785,21 @@ int map_cache_attend_shared(const map_cache* c, int layer, const map_heads* q, c
   p.parts = reinterpret_cast<float*>(w + s.parts);
   p.whole_stats = reinterpret_cast<float2*>(w + s.whole_stats);
   p.whole = reinterpret_cast<float*>(w + s.whole);
-  p.grid = shared_grid(c->dh);
+  p.m = shared_rows(c, q->heads, n, groups);
+  p.grid = shared_grid(c, p.m);
   a.skip = p.skip;
   a.stats = reinterpret_cast<float2*>(w + s.stats);
   a.own = reinterpret_cast<float*>(w + s.own);
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   const bool half = c->type == MAP_F16;
   cudaError_t e = launch_k(shared_plan_kernel, dim3(groups), dim3(kPlan), 0, st, p);
-  if (e == cudaSuccess) e = half ? launch_shared<__half>(p, st) : launch_shared<__nv_bfloat16>(p, st);
   if (e == cudaSuccess) e = launch_attend<kOwn>(a, st);
+  if (e == cudaSuccess) e = half ? launch_shared<__half>(p, st) : launch_shared<__nv_bfloat16>(p, st);
   if (e == cudaSuccess) {
-    const dim3 grid(static_cast<unsigned>((static_cast<long long>(n) * a.group + 7) / 8), c->heads), block(8 * (c->dh / 4));
-    e = half ? launch_k(shared_join_kernel<__half>, grid, block, 0, st, p) : launch_k(shared_join_kernel<__nv_bfloat16>, grid, block, 0, st, p);
+    const int cells = 2 * c->dh, splits = std::min(kSplit, 1024 / cells);
+    const dim3 grid(static_cast<unsigned>((static_cast<long long>(n) * a.group + 7) / 8), c->heads), block(splits * cells);
+    const size_t smem = static_cast<size_t>(splits - 1) * cells * 6 * 4;
+    e = half ? launch_k(shared_join_kernel<__half>, grid, block, smem, st, p) : launch_k(shared_join_kernel<__nv_bfloat16>, grid, block, smem, st, p);
   }
   return launch_err(e);
 }
