@@ -28,7 +28,7 @@ struct SharedArgs {
   float* parts;                                // [grid][2] parts of items that several CTAs share
   float2* whole_stats;                         // the others': (m, l) [n][q.heads]
   float* whole;                                //         o [n][q.heads][dh]
-  int grid, m;                                 // of shared_kernel: its CTAs, query rows of an item
+  int grid, m, box;                            // of shared_kernel: its CTAs, query rows of an item, rows of a TMA box (0: none)
 };
 
 constexpr int kPlan = 1024, kPlanEach = 8;
@@ -132,9 +132,9 @@ struct Shape {
   static constexpr int kBlocks = (DH + 63) / 64;             // boxes of 64 columns, 128 bytes a row, 16-byte units exchanged by the row's low bits
   static constexpr int kTileBytes = kBlocks * kN * 128, kQBytes = kBlocks * MT * kM * 128;
   static constexpr int kCtas = MT == 1 && DH <= 128 ? 2 : 1;
-  static constexpr int kRing = (227 * 1024 / kCtas - 1536 - kQBytes) / kTileBytes;           // tiles that fit
+  static constexpr int kRing = (227 * 1024 / kCtas - 3072 - kQBytes) / kTileBytes;           // tiles that fit
   static constexpr int kKeyRing = kRing >= 8 ? 4 : (kRing + 1) / 2, kValueRing = kRing >= 8 ? 4 : kRing / 2;
-  static constexpr int kTiles = kQBytes + (kKeyRing + kValueRing) * kTileBytes, kSmem = kTiles + 512;    // the barriers behind the tiles
+  static constexpr int kTiles = kQBytes + (kKeyRing + kValueRing) * kTileBytes, kSmem = kTiles + 512 + MT * kM * 8;        // the barriers and the queries' places behind the tiles
   static constexpr int kHi = kN, kLo = kN + kN / 2, kO = 2 * kN;       // TMEM columns of 128 rows: scores at 0
   static constexpr int kCols = kO + DH <= 256 ? 256 : 512;
   static_assert(kKeyRing <= 4 && kValueRing >= 2 && kCtas * (kSmem + 1024) <= 228 * 1024 && kCtas * MT * kCols <= 512, "an SM");
@@ -146,16 +146,36 @@ __host__ __device__ constexpr uint32_t idesc_of(int m, int n) {
   return std::is_same<T, __half>::value ? idesc_bf16(m, n) & ~kBf16Types : idesc_bf16(m, n);
 }
 
-// D[tmem] (+)= A[tmem] * B[smem]: A's 16-bit columns two to a 32-bit one.
-__device__ __forceinline__ void umma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+// A descriptor's low half, which has the address; the high half is the same for all (desc_sw128, desc_sw128_mn).  The 64-bit sums
+// of an address cost more to issue than the product takes.
+__device__ __forceinline__ uint32_t desc_low(uint32_t at) { return static_cast<uint32_t>(desc_sw128(0)) | at >> 4; }
+__device__ __forceinline__ uint32_t desc_low_mn(uint32_t at) { return static_cast<uint32_t>(desc_sw128_mn(0)) | at >> 4; }
+__device__ __forceinline__ uint32_t desc_high() { return static_cast<uint32_t>(desc_sw128(0) >> 32); }
+
+// D[tmem] (+)= A[smem] * B[smem].
+template <bool ACC>
+__device__ __forceinline__ void umma_ss(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc) {
   asm volatile(
-      "{\n\t.reg .pred p;\n\t"
-      "setp.ne.b32 p, %4, 0;\n\t"
-      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"(accumulate)
+      "{\n\t.reg .pred p;\n\t.reg .b64 x, y;\n\tmov.b64 x, {%1, %4};\n\tmov.b64 y, {%2, %4};\n\t"
+      "setp.ne.b32 p, %5, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], x, y, %3, p;\n\t}" ::"r"(d), "r"(a), "r"(b), "r"(idesc), "r"(desc_high()), "n"(ACC)
       : "memory");
 }
+// D[tmem] (+)= A[tmem] * B[smem]: A's 16-bit columns two to a 32-bit one.
+__device__ __forceinline__ void umma_ts(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t.reg .b64 y;\n\tmov.b64 y, {%2, %4};\n\t"
+      "setp.ne.b32 p, %5, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], y, %3, p;\n\t}" ::"r"(d), "r"(a), "r"(b), "r"(idesc), "r"(desc_high()), "r"(accumulate)
+      : "memory");
+}
+__device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap* map, uint64_t* bar, int c0, int c1, int c2) {
+  asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];" ::"r"(dst),
+               "l"(reinterpret_cast<uint64_t>(map)), "r"(smem_u32(bar)), "r"(c0), "r"(c1), "r"(c2)
+               : "memory");
+}
 
-// 64 columns of the warp's 32 TMEM lanes; eight columns, completed by tmem_wait_st.
+// 64 columns of the warp's 32 TMEM lanes; 8 columns, completed by tmem_wait_st.
 __device__ __forceinline__ void tmem_ld64(uint32_t at, uint32_t (&r)[64]) {
   asm volatile(
       "tcgen05.ld.sync.aligned.32x32b.x64.b32 "
@@ -165,7 +185,7 @@ __device__ __forceinline__ void tmem_ld64(uint32_t at, uint32_t (&r)[64]) {
       : "r"(at)
       : "memory");
 }
-__device__ __forceinline__ void tmem_st8(uint32_t at, const uint32_t (&r)[8]) {
+__device__ __forceinline__ void tmem_put8(uint32_t at, const uint32_t (&r)[8]) {
   asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"r"(at), "r"(r[0]), "r"(r[1]),
                "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]) : "memory");
 }
@@ -249,7 +269,7 @@ struct SharedBars {
 static_assert(sizeof(SharedBars) <= 512, "behind the tiles");
 
 template <typename T, int DH, int MT>
-__global__ void __launch_bounds__(Shape<DH, MT>::kThreads, Shape<DH, MT>::kCtas) shared_kernel(const __grid_constant__ SharedArgs p) {
+__global__ void __launch_bounds__(Shape<DH, MT>::kThreads, Shape<DH, MT>::kCtas) shared_kernel(const __grid_constant__ SharedArgs p, const __grid_constant__ CUtensorMap map) {
   using S = Shape<DH, MT>;
   constexpr int VPR = DH / 8, kWarpsAll = S::kThreads / 32, kKeys = 4 * MT, kValues = kKeys + 1, kProducts = kKeys + 2;
   extern __shared__ __align__(1024) unsigned char sh[];
@@ -299,10 +319,10 @@ __global__ void __launch_bounds__(Shape<DH, MT>::kThreads, Shape<DH, MT>::kCtas)
   }
   if (tid == 0) {
     for (int i = 0; i < 4; ++i) {
-      mbar_init(&b.k_full[i], 32);
-      mbar_init(&b.k_empty[i], 1);
-      mbar_init(&b.v_full[i], 32);
-      mbar_init(&b.v_empty[i], 1);
+      mbar_init(&b.k_full[i], p.box > 0 ? 1 : 32);
+      mbar_init(&b.k_empty[i], MT);
+      mbar_init(&b.v_full[i], p.box > 0 ? 1 : 32);
+      mbar_init(&b.v_empty[i], MT);
     }
     for (int i = 0; i < 2; ++i) {
       mbar_init(&b.q_full[i], 128);
@@ -311,7 +331,7 @@ __global__ void __launch_bounds__(Shape<DH, MT>::kThreads, Shape<DH, MT>::kCtas)
       mbar_init(&b.p_full[i], 4);
       mbar_init(&b.o_done[i], 1);
     }
-    mbar_init(&b.drain, 1);
+    mbar_init(&b.drain, MT);
     b.abort = 0;
     fence_mbar_init();
   }
@@ -334,6 +354,7 @@ __global__ void __launch_bounds__(Shape<DH, MT>::kThreads, Shape<DH, MT>::kCtas)
 
   if (warp < 4 * MT) {
     // ---- softmax: row `tid` of the item's queries
+    long long* q_at = reinterpret_cast<long long*>(sh + S::kTiles + 512);    // where the rows' queries are
     const int mt = MT > 1 ? warp >> 2 : 0;
     const uint32_t mine_at = tmem + mt * S::kCols + (static_cast<uint32_t>((warp & 3) * 32) << 16);
     float m = -INFINITY, l = 0.f;
@@ -347,12 +368,16 @@ __global__ void __launch_bounds__(Shape<DH, MT>::kThreads, Shape<DH, MT>::kCtas)
         q0 = pl.item % mb * p.m;               // of the group's rows (member, head)
         have = pl.have(p);
         if (mt * kM < have) {                  // (these rows' last scores are done with the queries)
-          const T* q = static_cast<const T*>(a.q.p) + kh * a.group * a.q.head;
-          for (int e = tid & 127; e < kM * VPR; e += 128) {
-            const int r = mt * kM + e / VPR, x = e % VPR, i = (q0 + r) / a.group, h = (q0 + r) % a.group;
-            const bool on = r < have;
-            cp_async16_or_zero(base + mt * (S::kQBytes / MT) + (x >> 3) * (kM * 128) + (r % kM) * 128 + (((x & 7) ^ (r & 7)) << 4),
-                               q + (on ? static_cast<long long>(pl.gr.first + i) * a.q.row + h * a.q.head : 0) + x * 8, on);
+          const int i = pl.gr.first + (q0 + tid) / a.group, h = kh * a.group + (q0 + tid) % a.group;
+          q_at[tid] = tid < have ? i * a.q.row + h * a.q.head : -1;
+          asm volatile("bar.sync %0, 128;" ::"r"(1 + mt) : "memory");
+          const T* q = static_cast<const T*>(a.q.p);
+#pragma unroll 4
+          for (int j = 0; j < VPR; ++j) {
+            const int e = (tid & 127) + 128 * j, r = e / VPR, x = e % VPR;
+            const long long at = q_at[mt * kM + r];
+            cp_async16_or_zero(base + mt * (S::kQBytes / MT) + (x >> 3) * (kM * 128) + r * 128 + (((x & 7) ^ (r & 7)) << 4),
+                               q + (at < 0 ? 0 : at) + x * 8, at >= 0);
           }
           cp_async_commit();
           cp_async_wait_group<0>();
@@ -429,14 +454,14 @@ __global__ void __launch_bounds__(Shape<DH, MT>::kThreads, Shape<DH, MT>::kCtas)
             }
           }
 #pragma unroll
-          for (int j = 0; j < 4; ++j) {
+          for (int j = 0; j < kN / 16; ++j) {
             uint32_t w[8];
 #pragma unroll
             for (int i = 0; i < 8; ++i) w[i] = z[16 * j + 2 * i];
-            tmem_st8(mine_at + S::kHi + 8 * j, w);
+            tmem_put8(mine_at + S::kHi + 8 * j, w);
 #pragma unroll
             for (int i = 0; i < 8; ++i) w[i] = z[16 * j + 2 * i + 1];
-            tmem_st8(mine_at + S::kLo + 8 * j, w);
+            tmem_put8(mine_at + S::kLo + 8 * j, w);
           }
           tmem_wait_st();
         }
@@ -480,92 +505,135 @@ __global__ void __launch_bounds__(Shape<DH, MT>::kThreads, Shape<DH, MT>::kCtas)
       if (begins) from_start = true;
     }
   } else if (warp <= kValues) {
-    // ---- loads: a row's page by the lane of its number, rows 32 .. 63 by the same lanes
+    // ---- loads.  Boxes of `box` rows, in one page each, by TMA where a page is a multiple of 8 rows, a box a lane; else 16 bytes a
+    // lane, a row's page by the lane of its number, rows 32 .. 63 by the same lanes.
+    constexpr int kAtOnce = 8;
     const bool of_keys = warp == kKeys;
     const int stages = of_keys ? S::kKeyRing : S::kValueRing;
     uint64_t *full = of_keys ? b.k_full : b.v_full, *empty = of_keys ? b.k_empty : b.v_empty;
     const uint32_t ring = of_keys ? keys : values;
-    const T* from = static_cast<const T*>(a.pk) + (of_keys ? 0 : a.plane);
-    int pid[2];
-    const auto pages_of = [&]() {
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const int tok = pl.t * kN + h * 32 + lane;
-        pid[h] = pl.g < p.groups && tok < pl.gr.rows
-                     ? __ldg(a.c.table + static_cast<long long>(pl.gr.seq) * a.c.max_pages + (a.page_shift >= 0 ? tok >> a.page_shift : tok / a.c.page))
-                     : 0;
-      }
-    };
-    pages_of();
-    int slot = 0, last = 0;
+    int slot = 0;
     uint32_t turn = 1;                         // parity of `empty`: the first pass finds the slots free
-    bool ok = true;
-    for (int n = 0; n < run; ++n) {
-      const int valid = pl.gr.rows - pl.t * kN, kh = pl.item / pl.blocks(p);
-      long long row[2];
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const int tok = pl.t * kN + h * 32 + lane, in_page = a.page_shift >= 0 ? tok & (a.c.page - 1) : tok % a.c.page;
-        if (h * 32 + lane < valid && !good_page(a.c, pid[h])) {
+    if (p.box > 0) {
+      const int past = a.c.pages * a.c.heads * a.c.page;     // rows from here on read as zeros
+      const auto page_of = [&]() {
+        const int tok = pl.t * kN + lane * p.box;
+        if (pl.g >= p.groups || lane * p.box >= kN || tok >= pl.gr.rows) return -1;
+        const int page = a.page_shift >= 0 ? tok >> a.page_shift : tok / a.c.page;
+        return __ldg(a.c.table + static_cast<long long>(pl.gr.seq) * a.c.max_pages + page);
+      };
+      int pid = page_of(), issued = 0;
+      for (; issued < run; ++issued) {
+        const int tok = pl.t * kN + lane * p.box, kh = pl.item / pl.blocks(p);
+        const bool on = lane * p.box < kN && tok < pl.gr.rows;
+        if (on && !good_page(a.c, pid)) {
           atomicOr(a.c.status, ST_BADINDEX);
-          pid[h] = 0;
+          pid = 0;
         }
-        row[h] = h * 32 + lane < valid ? ((static_cast<long long>(pid[h]) * a.c.heads + kh) * a.c.page + in_page) * DH : 0;
+        const int row = on ? (pid * a.c.heads + kh) * a.c.page + (a.page_shift >= 0 ? tok & (a.c.page - 1) : tok % a.c.page) : past;
+        pl.next(p);
+        pid = page_of();
+        if (!wait(&empty[slot], turn)) break;
+        if (lane == 0) mbar_arrive_expect_tx(&full[slot], S::kTileBytes);
+        __syncwarp();
+        if (lane * p.box < kN) {
+#pragma unroll
+          for (int x = 0; x < S::kBlocks; ++x)
+            tma_load_3d(ring + slot * S::kTileBytes + x * (kN * 128) + lane * p.box * 128, &map, &full[slot], x * 64, row, of_keys ? 0 : 1);
+        }
+        if (++slot == stages) {
+          slot = 0;
+          turn ^= 1;
+        }
       }
-      pl.next(p);
+      for (int i = 0; i < stages && i < issued; ++i)         // none is in flight at the end, whatever came before
+        mbar_wait(&full[i], (issued - 1 - i) / stages & 1, a.c.status, nullptr);
+    } else {
+      const T* from = static_cast<const T*>(a.pk) + (of_keys ? 0 : a.plane);
+      int last = 0, pid[2];
+      const auto pages_of = [&]() {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const int tok = pl.t * kN + h * 32 + lane;
+          pid[h] = pl.g < p.groups && tok < pl.gr.rows
+                       ? __ldg(a.c.table + static_cast<long long>(pl.gr.seq) * a.c.max_pages + (a.page_shift >= 0 ? tok >> a.page_shift : tok / a.c.page))
+                       : 0;
+        }
+      };
       pages_of();
-      ok = wait(&empty[slot], turn);
-      if (!ok) break;
-      const uint32_t dst = ring + slot * S::kTileBytes;
+      bool ok = true;
+      for (int n = 0; n < run; ++n) {
+        const int valid = pl.gr.rows - pl.t * kN, kh = pl.item / pl.blocks(p);
+        long long row[2];
 #pragma unroll
-      for (int h = 0; h < 2; ++h)
-#pragma unroll
-        for (int j = 0; j < VPR; ++j) {
-          const int e = lane + 32 * j, r = e / VPR, x = e % VPR;
-          const long long src = __shfl_sync(0xffffffffu, row[h], r) + x * 8;
-          cp_async16_or_zero(dst + h * (32 * 128) + (x >> 3) * (kN * 128) + r * 128 + (((x & 7) ^ (r & 7)) << 4), from + src, h * 32 + r < valid);
+        for (int h = 0; h < 2; ++h) {
+          const int tok = pl.t * kN + h * 32 + lane, in_page = a.page_shift >= 0 ? tok & (a.c.page - 1) : tok % a.c.page;
+          if (h * 32 + lane < valid && !good_page(a.c, pid[h])) {
+            atomicOr(a.c.status, ST_BADINDEX);
+            pid[h] = 0;
+          }
+          row[h] = h * 32 + lane < valid ? ((static_cast<long long>(pid[h]) * a.c.heads + kh) * a.c.page + in_page) * DH : 0;
         }
-      cp_async_commit();
-      if (n > 0) {
-        cp_async_wait_group<1>();
-        fence_proxy_async_smem();
-        mbar_arrive(&full[last]);
+        pl.next(p);
+        pages_of();
+        ok = wait(&empty[slot], turn);
+        if (!ok) break;
+        const uint32_t dst = ring + slot * S::kTileBytes;
+#pragma unroll 1
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int j0 = 0; j0 < VPR; j0 += kAtOnce) {
+            long long src[kAtOnce];              // (so many: a copy would wait for its own row's address otherwise)
+#pragma unroll
+            for (int j = 0; j < kAtOnce; ++j) src[j] = __shfl_sync(0xffffffffu, row[h], (lane + 32 * (j0 + j)) / VPR & 31);
+#pragma unroll
+            for (int j = 0; j < kAtOnce; ++j) {
+              const int e = lane + 32 * (j0 + j), r = e / VPR, x = e % VPR;
+              if (j0 + j < VPR)
+                cp_async16_or_zero(dst + h * (32 * 128) + (x >> 3) * (kN * 128) + r * 128 + (((x & 7) ^ (r & 7)) << 4), from + src[j] + x * 8, h * 32 + r < valid);
+            }
+          }
+        cp_async_commit();
+        if (n > 0) {
+          cp_async_wait_group<1>();
+          fence_proxy_async_smem();
+          mbar_arrive(&full[last]);
+        }
+        last = slot;
+        if (++slot == stages) {
+          slot = 0;
+          turn ^= 1;
+        }
       }
-      last = slot;
-      if (++slot == stages) {
-        slot = 0;
-        turn ^= 1;
-      }
+      cp_async_wait_group<0>();
+      fence_proxy_async_smem();
+      if (ok) mbar_arrive(&full[last]);
     }
-    cp_async_wait_group<0>();
-    fence_proxy_async_smem();
-    if (ok) mbar_arrive(&full[last]);
-  } else if (warp == kProducts && elect_one()) {
-    // ---- products
+  } else if (warp < kProducts + MT && elect_one()) {
+    // ---- products, of 128 rows a warp
     constexpr uint32_t kScores = idesc_of<T>(kM, kN), kSums = idesc_of<T>(kM, DH) | 1u << 16;
-    const uint64_t qd = desc_sw128(base), kd = desc_sw128(0), vd = desc_sw128_mn(0);
-    bool ok = true, first = true;              // of an item's tiles in this run
-    int vslot = 0, kslot = 0, active = 0;      // 128-row halves of the item
-    uint32_t vturn = 0, kturn = 0, asked[2] = {0, 0}, scored[2] = {0, 0}, weighed[2] = {0, 0};
+    const int mt = MT > 1 ? warp - kProducts : 0;
+    const uint32_t tm = tmem + mt * S::kCols, qd = desc_low(base + mt * (S::kQBytes / MT));
+    bool ok = true, first = true, active = false;            // first of an item's tiles in this run; whether it has queries here
+    int vslot = 0, kslot = 0;
+    uint32_t vturn = 0, kturn = 0, items = 0, scored = 0, weighed = 0;
     const auto weigh = [&]() {                 // sums += weights of the last tile * values
-      ok = ok && wait(&b.v_full[vslot], vturn);
-      const uint32_t at = values + vslot * S::kTileBytes;
-#pragma unroll
-      for (int mt = 0; mt < MT; ++mt) {
-        if (mt >= active) break;
-        ok = ok && wait(&b.p_full[mt], weighed[mt]);
-        if (!ok) return;
-        ++weighed[mt];
+      ok = ok && wait(&b.v_full[vslot], vturn) && (!active || wait(&b.p_full[mt], weighed));
+      if (!ok) return;
+      if (active) {
+        ++weighed;
         tc_fence_after();
-        const uint32_t tm = tmem + mt * S::kCols;
+        const uint32_t vd = desc_low_mn(values + vslot * S::kTileBytes);
 #pragma unroll
-        for (int k = 0; k < kN / 16; ++k) umma_ts(tm + S::kO, tm + S::kHi + 8 * k, vd + ((at + k * 2048) >> 4), kSums, !first || k != 0);
+        for (int k = 0; k < kN / 16; ++k) umma_ts(tm + S::kO, tm + S::kHi + 8 * k, vd + k * (2048 >> 4), kSums, !first || k != 0);
 #pragma unroll
-        for (int k = 0; k < kN / 16; ++k) umma_ts(tm + S::kO, tm + S::kLo + 8 * k, vd + ((at + k * 2048) >> 4), kSums, 1);
+        for (int k = 0; k < kN / 16; ++k) umma_ts(tm + S::kO, tm + S::kLo + 8 * k, vd + k * (2048 >> 4), kSums, 1);
+        first = false;
         umma_commit(&b.o_done[mt]);
+        umma_commit(&b.v_empty[vslot]);
+      } else {
+        mbar_arrive(&b.v_empty[vslot]);
       }
-      first = false;
-      umma_commit(&b.v_empty[vslot]);
       if (++vslot == S::kValueRing) {
         vslot = 0;
         vturn ^= 1;
@@ -576,28 +644,26 @@ __global__ void __launch_bounds__(Shape<DH, MT>::kThreads, Shape<DH, MT>::kCtas)
       if (begins) {
         if (n > 0) weigh();
         first = true;
-        active = MT == 1 || pl.have(p) <= kM ? 1 : 2;
-#pragma unroll
-        for (int mt = 0; mt < MT; ++mt)
-          if (mt < active) ok = ok && wait(&b.q_full[mt], asked[mt]++);
+        active = mt * kM < pl.have(p);
+        ok = ok && (!active || wait(&b.q_full[mt], items++));
       }
-      ok = ok && wait(&b.k_full[kslot], kturn);
-      const uint32_t at = keys + kslot * S::kTileBytes;
-#pragma unroll
-      for (int mt = 0; mt < MT; ++mt) {
-        if (mt >= active) break;
-        ok = ok && (scored[mt] == 0 || wait(&b.s_free[mt], scored[mt] - 1));
-        if (!ok) break;
-        ++scored[mt];
-        tc_fence_after();
-#pragma unroll
-        for (int k = 0; k < DH / 16; ++k)
-          umma_bf16(tmem + mt * S::kCols, qd + ((mt * (S::kQBytes / MT) + (k >> 2) * (kM * 128) + (k & 3) * 32) >> 4),
-                    kd + ((at + (k >> 2) * (kN * 128) + (k & 3) * 32) >> 4), kScores, k != 0);
-        umma_commit(&b.s_full[mt]);
-      }
+      ok = ok && wait(&b.k_full[kslot], kturn) && (!active || scored == 0 || wait(&b.s_free[mt], scored - 1));
       if (!ok) break;
-      umma_commit(&b.k_empty[kslot]);
+      if (active) {
+        ++scored;
+        tc_fence_after();
+        const uint32_t kd = desc_low(keys + kslot * S::kTileBytes);
+#pragma unroll
+        for (int k = 0; k < DH / 16; ++k) {
+          const uint32_t qk = qd + (((k >> 2) * (kM * 128) + (k & 3) * 32) >> 4), kk = kd + (((k >> 2) * (kN * 128) + (k & 3) * 32) >> 4);
+          if (k == 0) umma_ss<false>(tm, qk, kk, kScores);
+          else umma_ss<true>(tm, qk, kk, kScores);
+        }
+        umma_commit(&b.s_full[mt]);
+        umma_commit(&b.k_empty[kslot]);
+      } else {
+        mbar_arrive(&b.k_empty[kslot]);
+      }
       if (++kslot == S::kKeyRing) {
         kslot = 0;
         kturn ^= 1;
@@ -701,27 +767,43 @@ __global__ void __launch_bounds__(1024) shared_join_kernel(const __grid_constant
 }
 
 template <typename T, int DH, int MT>
-cudaError_t launch_shared_rows(const SharedArgs& p, cudaStream_t st) {
+cudaError_t launch_shared_rows(const SharedArgs& p, const CUtensorMap& map, cudaStream_t st) {
   using S = Shape<DH, MT>;
   const cudaError_t e = cudaFuncSetAttribute(shared_kernel<T, DH, MT>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kSmem);
-  return e != cudaSuccess ? e : launch_k(shared_kernel<T, DH, MT>, dim3(p.grid), dim3(S::kThreads), S::kSmem, st, p);
+  return e != cudaSuccess ? e : launch_k(shared_kernel<T, DH, MT>, dim3(p.grid), dim3(S::kThreads), S::kSmem, st, p, map);
 }
 template <typename T, int DH>
-cudaError_t launch_shared_width(const SharedArgs& p, cudaStream_t st) {
+cudaError_t launch_shared_width(const SharedArgs& p, const CUtensorMap& map, cudaStream_t st) {
   if constexpr (DH <= 128)
-    if (p.m > kM) return launch_shared_rows<T, DH, 2>(p, st);
-  return launch_shared_rows<T, DH, 1>(p, st);
+    if (p.m > kM) return launch_shared_rows<T, DH, 2>(p, map, st);
+  return launch_shared_rows<T, DH, 1>(p, map, st);
 }
 template <typename T>
-cudaError_t launch_shared(const SharedArgs& p, cudaStream_t st) {
+cudaError_t launch_shared(const SharedArgs& p, const CUtensorMap& map, cudaStream_t st) {
   switch (p.a.c.dh) {
-    case 64: return launch_shared_width<T, 64>(p, st);
-    case 80: return launch_shared_width<T, 80>(p, st);
-    case 96: return launch_shared_width<T, 96>(p, st);
-    case 128: return launch_shared_width<T, 128>(p, st);
-    case 192: return launch_shared_width<T, 192>(p, st);
-    default: return launch_shared_width<T, 256>(p, st);
+    case 64: return launch_shared_width<T, 64>(p, map, st);
+    case 80: return launch_shared_width<T, 80>(p, map, st);
+    case 96: return launch_shared_width<T, 96>(p, map, st);
+    case 128: return launch_shared_width<T, 128>(p, map, st);
+    case 192: return launch_shared_width<T, 192>(p, map, st);
+    default: return launch_shared_width<T, 256>(p, map, st);
   }
+}
+
+// Keys and values of the layer as [2][rows][dh], boxes of `box` rows of 64 columns.  0: a page is no multiple of 8 rows, or there are
+// more rows than a coordinate holds.
+int shared_box(const AttendArgs& a, CUtensorMap* map) {
+  const long long rows = static_cast<long long>(a.c.pages) * a.c.heads * a.c.page;
+  const int box = std::min(kN, a.c.page & -a.c.page);
+  const auto encode = tensor_map_encoder();
+  if (box < 8 || rows >= (1ll << 31) || !encode) return 0;
+  const cuuint64_t dims[3] = {static_cast<cuuint64_t>(a.c.dh), static_cast<cuuint64_t>(rows), 2};
+  const cuuint64_t strides[2] = {static_cast<cuuint64_t>(a.c.dh) * 2, static_cast<cuuint64_t>(a.plane) * 2};
+  const cuuint32_t sides[3] = {64, static_cast<cuuint32_t>(box), 1}, steps[3] = {1, 1, 1};
+  const CUresult r = encode(map, CU_TENSOR_MAP_DATA_TYPE_UINT16, 3, const_cast<void*>(a.pk), dims, strides, sides, steps,
+                            CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  return r == CUDA_SUCCESS ? box : 0;
 }
 
 // Rows of an item: 256, on an SM of its own, where groups have more than 128 on average.
@@ -787,6 +869,8 @@ int map_cache_attend_shared(const map_cache* c, int layer, const map_heads* q, c
   p.whole = reinterpret_cast<float*>(w + s.whole);
   p.m = shared_rows(c, q->heads, n, groups);
   p.grid = shared_grid(c, p.m);
+  CUtensorMap map{};
+  p.box = shared_box(a, &map);
   a.skip = p.skip;
   a.stats = reinterpret_cast<float2*>(w + s.stats);
   a.own = reinterpret_cast<float*>(w + s.own);
@@ -794,7 +878,7 @@ int map_cache_attend_shared(const map_cache* c, int layer, const map_heads* q, c
   const bool half = c->type == MAP_F16;
   cudaError_t e = launch_k(shared_plan_kernel, dim3(groups), dim3(kPlan), 0, st, p);
   if (e == cudaSuccess) e = launch_attend<kOwn>(a, st);
-  if (e == cudaSuccess) e = half ? launch_shared<__half>(p, st) : launch_shared<__nv_bfloat16>(p, st);
+  if (e == cudaSuccess) e = half ? launch_shared<__half>(p, map, st) : launch_shared<__nv_bfloat16>(p, map, st);
   if (e == cudaSuccess) {
     const int cells = 2 * c->dh, splits = std::min(kSplit, 1024 / cells);
     const dim3 grid(static_cast<unsigned>((static_cast<long long>(n) * a.group + 7) / 8), c->heads), block(splits * cells);

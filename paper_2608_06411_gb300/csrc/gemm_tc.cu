@@ -1146,7 +1146,9 @@ gemm_tc_kernel(const __grid_constant__ Maps maps, const __grid_constant__ KArgs 
   }
 }
 
-PFN_cuTensorMapEncodeTiled_v12000 encode_fn() {
+}  // namespace
+
+PFN_cuTensorMapEncodeTiled_v12000 tensor_map_encoder() {
   static PFN_cuTensorMapEncodeTiled_v12000 fn = nullptr;
   if (!fn) {
     void* p = nullptr;
@@ -1159,9 +1161,11 @@ PFN_cuTensorMapEncodeTiled_v12000 encode_fn() {
   return fn;
 }
 
+namespace {
+
 // 2D bf16 tensor map over [rows, K] (K contiguous), box 64 x box_rows, 128-byte swizzle.
 bool make_map(CUtensorMap* m, const void* base, long long rows, int K, int box_rows) {
-  auto fn = encode_fn();
+  auto fn = tensor_map_encoder();
   if (!fn) return false;
   cuuint64_t dims[2] = {static_cast<cuuint64_t>(K), static_cast<cuuint64_t>(rows)};
   cuuint64_t strides[1] = {static_cast<cuuint64_t>(K) * 2};
@@ -1185,7 +1189,7 @@ bool make_maps(const GemmDesc& d, CUtensorMap& ta, CUtensorMap& tb, CUtensorMap&
   if constexpr (TSTORE) {       // output [rows, ldc] bf16, 32x32 boxes, 64-byte swizzle
     // box stores clip at a_rows_total, which is the row bound M only for one flat batch
     if (d.batch != 1 || d.a_rows_total != d.M) return false;
-    auto fn = encode_fn();
+    auto fn = tensor_map_encoder();
     if (!fn) return false;
     cuuint64_t dims[2] = {static_cast<cuuint64_t>(d.ldc), static_cast<cuuint64_t>(d.a_rows_total)};
     cuuint64_t strides[1] = {static_cast<cuuint64_t>(d.ldc) * 2};
@@ -1198,7 +1202,7 @@ bool make_maps(const GemmDesc& d, CUtensorMap& ta, CUtensorMap& tb, CUtensorMap&
   }
   if constexpr (EPI == EPI_F32) {  // output [batch or ksplit][M][ldc] fp32, N columns, 32x32 boxes, 128-byte swizzle
     if (f32_box_store(d)) {
-      auto fn = encode_fn();
+      auto fn = tensor_map_encoder();
       if (!fn) return false;
       const long long slice = d.batch > 1 ? d.c_batch_stride
                               : d.ksplit > 1 ? d.c_split_stride : static_cast<long long>(d.M) * d.ldc;
