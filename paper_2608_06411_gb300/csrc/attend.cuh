@@ -10,8 +10,12 @@ namespace mapk {
 namespace {
 
 // What an item leaves: kOut its output; kWeigh also its rows' scores, and for each head what turns them into weights; kOwn the
-// largest score, the sum of weights and the unnormalised output of the rows from skip[entry] on, for a join with the others.
+// largest score, the sum of weights and the unnormalised output of an entry's own rows, for a join with the others (which
+// also joins the parts of items that several CTAs share).
 enum Mode { kOut, kWeigh, kOwn };
+
+// An entry that shares rows: the rows it shares (-1: it has no rows, -2: padding, or a bad sequence), its group, its other rows.
+struct Entry { int skip, group, own, pad; };
 
 constexpr int kWarps = 4, kThreads = kWarps * 32;
 constexpr int kTok = 16;                       // rows a warp takes of a tile
@@ -38,7 +42,8 @@ struct AttendArgs {
   int page_shift;                              // log2 of the page, -1: no power of two
   float scale2;                                // scale log2(e)
   float* ws;
-  const int32_t* skip;                         // kOwn: [n] rows that an entry begins after
+  const Entry* entries;                        // kOwn: [n]
+  long long* tile0;                            // kOwn: [n + 1] tiles before an entry, and the tiles of a CTA
   float2* stats;                               // kWeigh: (largest score, 1 / sum), kOwn: (largest score, sum), [n][q.heads]
   float* own;                                  // kOwn: [n][q.heads][dh]
   float* z;                                    // kWeigh: scores log2(e), [n][q.heads][z_row]
@@ -51,11 +56,19 @@ __device__ __forceinline__ int seq_len(const AttendArgs& a, int i) {
   return good_len(a.c, len) ? len : 0;
 }
 
-// First row of an entry, none of whose rows lie before it (a multiple of the page, at most the length).
+// First row of an entry's (a multiple of the page) and its length, 0 where it has none.
+struct Span { int from, len; };
 template <int MODE>
-__device__ __forceinline__ int seq_from(const AttendArgs& a, int i) { return MODE == kOwn ? __ldcg(a.skip + i) : 0; }
+__device__ __forceinline__ Span seq_span(const AttendArgs& a, int i) {
+  if (MODE != kOwn) return {0, seq_len(a, i)};
+  const int4 e = __ldcg(reinterpret_cast<const int4*>(a.entries + i));
+  return {max(e.x, 0), max(e.x, 0) + e.z};
+}
 template <int MODE>
-__device__ __forceinline__ int seq_tiles(const AttendArgs& a, int i) { return pieces_of(seq_len(a, i) - seq_from<MODE>(a, i), kTile); }
+__device__ __forceinline__ int seq_tiles(const AttendArgs& a, int i) {
+  const Span s = seq_span<MODE>(a, i);
+  return pieces_of(s.len - s.from, kTile);
+}
 
 // Sum over the block's threads before this one, and over all (red: a word a warp).
 template <int WARPS = kWarps>
@@ -146,8 +159,9 @@ struct Place {
   __device__ __forceinline__ void enter(const AttendArgs& a, int entry) {
     from = 0;
     for (i = entry; i < a.n; ++i) {
-      len = seq_len(a, i);
-      from = seq_from<MODE>(a, i);
+      const Span x = seq_span<MODE>(a, i);
+      len = x.len;
+      from = x.from;
       if (len > from) break;
     }
     if (i < a.n) s = __ldg(a.seqs + i);
@@ -305,6 +319,14 @@ __global__ void __launch_bounds__(kThreads, ctas_of(DH)) attend_kernel(const __g
       T* out = static_cast<T*>(a.out.p) + e * a.out.row;
       for (int x = tid; x < a.out.heads * DH; x += kThreads) out[x / DH * a.out.head + x % DH] = from_f32<T>(0.f);
     }
+  }
+  if (MODE == kOwn && blockIdx.x == 0) {       // for the join
+    long long at = at0;
+    for (int e = e0; e < e1; ++e) {
+      a.tile0[e] = at;
+      at += static_cast<long long>(seq_tiles<MODE>(a, e)) * items;
+    }
+    if (tid == 0) a.tile0[a.n] = per;
   }
   if (t0 >= total) return;
   const int run = static_cast<int>(t0 + per <= total ? per : total - t0);
@@ -559,7 +581,7 @@ __global__ void __launch_bounds__(kThreads, ctas_of(DH)) attend_kernel(const __g
           }
         }
       }
-      if (!done) {
+      if (MODE != kOwn && !done) {
         // the item's parts: CTAs c0 (whose run begins it) to c0 + parts - 1, in groups of kGroup.  The last CTA of a
         // group joins the group, the last group's the groups.  Counters: a group's at its first CTA, the groups' at c0;
         // a group of one needs none, so the next item's first group may begin where this one's last does.

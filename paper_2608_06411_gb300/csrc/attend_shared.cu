@@ -22,9 +22,8 @@ struct SharedArgs {
   const int32_t* starts;
   int groups;
   Group* group;                                // [groups]
-  int32_t* of;                                 // [n] an entry's group, -1: none
-  int32_t* skip;                               // [n] rows that it shares
-  long long* tile0;                            // [groups + 1] tiles before a group, and all (the list of shared_kernel)
+  Entry* entries;                              // [n]
+  long long* tile0;                            // [groups + 1] tiles before a group, and those of a CTA (the list of shared_kernel)
   float* parts;                                // [grid][2] parts of items that several CTAs share
   float2* whole_stats;                         // the others': (m, l) [n][q.heads]
   float* whole;                                //         o [n][q.heads][dh]
@@ -33,14 +32,14 @@ struct SharedArgs {
 
 constexpr int kPlan = 1024, kPlanEach = 8;
 
-// What a group shares: the pages that all its sequences with rows hold in front, as far as all are full.  A CTA a group, latency:
-// a group's sequences are looked up together, then the pages of all of them.
-__global__ void __launch_bounds__(kPlan) shared_plan_kernel(const __grid_constant__ SharedArgs p) {
+// What a group shares: the pages that all its sequences with rows hold in front, as far as all are full.  Latency: a cluster a group;
+// every CTA looks all of the group's sequences up, together, and compares a part of their pages.
+__global__ void __launch_bounds__(kPlan) shared_plan_kernel(const __grid_constant__ SharedArgs p, int ranks) {
   const AttendArgs& a = p.a;
   __shared__ int least, lead, valid;
   __shared__ int seq[kPlan];                   // of kPlan members; -1: without rows
   pdl_enter();
-  const int g = blockIdx.x, tid = threadIdx.x;
+  const int g = blockIdx.x / ranks, rank = blockIdx.x % ranks, tid = threadIdx.x;
   if (tid == 0) {
     least = a.c.max_pages;
     lead = a.n;
@@ -51,16 +50,9 @@ __global__ void __launch_bounds__(kPlan) shared_plan_kernel(const __grid_constan
     const int s = __ldg(p.starts + i), next = i < p.groups ? __ldg(p.starts + i + 1) : a.n;
     bad |= s > next || (i == 0 && s != 0) || (i == p.groups && s != a.n);
   }
-  if (__syncthreads_or(bad)) {
-    if (g == 0 && tid == 0) atomicOr(a.c.status, ST_BADINDEX);
-    for (int i = g * kPlan + tid; i < a.n; i += static_cast<int>(gridDim.x) * kPlan) {
-      p.of[i] = -1;
-      p.skip[i] = 0;
-    }
-    if (tid == 0) p.group[g] = Group{0, 0, 0, 0};
-    return;
-  }
-  const int first = __ldg(p.starts + g), last = __ldg(p.starts + g + 1);
+  const bool refused = __syncthreads_or(bad) != 0;           // nothing is shared then
+  if (refused && blockIdx.x == 0 && tid == 0) atomicOr(a.c.status, ST_BADINDEX);
+  const int first = refused ? 0 : __ldg(p.starts + g), last = refused ? 0 : __ldg(p.starts + g + 1);
   int mine = 0, from = a.n, pages = a.c.max_pages;
   for (int i = first + tid; i < last; i += kPlan) {
     const int len = seq_len(a, i);
@@ -80,8 +72,9 @@ __global__ void __launch_bounds__(kPlan) shared_plan_kernel(const __grid_constan
   __syncthreads();
   const int of = lead, full = valid > 1 ? least : 0;
   const int lead_seq = full > 0 ? __ldg(a.seqs + of) : 0;
-  int same = full;
+  __syncthreads();
   if (full > 0) {
+    int same = full;
     const int32_t* row = a.c.table + static_cast<long long>(lead_seq) * a.c.max_pages;
     for (int i0 = first; i0 < last; i0 += kPlan) {
       __syncthreads();
@@ -89,11 +82,11 @@ __global__ void __launch_bounds__(kPlan) shared_plan_kernel(const __grid_constan
       if (i < last) seq[tid] = seq_len(a, i) > 0 ? __ldg(a.seqs + i) : -1;
       __syncthreads();
       const long long all = static_cast<long long>(count) * full;
-      for (long long x0 = tid; x0 < all; x0 += kPlan * kPlanEach) {
+      for (long long x0 = rank * kPlan + tid; x0 < all; x0 += kPlan * kPlanEach * ranks) {
         int j[kPlanEach], page[kPlanEach], other[kPlanEach];
 #pragma unroll
         for (int k = 0; k < kPlanEach; ++k) {
-          const long long x = x0 + k * kPlan;
+          const long long x = x0 + k * kPlan * ranks;
           const int m = x < all ? (all < (1ll << 31) ? static_cast<int>(x) / full : static_cast<int>(x / full)) : 0;
           const int s = x < all ? seq[m] : -1;
           j[k] = static_cast<int>(x - static_cast<long long>(m) * full);
@@ -111,30 +104,52 @@ __global__ void __launch_bounds__(kPlan) shared_plan_kernel(const __grid_constan
     same = __reduce_min_sync(0xffffffffu, same);
     if (tid % 32 == 0) atomicMin(&least, same);
   }
-  __syncthreads();
-  const int rows = full > 0 ? least * a.c.page : 0;
-  for (int i = first + tid; i < last; i += kPlan) {
-    p.of[i] = g;
-    p.skip[i] = rows > 0 && seq_len(a, i) > 0 ? rows : 0;
+  int shared = 0;
+  if (ranks > 1) {                             // (full is the same in all of the cluster)
+    cluster_sync();
+    shared = a.c.max_pages;
+    for (int r = 0; r < ranks; ++r) {
+      int v;
+      asm volatile("ld.shared::cluster.s32 %0, [%1];" : "=r"(v) : "r"(mapa_u32(&least, r)) : "memory");
+      shared = min(shared, v);
+    }
+    cluster_sync();                            // no CTA leaves while another may read
+  } else {
+    __syncthreads();
+    shared = least;
   }
-  if (tid == 0) p.group[g] = Group{first, last - first, rows, lead_seq};
+  const int rows = full > 0 ? shared * a.c.page : 0;
+  // entries of the group; all of them where nothing is shared because the groups are bad
+  const int e0 = refused ? 0 : first, e1 = refused ? a.n : last;
+  for (int i = e0 + (refused ? static_cast<int>(blockIdx.x) : rank) * kPlan + tid; i < e1; i += (refused ? static_cast<int>(gridDim.x) : ranks) * kPlan) {
+    const int s = __ldg(a.seqs + i);
+    const bool known = s >= 0 && s < a.c.seqs;
+    const int len = known ? __ldg(a.c.len + s) : 0;
+    Entry e{rows, g, len - rows, 0};
+    if (!known) e = Entry{-2, 0, 0, 0};
+    else if (len == 0 || !good_len(a.c, len)) e = Entry{-1, 0, 0, 0};
+    if ((!known && s != -1) || (known && !good_len(a.c, len))) atomicOr(a.c.status, ST_BADINDEX);
+    *reinterpret_cast<int4*>(p.entries + i) = make_int4(e.skip, e.group, e.own, 0);
+  }
+  if (tid == 0 && rank == 0) p.group[g] = Group{first, last - first, rows, lead_seq};
 }
 
 // ---- the shared rows.  An item is up to M = 128 MT rows of queries (member, head) of one key head and group, 128 the M of a
 // tcgen05.mma.  64 keys are the N of the scores' product and the K of the values', whose first operand, the weights as two halves
-// of T, lies in TMEM.  Four warps for each 128 rows do the softmax, a row a thread; a warp loads keys and one values, each with a
-// ring of its own; a thread of a third issues the products: scores of a tile while the last one's weights are made.
+// of T, lies in TMEM.  Eight warps for each 128 rows do the softmax, a row of half a tile's keys a thread (a row of all of them, and
+// half the warps, waited for latency: 51 us where XX are taken now); a warp loads keys and one values, each with a ring of its own; a
+// thread of a warp for each 128 rows issues the products: scores of a tile while the last one's weights are made.
 constexpr int kM = 128, kN = 64;
 
 template <int DH, int MT>
 struct Shape {
-  static constexpr int kThreads = 128 * MT + 128;
+  static constexpr int kThreads = 256 * MT + 128;
   static constexpr int kBlocks = (DH + 63) / 64;             // boxes of 64 columns, 128 bytes a row, 16-byte units exchanged by the row's low bits
   static constexpr int kTileBytes = kBlocks * kN * 128, kQBytes = kBlocks * MT * kM * 128;
   static constexpr int kCtas = MT == 1 && DH <= 128 ? 2 : 1;
-  static constexpr int kRing = (227 * 1024 / kCtas - 3072 - kQBytes) / kTileBytes;           // tiles that fit
+  static constexpr int kRing = (227 * 1024 / kCtas - 8192 / kCtas - kQBytes) / kTileBytes;           // tiles that fit
   static constexpr int kKeyRing = kRing >= 8 ? 4 : (kRing + 1) / 2, kValueRing = kRing >= 8 ? 4 : kRing / 2;
-  static constexpr int kTiles = kQBytes + (kKeyRing + kValueRing) * kTileBytes, kSmem = kTiles + 512 + MT * kM * 8;        // the barriers and the queries' places behind the tiles
+  static constexpr int kTiles = kQBytes + (kKeyRing + kValueRing) * kTileBytes, kSmem = kTiles + 512 + MT * kM * 24;       // barriers, the queries' places and the rows' largest scores behind the tiles
   static constexpr int kHi = kN, kLo = kN + kN / 2, kO = 2 * kN;       // TMEM columns of 128 rows: scores at 0
   static constexpr int kCols = kO + DH <= 256 ? 256 : 512;
   static_assert(kKeyRing <= 4 && kValueRing >= 2 && kCtas * (kSmem + 1024) <= 228 * 1024 && kCtas * MT * kCols <= 512, "an SM");
@@ -175,16 +190,7 @@ __device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap* map
                : "memory");
 }
 
-// 64 columns of the warp's 32 TMEM lanes; 8 columns, completed by tmem_wait_st.
-__device__ __forceinline__ void tmem_ld64(uint32_t at, uint32_t (&r)[64]) {
-  asm volatile(
-      "tcgen05.ld.sync.aligned.32x32b.x64.b32 "
-      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32, %33, %34, %35, %36, %37, %38, %39, %40, %41, %42, %43, %44, %45, %46, %47, %48, %49, %50, %51, %52, %53, %54, %55, %56, %57, %58, %59, %60, %61, %62, %63}, [%64];\n\t"
-      "tcgen05.wait::ld.sync.aligned;"
-      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31]), "=r"(r[32]), "=r"(r[33]), "=r"(r[34]), "=r"(r[35]), "=r"(r[36]), "=r"(r[37]), "=r"(r[38]), "=r"(r[39]), "=r"(r[40]), "=r"(r[41]), "=r"(r[42]), "=r"(r[43]), "=r"(r[44]), "=r"(r[45]), "=r"(r[46]), "=r"(r[47]), "=r"(r[48]), "=r"(r[49]), "=r"(r[50]), "=r"(r[51]), "=r"(r[52]), "=r"(r[53]), "=r"(r[54]), "=r"(r[55]), "=r"(r[56]), "=r"(r[57]), "=r"(r[58]), "=r"(r[59]), "=r"(r[60]), "=r"(r[61]), "=r"(r[62]), "=r"(r[63])
-      : "r"(at)
-      : "memory");
-}
+// 8 columns of the warp's 32 TMEM lanes, completed by tmem_wait_st.
 __device__ __forceinline__ void tmem_put8(uint32_t at, const uint32_t (&r)[8]) {
   asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"r"(at), "r"(r[0]), "r"(r[1]),
                "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]) : "memory");
@@ -264,14 +270,14 @@ struct SharedBars {
   uint32_t tmem;
   int abort, group;
   long long tile;
-  long long red[12];
+  long long red[20];
 };
 static_assert(sizeof(SharedBars) <= 512, "behind the tiles");
 
 template <typename T, int DH, int MT>
 __global__ void __launch_bounds__(Shape<DH, MT>::kThreads, Shape<DH, MT>::kCtas) shared_kernel(const __grid_constant__ SharedArgs p, const __grid_constant__ CUtensorMap map) {
   using S = Shape<DH, MT>;
-  constexpr int VPR = DH / 8, kWarpsAll = S::kThreads / 32, kKeys = 4 * MT, kValues = kKeys + 1, kProducts = kKeys + 2;
+  constexpr int VPR = DH / 8, kWarpsAll = S::kThreads / 32, kKeys = 8 * MT, kValues = kKeys + 1, kProducts = kKeys + 2;
   extern __shared__ __align__(1024) unsigned char sh[];
   SharedBars& b = *reinterpret_cast<SharedBars*>(sh + S::kTiles);
   // The kernel launched before this one attends the sequences' own rows: it has waited for the plan, and so has this one when it
@@ -298,7 +304,7 @@ __global__ void __launch_bounds__(Shape<DH, MT>::kThreads, Shape<DH, MT>::kCtas)
       p.tile0[g] = at;
       at += tiles_of(g);
     }
-    if (tid == 0) p.tile0[p.groups] = total;
+    if (tid == 0) p.tile0[p.groups] = per;
   }
   if (t0 >= total || (smem_u32(sh) & 1023) != 0) {           // (the alignment is what its declaration asks for)
     if (t0 < total && tid == 0) atomicOr(a.c.status, ST_INTERNAL);
@@ -325,10 +331,10 @@ __global__ void __launch_bounds__(Shape<DH, MT>::kThreads, Shape<DH, MT>::kCtas)
       mbar_init(&b.v_empty[i], MT);
     }
     for (int i = 0; i < 2; ++i) {
-      mbar_init(&b.q_full[i], 128);
+      mbar_init(&b.q_full[i], 256);
       mbar_init(&b.s_full[i], 1);
-      mbar_init(&b.s_free[i], 4);
-      mbar_init(&b.p_full[i], 4);
+      mbar_init(&b.s_free[i], 8);
+      mbar_init(&b.p_full[i], 8);
       mbar_init(&b.o_done[i], 1);
     }
     mbar_init(&b.drain, MT);
@@ -352,11 +358,15 @@ __global__ void __launch_bounds__(Shape<DH, MT>::kThreads, Shape<DH, MT>::kCtas)
   pl.item = static_cast<int>(b.tile / pl.tiles);
   pl.t = static_cast<int>(b.tile % pl.tiles);
 
-  if (warp < 4 * MT) {
-    // ---- softmax: row `tid` of the item's queries
-    long long* q_at = reinterpret_cast<long long*>(sh + S::kTiles + 512);    // where the rows' queries are
-    const int mt = MT > 1 ? warp >> 2 : 0;
+  if (warp < 8 * MT) {
+    // ---- softmax: row `r` of the item's queries, keys 32 c .. of a tile; columns from 16 x0 to 16 x1 of its sums
+    constexpr int kHalf = kN / 2;
+    const int mt = MT > 1 ? warp >> 3 : 0, c = warp >> 2 & 1, r = mt * kM + (warp & 3) * 32 + lane;
+    const int x0 = c == 0 ? 0 : (DH / 16 + 1) / 2, x1 = c == 0 ? (DH / 16 + 1) / 2 : DH / 16;
     const uint32_t mine_at = tmem + mt * S::kCols + (static_cast<uint32_t>((warp & 3) * 32) << 16);
+    long long* q_at = reinterpret_cast<long long*>(sh + S::kTiles + 512);    // where the rows' queries are
+    float* tops = reinterpret_cast<float*>(q_at + MT * kM);                  // [2][2 halves][rows]
+    const auto both = [&]() { asm volatile("bar.sync %0, 64;" ::"r"(1 + MT + mt * 4 + (warp & 3)) : "memory"); };      // halves of 32 rows
     float m = -INFINITY, l = 0.f;
     bool begins = true, from_start = pl.t == 0;
     int have = 0, q0 = 0, kh = 0;
@@ -368,15 +378,17 @@ __global__ void __launch_bounds__(Shape<DH, MT>::kThreads, Shape<DH, MT>::kCtas)
         q0 = pl.item % mb * p.m;               // of the group's rows (member, head)
         have = pl.have(p);
         if (mt * kM < have) {                  // (these rows' last scores are done with the queries)
-          const int i = pl.gr.first + (q0 + tid) / a.group, h = kh * a.group + (q0 + tid) % a.group;
-          q_at[tid] = tid < have ? i * a.q.row + h * a.q.head : -1;
-          asm volatile("bar.sync %0, 128;" ::"r"(1 + mt) : "memory");
+          if (c == 0) {
+            const int i = pl.gr.first + (q0 + r) / a.group, h = kh * a.group + (q0 + r) % a.group;
+            q_at[r] = r < have ? i * a.q.row + h * a.q.head : -1;
+          }
+          asm volatile("bar.sync %0, 256;" ::"r"(1 + mt) : "memory");
           const T* q = static_cast<const T*>(a.q.p);
 #pragma unroll 4
-          for (int j = 0; j < VPR; ++j) {
-            const int e = (tid & 127) + 128 * j, r = e / VPR, x = e % VPR;
-            const long long at = q_at[mt * kM + r];
-            cp_async16_or_zero(base + mt * (S::kQBytes / MT) + (x >> 3) * (kM * 128) + r * 128 + (((x & 7) ^ (r & 7)) << 4),
+          for (int j = 0; j < VPR / 2; ++j) {
+            const int e = (tid & 255) + 256 * j, row = e / VPR, x = e % VPR;
+            const long long at = q_at[mt * kM + row];
+            cp_async16_or_zero(base + mt * (S::kQBytes / MT) + (x >> 3) * (kM * 128) + row * 128 + (((x & 7) ^ (row & 7)) << 4),
                                q + (at < 0 ? 0 : at) + x * 8, at >= 0);
           }
           cp_async_commit();
@@ -388,51 +400,57 @@ __global__ void __launch_bounds__(Shape<DH, MT>::kThreads, Shape<DH, MT>::kCtas)
         l = 0.f;
       }
       if (mt * kM < have) {
-        const bool busy = warp * 32 < have;    // rows of this warp hold queries
-        if (!wait(&b.s_full[mt], count)) break;
+        const bool busy = mt * kM + (warp & 3) * 32 < have;  // rows of this warp hold queries
+        wait(&b.s_full[mt], count);            // (a wait that gave up stops all others; the barriers between warps need every pass)
         tc_fence_after();
-        uint32_t z[kN];
-        if (busy) tmem_ld64(mine_at, z);
+        uint32_t z[kHalf];
+        if (busy) tmem_ld32(mine_at + c * kHalf, z);
         tc_fence_before();
         __syncwarp();
         if (lane == 0) mbar_arrive(&b.s_free[mt]);
         float f = 1.f;
         bool grows = false;
         if (busy) {
-          const int valid = pl.gr.rows - pl.t * kN;
+          const int valid = pl.gr.rows - pl.t * kN - c * kHalf;
           float mul = a.scale2;
-          if (valid < kN) {
+          if (valid < kHalf) {
 #pragma unroll
-            for (int j = 0; j < kN; ++j) z[j] = __float_as_uint(j < valid ? __uint_as_float(z[j]) * mul : -INFINITY);
+            for (int j = 0; j < kHalf; ++j) z[j] = __float_as_uint(j < valid ? __uint_as_float(z[j]) * mul : -INFINITY);
             mul = 1.f;
           }
-          float t[4];
-          const float sign = mul < 0.f ? -1.f : 1.f;
+          // the largest score: the least where the factor is below zero
+          float top = __uint_as_float(z[0]), other = __uint_as_float(z[1]);
           if (mul >= 0.f) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) t[i] = __uint_as_float(z[i]);
-#pragma unroll
-            for (int j = 4; j < kN; j += 8)
-#pragma unroll
-              for (int i = 0; i < 4; ++i) t[i] = j + 4 + i < kN ? fmaxf(fmaxf(t[i], __uint_as_float(z[j + i])), __uint_as_float(z[j + 4 + i])) : fmaxf(t[i], __uint_as_float(z[j + i]));
+            for (int j = 2; j < kHalf; j += 2) {
+              top = fmaxf(top, __uint_as_float(z[j]));
+              other = fmaxf(other, __uint_as_float(z[j + 1]));
+            }
+            top = fmaxf(top, other);
           } else {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) t[i] = -__uint_as_float(z[i]);
-#pragma unroll
-            for (int j = 4; j < kN; ++j) t[j & 3] = fmaxf(t[j & 3], -__uint_as_float(z[j]));
+            for (int j = 2; j < kHalf; j += 2) {
+              top = fminf(top, __uint_as_float(z[j]));
+              other = fminf(other, __uint_as_float(z[j + 1]));
+            }
+            top = fminf(top, other);
           }
-          const float top = fmaxf(fmaxf(t[0], t[1]), fmaxf(t[2], t[3])) * (sign * mul);
+          top *= mul;
+          float* t = tops + (count & 1) * (2 * MT * kM) + r;
+          t[c * (MT * kM)] = top;
+          both();
+          top = fmaxf(top, t[(c ^ 1) * (MT * kM)]);
           grows = __any_sync(0xffffffffu, top > m + kSlack<T>);
           if (grows) {
             const float next = fmaxf(m, top);
             f = exp2_fast(m - (next == -INFINITY ? 0.f : next));
             m = next;
           }
-          const float c = kLiftShared<T> - (m == -INFINITY ? 0.f : m);
+          const float add = kLiftShared<T> - (m == -INFINITY ? 0.f : m);
           float2 sum = make_float2(0.f, 0.f);
 #pragma unroll
-          for (int j = 0; j < kN; j += 2) {
-            float2 x = fma2(make_float2(__uint_as_float(z[j]), __uint_as_float(z[j + 1])), make_float2(mul, mul), make_float2(c, c));
+          for (int j = 0; j < kHalf; j += 2) {
+            float2 x = fma2(make_float2(__uint_as_float(z[j]), __uint_as_float(z[j + 1])), make_float2(mul, mul), make_float2(add, add));
             x = make_float2(exp2_fast(x.x), exp2_fast(x.y));
             sum = add2(sum, x);
             halves(x, z[j], z[j + 1], T());
@@ -440,66 +458,71 @@ __global__ void __launch_bounds__(Shape<DH, MT>::kThreads, Shape<DH, MT>::kCtas)
           l = l * f + (sum.x + sum.y);
         }
         // the last tile's product is done: its sums can be scaled, its weights overwritten
-        if (count > 0 && !wait(&b.o_done[mt], count - 1)) break;
+        if (count > 0) wait(&b.o_done[mt], count - 1);
         tc_fence_after();
         if (busy) {
           if (!begins && grows) {
 #pragma unroll 1
-            for (int x = 0; x < DH; x += 16) {
+            for (int x = x0; x < x1; ++x) {
               uint32_t o[16];
-              tmem_ld16(mine_at + S::kO + x, o);
+              tmem_ld16(mine_at + S::kO + 16 * x, o);
 #pragma unroll
               for (int j = 0; j < 16; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * f);
-              tmem_st16(mine_at + S::kO + x, o);
+              tmem_st16(mine_at + S::kO + 16 * x, o);
             }
           }
 #pragma unroll
-          for (int j = 0; j < kN / 16; ++j) {
+          for (int j = 0; j < kHalf / 16; ++j) {
             uint32_t w[8];
 #pragma unroll
             for (int i = 0; i < 8; ++i) w[i] = z[16 * j + 2 * i];
-            tmem_put8(mine_at + S::kHi + 8 * j, w);
+            tmem_put8(mine_at + S::kHi + c * (kHalf / 2) + 8 * j, w);
 #pragma unroll
             for (int i = 0; i < 8; ++i) w[i] = z[16 * j + 2 * i + 1];
-            tmem_put8(mine_at + S::kLo + 8 * j, w);
+            tmem_put8(mine_at + S::kLo + c * (kHalf / 2) + 8 * j, w);
           }
           tmem_wait_st();
         }
         tc_fence_before();
         __syncwarp();
         if (lane == 0) mbar_arrive(&b.p_full[mt]);
+        ++count;
 
         const bool ends = pl.t + 1 == pl.tiles;
         if (ends || n + 1 == run) {
-          if (!wait(&b.o_done[mt], count)) break;
+          wait(&b.o_done[mt], count - 1);
           tc_fence_after();
-          const bool done = ends && from_start, on = tid < have;
-          const int i = pl.gr.first + (q0 + tid) / a.group, head = kh * a.group + (q0 + tid) % a.group;
+          const bool done = ends && from_start, on = r < have;
+          const int i = pl.gr.first + (q0 + r) / a.group, head = kh * a.group + (q0 + r) % a.group;
           const long long at = static_cast<long long>(i) * a.q.heads + head;
           float* part = p.parts + static_cast<long long>(2 * blockIdx.x + (from_start ? 1 : 0)) * (MT * kM * (DH + 2));
           constexpr float up = kLift<T> - kLiftShared<T>;    // as the sequences' own rows have it
           if (busy) {
 #pragma unroll 1
-            for (int x = 0; x < DH; x += 16) {
+            for (int x = x0; x < x1; ++x) {
               uint32_t o[16];
-              tmem_ld16(mine_at + S::kO + x, o);
+              tmem_ld16(mine_at + S::kO + 16 * x, o);
 #pragma unroll
               for (int j = 0; j < 16; j += 4) {
                 const float4 v = make_float4(__uint_as_float(o[j]), __uint_as_float(o[j + 1]), __uint_as_float(o[j + 2]), __uint_as_float(o[j + 3]));
                 if (!on) continue;
-                if (done) *reinterpret_cast<float4*>(p.whole + at * DH + x + j) = v;
-                else *reinterpret_cast<float4*>(part + 2 * MT * kM + ((x + j) / 4 * (MT * kM) + tid) * 4) = v;
+                if (done) *reinterpret_cast<float4*>(p.whole + at * DH + 16 * x + j) = v;
+                else *reinterpret_cast<float4*>(part + 2 * MT * kM + ((4 * x + j / 4) * (MT * kM) + r) * 4) = v;
               }
             }
-            if (on && done) p.whole_stats[at] = make_float2(m + up, l);
-            if (on && !done) {
-              part[tid] = m + up;
-              part[MT * kM + tid] = l;
+            float* t = tops + (count & 1) * (2 * MT * kM) + r;               // (the halves' sums of weights)
+            if (c == 1) t[0] = l;
+            both();
+            if (c == 0 && on) {
+              l += t[0];
+              if (done) p.whole_stats[at] = make_float2(m + up, l);
+              if (!done) part[r] = m + up;
+              if (!done) part[MT * kM + r] = l;
             }
+            both();
           }
           tc_fence_before();
         }
-        ++count;
       }
       begins = pl.next(p);
       if (begins) from_start = true;
@@ -684,7 +707,8 @@ __global__ void __launch_bounds__(Shape<DH, MT>::kThreads, Shape<DH, MT>::kCtas)
   asm volatile("griddepcontrol.wait;" ::: "memory");
 }
 
-// ---- the join: 8 rows (entry, head of a key head) by dh / 4 pieces of four columns by kSplit runs of the parts a block.
+// ---- the join: 8 rows (entry, head of a key head) by dh / 4 pieces of four columns by kSplit runs of their parts a block.  Latency:
+// an entry, then its group and places in the lists, then its parts, kJoinEach of them together.
 constexpr int kSplit = 4, kJoinEach = 5;
 template <typename T>
 __global__ void __launch_bounds__(1024) shared_join_kernel(const __grid_constant__ SharedArgs p) {
@@ -695,66 +719,75 @@ __global__ void __launch_bounds__(1024) shared_join_kernel(const __grid_constant
   const int splits = blockDim.x / cells;
   const long long row = static_cast<long long>(blockIdx.x) * 8 + cell % 8;
   const bool real = row < static_cast<long long>(a.n) * a.group;
-  const int i = real ? static_cast<int>(row / a.group) : 0, head = kh * a.group + static_cast<int>(row % a.group);
-  const int s = real ? __ldg(a.seqs + i) : -1, len = real ? seq_len(a, i) : 0, skip = len > 0 ? __ldcg(p.skip + i) : 0;
+  const int i = real ? static_cast<int>(row / a.group) : 0, h = static_cast<int>(row - static_cast<long long>(i) * a.group), head = kh * a.group + h;
+  const int4 e = real ? __ldcg(reinterpret_cast<const int4*>(p.entries + i)) : make_int4(-2, 0, 0, 0);
   const long long at = static_cast<long long>(i) * a.q.heads + head;
+  // the CTAs that have parts of the shared rows (c0 .. c1) and of the others (d0 .. d1); one has all
+  int c0 = 0, c1 = -1, d0 = 0, d1 = -1, r = 0;
+  if (e.z > 0) {
+    const int tiles = pieces_of(e.z, kTile);
+    const long long tile = __ldcg(a.tile0 + i) + static_cast<long long>(kh * a.subs + h / kRows) * tiles, per = __ldcg(a.tile0 + a.n);
+    d0 = static_cast<int>(tile / per);
+    d1 = static_cast<int>((tile + tiles - 1) / per);
+  }
+  if (e.x > 0) {
+    const int4 gr = __ldcg(reinterpret_cast<const int4*>(p.group + e.y));
+    const int tiles = pieces_of(gr.z, kN), blocks = (gr.y * a.group + p.m - 1) / p.m, q = (i - gr.x) * a.group + h;
+    r = q % p.m;
+    const long long tile = __ldcg(p.tile0 + e.y) + static_cast<long long>(kh * blocks + q / p.m) * tiles, per = __ldcg(p.tile0 + p.groups);
+    c0 = static_cast<int>(tile / per);
+    c1 = static_cast<int>((tile + tiles - 1) / per);
+  }
+  const int shared = c1 - c0 + 1, all = shared + d1 - d0 + 1;
   float top = -INFINITY, l = 0.f;
   float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
   const auto add = [&](float m, float sum, float4 y) {
-    const float next = fmaxf(top, m), by = next == -INFINITY ? 0.f : next, f = exp2_fast(top - by), h = exp2_fast(m - by);
+    const float next = fmaxf(top, m), by = next == -INFINITY ? 0.f : next, f = exp2_fast(top - by), g = exp2_fast(m - by);
     top = next;
-    l = l * f + sum * h;
-    v = make_float4(v.x * f + y.x * h, v.y * f + y.y * h, v.z * f + y.z * h, v.w * f + y.w * h);
+    l = l * f + sum * g;
+    v = make_float4(v.x * f + y.x * g, v.y * f + y.y * g, v.z * f + y.z * g, v.w * f + y.w * g);
   };
-  if (skip > 0) {
-    const int g = __ldcg(p.of + i);
-    const int4 gr = __ldcg(reinterpret_cast<const int4*>(p.group + g));
-    const int tiles = pieces_of(gr.z, kN), blocks = (gr.y * a.group + p.m - 1) / p.m;
-    const int q = (i - gr.x) * a.group + static_cast<int>(row % a.group), r = q % p.m;
-    const long long total = __ldcg(p.tile0 + p.groups), per = (total + p.grid - 1) / p.grid;
-    const long long tile = __ldcg(p.tile0 + g) + static_cast<long long>(kh * blocks + q / p.m) * tiles;
-    const int c0 = static_cast<int>(tile / per), c1 = static_cast<int>((tile + tiles - 1) / per);
-    if (c0 < c1) {
-      const long long size = static_cast<long long>(p.m) * (dh + 2);
-      for (int c = c0 + split; c <= c1; c += splits * kJoinEach) {
-        float m[kJoinEach], sum[kJoinEach];
-        float4 y[kJoinEach];
+  for (int k0 = split; k0 < all; k0 += splits * kJoinEach) {
+    float m[kJoinEach], sum[kJoinEach];
+    float4 y[kJoinEach];
 #pragma unroll
-        for (int k = 0; k < kJoinEach; ++k) {
-          const int d = c + k * splits;
-          const float* part = p.parts + (2ll * d + (d == c0 ? 1 : 0)) * size;
-          const bool on = d <= c1;
-          m[k] = on ? __ldcg(part + r) : -INFINITY;
-          sum[k] = on ? __ldcg(part + p.m + r) : 0.f;
-          y[k] = on ? __ldcg(reinterpret_cast<const float4*>(part + 2 * p.m + (x / 4 * p.m + r) * 4)) : make_float4(0.f, 0.f, 0.f, 0.f);
-        }
-#pragma unroll
-        for (int k = 0; k < kJoinEach; ++k) add(m[k], sum[k], y[k]);
+    for (int k = 0; k < kJoinEach; ++k) {
+      const int part = k0 + k * splits;
+      const bool on = part < all, own = part >= shared;
+      const float *pm, *pl, *po;
+      if (own ? d0 == d1 : c0 == c1) {
+        pm = reinterpret_cast<const float*>((own ? a.stats : p.whole_stats) + at);
+        pl = pm + 1;
+        po = (own ? a.own : p.whole) + at * dh + x;
+      } else if (own) {
+        const int d = d0 + part - shared;
+        pm = a.ws + (2ll * d + (d == d0 ? 1 : 0)) * part_floats(dh) + h % kRows;
+        pl = pm + kRows;
+        po = pm + 2 * kRows + (h % kRows) * (dh - 1) + x;
+      } else {
+        const int c = c0 + part;
+        const float* base = p.parts + (2ll * c + (c == c0 ? 1 : 0)) * (static_cast<long long>(p.m) * (dh + 2));
+        pm = base + r;
+        pl = pm + p.m;
+        po = base + 2 * p.m + (x / 4 * p.m + r) * 4;
       }
-    } else if (split == 0) {
-      const float2 st = __ldcg(p.whole_stats + at);
-      add(st.x, st.y, __ldcg(reinterpret_cast<const float4*>(p.whole + at * dh + x)));
+      m[k] = on ? __ldcg(pm) : -INFINITY;
+      sum[k] = on ? __ldcg(pl) : 0.f;
+      y[k] = on ? __ldcg(reinterpret_cast<const float4*>(po)) : make_float4(0.f, 0.f, 0.f, 0.f);
     }
-  }
-  if (len > skip && split == splits - 1) {
-    const float2 st = __ldcg(a.stats + at);
-    add(st.x, st.y, __ldcg(reinterpret_cast<const float4*>(a.own + at * dh + x)));
+#pragma unroll
+    for (int k = 0; k < kJoinEach; ++k) add(m[k], sum[k], y[k]);
   }
   if (split > 0) {
-    float* mine = js + ((split - 1) * cells + cell) * 6;
-    reinterpret_cast<float2*>(mine)[0] = make_float2(top, l);
-    reinterpret_cast<float2*>(mine)[1] = make_float2(v.x, v.y);
-    reinterpret_cast<float2*>(mine)[2] = make_float2(v.z, v.w);
+    float2* mine = reinterpret_cast<float2*>(js + ((split - 1) * cells + cell) * 6);
+    mine[0] = make_float2(top, l);
+    mine[1] = make_float2(v.x, v.y);
+    mine[2] = make_float2(v.z, v.w);
   }
   __syncthreads();
-  if (split > 0 || !real) return;
-  if (s < 0 || s >= a.c.seqs) {
-    if (s != -1 && x == 0) atomicOr(a.c.status, ST_BADINDEX);
-    return;
-  }
+  if (split > 0 || e.x == -2) return;
   T* out = static_cast<T*>(a.out.p) + i * a.out.row + head * a.out.head + x;
-  if (len == 0) {
-    if (x == 0 && __ldg(a.c.len + s) != 0) atomicOr(a.c.status, ST_BADINDEX);
+  if (e.x == -1) {
     store4(out, make_float4(0.f, 0.f, 0.f, 0.f));
     return;
   }
@@ -812,7 +845,7 @@ int shared_rows(const map_cache* c, long long heads, long long n, long long grou
 }
 int shared_grid(const map_cache* c, int m) { return m == kM && c->dh <= 128 ? 2 * 152 : 152; }
 
-struct SharedSpace { size_t group, of, skip, tile0, stats, own, whole_stats, whole, parts, bytes; };
+struct SharedSpace { size_t group, entries, tile0, own_tile0, stats, own, whole_stats, whole, parts, bytes; };
 SharedSpace shared_space(const map_cache* c, long long heads, long long n, long long groups) {
   SharedSpace s;
   size_t at = (map_cache_attend_workspace(c) + 255) / 256 * 256;
@@ -822,9 +855,9 @@ SharedSpace shared_space(const map_cache* c, long long heads, long long n, long 
     return here;
   };
   s.group = take(groups * sizeof(Group));
-  s.of = take(n * 4);
-  s.skip = take(n * 4);
+  s.entries = take(n * sizeof(Entry));
   s.tile0 = take((groups + 1) * 8);
+  s.own_tile0 = take((n + 1) * 8);
   s.stats = take(n * heads * sizeof(float2));
   s.own = take(n * heads * c->dh * 4);
   s.whole_stats = take(n * heads * sizeof(float2));
@@ -861,8 +894,7 @@ int map_cache_attend_shared(const map_cache* c, int layer, const map_heads* q, c
   p.starts = starts;
   p.groups = groups;
   p.group = reinterpret_cast<Group*>(w + s.group);
-  p.of = reinterpret_cast<int32_t*>(w + s.of);
-  p.skip = reinterpret_cast<int32_t*>(w + s.skip);
+  p.entries = reinterpret_cast<Entry*>(w + s.entries);
   p.tile0 = reinterpret_cast<long long*>(w + s.tile0);
   p.parts = reinterpret_cast<float*>(w + s.parts);
   p.whole_stats = reinterpret_cast<float2*>(w + s.whole_stats);
@@ -871,12 +903,15 @@ int map_cache_attend_shared(const map_cache* c, int layer, const map_heads* q, c
   p.grid = shared_grid(c, p.m);
   CUtensorMap map{};
   p.box = shared_box(a, &map);
-  a.skip = p.skip;
+  a.entries = p.entries;
+  a.tile0 = reinterpret_cast<long long*>(w + s.own_tile0);
   a.stats = reinterpret_cast<float2*>(w + s.stats);
   a.own = reinterpret_cast<float*>(w + s.own);
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   const bool half = c->type == MAP_F16;
-  cudaError_t e = launch_k(shared_plan_kernel, dim3(groups), dim3(kPlan), 0, st, p);
+  // (a cluster a group where they have many sequences on average)
+  const int ranks = n / groups >= 16 ? 8 : 1;
+  cudaError_t e = launch_cluster(shared_plan_kernel, static_cast<unsigned>(groups * ranks), kPlan, ranks, st, p, ranks);
   if (e == cudaSuccess) e = launch_attend<kOwn>(a, st);
   if (e == cudaSuccess) e = half ? launch_shared<__half>(p, map, st) : launch_shared<__nv_bfloat16>(p, map, st);
   if (e == cudaSuccess) {

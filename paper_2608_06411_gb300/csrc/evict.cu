@@ -426,23 +426,6 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) evict_move_kernel(con
   }
 }
 
-template <typename... P, typename... Args>
-cudaError_t launch_cluster(void (*kern)(P...), unsigned grid, unsigned threads, int ranks, cudaStream_t st, const Args&... args) {
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(grid);
-  cfg.blockDim = dim3(threads);
-  cfg.stream = st;
-  cudaLaunchAttribute at[2];
-  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  at[0].val.programmaticStreamSerializationAllowed = pdl_disabled() ? 0 : 1;
-  at[1].id = cudaLaunchAttributeClusterDimension;
-  at[1].val.clusterDim.x = ranks;
-  at[1].val.clusterDim.y = at[1].val.clusterDim.z = 1;
-  cfg.attrs = at;
-  cfg.numAttrs = 2;
-  return cudaLaunchKernelEx(&cfg, kern, args...);
-}
-
 struct EvictSpace { size_t was, taken, kept, bytes; };
 EvictSpace evict_space(const map_cache* c, long long n, long long k) {
   EvictSpace s;

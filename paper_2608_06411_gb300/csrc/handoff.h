@@ -50,6 +50,24 @@ __host__ __device__ __forceinline__ int pieces_of(int len, int size) { return st
 // MAP_OK, MAP_EINVAL or MAP_EUNSUPPORTED for a cache's description (host values only).
 int check_cache(const map_cache* c);
 
+// launch_k of clusters of `ranks` CTAs.
+template <typename... P, typename... Args>
+cudaError_t launch_cluster(void (*kern)(P...), unsigned grid, unsigned threads, int ranks, cudaStream_t st, const Args&... args) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(grid);
+  cfg.blockDim = dim3(threads);
+  cfg.stream = st;
+  cudaLaunchAttribute at[2];
+  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at[0].val.programmaticStreamSerializationAllowed = pdl_disabled() ? 0 : 1;
+  at[1].id = cudaLaunchAttributeClusterDimension;
+  at[1].val.clusterDim.x = ranks;
+  at[1].val.clusterDim.y = at[1].val.clusterDim.z = 1;
+  cfg.attrs = at;
+  cfg.numAttrs = 2;
+  return cudaLaunchKernelEx(&cfg, kern, args...);
+}
+
 // A launch's status as a call's, the runtime's sticky copy of it cleared.
 inline int launch_err(cudaError_t e) {
   if (e == cudaSuccess) return MAP_OK;
