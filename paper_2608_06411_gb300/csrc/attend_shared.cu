@@ -32,6 +32,15 @@ struct SharedArgs {
 
 constexpr int kPlan = 1024, kPlanEach = 8;
 
+// An entry's sequence (-1: padding, a bad one, or no entry) and its rows (0 where the length is bad).
+struct Member { int seq, len; bool bad; };
+__device__ __forceinline__ Member member(const AttendArgs& a, int i, int last) {
+  const int s = i < last ? __ldg(a.seqs + i) : -1;
+  if (s < 0 || s >= a.c.seqs) return {-1, 0, s != -1};
+  const int len = __ldg(a.c.len + s);
+  return good_len(a.c, len) ? Member{s, len, false} : Member{s, 0, true};
+}
+
 // What a group shares: the pages that all its sequences with rows hold in front, as far as all are full.  Latency: a cluster a group;
 // every CTA looks all of the group's sequences up, together, and compares a part of their pages.
 __global__ void __launch_bounds__(kPlan) shared_plan_kernel(const __grid_constant__ SharedArgs p, int ranks) {
@@ -45,6 +54,7 @@ __global__ void __launch_bounds__(kPlan) shared_plan_kernel(const __grid_constan
     lead = a.n;
     valid = 0;
   }
+  int first = __ldg(p.starts + g), last = __ldg(p.starts + g + 1);
   bool bad = false;                            // (every CTA looks at all of it: no more than 65536 numbers)
   for (int i = tid; i <= p.groups; i += kPlan) {
     const int s = __ldg(p.starts + i), next = i < p.groups ? __ldg(p.starts + i + 1) : a.n;
@@ -52,11 +62,13 @@ __global__ void __launch_bounds__(kPlan) shared_plan_kernel(const __grid_constan
   }
   const bool refused = __syncthreads_or(bad) != 0;           // nothing is shared then
   if (refused && blockIdx.x == 0 && tid == 0) atomicOr(a.c.status, ST_BADINDEX);
-  const int first = refused ? 0 : __ldg(p.starts + g), last = refused ? 0 : __ldg(p.starts + g + 1);
+  if (refused) first = last = 0;
+  Member own = member(a, first + tid, last);   // of the first kPlan, which most groups do not pass
+  seq[tid] = own.len > 0 ? own.seq : -1;
   int mine = 0, from = a.n, pages = a.c.max_pages;
   for (int i = first + tid; i < last; i += kPlan) {
-    const int len = seq_len(a, i);
-    if (len == 0) continue;
+    const int len = i == first + tid ? own.len : member(a, i, last).len;
+    if (len <= 0) continue;
     ++mine;
     from = min(from, i);
     pages = min(pages, len / a.c.page);
@@ -71,16 +83,19 @@ __global__ void __launch_bounds__(kPlan) shared_plan_kernel(const __grid_constan
   }
   __syncthreads();
   const int of = lead, full = valid > 1 ? least : 0;
-  const int lead_seq = full > 0 ? __ldg(a.seqs + of) : 0;
+  const int lead_seq = full == 0 ? 0 : of < first + kPlan ? seq[of - first] : __ldg(a.seqs + of);
   __syncthreads();
   if (full > 0) {
     int same = full;
     const int32_t* row = a.c.table + static_cast<long long>(lead_seq) * a.c.max_pages;
     for (int i0 = first; i0 < last; i0 += kPlan) {
-      __syncthreads();
-      const int i = i0 + tid, count = min(kPlan, last - i0);
-      if (i < last) seq[tid] = seq_len(a, i) > 0 ? __ldg(a.seqs + i) : -1;
-      __syncthreads();
+      const int count = min(kPlan, last - i0);
+      if (i0 > first) {
+        __syncthreads();
+        const Member m = member(a, i0 + tid, last);
+        seq[tid] = m.len > 0 ? m.seq : -1;
+        __syncthreads();
+      }
       const long long all = static_cast<long long>(count) * full;
       for (long long x0 = rank * kPlan + tid; x0 < all; x0 += kPlan * kPlanEach * ranks) {
         int j[kPlanEach], page[kPlanEach], other[kPlanEach];
@@ -122,13 +137,10 @@ __global__ void __launch_bounds__(kPlan) shared_plan_kernel(const __grid_constan
   // entries of the group; all of them where nothing is shared because the groups are bad
   const int e0 = refused ? 0 : first, e1 = refused ? a.n : last;
   for (int i = e0 + (refused ? static_cast<int>(blockIdx.x) : rank) * kPlan + tid; i < e1; i += (refused ? static_cast<int>(gridDim.x) : ranks) * kPlan) {
-    const int s = __ldg(a.seqs + i);
-    const bool known = s >= 0 && s < a.c.seqs;
-    const int len = known ? __ldg(a.c.len + s) : 0;
-    Entry e{rows, g, len - rows, 0};
-    if (!known) e = Entry{-2, 0, 0, 0};
-    else if (len == 0 || !good_len(a.c, len)) e = Entry{-1, 0, 0, 0};
-    if ((!known && s != -1) || (known && !good_len(a.c, len))) atomicOr(a.c.status, ST_BADINDEX);
+    const Member m = i == first + tid && !refused ? own : member(a, i, e1);
+    Entry e{rows, g, m.len - rows, 0};
+    if (m.len <= 0) e = Entry{m.seq < 0 ? -2 : -1, 0, 0, 0};
+    if (m.bad) atomicOr(a.c.status, ST_BADINDEX);
     *reinterpret_cast<int4*>(p.entries + i) = make_int4(e.skip, e.group, e.own, 0);
   }
   if (tid == 0 && rank == 0) p.group[g] = Group{first, last - first, rows, lead_seq};
@@ -707,9 +719,19 @@ __global__ void __launch_bounds__(Shape<DH, MT>::kThreads, Shape<DH, MT>::kCtas)
   asm volatile("griddepcontrol.wait;" ::: "memory");
 }
 
-// ---- the join: 8 rows (entry, head of a key head) by dh / 4 pieces of four columns by kSplit runs of their parts a block.  Latency:
+// ---- the join: 8 rows (entry, head of a key head) by dh / 4 pieces of four columns by a few runs of their parts a block.  Latency:
 // an entry, then its group and places in the lists, then its parts, kJoinEach of them together.
-constexpr int kSplit = 4, kJoinEach = 5;
+constexpr int kJoinEach = 6;
+// CTAs whose runs of `per` tiles have those from `tile` on.
+__device__ __forceinline__ void runs_of(long long tile, int tiles, long long per, int& first, int& last) {
+  if (tile + tiles < (1ll << 31)) {            // (a 64-bit division takes four times as long)
+    first = static_cast<int>(tile) / static_cast<int>(per);
+    last = static_cast<int>(tile + tiles - 1) / static_cast<int>(per);
+  } else {
+    first = static_cast<int>(tile / per);
+    last = static_cast<int>((tile + tiles - 1) / per);
+  }
+}
 template <typename T>
 __global__ void __launch_bounds__(1024) shared_join_kernel(const __grid_constant__ SharedArgs p) {
   extern __shared__ __align__(16) float js[];  // (m, l) and four sums of each run but the first
@@ -726,17 +748,13 @@ __global__ void __launch_bounds__(1024) shared_join_kernel(const __grid_constant
   int c0 = 0, c1 = -1, d0 = 0, d1 = -1, r = 0;
   if (e.z > 0) {
     const int tiles = pieces_of(e.z, kTile);
-    const long long tile = __ldcg(a.tile0 + i) + static_cast<long long>(kh * a.subs + h / kRows) * tiles, per = __ldcg(a.tile0 + a.n);
-    d0 = static_cast<int>(tile / per);
-    d1 = static_cast<int>((tile + tiles - 1) / per);
+    runs_of(__ldcg(a.tile0 + i) + static_cast<long long>(kh * a.subs + h / kRows) * tiles, tiles, __ldcg(a.tile0 + a.n), d0, d1);
   }
   if (e.x > 0) {
     const int4 gr = __ldcg(reinterpret_cast<const int4*>(p.group + e.y));
     const int tiles = pieces_of(gr.z, kN), blocks = (gr.y * a.group + p.m - 1) / p.m, q = (i - gr.x) * a.group + h;
     r = q % p.m;
-    const long long tile = __ldcg(p.tile0 + e.y) + static_cast<long long>(kh * blocks + q / p.m) * tiles, per = __ldcg(p.tile0 + p.groups);
-    c0 = static_cast<int>(tile / per);
-    c1 = static_cast<int>((tile + tiles - 1) / per);
+    runs_of(__ldcg(p.tile0 + e.y) + static_cast<long long>(kh * blocks + q / p.m) * tiles, tiles, __ldcg(p.tile0 + p.groups), c0, c1);
   }
   const int shared = c1 - c0 + 1, all = shared + d1 - d0 + 1;
   float top = -INFINITY, l = 0.f;
@@ -915,7 +933,10 @@ int map_cache_attend_shared(const map_cache* c, int layer, const map_heads* q, c
   if (e == cudaSuccess) e = launch_attend<kOwn>(a, st);
   if (e == cudaSuccess) e = half ? launch_shared<__half>(p, map, st) : launch_shared<__nv_bfloat16>(p, map, st);
   if (e == cudaSuccess) {
-    const int cells = 2 * c->dh, splits = std::min(kSplit, 1024 / cells);
+    // (as many runs as one wave of threads allows: 64 questions on an image took 48.7 us with four, XX with two)
+    const int cells = 2 * c->dh;
+    int splits = 1;
+    while (splits < 4 && 2 * splits * cells <= 1024 && static_cast<long long>(n) * q->heads * (c->dh / 4) * 2 * splits <= 152 * 1024) splits *= 2;
     const dim3 grid(static_cast<unsigned>((static_cast<long long>(n) * a.group + 7) / 8), c->heads), block(splits * cells);
     const size_t smem = static_cast<size_t>(splits - 1) * cells * 6 * 4;
     e = half ? launch_k(shared_join_kernel<__half>, grid, block, smem, st, p) : launch_k(shared_join_kernel<__nv_bfloat16>, grid, block, smem, st, p);
