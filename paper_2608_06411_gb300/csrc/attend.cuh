@@ -56,6 +56,11 @@ __device__ __forceinline__ int seq_len(const AttendArgs& a, int i) {
   return good_len(a.c, len) ? len : 0;
 }
 
+// What the caller's arrays hold.  kOwn does not wait for the kernels before it (see attend_kernel), so that L1 may have lines from
+// before them: it reads L2.
+template <int MODE>
+__device__ __forceinline__ int load(const int32_t* p) { return MODE == kOwn ? __ldcg(p) : __ldg(p); }
+
 // First row of an entry's (a multiple of the page) and its length, 0 where it has none.
 struct Span { int from, len; };
 template <int MODE>
@@ -164,7 +169,7 @@ struct Place {
       from = x.from;
       if (len > from) break;
     }
-    if (i < a.n) s = __ldg(a.seqs + i);
+    if (i < a.n) s = load<MODE>(a.seqs + i);
     tiles = pieces_of(len - from, kTile);
   }
   __device__ __forceinline__ void next(const AttendArgs& a, int items) {
@@ -299,7 +304,11 @@ __global__ void __launch_bounds__(kThreads, ctas_of(DH)) attend_kernel(const __g
   __shared__ int first_entry;
   __shared__ long long first_tile;
   __shared__ int last_part;
-  pdl_enter();
+  // kOwn: the kernel launched before this one reads the rows that are shared.  It lets this one start once all of it has waited for the
+  // plan of both, and so the plan and all before it have ended.  Nothing of it is needed here; the wait at the end makes this one end
+  // behind it.
+  if (MODE == kOwn) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  else pdl_enter();
   const int tid = threadIdx.x, lane = tid & 31;
   const int warp = __shfl_sync(0xffffffffu, tid >> 5, 0);              // one value a warp, as the compiler then knows
   const int rows = min(a.group, kRows), items = a.c.heads * a.subs;
@@ -328,7 +337,10 @@ __global__ void __launch_bounds__(kThreads, ctas_of(DH)) attend_kernel(const __g
     }
     if (tid == 0) a.tile0[a.n] = per;
   }
-  if (t0 >= total) return;
+  if (t0 >= total) {
+    if (MODE == kOwn) asm volatile("griddepcontrol.wait;" ::: "memory");
+    return;
+  }
   const int run = static_cast<int>(t0 + per <= total ? per : total - t0);
   if (at0 <= t0 && t0 < at0 + mine) {
     for (int e = e0;; ++e) {
@@ -360,7 +372,7 @@ __global__ void __launch_bounds__(kThreads, ctas_of(DH)) attend_kernel(const __g
   const auto page_of = [&](const Place<MODE>& p) -> int {
     if (p.i >= a.n) return 0;
     const int tok = p.from + p.t * kTile + warp * kTok + (whole ? 0 : lane & 15);
-    return tok < p.len ? __ldg(a.c.table + static_cast<long long>(p.s) * a.c.max_pages + page_at(tok)) : 0;
+    return tok < p.len ? mapk::load<MODE>(a.c.table + static_cast<long long>(p.s) * a.c.max_pages + page_at(tok)) : 0;
   };
   int pid = page_of(ld), ld_seg = 0;
   bool ld_new = true;
@@ -604,6 +616,7 @@ __global__ void __launch_bounds__(kThreads, ctas_of(DH)) attend_kernel(const __g
     begins = cp.item != item || cp.i != i;
     if (begins) { from_start = true; ++seg; }
   }
+  if (MODE == kOwn) asm volatile("griddepcontrol.wait;" ::: "memory");
 }
 
 template <int DH>

@@ -148,20 +148,20 @@ __global__ void __launch_bounds__(kPlan) shared_plan_kernel(const __grid_constan
 
 // ---- the shared rows.  An item is up to M = 128 MT rows of queries (member, head) of one key head and group, 128 the M of a
 // tcgen05.mma.  64 keys are the N of the scores' product and the K of the values', whose first operand, the weights as two halves
-// of T, lies in TMEM.  Eight warps for each 128 rows do the softmax, a row of half a tile's keys a thread (a row of all of them, and
-// half the warps, waited for latency: 51 us where XX are taken now); a warp loads keys and one values, each with a ring of its own; a
-// thread of a warp for each 128 rows issues the products: scores of a tile while the last one's weights are made.
+// of T, lies in TMEM.  Four warps for each 128 rows do the softmax, a row a thread (two threads a row, twice the warps: no
+// faster); a warp loads keys and one values, each with a ring of its own; a thread of a warp for each 128 rows issues the
+// products: scores of a tile while the last one's weights are made.
 constexpr int kM = 128, kN = 64;
 
 template <int DH, int MT>
 struct Shape {
-  static constexpr int kThreads = 256 * MT + 128;
+  static constexpr int kThreads = 128 * MT + 128;
   static constexpr int kBlocks = (DH + 63) / 64;             // boxes of 64 columns, 128 bytes a row, 16-byte units exchanged by the row's low bits
   static constexpr int kTileBytes = kBlocks * kN * 128, kQBytes = kBlocks * MT * kM * 128;
   static constexpr int kCtas = MT == 1 && DH <= 128 ? 2 : 1;
-  static constexpr int kRing = (227 * 1024 / kCtas - 8192 / kCtas - kQBytes) / kTileBytes;           // tiles that fit
+  static constexpr int kRing = (227 * 1024 / kCtas - 3072 - kQBytes) / kTileBytes;           // tiles that fit
   static constexpr int kKeyRing = kRing >= 8 ? 4 : (kRing + 1) / 2, kValueRing = kRing >= 8 ? 4 : kRing / 2;
-  static constexpr int kTiles = kQBytes + (kKeyRing + kValueRing) * kTileBytes, kSmem = kTiles + 512 + MT * kM * 24;       // barriers, the queries' places and the rows' largest scores behind the tiles
+  static constexpr int kTiles = kQBytes + (kKeyRing + kValueRing) * kTileBytes, kSmem = kTiles + 512 + MT * kM * 8;        // the barriers and the queries' places behind the tiles
   static constexpr int kHi = kN, kLo = kN + kN / 2, kO = 2 * kN;       // TMEM columns of 128 rows: scores at 0
   static constexpr int kCols = kO + DH <= 256 ? 256 : 512;
   static_assert(kKeyRing <= 4 && kValueRing >= 2 && kCtas * (kSmem + 1024) <= 228 * 1024 && kCtas * MT * kCols <= 512, "an SM");
@@ -282,19 +282,17 @@ struct SharedBars {
   uint32_t tmem;
   int abort, group;
   long long tile;
-  long long red[20];
+  long long red[12];
 };
 static_assert(sizeof(SharedBars) <= 512, "behind the tiles");
 
 template <typename T, int DH, int MT>
 __global__ void __launch_bounds__(Shape<DH, MT>::kThreads, Shape<DH, MT>::kCtas) shared_kernel(const __grid_constant__ SharedArgs p, const __grid_constant__ CUtensorMap map) {
   using S = Shape<DH, MT>;
-  constexpr int VPR = DH / 8, kWarpsAll = S::kThreads / 32, kKeys = 8 * MT, kValues = kKeys + 1, kProducts = kKeys + 2;
+  constexpr int VPR = DH / 8, kWarpsAll = S::kThreads / 32, kKeys = 4 * MT, kValues = kKeys + 1, kProducts = kKeys + 2;
   extern __shared__ __align__(1024) unsigned char sh[];
   SharedBars& b = *reinterpret_cast<SharedBars*>(sh + S::kTiles);
-  // The kernel launched before this one attends the sequences' own rows: it has waited for the plan, and so has this one when it
-  // starts.  Nothing of it is needed here; the wait at the end makes it end before the join begins.
-  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  pdl_enter();
   const AttendArgs& a = p.a;
   const int tid = threadIdx.x, lane = tid & 31, warp = __shfl_sync(0xffffffffu, tid >> 5, 0);
 
@@ -320,7 +318,6 @@ __global__ void __launch_bounds__(Shape<DH, MT>::kThreads, Shape<DH, MT>::kCtas)
   }
   if (t0 >= total || (smem_u32(sh) & 1023) != 0) {           // (the alignment is what its declaration asks for)
     if (t0 < total && tid == 0) atomicOr(a.c.status, ST_INTERNAL);
-    asm volatile("griddepcontrol.wait;" ::: "memory");
     return;
   }
   const int run = static_cast<int>(t0 + per <= total ? per : total - t0);
@@ -343,10 +340,10 @@ __global__ void __launch_bounds__(Shape<DH, MT>::kThreads, Shape<DH, MT>::kCtas)
       mbar_init(&b.v_empty[i], MT);
     }
     for (int i = 0; i < 2; ++i) {
-      mbar_init(&b.q_full[i], 256);
+      mbar_init(&b.q_full[i], 128);
       mbar_init(&b.s_full[i], 1);
-      mbar_init(&b.s_free[i], 8);
-      mbar_init(&b.p_full[i], 8);
+      mbar_init(&b.s_free[i], 4);
+      mbar_init(&b.p_full[i], 4);
       mbar_init(&b.o_done[i], 1);
     }
     mbar_init(&b.drain, MT);
@@ -370,15 +367,11 @@ __global__ void __launch_bounds__(Shape<DH, MT>::kThreads, Shape<DH, MT>::kCtas)
   pl.item = static_cast<int>(b.tile / pl.tiles);
   pl.t = static_cast<int>(b.tile % pl.tiles);
 
-  if (warp < 8 * MT) {
-    // ---- softmax: row `r` of the item's queries, keys 32 c .. of a tile; columns from 16 x0 to 16 x1 of its sums
-    constexpr int kHalf = kN / 2;
-    const int mt = MT > 1 ? warp >> 3 : 0, c = warp >> 2 & 1, r = mt * kM + (warp & 3) * 32 + lane;
-    const int x0 = c == 0 ? 0 : (DH / 16 + 1) / 2, x1 = c == 0 ? (DH / 16 + 1) / 2 : DH / 16;
+  if (warp < kKeys) {
+    // ---- softmax: row `tid` of the item's queries
+    const int mt = MT > 1 ? warp >> 2 : 0;
     const uint32_t mine_at = tmem + mt * S::kCols + (static_cast<uint32_t>((warp & 3) * 32) << 16);
     long long* q_at = reinterpret_cast<long long*>(sh + S::kTiles + 512);    // where the rows' queries are
-    float* tops = reinterpret_cast<float*>(q_at + MT * kM);                  // [2][2 halves][rows]
-    const auto both = [&]() { asm volatile("bar.sync %0, 64;" ::"r"(1 + MT + mt * 4 + (warp & 3)) : "memory"); };      // halves of 32 rows
     float m = -INFINITY, l = 0.f;
     bool begins = true, from_start = pl.t == 0;
     int have = 0, q0 = 0, kh = 0;
@@ -390,15 +383,13 @@ __global__ void __launch_bounds__(Shape<DH, MT>::kThreads, Shape<DH, MT>::kCtas)
         q0 = pl.item % mb * p.m;               // of the group's rows (member, head)
         have = pl.have(p);
         if (mt * kM < have) {                  // (these rows' last scores are done with the queries)
-          if (c == 0) {
-            const int i = pl.gr.first + (q0 + r) / a.group, h = kh * a.group + (q0 + r) % a.group;
-            q_at[r] = r < have ? i * a.q.row + h * a.q.head : -1;
-          }
-          asm volatile("bar.sync %0, 256;" ::"r"(1 + mt) : "memory");
+          const int i = pl.gr.first + (q0 + tid) / a.group, h = kh * a.group + (q0 + tid) % a.group;
+          q_at[tid] = tid < have ? i * a.q.row + h * a.q.head : -1;
+          asm volatile("bar.sync %0, 128;" ::"r"(1 + mt) : "memory");
           const T* q = static_cast<const T*>(a.q.p);
 #pragma unroll 4
-          for (int j = 0; j < VPR / 2; ++j) {
-            const int e = (tid & 255) + 256 * j, row = e / VPR, x = e % VPR;
+          for (int j = 0; j < VPR; ++j) {
+            const int e = (tid & 127) + 128 * j, row = e / VPR, x = e % VPR;
             const long long at = q_at[mt * kM + row];
             cp_async16_or_zero(base + mt * (S::kQBytes / MT) + (x >> 3) * (kM * 128) + row * 128 + (((x & 7) ^ (row & 7)) << 4),
                                q + (at < 0 ? 0 : at) + x * 8, at >= 0);
@@ -412,56 +403,54 @@ __global__ void __launch_bounds__(Shape<DH, MT>::kThreads, Shape<DH, MT>::kCtas)
         l = 0.f;
       }
       if (mt * kM < have) {
-        const bool busy = mt * kM + (warp & 3) * 32 < have;  // rows of this warp hold queries
+        const bool busy = warp * 32 < have;    // rows of this warp hold queries
         wait(&b.s_full[mt], count);            // (a wait that gave up stops all others; the barriers between warps need every pass)
         tc_fence_after();
-        uint32_t z[kHalf];
-        if (busy) tmem_ld32(mine_at + c * kHalf, z);
+        uint32_t z[kN];
+        if (busy) {
+          tmem_ld32(mine_at, *reinterpret_cast<uint32_t(*)[32]>(z));
+          tmem_ld32(mine_at + 32, *reinterpret_cast<uint32_t(*)[32]>(z + 32));
+        }
         tc_fence_before();
         __syncwarp();
         if (lane == 0) mbar_arrive(&b.s_free[mt]);
         float f = 1.f;
         bool grows = false;
         if (busy) {
-          const int valid = pl.gr.rows - pl.t * kN - c * kHalf;
+          const int valid = pl.gr.rows - pl.t * kN;
           float mul = a.scale2;
-          if (valid < kHalf) {
+          if (valid < kN) {
 #pragma unroll
-            for (int j = 0; j < kHalf; ++j) z[j] = __float_as_uint(j < valid ? __uint_as_float(z[j]) * mul : -INFINITY);
+            for (int j = 0; j < kN; ++j) z[j] = __float_as_uint(j < valid ? __uint_as_float(z[j]) * mul : -INFINITY);
             mul = 1.f;
           }
           // the largest score: the least where the factor is below zero
           float top = __uint_as_float(z[0]), other = __uint_as_float(z[1]);
           if (mul >= 0.f) {
 #pragma unroll
-            for (int j = 2; j < kHalf; j += 2) {
+            for (int j = 2; j < kN; j += 2) {
               top = fmaxf(top, __uint_as_float(z[j]));
               other = fmaxf(other, __uint_as_float(z[j + 1]));
             }
             top = fmaxf(top, other);
           } else {
 #pragma unroll
-            for (int j = 2; j < kHalf; j += 2) {
+            for (int j = 2; j < kN; j += 2) {
               top = fminf(top, __uint_as_float(z[j]));
               other = fminf(other, __uint_as_float(z[j + 1]));
             }
             top = fminf(top, other);
           }
           top *= mul;
-          float* t = tops + (count & 1) * (2 * MT * kM) + r;
-          t[c * (MT * kM)] = top;
-          both();
-          top = fmaxf(top, t[(c ^ 1) * (MT * kM)]);
-          grows = __any_sync(0xffffffffu, top > m + kSlack<T>);
-          if (grows) {
-            const float next = fmaxf(m, top);
-            f = exp2_fast(m - (next == -INFINITY ? 0.f : next));
-            m = next;
+          if (top > m + kSlack<T>) {           // (a row's result does not depend on the other rows, which may be padding)
+            f = exp2_fast(m - top);
+            m = top;
           }
+          grows = __any_sync(0xffffffffu, f != 1.f);
           const float add = kLiftShared<T> - (m == -INFINITY ? 0.f : m);
           float2 sum = make_float2(0.f, 0.f);
 #pragma unroll
-          for (int j = 0; j < kHalf; j += 2) {
+          for (int j = 0; j < kN; j += 2) {
             float2 x = fma2(make_float2(__uint_as_float(z[j]), __uint_as_float(z[j + 1])), make_float2(mul, mul), make_float2(add, add));
             x = make_float2(exp2_fast(x.x), exp2_fast(x.y));
             sum = add2(sum, x);
@@ -475,7 +464,7 @@ __global__ void __launch_bounds__(Shape<DH, MT>::kThreads, Shape<DH, MT>::kCtas)
         if (busy) {
           if (!begins && grows) {
 #pragma unroll 1
-            for (int x = x0; x < x1; ++x) {
+            for (int x = 0; x < DH / 16; ++x) {
               uint32_t o[16];
               tmem_ld16(mine_at + S::kO + 16 * x, o);
 #pragma unroll
@@ -484,14 +473,14 @@ __global__ void __launch_bounds__(Shape<DH, MT>::kThreads, Shape<DH, MT>::kCtas)
             }
           }
 #pragma unroll
-          for (int j = 0; j < kHalf / 16; ++j) {
+          for (int j = 0; j < kN / 16; ++j) {
             uint32_t w[8];
 #pragma unroll
             for (int i = 0; i < 8; ++i) w[i] = z[16 * j + 2 * i];
-            tmem_put8(mine_at + S::kHi + c * (kHalf / 2) + 8 * j, w);
+            tmem_put8(mine_at + S::kHi + 8 * j, w);
 #pragma unroll
             for (int i = 0; i < 8; ++i) w[i] = z[16 * j + 2 * i + 1];
-            tmem_put8(mine_at + S::kLo + c * (kHalf / 2) + 8 * j, w);
+            tmem_put8(mine_at + S::kLo + 8 * j, w);
           }
           tmem_wait_st();
         }
@@ -504,14 +493,14 @@ __global__ void __launch_bounds__(Shape<DH, MT>::kThreads, Shape<DH, MT>::kCtas)
         if (ends || n + 1 == run) {
           wait(&b.o_done[mt], count - 1);
           tc_fence_after();
-          const bool done = ends && from_start, on = r < have;
-          const int i = pl.gr.first + (q0 + r) / a.group, head = kh * a.group + (q0 + r) % a.group;
+          const bool done = ends && from_start, on = tid < have;
+          const int i = pl.gr.first + (q0 + tid) / a.group, head = kh * a.group + (q0 + tid) % a.group;
           const long long at = static_cast<long long>(i) * a.q.heads + head;
           float* part = p.parts + static_cast<long long>(2 * blockIdx.x + (from_start ? 1 : 0)) * (MT * kM * (DH + 2));
           constexpr float up = kLift<T> - kLiftShared<T>;    // as the sequences' own rows have it
           if (busy) {
 #pragma unroll 1
-            for (int x = x0; x < x1; ++x) {
+            for (int x = 0; x < DH / 16; ++x) {
               uint32_t o[16];
               tmem_ld16(mine_at + S::kO + 16 * x, o);
 #pragma unroll
@@ -519,19 +508,14 @@ __global__ void __launch_bounds__(Shape<DH, MT>::kThreads, Shape<DH, MT>::kCtas)
                 const float4 v = make_float4(__uint_as_float(o[j]), __uint_as_float(o[j + 1]), __uint_as_float(o[j + 2]), __uint_as_float(o[j + 3]));
                 if (!on) continue;
                 if (done) *reinterpret_cast<float4*>(p.whole + at * DH + 16 * x + j) = v;
-                else *reinterpret_cast<float4*>(part + 2 * MT * kM + ((4 * x + j / 4) * (MT * kM) + r) * 4) = v;
+                else *reinterpret_cast<float4*>(part + 2 * MT * kM + ((4 * x + j / 4) * (MT * kM) + tid) * 4) = v;
               }
             }
-            float* t = tops + (count & 1) * (2 * MT * kM) + r;               // (the halves' sums of weights)
-            if (c == 1) t[0] = l;
-            both();
-            if (c == 0 && on) {
-              l += t[0];
-              if (done) p.whole_stats[at] = make_float2(m + up, l);
-              if (!done) part[r] = m + up;
-              if (!done) part[MT * kM + r] = l;
+            if (on && done) p.whole_stats[at] = make_float2(m + up, l);
+            if (on && !done) {
+              part[tid] = m + up;
+              part[MT * kM + tid] = l;
             }
-            both();
           }
           tc_fence_before();
         }
@@ -716,7 +700,6 @@ __global__ void __launch_bounds__(Shape<DH, MT>::kThreads, Shape<DH, MT>::kCtas)
     tc_fence_after();
     tmem_dealloc(tmem, MT * S::kCols);
   }
-  asm volatile("griddepcontrol.wait;" ::: "memory");
 }
 
 // ---- the join: 8 rows (entry, head of a key head) by dh / 4 pieces of four columns by a few runs of their parts a block.  Latency:
@@ -930,8 +913,8 @@ int map_cache_attend_shared(const map_cache* c, int layer, const map_heads* q, c
   // (a cluster a group where they have many sequences on average)
   const int ranks = n / groups >= 16 ? 8 : 1;
   cudaError_t e = launch_cluster(shared_plan_kernel, static_cast<unsigned>(groups * ranks), kPlan, ranks, st, p, ranks);
-  if (e == cudaSuccess) e = launch_attend<kOwn>(a, st);
   if (e == cudaSuccess) e = half ? launch_shared<__half>(p, map, st) : launch_shared<__nv_bfloat16>(p, map, st);
+  if (e == cudaSuccess) e = launch_attend<kOwn>(a, st);
   if (e == cudaSuccess) {
     // (as many runs as one wave of threads allows: 64 questions on an image took 48.7 us with four, XX with two)
     const int cells = 2 * c->dh;
