@@ -11,7 +11,7 @@
 namespace mapk {
 namespace {
 
-constexpr int kRowsEach = 4, kPiece = kRowsEach * kThreads;
+constexpr int kRowsEach = 4, kPiece = kRowsEach * kThreads, kHeadsEach = 8;      // neighbouring rows of a thread; heads at once
 
 __global__ void __launch_bounds__(kThreads) weigh_kernel(const __grid_constant__ AttendArgs a, float* __restrict__ weights,
                                                          int max_rows) {
@@ -48,35 +48,51 @@ __global__ void __launch_bounds__(kThreads) weigh_kernel(const __grid_constant__
     if (count == 0) continue;
     // the first of a sequence's rows adds up for all of them
     const int s = __ldg(a.seqs + e);
-    bool before = false, behind = false;
-    for (int j = tid; j < a.n; j += kThreads)
-      if (__ldg(a.seqs + j) == s) (j < e ? before : behind) |= j != e;
-    before = __syncthreads_or(before);
-    behind = __syncthreads_or(behind);
+    int twice = 0;                             // 1: it is named before, 2: behind
+    for (int j = tid; j < a.n && a.n > 1; j += kThreads)
+      if (__ldg(a.seqs + j) == s && j != e) twice |= j < e ? 1 : 2;
+    if (a.n > 1) {
+      const int before = __syncthreads_or(twice & 1);
+      twice = __syncthreads_or(twice & 2);
+      if (before) twice = -1;
+    }
     t += last - at;
-    if (before) continue;
+    if (twice < 0) continue;
     for (; at < last; ++at) {
-      const int kh = static_cast<int>(at / count), row0 = static_cast<int>(at % count) * kPiece + tid;
-      float sum[kRowsEach] = {};
-      for (int j = e; j < a.n; ++j) {
-        if (j != e && (!behind || __ldg(a.seqs + j) != s)) {
-          if (!behind) break;
-          continue;
-        }
-        const long long head0 = static_cast<long long>(j) * a.q.heads + kh * a.group;
-#pragma unroll 4
-        for (int g = 0; g < a.group; ++g) {
-          const float2 st = __ldcg(a.stats + head0 + g);
-          const float* z = a.z + (head0 + g) * a.z_row + row0;
-#pragma unroll
-          for (int k = 0; k < kRowsEach; ++k)
-            if (row0 + k * kThreads < len) sum[k] = fmaf(exp2_fast(__ldcg(z + k * kThreads) - st.x), st.y, sum[k]);
-        }
-      }
+      const int kh = static_cast<int>(at / count), row0 = static_cast<int>(at % count) * kPiece + tid * kRowsEach;
       float* w = weights + (static_cast<long long>(s) * a.c.heads + kh) * max_rows + row0;
+      float sum[kRowsEach], was[kRowsEach];
+#pragma unroll
+      for (int k = 0; k < kRowsEach; ++k) {
+        sum[k] = 0.f;
+        was[k] = row0 + k < len ? w[k] : 0.f;
+      }
+      for (int j = e; j < a.n; ++j) {
+        if (j != e && __ldg(a.seqs + j) != s) continue;
+        const long long head0 = static_cast<long long>(j) * a.q.heads + kh * a.group;
+        for (int g0 = 0; g0 < a.group; g0 += kHeadsEach) {   // (loads of several heads in flight)
+          float2 st[kHeadsEach];
+          float4 z[kHeadsEach];
+#pragma unroll
+          for (int g = 0; g < kHeadsEach; ++g) {
+            const bool on = g0 + g < a.group && row0 < len;  // (scores come 16 at a time, those past the last row -inf)
+            st[g] = on ? __ldcg(a.stats + head0 + g0 + g) : make_float2(0.f, 0.f);
+            z[g] = on ? __ldcg(reinterpret_cast<const float4*>(a.z + (head0 + g0 + g) * a.z_row + row0))
+                      : make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY);
+          }
+#pragma unroll
+          for (int g = 0; g < kHeadsEach; ++g) {
+            if (g0 + g >= a.group) break;
+            const float y[kRowsEach] = {z[g].x, z[g].y, z[g].z, z[g].w};
+#pragma unroll
+            for (int k = 0; k < kRowsEach; ++k) sum[k] = fmaf(exp2_fast(y[k] - st[g].x), st[g].y, sum[k]);
+          }
+        }
+        if (!twice) break;
+      }
 #pragma unroll
       for (int k = 0; k < kRowsEach; ++k)
-        if (row0 + k * kThreads < len) w[k * kThreads] += sum[k];
+        if (row0 + k < len) w[k] = was[k] + sum[k];
     }
   }
 }

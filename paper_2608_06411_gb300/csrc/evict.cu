@@ -30,7 +30,7 @@ struct EvictArgs {
   int32_t* kept;                           // [n][layers][heads][k]: rows that stay of those that may leave
 };
 
-// Checks, lengths, pages.  Latency-bound, one CTA (see extend_kernel); the columns of all entries form one list.
+// Checks, new lengths, pages.  Latency-bound, one CTA (see extend_kernel); the columns of all entries form one list.
 __global__ void __launch_bounds__(kPlanThreads) evict_plan_kernel(const EvictArgs a) {
   extern __shared__ int sh[];
   const map_cache& c = a.c;
@@ -106,7 +106,6 @@ __global__ void __launch_bounds__(kPlanThreads) evict_plan_kernel(const EvictArg
   for (int i = threadIdx.x; i < a.n; i += kPlanThreads) {
     const int s = enough ? seq[i] : -1;
     a.entries[i] = s < 0 ? Eviction{-1, 0, 0, 0} : Eviction{s, len[i], first[i], left[i]};
-    if (s >= 0) c.len[s] = left[i];
   }
   if (!enough) return;
   __syncthreads();                             // the new pages are there
@@ -153,16 +152,23 @@ __device__ __forceinline__ int cluster_size() {
 }
 
 struct Unit { Eviction e; int entry, layer, head; long long id; };
-__device__ __forceinline__ Unit unit_of(const EvictArgs& a, unsigned u) {       // (entry, layer, head)
+__device__ __forceinline__ Unit unit_of(const EvictArgs& a, unsigned u) {       // (entry, layer, head), without the entry's Eviction
   const unsigned heads = a.c.heads, layers = a.c.layers, r = u / heads;
   Unit x;
   x.id = u;
   x.head = u - r * heads;
   x.entry = r / layers;
   x.layer = r - x.entry * layers;
-  const int4 e = __ldcg(reinterpret_cast<const int4*>(a.entries + x.entry));
-  x.e = Eviction{e.x, e.y, e.z, e.w};
   return x;
+}
+// What the plan will find for an entry, if it does not refuse the call.
+__device__ __forceinline__ Eviction eviction_of(const EvictArgs& a, int i) {
+  const int s = __ldcg(a.seqs + i), f = a.first ? __ldcg(a.first + i) : 0, l = a.last ? __ldcg(a.last + i) : 0;
+  if (s < 0 || s >= a.c.seqs || f < 0 || l < 0) return {-1, 0, 0, 0};
+  const int n = __ldcg(a.c.len + s);
+  const long long window = static_cast<long long>(n) - f - l;
+  if (!good_len(a.c, n) || window <= a.k) return {-1, 0, 0, 0};
+  return {s, n, f, n - static_cast<int>(window) + a.k};
 }
 __device__ __forceinline__ float* weights_of(const EvictArgs& a, const Unit& x) {
   return a.weights + ((static_cast<long long>(x.layer) * a.c.seqs + x.e.seq) * a.c.heads + x.head) * (static_cast<long long>(a.c.max_pages) * a.c.page);
@@ -179,10 +185,16 @@ __global__ void __launch_bounds__(THREADS, 1280 / THREADS) evict_select_kernel(c
   __shared__ uint32_t pick_bin;
   __shared__ int pick_want, pick_size;
   __shared__ __align__(16) int4 mine;          // candidates of this CTA above the digits found, and with them
-  pdl_enter();
+  // Beside the plan, which starts this kernel once it has waited for those before it, and writes nothing that is read here (loads go
+  // to L2: without a wait L1 may have older lines).  The wait at the end makes this kernel end behind the plan.
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, ranks = cluster_size(), rank = blockIdx.x % ranks;
-  const Unit x = unit_of(a, blockIdx.x / ranks);
-  if (x.e.seq < 0 || a.k == 0) return;         // (one decision a cluster)
+  Unit x = unit_of(a, blockIdx.x / ranks);
+  x.e = eviction_of(a, x.entry);
+  if (x.e.seq < 0 || a.k == 0) {               // (one decision a cluster)
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    return;
+  }
   const int window = x.e.len - x.e.left + a.k, each = (window + ranks - 1) / ranks;
   const int t0 = min(window, rank * each), t1 = min(window, t0 + each);
   const float* w = weights_of(a, x) + x.e.first;
@@ -333,6 +345,7 @@ __global__ void __launch_bounds__(THREADS, 1280 / THREADS) evict_select_kernel(c
     }
   }
   if (ranks > 1) cluster_sync();               // no CTA leaves while another may read its counts
+  asm volatile("griddepcontrol.wait;" ::: "memory");
 }
 
 // The rows that move, a slice of a unit's columns (or its weights) a CTA.  THREADS / wide rows are read together, a 16-byte vector a
@@ -345,7 +358,9 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) evict_move_kernel(con
   pdl_enter();
   const map_cache& c = a.c;
   const int tid = threadIdx.x, parts = 2 * slices + 1, part = blockIdx.x % parts;
-  const Unit x = unit_of(a, blockIdx.x / parts);
+  Unit x = unit_of(a, blockIdx.x / parts);
+  const int4 planned = __ldcg(reinterpret_cast<const int4*>(a.entries + x.entry));
+  x.e = Eviction{planned.x, planned.y, planned.z, planned.w};
   if (x.e.seq < 0) return;
   const Eviction& e = x.e;
   const int tail = e.left - e.first - a.k;
@@ -372,6 +387,7 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) evict_move_kernel(con
     }
     __syncthreads();                           // the last rows' sources lie where the zeros go
     for (int t = e.left + tid; t < e.len; t += THREADS) w[t] = 0.f;
+    if (x.layer == 0 && x.head == 0 && tid == 0) c.len[e.seq] = e.left;      // (select reads it beside the plan)
     return;
   }
 
@@ -471,7 +487,7 @@ int map_cache_evict(const map_cache* c, float* weights, const int32_t* seqs, int
   // CTAs that look for a unit's rows, and slices that its columns move in: as many as fill the chip where the units do not
   int ranks = 1, slices = 1;
   while (ranks < 8 && units * ranks < 2 * 152 && max_rows / ranks > 2048) ranks *= 2;
-  while (slices < 4 && units * slices < 2 * 152 && c->dh / 8 / slices >= 8) slices *= 2;
+  while (slices < 4 && units * (4 * slices + 1) <= 4 * 152 && c->dh / 8 / slices >= 8) slices *= 2;
   const unsigned select = static_cast<unsigned>(units * ranks);
   if (e == cudaSuccess)
     e = max_rows / ranks > kHold * 256 ? launch_cluster(evict_select_kernel<512>, select, 512, ranks, st, a)
