@@ -704,7 +704,7 @@ __global__ void __launch_bounds__(Shape<DH, MT>::kThreads, Shape<DH, MT>::kCtas)
 
 // ---- the join: 8 rows (entry, head of a key head) by dh / 4 pieces of four columns by a few runs of their parts a block.  Latency:
 // an entry, then its group and places in the lists, then its parts, kJoinEach of them together.
-constexpr int kJoinEach = 6;
+constexpr int kJoinEach = 3;
 // CTAs whose runs of `per` tiles have those from `tile` on.
 __device__ __forceinline__ void runs_of(long long tile, int tiles, long long per, int& first, int& last) {
   if (tile + tiles < (1ll << 31)) {            // (a 64-bit division takes four times as long)
