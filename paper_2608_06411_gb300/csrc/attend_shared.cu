@@ -162,7 +162,7 @@ struct Shape {
   static constexpr int kRing = (227 * 1024 / kCtas - 3072 - kQBytes) / kTileBytes;           // tiles that fit
   static constexpr int kKeyRing = kRing >= 8 ? 4 : (kRing + 1) / 2, kValueRing = kRing >= 8 ? 4 : kRing / 2;
   static constexpr int kTiles = kQBytes + (kKeyRing + kValueRing) * kTileBytes, kSmem = kTiles + 512 + MT * kM * 8;        // the barriers and the queries' places behind the tiles
-  static constexpr int kHi = kN, kLo = kN + kN / 2, kO = 2 * kN;       // TMEM columns of 128 rows: scores at 0
+  static constexpr int kLo = kN / 2, kO = 2 * kN;            // TMEM columns of 128 rows: two tiles' scores, weights in their place; sums
   static constexpr int kCols = kO + DH <= 256 ? 256 : 512;
   static_assert(kKeyRing <= 4 && kValueRing >= 2 && kCtas * (kSmem + 1024) <= 228 * 1024 && kCtas * MT * kCols <= 512, "an SM");
 };
@@ -278,7 +278,7 @@ struct SharedPlace {
 };
 
 struct SharedBars {
-  uint64_t k_full[4], k_empty[4], v_full[4], v_empty[4], q_full[2], s_full[2], s_free[2], p_full[2], o_done[2], drain;
+  uint64_t k_full[4], k_empty[4], v_full[4], v_empty[4], q_full[2], s_full[2][2], p_full[2][2], o_done[2][2], drain;
   uint32_t tmem;
   int abort, group;
   long long tile;
@@ -341,10 +341,11 @@ __global__ void __launch_bounds__(Shape<DH, MT>::kThreads, Shape<DH, MT>::kCtas)
     }
     for (int i = 0; i < 2; ++i) {
       mbar_init(&b.q_full[i], 128);
-      mbar_init(&b.s_full[i], 1);
-      mbar_init(&b.s_free[i], 4);
-      mbar_init(&b.p_full[i], 4);
-      mbar_init(&b.o_done[i], 1);
+      for (int j = 0; j < 2; ++j) {            // (scores, and some of the warps, can be a tile ahead of the others: by the tile's parity)
+        mbar_init(&b.s_full[i][j], 1);
+        mbar_init(&b.p_full[i][j], 4);
+        mbar_init(&b.o_done[i][j], 1);
+      }
     }
     mbar_init(&b.drain, MT);
     b.abort = 0;
@@ -404,19 +405,15 @@ __global__ void __launch_bounds__(Shape<DH, MT>::kThreads, Shape<DH, MT>::kCtas)
       }
       if (mt * kM < have) {
         const bool busy = warp * 32 < have;    // rows of this warp hold queries
-        wait(&b.s_full[mt], count);            // (a wait that gave up stops all others; the barriers between warps need every pass)
+        wait(&b.s_full[mt][count & 1], count >> 1);          // (a wait that gave up stops all others; the barriers between warps need every pass)
         tc_fence_after();
         uint32_t z[kN];
-        if (busy) {
-          tmem_ld32(mine_at, *reinterpret_cast<uint32_t(*)[32]>(z));
-          tmem_ld32(mine_at + 32, *reinterpret_cast<uint32_t(*)[32]>(z + 32));
-        }
-        tc_fence_before();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(&b.s_free[mt]);
         float f = 1.f;
         bool grows = false;
         if (busy) {
+          const uint32_t scores = mine_at + (count & 1) * kN;
+          tmem_ld32(scores, *reinterpret_cast<uint32_t(*)[32]>(z));
+          tmem_ld32(scores + 32, *reinterpret_cast<uint32_t(*)[32]>(z + 32));
           const int valid = pl.gr.rows - pl.t * kN;
           float mul = a.scale2;
           if (valid < kN) {
@@ -458,40 +455,40 @@ __global__ void __launch_bounds__(Shape<DH, MT>::kThreads, Shape<DH, MT>::kCtas)
           }
           l = l * f + (sum.x + sum.y);
         }
-        // the last tile's product is done: its sums can be scaled, its weights overwritten
-        if (count > 0) wait(&b.o_done[mt], count - 1);
-        tc_fence_after();
-        if (busy) {
-          if (!begins && grows) {
+        if (!begins && grows) {                // the sums so far, once the last tile's product is done
+          wait(&b.o_done[mt][(count - 1) & 1], (count - 1) >> 1);
+          tc_fence_after();
 #pragma unroll 1
-            for (int x = 0; x < DH / 16; ++x) {
-              uint32_t o[16];
-              tmem_ld16(mine_at + S::kO + 16 * x, o);
+          for (int x = 0; x < DH / 16; ++x) {
+            uint32_t o[16];
+            tmem_ld16(mine_at + S::kO + 16 * x, o);
 #pragma unroll
-              for (int j = 0; j < 16; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * f);
-              tmem_st16(mine_at + S::kO + 16 * x, o);
-            }
+            for (int j = 0; j < 16; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * f);
+            tmem_st16(mine_at + S::kO + 16 * x, o);
           }
+        }
+        if (busy) {
+          const uint32_t weights = mine_at + (count & 1) * kN;
 #pragma unroll
           for (int j = 0; j < kN / 16; ++j) {
             uint32_t w[8];
 #pragma unroll
             for (int i = 0; i < 8; ++i) w[i] = z[16 * j + 2 * i];
-            tmem_put8(mine_at + S::kHi + 8 * j, w);
+            tmem_put8(weights + 8 * j, w);
 #pragma unroll
             for (int i = 0; i < 8; ++i) w[i] = z[16 * j + 2 * i + 1];
-            tmem_put8(mine_at + S::kLo + 8 * j, w);
+            tmem_put8(weights + S::kLo + 8 * j, w);
           }
           tmem_wait_st();
         }
         tc_fence_before();
         __syncwarp();
-        if (lane == 0) mbar_arrive(&b.p_full[mt]);
+        if (lane == 0) mbar_arrive(&b.p_full[mt][count & 1]);
         ++count;
 
         const bool ends = pl.t + 1 == pl.tiles;
         if (ends || n + 1 == run) {
-          wait(&b.o_done[mt], count - 1);
+          wait(&b.o_done[mt][(count - 1) & 1], (count - 1) >> 1);
           tc_fence_after();
           const bool done = ends && from_start, on = tid < have;
           const int i = pl.gr.first + (q0 + tid) / a.group, head = kh * a.group + (q0 + tid) % a.group;
@@ -637,18 +634,18 @@ __global__ void __launch_bounds__(Shape<DH, MT>::kThreads, Shape<DH, MT>::kCtas)
     int vslot = 0, kslot = 0;
     uint32_t vturn = 0, kturn = 0, items = 0, scored = 0, weighed = 0;
     const auto weigh = [&]() {                 // sums += weights of the last tile * values
-      ok = ok && wait(&b.v_full[vslot], vturn) && (!active || wait(&b.p_full[mt], weighed));
+      ok = ok && wait(&b.v_full[vslot], vturn) && (!active || wait(&b.p_full[mt][weighed & 1], weighed >> 1));
       if (!ok) return;
       if (active) {
-        ++weighed;
         tc_fence_after();
-        const uint32_t vd = desc_low_mn(values + vslot * S::kTileBytes);
+        const uint32_t vd = desc_low_mn(values + vslot * S::kTileBytes), w = tm + (weighed & 1) * kN;
 #pragma unroll
-        for (int k = 0; k < kN / 16; ++k) umma_ts(tm + S::kO, tm + S::kHi + 8 * k, vd + k * (2048 >> 4), kSums, !first || k != 0);
+        for (int k = 0; k < kN / 16; ++k) umma_ts(tm + S::kO, w + 8 * k, vd + k * (2048 >> 4), kSums, !first || k != 0);
 #pragma unroll
-        for (int k = 0; k < kN / 16; ++k) umma_ts(tm + S::kO, tm + S::kLo + 8 * k, vd + k * (2048 >> 4), kSums, 1);
+        for (int k = 0; k < kN / 16; ++k) umma_ts(tm + S::kO, w + S::kLo + 8 * k, vd + k * (2048 >> 4), kSums, 1);
         first = false;
-        umma_commit(&b.o_done[mt]);
+        umma_commit(&b.o_done[mt][weighed & 1]);
+        ++weighed;
         umma_commit(&b.v_empty[vslot]);
       } else {
         mbar_arrive(&b.v_empty[vslot]);
@@ -666,19 +663,20 @@ __global__ void __launch_bounds__(Shape<DH, MT>::kThreads, Shape<DH, MT>::kCtas)
         active = mt * kM < pl.have(p);
         ok = ok && (!active || wait(&b.q_full[mt], items++));
       }
-      ok = ok && wait(&b.k_full[kslot], kturn) && (!active || scored == 0 || wait(&b.s_free[mt], scored - 1));
+      ok = ok && wait(&b.k_full[kslot], kturn) && (!active || scored < 2 || wait(&b.o_done[mt][scored & 1], (scored - 2) >> 1));
       if (!ok) break;
       if (active) {
-        ++scored;
         tc_fence_after();
+        const uint32_t to = tm + (scored & 1) * kN;          // (free: the weights there have been used)
         const uint32_t kd = desc_low(keys + kslot * S::kTileBytes);
 #pragma unroll
         for (int k = 0; k < DH / 16; ++k) {
           const uint32_t qk = qd + (((k >> 2) * (kM * 128) + (k & 3) * 32) >> 4), kk = kd + (((k >> 2) * (kN * 128) + (k & 3) * 32) >> 4);
-          if (k == 0) umma_ss<false>(tm, qk, kk, kScores);
-          else umma_ss<true>(tm, qk, kk, kScores);
+          if (k == 0) umma_ss<false>(to, qk, kk, kScores);
+          else umma_ss<true>(to, qk, kk, kScores);
         }
-        umma_commit(&b.s_full[mt]);
+        umma_commit(&b.s_full[mt][scored & 1]);
+        ++scored;
         umma_commit(&b.k_empty[kslot]);
       } else {
         mbar_arrive(&b.k_empty[kslot]);

@@ -130,6 +130,66 @@ def test_attend_shared_matches_the_formula(mb, case):  # noqa: F811
     cache.check()
 
 
+LONG = [
+    # many tiles a CTA: type, dh, hk, query heads a key head, page, rows in front, rows of each member
+    ("bf16", 128, 2, 4, 16, 60000, [5, 70]),
+    ("f16", 128, 2, 4, 64, 50001, [1 + 3 * i for i in range(40)]),
+    ("bf16", 64, 4, 7, 8, 40000, [9] * 30),
+    ("f16", 96, 2, 3, 5, 31003, [2, 3]),
+    ("bf16", 80, 2, 5, 7, 33333, [1] * 64),
+    ("f16", 192, 1, 2, 32, 60000, [40, 1, 1]),
+    ("bf16", 256, 1, 8, 16, 50000, [33] * 20),
+]
+
+
+@pytest.mark.parametrize("case", LONG, ids=["-".join(str(v) for v in c[:6]) for c in LONG])
+def test_attend_shared_of_long_beginnings(mb, case):  # noqa: F811
+    """As `check`, with the 64-bit values computed by torch."""
+    typ, dh, hk, group, page, front, own = case
+    typ, n, scale = TYPES[typ], len(own), dh ** -0.5
+    cache = grouped(mb, typ, dh, hk, page, [(front, own)], 9)
+    q = randn(gen(6), n, hk * group, dh, typ=typ) * 1.5
+    q[:, 1] *= 3                                                     # a head whose largest score rises by far along the rows
+    out = cache.attend_shared(q, ints(range(n)), 0, ints([0, n]))
+    cache.check()
+    for i in (0, n // 2, n - 1):
+        slots = torch.tensor(slots_of(cache, i), device=DEV)
+        k, v = (cache.pool[0, j][slots // page, :, slots % page].double().transpose(0, 1) for j in (0, 1))
+        qi = q[i].double().view(hk, group, dh)
+        p = torch.softmax(qi @ k.transpose(1, 2) * scale, -1)
+        want, mag = p @ v, p @ v.abs()
+        dz = float((qi.abs() @ k.abs().transpose(1, 2)).max()) * scale
+        e = 2 * (dh / 16 + 3) * 2.0 ** -23 * dz + 2.0 ** -19 + 2.0 ** -16 + (len(slots) / 8 + len(slots) / 64 + 64) * 2.0 ** -23
+        off = (out[i].double().view_as(want) - want).abs()
+        tol = half_step(typ) * want.abs() * 1.001 + e * mag + tiny(typ)
+        assert bool((off <= tol).all()), (i, float((off / tol).max()))
+    assert torch.equal(cache.attend_shared(q, ints(range(n)), 0, ints([0, n])), out)
+
+
+def test_attend_shared_does_not_depend_on_padding(mb):  # noqa: F811
+    """What lies in a padding entry's queries changes nothing, bit for bit; two graphs of calls on one cache replayed in turn."""
+    cache = grouped(mb, torch.float16, 64, 2, 16, [(330, [1, 1, 1])], 4)
+    seqs, starts, q = ints([0, -1, 1, 2]), ints([0, 4]), randn(gen(1), 4, 8, 64, typ=torch.float16)
+    want, graphs = None, []
+    for fill in (0.0, 100.0, float("nan"), float("inf")):
+        q[1] = fill
+        out = cache.attend_shared(q, seqs, 0, starts)
+        want = out[[0, 2, 3]].clone() if want is None else want
+        assert torch.equal(out[[0, 2, 3]], want)
+    for _ in range(2):
+        g, x = torch.cuda.CUDAGraph(), q.clone()
+        with torch.cuda.graph(g):
+            y = cache.attend_shared(x, seqs, 0, starts)
+        graphs.append((g, x, y))
+    for _ in range(3):
+        for i, (g, x, y) in enumerate(graphs):
+            x.copy_(q * (1.0 - 0.5 * i))
+            g.replay()
+        for i, (g, x, y) in enumerate(graphs):
+            assert torch.equal(y[[0, 2, 3]], cache.attend_shared(x, seqs, 0, starts)[[0, 2, 3]])
+    cache.check()
+
+
 def test_attend_shared_of_empty_and_bad_entries(mb):  # noqa: F811
     cache = grouped(mb, torch.bfloat16, 64, 2, 16, [(100, [5, 9, 0]), (40, [1, 30])], 3)
     cache.free(ints([2]))                                            # an empty sequence in a group
