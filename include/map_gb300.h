@@ -477,7 +477,7 @@ int map_cache_attend(const map_cache *cache, int layer, const map_heads *q, cons
  *             rows) have in common in front; a group whose sequences have none is attended as by map_cache_attend.
  *   ws        device scratch of map_cache_attend_shared_workspace(cache, q heads, n, groups) bytes, 16-byte aligned, the
  *             caller's until the call's work completes.
- * groups 1 .. 65535 (MAP_EUNSUPPORTED beyond); everything else as for map_cache_attend.
+ * groups 1 .. 65535, n * q heads < 2^31 (MAP_EUNSUPPORTED beyond); everything else as for map_cache_attend.
  */
 size_t map_cache_attend_shared_workspace(const map_cache *cache, int heads, int n, int groups);
 int map_cache_attend_shared(const map_cache *cache, int layer, const map_heads *q, const int32_t *seqs, int n,

@@ -875,6 +875,7 @@ extern "C" {
 
 size_t map_cache_attend_shared_workspace(const map_cache* c, int heads, int n, int groups) {
   if (check_cache(c) != MAP_OK || heads < 1 || heads > 65535 || n < 0 || n > 65535 || groups < 1 || groups > 65535) return 0;
+  if (static_cast<long long>(n) * heads >= (1ll << 31)) return 0;
   return shared_space(c, heads, n, groups).bytes;
 }
 
@@ -885,7 +886,7 @@ int map_cache_attend_shared(const map_cache* c, int layer, const map_heads* q, c
   const int rc = attend_args(c, layer, q, seqs, n, scale, out, ws, a);
   if (rc != MAP_OK) return rc;
   if (groups < 1) return MAP_EINVAL;
-  if (groups > 65535) return MAP_EUNSUPPORTED;
+  if (groups > 65535 || static_cast<long long>(n) * q->heads >= (1ll << 31)) return MAP_EUNSUPPORTED;      // a group's rows of queries: 32 bits
   if (a.n == 0) return MAP_OK;
   if (!starts) return MAP_EINVAL;
   const SharedSpace s = shared_space(c, q->heads, n, groups);

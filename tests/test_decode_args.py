@@ -11,19 +11,27 @@ BAD_CACHES = (("E", dict(pool=0)), ("E", dict(pool=F + 8)), ("E", dict(table=0))
               ("U", dict(dh=60)), ("U", dict(dh=264)), ("U", dict(page=1025)), ("U", dict(seqs=262145)), ("U", dict(max_pages=1 << 27)))
 
 
-def calls(mb, c, layer=0, q=None, seqs=F, n=2, starts=F, groups=1, scale=1.0, out=None, weights=F, ws=F):  # noqa: F811
-    """What the two attentions answer to the same arguments."""
+def shared(mb, c, layer=0, q=None, seqs=F, n=2, starts=F, groups=1, scale=1.0, out=None, ws=F):  # noqa: F811
     h = heads(mb, n=2, row=128)
-    q, out = h if q is None else q, h if out is None else out
-    return (mb.lib.map_cache_attend_shared(c, layer, q, seqs, n, starts, groups, scale, out, ws, None),
-            mb.lib.map_cache_attend_weigh(c, layer, q, seqs, n, scale, out, weights, ws, None))
+    return mb.lib.map_cache_attend_shared(c, layer, h if q is None else q, seqs, n, starts, groups, scale,
+                                          h if out is None else out, ws, None)
+
+
+def weigh(mb, c, layer=0, q=None, seqs=F, n=2, scale=1.0, out=None, weights=F, ws=F):  # noqa: F811
+    h = heads(mb, n=2, row=128)
+    return mb.lib.map_cache_attend_weigh(c, layer, h if q is None else q, seqs, n, scale, h if out is None else out, weights, ws, None)
+
+
+def both(mb, c, **bad):  # noqa: F811
+    """What the two attentions answer to the same bad arguments."""
+    return shared(mb, c, **bad), weigh(mb, c, **bad)
 
 
 def test_attend_refusals(mb):  # noqa: F811
     code, c = {"E": mb.MAP_EINVAL, "U": mb.MAP_EUNSUPPORTED}, cache(mb)
     for kind, bad in BAD_CACHES:
         b = cache(mb, **bad)
-        assert calls(mb, b) == (code[kind],) * 2, bad
+        assert both(mb, b) == (code[kind],) * 2, bad
         assert mb.lib.map_cache_attend_shared_workspace(b, 4, 4, 2) == 0
         assert mb.lib.map_cache_attend_weigh_workspace(b, 4, 4) == 0
     h = heads(mb, n=2, row=128)
@@ -32,23 +40,23 @@ def test_attend_refusals(mb):  # noqa: F811
                 dict(q=heads(mb, p=0, n=2)), dict(q=heads(mb, p=F + 8, n=2)), dict(q=heads(mb, row=-8, n=2)),
                 dict(q=heads(mb, row=132, n=2)), dict(out=heads(mb, row=127, n=2)), dict(out=heads(mb, row=120, n=2)),
                 dict(out=heads(mb, row=0, n=2))):
-        assert calls(mb, c, **bad) == (mb.MAP_EINVAL,) * 2, bad
+        assert both(mb, c, **bad) == (mb.MAP_EINVAL,) * 2, bad
     for bad in (dict(n=65536, out=h, q=h),):
-        assert calls(mb, c, **bad) == (mb.MAP_EUNSUPPORTED,) * 2
+        assert both(mb, c, **bad) == (mb.MAP_EUNSUPPORTED,) * 2
     for dh in (8, 40, 72, 112, 160, 248):
-        assert calls(mb, cache(mb, dh=dh), q=heads(mb, n=2, row=512, head=256), out=heads(mb, n=2, row=512, head=256)) == \
+        assert both(mb, cache(mb, dh=dh), q=heads(mb, n=2, row=512, head=256), out=heads(mb, n=2, row=512, head=256)) == \
             (mb.MAP_EUNSUPPORTED,) * 2
     # each call's own arguments
-    assert calls(mb, c, starts=None)[0] == mb.MAP_EINVAL
-    assert calls(mb, c, groups=0)[0] == calls(mb, c, groups=-1)[0] == mb.MAP_EINVAL
-    assert calls(mb, c, groups=65536)[0] == mb.MAP_EUNSUPPORTED
-    assert calls(mb, c, weights=None)[1] == calls(mb, c, weights=F + 2)[1] == mb.MAP_EINVAL
-    assert calls(mb, c, n=0, seqs=None, ws=None, starts=None, weights=None) == (mb.MAP_OK,) * 2
-    # scores of more than 2^46 bytes
-    wide = cache(mb, max_pages=(1 << 27) - 1)
-    many = mb._pack_heads(F, 65534 * 64, 64, 65534)
-    assert calls(mb, wide, q=many, out=many, n=65535)[1] == mb.MAP_EUNSUPPORTED
+    assert shared(mb, c, starts=None) == shared(mb, c, groups=0) == shared(mb, c, groups=-1) == mb.MAP_EINVAL
+    assert shared(mb, c, groups=65536) == mb.MAP_EUNSUPPORTED
+    assert weigh(mb, c, weights=None) == weigh(mb, c, weights=F + 2) == mb.MAP_EINVAL
+    assert shared(mb, c, n=0, seqs=None, ws=None, starts=None) == weigh(mb, c, n=0, seqs=None, ws=None, weights=None) == mb.MAP_OK
+    # scores of more than 2^46 bytes; 2^31 rows of queries
+    wide, many = cache(mb, max_pages=(1 << 27) - 1), mb._pack_heads(F, 65534 * 64, 64, 65534)
+    assert weigh(mb, wide, q=many, out=many, n=65535) == mb.MAP_EUNSUPPORTED
     assert mb.lib.map_cache_attend_weigh_workspace(wide, 65534, 65535) == 0
+    assert shared(mb, c, q=many, out=many, n=65535) == shared(mb, c, q=many, out=many, n=32770) == mb.MAP_EUNSUPPORTED
+    assert mb.lib.map_cache_attend_shared_workspace(c, 65534, 32770, 1) == 0 < mb.lib.map_cache_attend_shared_workspace(c, 65534, 32769, 1)
     for bad in ((0, 4, 1), (65536, 4, 1), (4, -1, 1), (4, 65536, 1), (4, 4, 0), (4, 4, 65536)):
         assert mb.lib.map_cache_attend_shared_workspace(c, *bad) == 0, bad
         if bad[2] == 1:
