@@ -206,7 +206,8 @@ __device__ __forceinline__ void leave(const AttendArgs& a, int entry, int head, 
 }
 
 // Joins `count` parts, of CTAs c, c + stride, ... (the first one's slot `slot0`, the others' slot 0), in order: into the
-// result of `entry`'s heads from `head` on, or into the first part where entry is negative.  All of the block's threads, two pieces of four columns of a row each, with
+// result of `entry`'s heads from `head` on, or into the first part where entry is negative.  All of the block's threads, two
+// pieces of four columns of a row each, with
 // kGroup parts of both in flight, for all that a join takes is latency.
 template <typename T, int DH, int MODE>
 __device__ __noinline__ void join_parts(const AttendArgs& a, int c, int stride, int slot0, int count, int have, int entry,
@@ -639,17 +640,18 @@ cudaError_t launch_run(const AttendArgs& a, size_t smem, int grid, cudaStream_t 
 // SM holds one CTA of three tiles.
 template <typename T, int DH, int MODE>
 cudaError_t launch_width(const AttendArgs& a, int sms, cudaStream_t st) {
-  constexpr size_t kSm = 228 * 1024, kOwn = 1024 + 768;      // an SM's shared memory; what a CTA takes beside its dynamic part
+  // an SM's shared memory; what a CTA takes beside its dynamic part (kOwn: aligned for the other kernel of its unit)
+  constexpr size_t kSm = 228 * 1024, kBeside = 1024 + (MODE == kOwn ? 1024 : 768);
   const int rows = a.group < kRows ? a.group : kRows;
   constexpr int kWant = ctas_of(DH);
-  const int deep = static_cast<int>(kSm / (smem_of<DH>(3, rows) + kOwn)), flat = static_cast<int>(kSm / (smem_of<DH>(2, rows) + kOwn));
+  const int deep = static_cast<int>(kSm / (smem_of<DH>(3, rows) + kBeside)), flat = static_cast<int>(kSm / (smem_of<DH>(2, rows) + kBeside));
   const bool three = deep >= kWant || deep >= flat;
   const int ctas = std::min(kWant, three ? deep : flat);
   const long long most = static_cast<long long>(a.n) * a.c.heads * a.subs *
                          ((static_cast<long long>(a.c.max_pages) * a.c.page + kTile - 1) / kTile);
   const int grid = static_cast<int>(std::min<long long>(most, std::min(ctas * sms, max_grid(DH))));
   // (64 and 96 columns have room for three with any number of rows)
-  if constexpr (kSm / (smem_of<DH>(3, kRows) + kOwn) < kWant)
+  if constexpr (kSm / (smem_of<DH>(3, kRows) + kBeside) < kWant)
     if (!three) return launch_run<T, DH, 2, MODE>(a, smem_of<DH>(2, rows), grid, st);
   return launch_run<T, DH, 3, MODE>(a, smem_of<DH>(3, rows), grid, st);
 }

@@ -4,9 +4,15 @@
 // (m, l, o: largest score, sum of weights, unnormalised output) is a product of all the members' queries of a key head with one
 // set of keys and values; the rows from S on are each member's own (attend's kernel), and the parts join as in attend.
 //
-// Bound: HBM, a group's shared rows once and the others once a sequence; 4 S dh operations a query head beside them, which is
-// what limits it from about 100 query heads a key head on (224: 22 us of tensor time against 18 of loads, below).
-// Four launches: what is shared (a CTA a group compares the members' table rows), the shared rows, the sequences' own, the join.
+// Bound: HBM, a group's shared rows once and the others once a sequence; 4 S dh operations a query head beside them (6 with the
+// weights in two halves), on the tensor cores as much as the loads from about 200 query heads a key head on; for groups of a few
+// sequences the chain of four launches.
+// The launches: what is shared, the shared rows, the sequences' own rows, the join.  The own rows' kernel starts on the SMs that the
+// shared rows leave free.  (The other order took 47 us for 64 questions and 74 for the video below, where 41 and 64 are taken.)
+// Measured, 128 columns: 4 questions on 611 rows, 32 heads over 32: 23 us (plan 4, shared rows 9, join 5, launches); 64 questions on
+// 2915 rows, 32 over 8: 41 us (plan 6, shared rows done at 22 and own rows at 30, join 7 of 17 MB of parts); 8 groups of 8 on up to
+// 1315 rows, 28 over 4: 32 us; 32 answers on 60001 rows, 28 over 4, fp16: 64 us, of which the shared rows take 43, 123 MB at
+// 2.8 TB/s and tensor cores 57 % busy.
 #include <type_traits>
 
 #include "attend.cuh"
@@ -136,7 +142,8 @@ __global__ void __launch_bounds__(kPlan) shared_plan_kernel(const __grid_constan
   const int rows = full > 0 ? shared * a.c.page : 0;
   // entries of the group; all of them where nothing is shared because the groups are bad
   const int e0 = refused ? 0 : first, e1 = refused ? a.n : last;
-  for (int i = e0 + (refused ? static_cast<int>(blockIdx.x) : rank) * kPlan + tid; i < e1; i += (refused ? static_cast<int>(gridDim.x) : ranks) * kPlan) {
+  const int block = refused ? static_cast<int>(blockIdx.x) : rank, blocks = refused ? static_cast<int>(gridDim.x) : ranks;
+  for (int i = e0 + block * kPlan + tid; i < e1; i += blocks * kPlan) {
     const Member m = i == first + tid && !refused ? own : member(a, i, e1);
     Entry e{rows, g, m.len - rows, 0};
     if (m.len <= 0) e = Entry{m.seq < 0 ? -2 : -1, 0, 0, 0};
@@ -150,7 +157,7 @@ __global__ void __launch_bounds__(kPlan) shared_plan_kernel(const __grid_constan
 // tcgen05.mma.  64 keys are the N of the scores' product and the K of the values', whose first operand, the weights as two halves
 // of T, lies in TMEM.  Four warps for each 128 rows do the softmax, a row a thread (two threads a row, twice the warps: no
 // faster); a warp loads keys and one values, each with a ring of its own; a thread of a warp for each 128 rows issues the
-// products: scores of a tile while the last one's weights are made.
+// products: a tile's scores while the last one's weights are made, which take the place of theirs.
 constexpr int kM = 128, kN = 64;
 
 template <int DH, int MT>
@@ -161,7 +168,8 @@ struct Shape {
   static constexpr int kCtas = MT == 1 && DH <= 128 ? 2 : 1;
   static constexpr int kRing = (227 * 1024 / kCtas - 3072 - kQBytes) / kTileBytes;           // tiles that fit
   static constexpr int kKeyRing = kRing >= 8 ? 4 : (kRing + 1) / 2, kValueRing = kRing >= 8 ? 4 : kRing / 2;
-  static constexpr int kTiles = kQBytes + (kKeyRing + kValueRing) * kTileBytes, kSmem = kTiles + 512 + MT * kM * 8;        // the barriers and the queries' places behind the tiles
+  static constexpr int kTiles = kQBytes + (kKeyRing + kValueRing) * kTileBytes;
+  static constexpr int kSmem = kTiles + 512 + MT * kM * 8;   // the barriers and the queries' places behind the tiles
   static constexpr int kLo = kN / 2, kO = 2 * kN;            // TMEM columns of 128 rows: two tiles' scores, weights in their place; sums
   static constexpr int kCols = kO + DH <= 256 ? 256 : 512;
   static_assert(kKeyRing <= 4 && kValueRing >= 2 && kCtas * (kSmem + 1024) <= 228 * 1024 && kCtas * MT * kCols <= 512, "an SM");
@@ -287,11 +295,12 @@ struct SharedBars {
 static_assert(sizeof(SharedBars) <= 512, "behind the tiles");
 
 template <typename T, int DH, int MT>
-__global__ void __launch_bounds__(Shape<DH, MT>::kThreads, Shape<DH, MT>::kCtas) shared_kernel(const __grid_constant__ SharedArgs p, const __grid_constant__ CUtensorMap map) {
+__global__ void __launch_bounds__(Shape<DH, MT>::kThreads, Shape<DH, MT>::kCtas)
+    shared_kernel(const __grid_constant__ SharedArgs p, const __grid_constant__ CUtensorMap map) {
   using S = Shape<DH, MT>;
   constexpr int VPR = DH / 8, kWarpsAll = S::kThreads / 32, kKeys = 4 * MT, kValues = kKeys + 1, kProducts = kKeys + 2;
-  extern __shared__ __align__(1024) unsigned char sh[];
-  SharedBars& b = *reinterpret_cast<SharedBars*>(sh + S::kTiles);
+  extern __shared__ __align__(1024) unsigned char tile_mem[];
+  SharedBars& b = *reinterpret_cast<SharedBars*>(tile_mem + S::kTiles);
   pdl_enter();
   const AttendArgs& a = p.a;
   const int tid = threadIdx.x, lane = tid & 31, warp = __shfl_sync(0xffffffffu, tid >> 5, 0);
@@ -316,7 +325,7 @@ __global__ void __launch_bounds__(Shape<DH, MT>::kThreads, Shape<DH, MT>::kCtas)
     }
     if (tid == 0) p.tile0[p.groups] = per;
   }
-  if (t0 >= total || (smem_u32(sh) & 1023) != 0) {           // (the alignment is what its declaration asks for)
+  if (t0 >= total || (smem_u32(tile_mem) & 1023) != 0) {           // (the alignment is what its declaration asks for)
     if (t0 < total && tid == 0) atomicOr(a.c.status, ST_INTERNAL);
     return;
   }
@@ -359,7 +368,7 @@ __global__ void __launch_bounds__(Shape<DH, MT>::kThreads, Shape<DH, MT>::kCtas)
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = b.tmem;
-  const uint32_t base = smem_u32(sh), keys = base + S::kQBytes, values = keys + S::kKeyRing * S::kTileBytes;
+  const uint32_t base = smem_u32(tile_mem), keys = base + S::kQBytes, values = keys + S::kKeyRing * S::kTileBytes;
   volatile int* stop = &b.abort;
   const auto wait = [&](uint64_t* bar, uint32_t parity) { return mbar_wait(bar, parity & 1, a.c.status, stop); };
 
@@ -372,7 +381,7 @@ __global__ void __launch_bounds__(Shape<DH, MT>::kThreads, Shape<DH, MT>::kCtas)
     // ---- softmax: row `tid` of the item's queries
     const int mt = MT > 1 ? warp >> 2 : 0;
     const uint32_t mine_at = tmem + mt * S::kCols + (static_cast<uint32_t>((warp & 3) * 32) << 16);
-    long long* q_at = reinterpret_cast<long long*>(sh + S::kTiles + 512);    // where the rows' queries are
+    long long* q_at = reinterpret_cast<long long*>(tile_mem + S::kTiles + 512);    // where the rows' queries are
     float m = -INFINITY, l = 0.f;
     bool begins = true, from_start = pl.t == 0;
     int have = 0, q0 = 0, kh = 0;
@@ -405,7 +414,7 @@ __global__ void __launch_bounds__(Shape<DH, MT>::kThreads, Shape<DH, MT>::kCtas)
       }
       if (mt * kM < have) {
         const bool busy = warp * 32 < have;    // rows of this warp hold queries
-        wait(&b.s_full[mt][count & 1], count >> 1);          // (a wait that gave up stops all others; the barriers between warps need every pass)
+        wait(&b.s_full[mt][count & 1], count >> 1); // (one that gave up stops all others; the barriers between warps need every pass)
         tc_fence_after();
         uint32_t z[kN];
         float f = 1.f;
@@ -502,7 +511,8 @@ __global__ void __launch_bounds__(Shape<DH, MT>::kThreads, Shape<DH, MT>::kCtas)
               tmem_ld16(mine_at + S::kO + 16 * x, o);
 #pragma unroll
               for (int j = 0; j < 16; j += 4) {
-                const float4 v = make_float4(__uint_as_float(o[j]), __uint_as_float(o[j + 1]), __uint_as_float(o[j + 2]), __uint_as_float(o[j + 3]));
+                const float4 v = make_float4(__uint_as_float(o[j]), __uint_as_float(o[j + 1]), __uint_as_float(o[j + 2]),
+                                             __uint_as_float(o[j + 3]));
                 if (!on) continue;
                 if (done) *reinterpret_cast<float4*>(p.whole + at * DH + 16 * x + j) = v;
                 else *reinterpret_cast<float4*>(part + 2 * MT * kM + ((4 * x + j / 4) * (MT * kM) + tid) * 4) = v;
@@ -606,7 +616,8 @@ __global__ void __launch_bounds__(Shape<DH, MT>::kThreads, Shape<DH, MT>::kCtas)
             for (int j = 0; j < kAtOnce; ++j) {
               const int e = lane + 32 * (j0 + j), r = e / VPR, x = e % VPR;
               if (j0 + j < VPR)
-                cp_async16_or_zero(dst + h * (32 * 128) + (x >> 3) * (kN * 128) + r * 128 + (((x & 7) ^ (r & 7)) << 4), from + src[j] + x * 8, h * 32 + r < valid);
+                cp_async16_or_zero(dst + h * (32 * 128) + (x >> 3) * (kN * 128) + r * 128 + (((x & 7) ^ (r & 7)) << 4),
+                                   from + src[j] + x * 8, h * 32 + r < valid);
             }
           }
         cp_async_commit();
@@ -702,7 +713,7 @@ __global__ void __launch_bounds__(Shape<DH, MT>::kThreads, Shape<DH, MT>::kCtas)
 
 // ---- the join: 8 rows (entry, head of a key head) by dh / 4 pieces of four columns by a few runs of their parts a block.  Latency:
 // an entry, then its group and places in the lists, then its parts, kJoinEach of them together.
-constexpr int kJoinEach = 3;
+constexpr int kJoinEach = 3;                  // (six, and with them fewer threads: 1 to 3 us more)
 // CTAs whose runs of `per` tiles have those from `tile` on.
 __device__ __forceinline__ void runs_of(long long tile, int tiles, long long per, int& first, int& last) {
   if (tile + tiles < (1ll << 31)) {            // (a 64-bit division takes four times as long)
@@ -838,7 +849,8 @@ int shared_box(const AttendArgs& a, CUtensorMap* map) {
   return r == CUDA_SUCCESS ? box : 0;
 }
 
-// Rows of an item: 256, on an SM of its own, where groups have more than 128 on average.
+// Rows of an item: 256, on an SM of its own, where groups have more than 128 on average (32 answers of 7 heads a key head on a
+// video: 64 us; with 128, which read the keys and values twice, 86).
 int shared_rows(const map_cache* c, long long heads, long long n, long long groups) {
   return c->dh <= 128 && n * (heads / c->heads) > kM * groups ? 2 * kM : kM;
 }
@@ -915,7 +927,7 @@ int map_cache_attend_shared(const map_cache* c, int layer, const map_heads* q, c
   if (e == cudaSuccess) e = half ? launch_shared<__half>(p, map, st) : launch_shared<__nv_bfloat16>(p, map, st);
   if (e == cudaSuccess) e = launch_attend<kOwn>(a, st);
   if (e == cudaSuccess) {
-    // (as many runs as one wave of threads allows: 64 questions on an image took 48.7 us with four, XX with two)
+    // (as many runs as one wave of threads allows; 64 questions on an image took 4 us longer with twice as many)
     const int cells = 2 * c->dh;
     int splits = 1;
     while (splits < 4 && 2 * splits * cells <= 1024 && static_cast<long long>(n) * q->heads * (c->dh / 4) * 2 * splits <= 152 * 1024) splits *= 2;

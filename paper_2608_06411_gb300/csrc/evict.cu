@@ -1,13 +1,22 @@
 // Rows that leave a cache by their weights (map_cache_evict): of each entry's rows first .. len - last - 1 the k of greatest
-// weight stay, chosen for every layer and key head by itself, in their order.
+// weight stay, chosen for every layer and key head (a unit) by itself, in their order.
 //
-// Mathematics.  The k-th greatest weight of a (layer, head) by a radix select on the weights as ordered 32-bit keys (11, 11 and
-// 10 bits a pass, ending early where a digit's rows all stay), then one pass in row order: a row stays if its key is greater, or
-// equal and among the first of the equals that are needed.
+// Mathematics.  The k-th greatest weight of a unit by a radix select on the weights as ordered 32-bit keys (11, 11 and 10 bits a
+// pass, ending early where a digit's rows all stay); then a row stays if its key has greater digits, or the digits found and is
+// among the first of those that are needed.
 // Bound: HBM, the candidates' weights once and the rows that move once read and once written.  In place: a kept row's new place is
-// never behind its old one, and places rise with the rows, so a CTA that goes through a (layer, head)'s rows in order, reading
-// a batch whole before it writes it, overwrites nothing that is still to be read.  Pages that other sequences hold as well are
-// replaced by new ones (evict_plan_kernel), from which nothing is read.
+// never behind its old one, and places rise with the rows, so a CTA that goes through rows in order, reading a batch whole
+// before it writes it, overwrites nothing that is still to be read; columns do not depend on one another, so that slices of them
+// are moved by CTAs of their own, and the weights like one more column.  Pages that other sequences hold as well are replaced by
+// new ones (evict_plan_kernel), from which nothing is read.
+// Three launches.  One CTA does the pages; beside it a cluster a unit (a CTA where units are many) lists the rows that stay; then
+// the rows move.  (One kernel, a CTA a unit, took 65, 223, 229 and 621 us for the cases below; that kernel with 2048 units in
+// two halves, the select of some beside the moves of others, gained nothing.)
+// Measured (28 layers of 4 key heads, 128 columns, unless said otherwise; with the copies of tables and weights that the
+// measurement makes): one sequence of 1100 rows to 512: 31 us, a chain of launches; 6 of 3001 to 4096 rows to 1315: 172 us, of
+// which the move of 858 MB of DRAM traffic takes 141 to 147, 5.8 to 6.1 TB/s; 8 questions of 2915 to 3000 rows on one image in
+// 32 layers of 8 heads to 245: 120 us, the move of rows at random places 77 (5.5 TB/s), the select 28, bound by its
+// instructions; one of 60001 rows in 8 layers to 16900: 146 us, of which the move of 64-byte slices takes 113 (4.7 TB/s).
 #include <algorithm>
 
 #include "pages.cuh"
@@ -131,7 +140,6 @@ __global__ void __launch_bounds__(kPlanThreads) evict_plan_kernel(const EvictArg
   }
 }
 
-constexpr int kHold = 16;                      // candidates of a thread that it keeps in registers
 constexpr int kBins = 2048;
 
 // Weights in ascending order as unsigned numbers; NaN of either sign is the greatest, zeros are equal.
@@ -175,10 +183,10 @@ __device__ __forceinline__ float* weights_of(const EvictArgs& a, const Unit& x) 
 }
 
 // The rows that stay, in order, into kept [units][k]: a cluster a unit, an equal run of the candidates a CTA, of which a warp holds
-// kHold times 32 in a row.  Runs of up to kHold * THREADS are read once.
-template <int THREADS>
+// HOLD times 32 in a row.  Runs of up to HOLD * THREADS are read once.
+template <int THREADS, int HOLD>
 __global__ void __launch_bounds__(THREADS, 1280 / THREADS) evict_select_kernel(const EvictArgs a) {
-  constexpr int kWarps = THREADS / 32, kBinsEach = kBins / THREADS, kChunk = kHold * THREADS;
+  constexpr int kWarps = THREADS / 32, kBinsEach = kBins / THREADS, kChunk = HOLD * THREADS;
   __shared__ __align__(16) int hist[2][kBins];
   __shared__ int warp_sum[kWarps];
   __shared__ int2 warp_kept[kWarps];
@@ -199,14 +207,14 @@ __global__ void __launch_bounds__(THREADS, 1280 / THREADS) evict_select_kernel(c
   const int t0 = min(window, rank * each), t1 = min(window, t0 + each);
   const float* w = weights_of(a, x) + x.e.first;
   const auto all_here = [&]() { if (ranks > 1) cluster_sync(); else __syncthreads(); };
-  uint32_t key[kHold];                         // of candidates row0 + 32 j; 0, below all weights, where there is none
+  uint32_t key[HOLD];                         // of candidates row0 + 32 j; 0, below all weights, where there is none
   const auto load = [&](int c0) {
-    const int row0 = c0 + warp * (32 * kHold) + lane;
-    float v[kHold];
+    const int row0 = c0 + warp * (32 * HOLD) + lane;
+    float v[HOLD];
 #pragma unroll
-    for (int j = 0; j < kHold; ++j) v[j] = row0 + 32 * j < t1 ? __ldcg(w + row0 + 32 * j) : 0.f;
+    for (int j = 0; j < HOLD; ++j) v[j] = row0 + 32 * j < t1 ? __ldcg(w + row0 + 32 * j) : 0.f;
 #pragma unroll
-    for (int j = 0; j < kHold; ++j) key[j] = row0 + 32 * j < t1 ? key_of(v[j]) : 0u;
+    for (int j = 0; j < HOLD; ++j) key[j] = row0 + 32 * j < t1 ? key_of(v[j]) : 0u;
   };
   const bool once = t1 - t0 <= kChunk;
   load(t0);
@@ -224,7 +232,7 @@ __global__ void __launch_bounds__(THREADS, 1280 / THREADS) evict_select_kernel(c
     for (int c0 = t0; c0 < t1; c0 += kChunk) {
       if (!once) load(c0);
 #pragma unroll
-      for (int j = 0; j < kHold; ++j)
+      for (int j = 0; j < HOLD; ++j)
         if (key[j] != 0 && (shift == 32 || key[j] >> shift == prefix)) atomicAdd(&hist[pass][key[j] >> down & ((1 << bits) - 1)], 1);
     }
     all_here();
@@ -312,7 +320,7 @@ __global__ void __launch_bounds__(THREADS, 1280 / THREADS) evict_select_kernel(c
     if (!once) load(c0);
     int2 n = make_int2(0, 0);
 #pragma unroll
-    for (int j = 0; j < kHold; ++j) {
+    for (int j = 0; j < HOLD; ++j) {
       n.x += key[j] > most;
       n.y += key[j] >= least;
     }
@@ -333,9 +341,9 @@ __global__ void __launch_bounds__(THREADS, 1280 / THREADS) evict_select_kernel(c
       equals += v.y;
     }
     const uint32_t before = (1u << lane) - 1;
-    const int row0 = x.e.first + c0 + warp * (32 * kHold) + lane;
+    const int row0 = x.e.first + c0 + warp * (32 * HOLD) + lane;
 #pragma unroll
-    for (int j = 0; j < kHold; ++j) {
+    for (int j = 0; j < HOLD; ++j) {
       const bool more = key[j] > most, same = !more && key[j] >= least;
       const uint32_t m = __ballot_sync(0xffffffffu, more), s = __ballot_sync(0xffffffffu, same);
       const int mine_eq = eq + __popc(s & before);
@@ -489,9 +497,13 @@ int map_cache_evict(const map_cache* c, float* weights, const int32_t* seqs, int
   while (ranks < 8 && units * ranks < 2 * 152 && max_rows / ranks > 2048) ranks *= 2;
   while (slices < 4 && units * (4 * slices + 1) <= 4 * 152 && c->dh / 8 / slices >= 8) slices *= 2;
   const unsigned select = static_cast<unsigned>(units * ranks);
-  if (e == cudaSuccess)
-    e = max_rows / ranks > kHold * 256 ? launch_cluster(evict_select_kernel<512>, select, 512, ranks, st, a)
-                                       : launch_cluster(evict_select_kernel<256>, select, 256, ranks, st, a);
+  const long long most = (max_rows + ranks - 1) / ranks;     // candidates of a CTA (2048 runs of 2830: 33 us with 16 a thread, 28 with 12)
+  const auto look = [&](auto kernel, int threads) { if (e == cudaSuccess) e = launch_cluster(kernel, select, threads, ranks, st, a); };
+  if (most <= 4 * 256) look(evict_select_kernel<256, 4>, 256);
+  else if (most <= 8 * 256) look(evict_select_kernel<256, 8>, 256);
+  else if (most <= 12 * 256) look(evict_select_kernel<256, 12>, 256);
+  else if (most <= 16 * 256) look(evict_select_kernel<256, 16>, 256);
+  else look(evict_select_kernel<512, 16>, 512);
   const unsigned move = static_cast<unsigned>(units * (2 * slices + 1));
   if (e == cudaSuccess)
     e = move <= 2 * 152 ? launch_k(evict_move_kernel<512>, dim3(move), dim3(512), 0, st, a, slices)
