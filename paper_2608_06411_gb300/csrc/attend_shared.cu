@@ -559,7 +559,7 @@ __global__ void __launch_bounds__(Shape<DH, MT>::kThreads, Shape<DH, MT>::kCtas)
         const int row = on ? (pid * a.c.heads + kh) * a.c.page + (a.page_shift >= 0 ? tok & (a.c.page - 1) : tok % a.c.page) : past;
         pl.next(p);
         pid = page_of();
-        if (!wait(&empty[slot], turn)) break;
+        if (!__all_sync(0xffffffffu, wait(&empty[slot], turn))) break;       // (the warp gives up as one)
         if (lane == 0) mbar_arrive_expect_tx(&full[slot], S::kTileBytes);
         __syncwarp();
         if (lane * p.box < kN) {
@@ -602,7 +602,7 @@ __global__ void __launch_bounds__(Shape<DH, MT>::kThreads, Shape<DH, MT>::kCtas)
         }
         pl.next(p);
         pages_of();
-        ok = wait(&empty[slot], turn);
+        ok = __all_sync(0xffffffffu, wait(&empty[slot], turn));
         if (!ok) break;
         const uint32_t dst = ring + slot * S::kTileBytes;
 #pragma unroll 1
@@ -713,7 +713,7 @@ __global__ void __launch_bounds__(Shape<DH, MT>::kThreads, Shape<DH, MT>::kCtas)
 
 // ---- the join: 8 rows (entry, head of a key head) by dh / 4 pieces of four columns by a few runs of their parts a block.  Latency:
 // an entry, then its group and places in the lists, then its parts, kJoinEach of them together.
-constexpr int kJoinEach = 3;                  // (six, and with them fewer threads: 1 to 3 us more)
+constexpr int kJoinEach = 3;                   // (six, and with them fewer threads: 1 to 3 us more)
 // CTAs whose runs of `per` tiles have those from `tile` on.
 __device__ __forceinline__ void runs_of(long long tile, int tiles, long long per, int& first, int& last) {
   if (tile + tiles < (1ll << 31)) {            // (a 64-bit division takes four times as long)
