@@ -166,7 +166,7 @@ struct Shape {
   static constexpr int kBlocks = (DH + 63) / 64;             // boxes of 64 columns, 128 bytes a row, 16-byte units exchanged by the row's low bits
   static constexpr int kTileBytes = kBlocks * kN * 128, kQBytes = kBlocks * MT * kM * 128;
   static constexpr int kCtas = MT == 1 && DH <= 128 ? 2 : 1;
-  static constexpr int kRing = (227 * 1024 / kCtas - 3072 - kQBytes) / kTileBytes;           // tiles that fit
+  static constexpr int kRing = (227 * 1024 / kCtas - 3 * 1024 - kQBytes) / kTileBytes;           // tiles that fit
   static constexpr int kKeyRing = kRing >= 8 ? 4 : (kRing + 1) / 2, kValueRing = kRing >= 8 ? 4 : kRing / 2;
   static constexpr int kTiles = kQBytes + (kKeyRing + kValueRing) * kTileBytes;
   static constexpr int kSmem = kTiles + 512 + MT * kM * 8;   // the barriers and the queries' places behind the tiles

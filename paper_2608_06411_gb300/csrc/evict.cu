@@ -497,11 +497,11 @@ int map_cache_evict(const map_cache* c, float* weights, const int32_t* seqs, int
   while (ranks < 8 && units * ranks < 2 * 152 && max_rows / ranks > 2048) ranks *= 2;
   while (slices < 4 && units * (4 * slices + 1) <= 4 * 152 && c->dh / 8 / slices >= 8) slices *= 2;
   const unsigned select = static_cast<unsigned>(units * ranks);
-  const long long most = (max_rows + ranks - 1) / ranks;     // candidates of a CTA (2048 runs of 2830: 33 us with 16 a thread, 28 with 12)
+  const long long most = (max_rows + ranks - 1) / ranks;     // candidates of a CTA (2048 runs of 2830: 33 us with 16 a thread, 28 with 13)
   const auto look = [&](auto kernel, int threads) { if (e == cudaSuccess) e = launch_cluster(kernel, select, threads, ranks, st, a); };
   if (most <= 4 * 256) look(evict_select_kernel<256, 4>, 256);
   else if (most <= 8 * 256) look(evict_select_kernel<256, 8>, 256);
-  else if (most <= 12 * 256) look(evict_select_kernel<256, 12>, 256);
+  else if (most <= 13 * 256) look(evict_select_kernel<256, 13>, 256);
   else if (most <= 16 * 256) look(evict_select_kernel<256, 16>, 256);
   else look(evict_select_kernel<512, 16>, 512);
   const unsigned move = static_cast<unsigned>(units * (2 * slices + 1));
