@@ -99,6 +99,7 @@ SHARED = [
     ("f16", 64, 2, 130, 1024, [(2100, [5, 1000])]),
     ("bf16", 128, 1, 4, 16, [(48 + i % 40, [1] * (1 + i % 3)) for i in range(400)]),
     ("bf16", 80, 2, 33, 16, [(3000, [40] * 9)]),
+    ("f16", 64, 1, 1, 16, [(64, [1, 5] * 700), (130, [3] * 1100)]),
 ]
 
 
@@ -537,6 +538,27 @@ def test_evict_refuses_what_it_cannot_do_whole(mb):  # noqa: F811
     cache.evict(weights, ints([0, 2]), ints([64, 0]), ints([0, 0]), 1)       # behind the shared pages: in place
     cache.check()
     assert cache.length.cpu().tolist() == [65, 104, 1]
+
+
+def test_evict_of_many_sequences(mb):  # noqa: F811
+    """More entries than a block has threads, every third the fork of another, some padding, some left as they are."""
+    n, page, hk = 2100, 4, 2
+    cache = mb.Cache.empty(1, 40000, hk, page, 16, n, 16)
+    cache.pool.normal_(generator=gen(1))
+    model = H.Pages(40000, page, n, 16)
+    own = [s for s in range(n) if s % 3]
+    lens = [(7 * s) % 53 for s in own]
+    cache.extend(ints(own), ints(lens), rows=sum(lens))
+    model.extend(own, lens, sum(lens))
+    forks = [s for s in range(n) if s % 3 == 0]
+    cache.fork(ints([s + 1 for s in forks]), ints(forks))
+    for to, at in model.fork([s + 1 for s in forks], forks):
+        assert to >= 0 and at >= 0
+    weights = torch.rand(1, n, hk, 16 * page, generator=gen(2), device=DEV)
+    ask = [-1 if s % 11 == 0 else s for s in range(n - 1, -1, -1)]
+    first, last = [s % 3 for s in range(n)], [s % 5 for s in range(n)]
+    assert run_evict(mb, cache, model, weights, ask, first, last, 9)
+    cache.check()
 
 
 def test_evict_past_32_bits(mb):  # noqa: F811
