@@ -434,6 +434,8 @@ _pack_cache = struct.Struct("@5P8i").pack                            # map_cache
 
 _current_device = torch._C._cuda_getDevice              # as torch.cuda.current_device and current_stream, without their
 _current_stream = torch._C._cuda_getCurrentRawStream    # Python objects: 1.5 us a call less
+_capturing = torch._C._cuda_isCurrentStreamCapturing
+_KEEP = 1 << 26                                         # bytes of scratch that a Cache keeps
 
 
 class _on:
@@ -645,7 +647,9 @@ class Cache:
         # attend's scratch: calls on one cache are ordered by the caller, so they can share it
         self._ws = torch.empty(int(lib.map_cache_attend_workspace(self.desc)), dtype=torch.uint8, device=dev)
         self._streams = set()                # that the allocator knows of
-        self._tensors = (pool, table, length, refs, status, self._ws)
+        # the other calls', as large as the largest so far (see _scratch)
+        self._kept, self._sizes = torch.empty(256, dtype=torch.uint8, device=dev), {}
+        self._tensors = (pool, table, length, refs, status, self._ws, self._kept)
 
     def _stream(self) -> int:
         """The current stream.  The allocator hears of it once, so that the memory of a Cache that is dropped waits for it."""
@@ -732,9 +736,19 @@ class Cache:
                "map_cache_attend")
         return out
 
-    def _scratch(self, size: int):
-        """A call's workspace: torch's allocator keeps it for the current stream (and a graph's capture for the graph)."""
-        return torch.empty(size, dtype=torch.uint8, device=self.device)
+    def _scratch(self, call: str, *args) -> torch.Tensor:
+        """A workspace of <call>_workspace(description, *args) bytes.  Up to _KEEP bytes the Cache keeps it for its next calls; a
+        larger one is a call's own, and so is one of a call that is captured, whose memory then belongs to the graph."""
+        size = self._sizes.get((call, args))
+        if size is None:
+            size = self._sizes[call, args] = int(getattr(lib, call + "_workspace")(self.desc, *args))
+        if size > _KEEP or _capturing():
+            return torch.empty(max(size, 256), dtype=torch.uint8, device=self.device)
+        if size > self._kept.shape[0]:
+            self._kept = torch.empty(size, dtype=torch.uint8, device=self.device)
+            self._tensors = self._tensors[:-1] + (self._kept,)
+            self._streams.clear()            # (the allocator is to hear of it for every stream)
+        return self._kept
 
     def attend_shared(self, q, seqs, layer: int, starts, scale: float | None = None, out=None, stream=None):
         """map_cache_attend_shared: attend, for groups of entries starts[g] .. starts[g + 1] - 1 (int32 [groups + 1] on the
@@ -749,7 +763,7 @@ class Cache:
             out, oa = _like(q, dh)
         else:
             oa = _heads(out, n, dh, dt, dev)
-        ws = self._scratch(lib.map_cache_attend_shared_workspace(self.desc, q.shape[1], n, groups))
+        ws = self._scratch("map_cache_attend_shared", q.shape[1], n, groups)
         _check(lib.map_cache_attend_shared(self.desc, layer, a, _dense(seqs, torch.int32, dev, (n,), "seqs"), n,
                                            _dense(starts, torch.int32, dev, (groups + 1,), "starts"), groups,
                                            dh ** -0.5 if scale is None else scale, oa, ws.data_ptr(), self._stream()),
@@ -769,7 +783,7 @@ class Cache:
             out, oa = _like(q, dh)
         else:
             oa = _heads(out, n, dh, dt, dev)
-        ws = self._scratch(lib.map_cache_attend_weigh_workspace(self.desc, q.shape[1], n))
+        ws = self._scratch("map_cache_attend_weigh", q.shape[1], n)
         _check(lib.map_cache_attend_weigh(self.desc, layer, a, _dense(seqs, torch.int32, dev, (n,), "seqs"), n,
                                           dh ** -0.5 if scale is None else scale, oa,
                                           _dense(weights, torch.float32, dev, self._weights_shape, "weights"), ws.data_ptr(),
@@ -785,7 +799,7 @@ class Cache:
             with _on(dev, stream, weights, seqs, first, last):
                 return self.evict(weights, seqs, first, last, k)
         n, i32 = seqs.shape[0], torch.int32
-        ws = self._scratch(lib.map_cache_evict_workspace(self.desc, n, k))
+        ws = self._scratch("map_cache_evict", n, k)
         _check(lib.map_cache_evict(self.desc, _dense(weights, torch.float32, dev, self._weights_shape, "weights"),
                                    _dense(seqs, i32, dev, (n,), "seqs"), n, _dense(first, i32, dev, (n,), "first"),
                                    _dense(last, i32, dev, (n,), "last"), k, ws.data_ptr(), self._stream()), "map_cache_evict")

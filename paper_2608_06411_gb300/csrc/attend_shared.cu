@@ -9,7 +9,7 @@
 // sequences the chain of four launches.
 // The launches: what is shared, the shared rows, the sequences' own rows, the join.  The own rows' kernel starts on the SMs that the
 // shared rows leave free.  (The other order took 47 us for 64 questions and 74 for the video below, where 41 and 64 are taken.)
-// Measured, 128 columns: 4 questions on 611 rows, 32 heads over 32: 23 us (plan 4, shared rows 9, join 5, launches); 64 questions on
+// Measured, 128 columns: 4 questions on 611 rows, 32 heads over 32: 22 us (plan 4, shared rows 9, join 5, launches); 64 questions on
 // 2915 rows, 32 over 8: 41 us (plan 6, shared rows done at 22 and own rows at 30, join 7 of 17 MB of parts); 8 groups of 8 on up to
 // 1315 rows, 28 over 4: 32 us; 32 answers on 60001 rows, 28 over 4, fp16: 64 us, of which the shared rows take 43, 123 MB at
 // 2.8 TB/s and tensor cores 57 % busy.

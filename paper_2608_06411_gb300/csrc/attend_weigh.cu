@@ -7,7 +7,7 @@
 // they do not leave L2), and a second kernel turns them into weights: equal runs of a list of 512-row pieces a CTA, four
 // neighbouring rows a thread, eight heads' scores in flight.
 // A sequence's sums are added up by one thread a row, over its rows of the call in their order: no atomics, one result.
-// Measured, bf16 or fp16: one sequence of 701 rows, 28 heads over 4 of 128: 17 us, latency; 64 of 200 to 1600 rows, 32 over 8:
+// Measured, bf16 or fp16: one sequence of 701 rows, 28 heads over 4 of 128: 16 us, latency; 64 of 200 to 1600 rows, 32 over 8:
 // 57 us, 4.0 TB/s (attend alone 50); one of 120001 rows, 28 over 4: 68 us, 3.7 TB/s (attend alone 51: its scores' stores cost 4,
 // the second kernel 9 to 13); 7 of up to 5001 rows, 40 heads over 10 of 96, pages of 24 rows: 27 us.
 #include "attend.cuh"

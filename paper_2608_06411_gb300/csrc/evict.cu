@@ -13,7 +13,7 @@
 // the rows move.  (One kernel, a CTA a unit, took 65, 223, 229 and 621 us for the cases below; that kernel with 2048 units in
 // two halves, the select of some beside the moves of others, gained nothing.)
 // Measured (28 layers of 4 key heads, 128 columns, unless said otherwise; with the copies of tables and weights that the
-// measurement makes): one sequence of 1100 rows to 512: 31 us, a chain of launches; 6 of 3001 to 4096 rows to 1315: 172 us, of
+// measurement makes): one sequence of 1100 rows to 512: 26 us, a chain of launches; 6 of 3001 to 4096 rows to 1315: 172 us, of
 // which the move of 858 MB of DRAM traffic takes 141 to 147, 5.8 to 6.1 TB/s; 8 questions of 2915 to 3000 rows on one image in
 // 32 layers of 8 heads to 245: 120 us, the move of rows at random places 77 (5.5 TB/s), the select 28, bound by its
 // instructions; one of 60001 rows in 8 layers to 16900: 146 us, of which the move of 64-byte slices takes 113 (4.7 TB/s).

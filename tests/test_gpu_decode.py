@@ -695,6 +695,33 @@ def test_decode_calls_on_a_stream_of_the_callers(mb):  # noqa: F811
     assert int(cache.length[0]) == 40
 
 
+def test_workspaces_that_grow_between_a_graphs_replays(mb):  # noqa: F811
+    """A graph's calls have memory of their own: eager calls before, between and after its replays may need more and less."""
+    groups = [(500, [9, 40, 3]), (64, [1, 1])]
+    cache = grouped(mb, torch.bfloat16, 128, 2, 16, groups, 2, spare=200, room=10)
+    few, many = ints([0, 1]), ints(list(range(5)) * 40)
+    q = [randn(gen(i), n, 8, 128, typ=torch.bfloat16) for i, n in enumerate((2, 200))]
+    starts = [ints([0, 2]), ints([0, 200])]
+    weights = torch.zeros(1, 5, 2, cache.table.shape[1] * 16, device=DEV)
+    want = [cache.attend_shared(q[0], few, 0, starts[0]), cache.attend(q[1], many, 0)]
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        held = cache.attend_shared(q[0], few, 0, starts[0]), cache.attend_weigh(q[0], few, 0, weights)
+    for _ in range(3):
+        g.replay()
+        a, b = cache.attend_weigh(q[1], many, 0, weights), cache.attend_shared(q[1], many, 0, starts[1])
+        g.replay()
+        c = cache.attend_shared(q[0], few, 0, starts[0])
+        torch.cuda.synchronize()
+        assert torch.equal(a, want[1]) and torch.equal(c, want[0]) and torch.equal(held[0], want[0])
+        check(b, q[1], cache, 0, many.tolist(), 128 ** -0.5, torch.bfloat16)
+    cache.evict(weights, many[:5], None, None, 30)
+    g.replay()
+    check(held[0], q[0], cache, 0, [0, 1], 128 ** -0.5, torch.bfloat16)
+    cache.check()
+    assert cache._kept.shape[0] <= 1 << 26
+
+
 @pytest.mark.parametrize("call", ["shared", "weigh", "evict"])
 def test_decode_calls_of_two_caches_from_two_threads(mb, call):  # noqa: F811
     calls, held = [], []
