@@ -233,24 +233,30 @@ __device__ __forceinline__ float2 add2(float2 a, float2 b) {
   return d;
 }
 
-// Weights as two halves like split_weights, with fewer instructions: every half is raised to its type's smallest number, not only
-// those of weights above zero.  (A weight of zero is a score of minus infinity, or a row past the last, whose value is 0 here.)
-// Weights are 2^lift times what they are to the row's base, which the largest score passes by kSlack at most: sums are scaled
-// only then, not whenever a tile has a greater score.  What is raised adds 2^-24 / 2^lift of the base's weight (f16: 2^-35).
+// Weights as two halves like split_weights, two at once: both halves of a weight above zero are raised to their type's smallest
+// number, those of a weight of zero are zero.  Weights are 2^kLift times what they are to the row's base, which the largest score
+// passes by kSlack at most: sums are scaled only then, not whenever a tile has a greater score.  fp16 has room for a little less
+// than 2^16, so that a half that is raised adds 2^-39 of the base's weight there as in split_weights.  (A smaller lift under a
+// slack of 4 and halves raised whatever the weight took 4 us less of the video's 69 above and added 2^-34 a row.)
 template <typename T> constexpr float kSlack = 8.f;
-template <> constexpr float kSlack<__half> = 4.f;
-template <typename T> constexpr float kLiftShared = 0.f;
-template <> constexpr float kLiftShared<__half> = 11.f;      // 2^(11 + 4) is below f16's largest
+template <> constexpr float kSlack<__half> = 0.99f;
+__device__ __forceinline__ uint32_t min_u16x2(uint32_t a, uint32_t b) {
+  uint32_t r;
+  asm("min.u16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  return r;
+}
 __device__ __forceinline__ void halves(float2 x, uint32_t& hi, uint32_t& lo, __nv_bfloat16) {
   const uint32_t a = __float_as_uint(x.x), b = __float_as_uint(x.y);
   hi = __byte_perm(a, b, 0x7632);
+  const uint32_t least = min_u16x2(hi, 0x00800080u);         // 2^-126 where x is above zero (ex2 gives no subnormal numbers)
   const float2 rest = fma2(make_float2(__uint_as_float(a & 0xffff0000u), __uint_as_float(b & 0xffff0000u)), make_float2(-1.f, -1.f), x);
-  const __nv_bfloat162 r = __hmax2(__floats2bfloat162_rn(rest.x, rest.y), __float2bfloat162_rn(0x1p-126f));
+  const __nv_bfloat162 r = __hmax2(__floats2bfloat162_rn(rest.x, rest.y), *reinterpret_cast<const __nv_bfloat162*>(&least));
   lo = *reinterpret_cast<const uint32_t*>(&r);
 }
 __device__ __forceinline__ void halves(float2 x, uint32_t& hi, uint32_t& lo, __half) {
   asm("cvt.rz.f16x2.f32 %0, %1, %2;" : "=r"(hi) : "f"(x.y), "f"(x.x));
-  const __half2 least = __float2half2_rn(0x1p-24f), h = __hmax2_nan(*reinterpret_cast<const __half2*>(&hi), least);
+  const uint32_t some = min_u16x2(__byte_perm(__float_as_uint(x.x), __float_as_uint(x.y), 0x7632), 0x00010001u);     // 2^-24 likewise
+  const __half2 least = *reinterpret_cast<const __half2*>(&some), h = __hmax2_nan(*reinterpret_cast<const __half2*>(&hi), least);
   const float2 rest = fma2(__half22float2(h), make_float2(-1.f, -1.f), x);
   const __half2 r = __hmax2(__floats2half2_rn(rest.x, rest.y), least);
   hi = *reinterpret_cast<const uint32_t*>(&h);
@@ -453,7 +459,7 @@ __global__ void __launch_bounds__(Shape<DH, MT>::kThreads, Shape<DH, MT>::kCtas)
             m = top;
           }
           grows = __any_sync(0xffffffffu, f != 1.f);
-          const float add = kLiftShared<T> - (m == -INFINITY ? 0.f : m);
+          const float add = kLift<T> - (m == -INFINITY ? 0.f : m);
           float2 sum = make_float2(0.f, 0.f);
 #pragma unroll
           for (int j = 0; j < kN; j += 2) {
@@ -503,7 +509,6 @@ __global__ void __launch_bounds__(Shape<DH, MT>::kThreads, Shape<DH, MT>::kCtas)
           const int i = pl.gr.first + (q0 + tid) / a.group, head = kh * a.group + (q0 + tid) % a.group;
           const long long at = static_cast<long long>(i) * a.q.heads + head;
           float* part = p.parts + static_cast<long long>(2 * blockIdx.x + (from_start ? 1 : 0)) * (MT * kM * (DH + 2));
-          constexpr float up = kLift<T> - kLiftShared<T>;    // as the sequences' own rows have it
           if (busy) {
 #pragma unroll 1
             for (int x = 0; x < DH / 16; ++x) {
@@ -518,9 +523,9 @@ __global__ void __launch_bounds__(Shape<DH, MT>::kThreads, Shape<DH, MT>::kCtas)
                 else *reinterpret_cast<float4*>(part + 2 * MT * kM + ((4 * x + j / 4) * (MT * kM) + tid) * 4) = v;
               }
             }
-            if (on && done) p.whole_stats[at] = make_float2(m + up, l);
+            if (on && done) p.whole_stats[at] = make_float2(m, l);
             if (on && !done) {
-              part[tid] = m + up;
+              part[tid] = m;
               part[MT * kM + tid] = l;
             }
           }
@@ -805,8 +810,7 @@ __global__ void __launch_bounds__(1024) shared_join_kernel(const __grid_constant
     const float2* other = reinterpret_cast<const float2*>(js + ((k - 1) * cells + cell) * 6);
     add(other[0].x, other[0].y, make_float4(other[1].x, other[1].y, other[2].x, other[2].y));
   }
-  const float none = l == 0.f ? NAN : 1.f;     // scores of minus infinity alone: raised halves are no weights
-  store4(out, make_float4(v.x / l * none, v.y / l * none, v.z / l * none, v.w / l * none));
+  store4(out, make_float4(v.x / l, v.y / l, v.z / l, v.w / l));
 }
 
 template <typename T, int DH, int MT>
