@@ -459,7 +459,15 @@ __global__ void __launch_bounds__(Shape<DH, MT>::kThreads, Shape<DH, MT>::kCtas)
             m = top;
           }
           grows = __any_sync(0xffffffffu, f != 1.f);
-          const float add = kLift<T> - (m == -INFINITY ? 0.f : m);
+          const float base_at = m == -INFINITY ? 0.f : m;
+          // The base is a rounded product, the scores below are not: 2^-17 off up to here, whole powers of two for large scores.
+          // From here on they are rounded alike, so that equal scores have equal weights, in other tiles and kernels too.
+          if (fabsf(base_at) >= 256.f) {
+#pragma unroll
+            for (int j = 0; j < kN; ++j) z[j] = __float_as_uint(__fmul_rn(__uint_as_float(z[j]), mul));
+            mul = 1.f;
+          }
+          const float add = kLift<T> - base_at;
           float2 sum = make_float2(0.f, 0.f);
 #pragma unroll
           for (int j = 0; j < kN; j += 2) {

@@ -7,6 +7,7 @@ import math
 import pytest
 import torch
 
+from test_gpu_decode import grouped
 from test_gpu_handoff import DEV, TYPES, half_step, ints, mb, tiny  # noqa: F401
 
 pytestmark = pytest.mark.gpu
@@ -41,4 +42,38 @@ def test_attend_shared_of_a_row_that_takes_all(mb, typ, gap):  # noqa: F811
     for out in (cache.attend(q, ints([0, 1]), 0), cache.attend_shared(q, ints([0, 1]), 0, ints([0, 2]))):
         off = (out.double() - want).abs().max().item()
         assert off <= tol, (off, tol)
+    cache.check()
+
+
+LARGE = [("f16", 4, 1365), ("f16", 256, 1365), ("f16", 512, 1365), ("f16", 2048, 43680), ("f16", 8192, 43680),
+         ("bf16", 256, 213), ("bf16", 1 << 28, 213 << 30)]
+
+
+def large_scores(mb, typ, unit, key):  # noqa: F811
+    """(cache, q, rows): four rows of each sequence have the same largest score by far: q's columns are 1, 3, 5 or 7 units, those
+    rows' keys `key` (so that all sums are exact), other keys 1/64 of it at most, at random."""
+    groups = [(1000, [9, 40, 3])]
+    cache = grouped(mb, typ, 128, 2, 16, groups, 2)
+    cache.pool[0, 0] = cache.pool[0, 0].clamp(-3, 3) * (key / 192)
+    rows = [100, 900, 985, 995]                                      # the third in a tile of 32 rows, the last each sequence's own
+    for s in range(3):
+        for t in rows:
+            cache.pool[0, 0, cache.table[s, t // 16].long(), :, t % 16] = key
+    q = torch.ones(3, 8, 128, dtype=typ, device=DEV) * (torch.tensor([1.0, 3.0, 5.0, 7.0] * 2, device=DEV) * unit)[None, :, None].to(typ)
+    return cache, q, rows
+
+
+@pytest.mark.parametrize("case", LARGE, ids=["-".join(str(v) for v in c) for c in LARGE])
+def test_attend_of_large_scores(mb, case):  # noqa: F811
+    """Scores of 2^16 to 2^72 (in powers of two): what fp32 keeps of one is coarser than the weights' range, and equal scores have equal weights."""
+    typ, unit, key = case
+    typ = TYPES[typ]
+    cache, q, rows = large_scores(mb, typ, unit, key)
+    for out in (cache.attend(q, ints([0, 1, 2]), 0), cache.attend_shared(q, ints([0, 1, 2]), 0, ints([0, 3]))):
+        for s in range(3):
+            v = torch.stack([cache.pool[0, 1, cache.table[s, t // 16].long(), :, t % 16].double() for t in rows])
+            want, mag = (x.mean(0).repeat_interleave(4, 0) for x in (v, v.abs()))
+            tol = half_step(typ) * want.abs() * 1.001 + sums_error(128, 1040, 0.0) * mag + tiny(typ)
+            off = (out[s].double() - want).abs()
+            assert bool((off <= tol).all()), (s, float((off / tol).max()))
     cache.check()
