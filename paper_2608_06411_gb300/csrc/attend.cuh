@@ -201,7 +201,8 @@ __device__ __forceinline__ void leave(const AttendArgs& a, int entry, int head, 
     if (x == 0) a.stats[at] = make_float2(top, l);
   } else {
     store4(static_cast<T*>(a.out.p) + entry * a.out.row + head * a.out.head + x, make_float4(v.x / l, v.y / l, v.z / l, v.w / l));
-    if (MODE == kWeigh && x == 0) a.stats[static_cast<long long>(entry) * a.q.heads + head] = make_float2(top, exp2f(kLift<T>) / l);
+    // (what l was lifted by: top - kLift has fewer bits where top is large)
+    if (MODE == kWeigh && x == 0) a.stats[static_cast<long long>(entry) * a.q.heads + head] = make_float2(top, exp2f(top - (top - kLift<T>)) / l);
   }
 }
 

@@ -77,3 +77,18 @@ def test_attend_of_large_scores(mb, case):  # noqa: F811
             off = (out[s].double() - want).abs()
             assert bool((off <= tol).all()), (s, float((off / tol).max()))
     cache.check()
+
+
+@pytest.mark.parametrize("case", LARGE, ids=["-".join(str(v) for v in c) for c in LARGE])
+def test_attend_weigh_of_large_scores(mb, case):  # noqa: F811
+    """The same rows share the weight of each head between them."""
+    typ, unit, key = case
+    cache, q, rows = large_scores(mb, TYPES[typ], unit, key)
+    weights = torch.zeros(1, 3, 2, cache.table.shape[1] * 16, device=DEV)
+    out = cache.attend_weigh(q, ints([0, 1, 2]), 0, weights)
+    assert torch.equal(out, cache.attend(q, ints([0, 1, 2]), 0))
+    want = torch.zeros_like(weights)
+    want[..., rows] = 1.0                                            # four heads, a quarter each
+    off = float((weights - want).abs().max())
+    assert off <= 2.0 ** -19 + (1040 / 16 + 64) * 2.0 ** -23, off
+    cache.check()
