@@ -93,10 +93,10 @@ __global__ void __launch_bounds__(kPlanThreads) evict_plan_kernel(const EvictArg
     return col < pieces_of(left[i], c.page) ? a.was + static_cast<long long>(i) * c.max_pages + col : nullptr;
   };
   int need = 0;
-  for (int x0 = 0; x0 < cols; x0 += kPlanThreads) {
-    const int x = x0 + threadIdx.x;
+  for (unsigned x0 = 0; x0 < static_cast<unsigned>(cols); x0 += kPlanThreads) {        // (columns and a block can add up past 2^31)
+    const unsigned x = x0 + threadIdx.x;
     int replaced = 0;
-    if (x < cols) {
+    if (x < static_cast<unsigned>(cols)) {
       int i;
       int32_t *word, *was = column(x, i, word);
       const int page = *word;
@@ -119,12 +119,12 @@ __global__ void __launch_bounds__(kPlanThreads) evict_plan_kernel(const EvictArg
   if (!enough) return;
   __syncthreads();                             // the new pages are there
   int before = 0;
-  for (int x0 = 0; x0 < cols; x0 += kPlanThreads) {
-    const int x = x0 + threadIdx.x;
+  for (unsigned x0 = 0; x0 < static_cast<unsigned>(cols); x0 += kPlanThreads) {
+    const unsigned x = x0 + threadIdx.x;
     int replaced = 0, page = 0;
     int32_t* word = nullptr;
     bool gone = false;
-    if (x < cols) {
+    if (x < static_cast<unsigned>(cols)) {
       int i;
       const int32_t* was = column(x, i, word);
       page = was ? *was : *word;
@@ -203,13 +203,14 @@ __global__ void __launch_bounds__(THREADS, 1280 / THREADS) evict_select_kernel(c
     asm volatile("griddepcontrol.wait;" ::: "memory");
     return;
   }
-  const int window = x.e.len - x.e.left + a.k, each = (window + ranks - 1) / ranks;
-  const int t0 = min(window, rank * each), t1 = min(window, t0 + each);
+  // (unsigned: a window and a chunk can add up past 2^31)
+  const unsigned window = x.e.len - x.e.left + a.k, each = pieces_of(static_cast<int>(window), ranks);
+  const unsigned t0 = min(window, rank * each), t1 = min(window, t0 + each);
   const float* w = weights_of(a, x) + x.e.first;
   const auto all_here = [&]() { if (ranks > 1) cluster_sync(); else __syncthreads(); };
   uint32_t key[HOLD];                         // of candidates row0 + 32 j; 0, below all weights, where there is none
-  const auto load = [&](int c0) {
-    const int row0 = c0 + warp * (32 * HOLD) + lane;
+  const auto load = [&](unsigned c0) {
+    const unsigned row0 = c0 + warp * (32 * HOLD) + lane;
     float v[HOLD];
 #pragma unroll
     for (int j = 0; j < HOLD; ++j) v[j] = row0 + 32 * j < t1 ? __ldcg(w + row0 + 32 * j) : 0.f;
@@ -229,7 +230,7 @@ __global__ void __launch_bounds__(THREADS, 1280 / THREADS) evict_select_kernel(c
   for (; shift > 0; pass ^= 1) {
     const int bits = shift > 10 ? 11 : 10, down = shift - bits;
 #pragma unroll 1
-    for (int c0 = t0; c0 < t1; c0 += kChunk) {
+    for (unsigned c0 = t0; c0 < t1; c0 += kChunk) {
       if (!once) load(c0);
 #pragma unroll
       for (int j = 0; j < HOLD; ++j)
@@ -316,7 +317,7 @@ __global__ void __launch_bounds__(THREADS, 1280 / THREADS) evict_select_kernel(c
   }
   int32_t* out = a.kept + x.id * a.k;
 #pragma unroll 1
-  for (int c0 = t0; c0 < t1; c0 += kChunk) {
+  for (unsigned c0 = t0; c0 < t1; c0 += kChunk) {
     if (!once) load(c0);
     int2 n = make_int2(0, 0);
 #pragma unroll
@@ -341,7 +342,7 @@ __global__ void __launch_bounds__(THREADS, 1280 / THREADS) evict_select_kernel(c
       equals += v.y;
     }
     const uint32_t before = (1u << lane) - 1;
-    const int row0 = x.e.first + c0 + warp * (32 * HOLD) + lane;
+    const unsigned row0 = x.e.first + c0 + warp * (32 * HOLD) + lane;
 #pragma unroll
     for (int j = 0; j < HOLD; ++j) {
       const bool more = key[j] > most, same = !more && key[j] >= least;
@@ -374,27 +375,28 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) evict_move_kernel(con
   const int tail = e.left - e.first - a.k;
   const int32_t* kept = a.kept + x.id * a.k;
   // row r of those from e.first on: where it comes from
-  const auto source = [&](int r) { return r < a.k ? __ldcg(kept + r) : e.len - tail + r - a.k; };
+  const auto source = [&](int r) { return r < a.k ? __ldcg(kept + r) : e.len - tail + (r - a.k); };
 
   if (part == parts - 1) {                     // the weights, and zeros behind them
     float* w = weights_of(a, x);
     constexpr int kBatch = THREADS * kMoveEach;
-    for (int r0 = 0; r0 < a.k + tail; r0 += kBatch) {
+    const unsigned moved = a.k + tail;         // (unsigned: these and a batch, and a length and a block, can add up past 2^31)
+    for (unsigned r0 = 0; r0 < moved; r0 += kBatch) {
       float v[kMoveEach];
 #pragma unroll
       for (int j = 0; j < kMoveEach; ++j) {
-        const int r = r0 + tid + j * THREADS;
-        v[j] = r < a.k + tail ? w[source(r)] : 0.f;
+        const unsigned r = r0 + tid + j * THREADS;
+        v[j] = r < moved ? w[source(r)] : 0.f;
       }
       __syncthreads();                         // the batch has been read
 #pragma unroll
       for (int j = 0; j < kMoveEach; ++j) {
-        const int r = r0 + tid + j * THREADS;
-        if (r < a.k + tail) w[e.first + r] = v[j];
+        const unsigned r = r0 + tid + j * THREADS;
+        if (r < moved) w[e.first + r] = v[j];
       }
     }
     __syncthreads();                           // the last rows' sources lie where the zeros go
-    for (int t = e.left + tid; t < e.len; t += THREADS) w[t] = 0.f;
+    for (unsigned t = e.left + tid; t < static_cast<unsigned>(e.len); t += THREADS) w[t] = 0.f;
     if (x.layer == 0 && x.head == 0 && tid == 0) c.len[e.seq] = e.left;      // (select reads it beside the plan)
     return;
   }
@@ -411,18 +413,19 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) evict_move_kernel(con
   // rows before e.first in its page move too, where the page is replaced
   const int head = e.first - page_of(e.first) * c.page, rows = head + a.k + tail, batch = together * kMoveEach;
   int src[kMoveRowsEach];                      // of the batch to be looked up next
-  const auto sources = [&](int r0, int n) {
+  const auto sources = [&](unsigned r0, int n) {       // (r0 of a batch behind the last can pass 2^31; n says that it has no rows)
 #pragma unroll
     for (int k = 0; k < kMoveRowsEach; ++k) {
       const int i = tid + k * THREADS;
-      src[k] = i < min(batch, n) ? (r0 + i < head ? e.first + r0 + i - head : source(r0 + i - head)) : -1;
+      src[k] = i < min(batch, n) ? (r0 + i < static_cast<unsigned>(head) ? static_cast<int>(e.first + r0 + i - head) : source(r0 + i - head)) : -1;
     }
   };
-  const auto look_up = [&](int r0, Row* to) {
+  const auto look_up = [&](unsigned r0, Row* to) {
 #pragma unroll
     for (int k = 0; k < kMoveRowsEach; ++k) {
-      const int s = src[k], t = e.first + r0 + tid + k * THREADS - head;
+      const int s = src[k];
       if (s < 0) continue;
+      const int t = e.first + r0 + tid + k * THREADS - head;
       const int cf = page_of(s), ct = page_of(t);
       const int old = cf < moved_to ? __ldcg(was + cf) & ~kReplaced : __ldcg(row + cf), now = __ldcg(row + ct);
       to[tid + k * THREADS] = Row{s == t && old == now ? -1 : place(old, s - cf * c.page), place(now, t - ct * c.page)};
@@ -433,7 +436,8 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) evict_move_kernel(con
   sources(batch, rows - batch);
   __syncthreads();
   int at = 0;
-  for (int r0 = 0, n = rows; n > 0; r0 += batch, n -= batch) {
+  unsigned r0 = 0;
+  for (int n = rows; n > 0; r0 += batch, n -= batch) {
     const Row* here = list[at] + mine;
     at = at == 2 ? 0 : at + 1;
     const int here_n = mine < together ? min(batch, n) - mine : 0;       // this thread's rows: 0, together, ... below it
@@ -442,7 +446,7 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) evict_move_kernel(con
     for (int j = 0; j < kMoveEach; ++j)
       if (j * together < here_n && here[j * together].from >= 0) v[j] = pool[here[j * together].from];
     look_up(r0 + batch, list[at]);
-    sources(r0 + 2 * batch, n - 2 * batch);    // (past 2^31 only where there is none)
+    sources(r0 + 2 * batch, n - 2 * batch);
     __syncthreads();                           // the batch has been read, the next one looked up
 #pragma unroll
     for (int j = 0; j < kMoveEach; ++j)

@@ -8,7 +8,7 @@ import pytest
 import torch
 
 from test_gpu_decode import grouped
-from test_gpu_handoff import DEV, TYPES, half_step, ints, mb, tiny  # noqa: F401
+from test_gpu_handoff import DEV, TYPES, gen, half_step, ints, mb, tiny  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -92,3 +92,60 @@ def test_attend_weigh_of_large_scores(mb, case):  # noqa: F811
     off = float((weights - want).abs().max())
     assert off <= 2.0 ** -19 + (1040 / 16 + 64) * 2.0 ** -23, off
     cache.check()
+
+
+# ----------------------------------------------------------------------------- lengths just below 2^31
+
+def long_cache(mb, last, dh=8):  # noqa: F811
+    """A cache of one sequence of 2^31 - 20 rows in pages of 16, all of them page 0 but the last `last`, which are 1, 2, ..."""
+    cols = (1 << 27) - 1
+    cache = mb.Cache.empty(1, last + 3, 1, 16, dh, 1, cols, torch.float16)
+    cache.pool.normal_(generator=gen(3))
+    cache.table[0, cols - last:] = torch.arange(1, last + 1, dtype=torch.int32, device=DEV)
+    cache.length[0] = (1 << 31) - 20
+    cache.refs[: last + 1] = 1
+    return cache
+
+
+def test_evict_at_lengths_just_below_32_bits(mb):  # noqa: F811
+    """A window behind 2^31 - 720 rows: what lies in front of it, its pages' other rows among them, stays."""
+    cache = long_cache(mb, 60)
+    n, first, last, k = (1 << 31) - 20, (1 << 31) - 720, 100, 50
+    before = cache.pool.clone()
+    weights = torch.full((1, 1, 1, cache.table.shape[1] * 16), 3.0, device=DEV)
+    weights[..., first: n] = torch.rand(n - first, generator=gen(1), device=DEV)
+    was = weights[0, 0, 0, first: n].clone()
+    cache.evict(weights, ints([0]), ints([first]), ints([last]), k)
+    cache.check()
+    left = first + k + last
+    assert int(cache.length[0]) == left and bool((cache.refs[1: 61] == (torch.arange(60, device=DEV) < 26).int()).all())
+    src = torch.cat((was[: n - first - last].sort(descending=True, stable=True).indices[:k].sort().values,
+                     torch.arange(n - first - last, n - first, device=DEV)))
+    w = weights[0, 0, 0]
+    assert torch.equal(w[first: left], was[src]) and bool((w[left: n] == 0).all())
+    assert bool((w[:first] == 3).all()) and bool((w[n:] == 3).all())
+    # rows in the last 60 pages, in order
+    rows, had = (p[0, :, 1: 61, 0].reshape(2, 960, 8) for p in (cache.pool, before))
+    base = (1 << 31) - 16 - 960
+    assert torch.equal(rows[:, first - base: left - base], had[:, src + first - base])
+    assert torch.equal(rows[:, : first - base], had[:, : first - base]) and torch.equal(cache.pool[0, :, 0], before[0, :, 0])
+
+
+def test_evict_of_all_rows_of_a_length_just_below_32_bits(mb):  # noqa: F811
+    """All rows but five stay: every loop over rows goes almost to 2^31.  (Pages repeat, so that all rows are alike.)"""
+    cache = long_cache(mb, 0)
+    cache.pool.fill_(2.0)
+    n, gone = (1 << 31) - 20, [10, 1000, 1 << 30, (1 << 31) - 23, (1 << 31) - 21]
+    weights = torch.zeros(1, 1, 1, n + 4, device=DEV)
+    w = weights[0, 0, 0]
+    for at in range(0, n, 1 << 28):
+        to = min(n, at + (1 << 28))
+        w[at: to] = torch.arange(at, to, dtype=torch.int32, device=DEV) % 1021 + 1
+    w[gone] = 0.0
+    was = w.clone()
+    cache.evict(weights, ints([0]), None, None, n - 5)
+    cache.check()
+    assert int(cache.length[0]) == n - 5 and cache.refs.cpu().tolist() == [1, 0, 0] and bool((cache.pool == 2).all())
+    for i, (a, b) in enumerate(zip([-1] + gone, gone + [n])):
+        assert torch.equal(w[a + 1 - i: b - i], was[a + 1: b]), i
+    assert bool((w[n - 5:] == 0).all())
