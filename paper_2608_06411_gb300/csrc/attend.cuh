@@ -367,14 +367,16 @@ __global__ void __launch_bounds__(kThreads, ctas_of(DH)) attend_kernel(const __g
   const T* pk = static_cast<const T*>(a.pk);
   const T* pv = pk + a.plane;
   const bool whole = a.c.page % kTok == 0;     // a warp's 16 rows lie in one page
-  const auto page_at = [&](int tok) { return a.page_shift >= 0 ? tok >> a.page_shift : tok / a.c.page; };
-  const auto row_in_page = [&](int tok) { return a.page_shift >= 0 ? tok & (a.c.page - 1) : tok % a.c.page; };
+  // (rows as unsigned numbers, compared by how far they are behind `from`: kOwn's tiles begin at any page's first row, so that a tile's
+  // rows past a length just below 2^31 pass it)
+  const auto page_at = [&](unsigned tok) { return a.page_shift >= 0 ? tok >> a.page_shift : tok / a.c.page; };
+  const auto row_in_page = [&](unsigned tok) { return a.page_shift >= 0 ? tok & (a.c.page - 1) : tok % a.c.page; };
 
   // ---- loads.  pid: page of the warp's first row (whole), else of row lane & 15, read a tile ahead.
   const auto page_of = [&](const Place<MODE>& p) -> int {
     if (p.i >= a.n) return 0;
-    const int tok = p.from + p.t * kTile + warp * kTok + (whole ? 0 : lane & 15);
-    return tok < p.len ? mapk::load<MODE>(a.c.table + static_cast<long long>(p.s) * a.c.max_pages + page_at(tok)) : 0;
+    const int off = p.t * kTile + warp * kTok + (whole ? 0 : lane & 15);
+    return off < p.len - p.from ? mapk::load<MODE>(a.c.table + static_cast<long long>(p.s) * a.c.max_pages + page_at(static_cast<unsigned>(p.from) + off)) : 0;
   };
   int pid = page_of(ld), ld_seg = 0;
   bool ld_new = true;
@@ -388,7 +390,8 @@ __global__ void __launch_bounds__(kThreads, ctas_of(DH)) attend_kernel(const __g
         cp_async16_or_zero(qbuf + (ld_seg % STAGES) * rows * R::kRow + R::at(r, x), q + (r < have ? r : 0) * a.q.head + x * 8, r < have);
       }
     }
-    const int tok0 = ld.from + ld.t * kTile + warp * kTok, valid = ld.len - tok0;
+    const int off0 = ld.t * kTile + warp * kTok, valid = ld.len - ld.from - off0;
+    const unsigned tok0 = static_cast<unsigned>(ld.from) + off0;
     if (valid > 0) {
       if (!good_page(a.c, pid)) {              // (here, a tile after it was asked for: a check there would wait for it)
         atomicOr(a.c.status, ST_BADINDEX);

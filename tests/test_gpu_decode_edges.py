@@ -8,7 +8,7 @@ import pytest
 import torch
 
 from test_gpu_decode import grouped
-from test_gpu_handoff import DEV, TYPES, gen, half_step, ints, mb, tiny  # noqa: F401
+from test_gpu_handoff import DEV, TYPES, gen, half_step, ints, mb, randn, tiny  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -149,3 +149,28 @@ def test_evict_of_all_rows_of_a_length_just_below_32_bits(mb):  # noqa: F811
     for i, (a, b) in enumerate(zip([-1] + gone, gone + [n])):
         assert torch.equal(w[a + 1 - i: b - i], was[a + 1: b]), i
     assert bool((w[n - 5:] == 0).all())
+
+
+@pytest.mark.parametrize("page", [16, 24, 5])
+def test_attend_shared_at_lengths_just_below_32_bits(mb, page):  # noqa: F811
+    """Two sequences with all but their last pages in common: their own rows begin at no multiple of a tile, and the tile behind
+    their last row passes 2^31.  The own rows take all weight."""
+    cols = ((1 << 31) - 1) // page
+    own = 160 // page
+    n, front = cols * page - 4, (cols - own) * page
+    assert front % 64 != 0 and front + (n - front + 63) // 64 * 64 >= 1 << 31
+    cache = mb.Cache.empty(1, 2 * own + 2, 1, page, 64, 2, cols, torch.float16)
+    cache.pool[0, 0], cache.pool[0, 1] = 0.0, 1.0
+    cache.pool[0, 0, 1:, :, :, 0] = 1600.0
+    cache.pool[0, 1, 1:] = randn(gen(2), 2 * own + 1, 1, page, 64, typ=torch.float16)
+    for s in range(2):
+        cache.table[s, cols - own:] = 1 + s * own + torch.arange(own, dtype=torch.int32, device=DEV)
+    cache.length[:] = n
+    q = torch.ones(2, 1, 64, dtype=torch.float16, device=DEV)
+    out = cache.attend_shared(q, ints([0, 1]), 0, ints([0, 2]))
+    cache.check()
+    for s in range(2):
+        v = cache.pool[0, 1, 1 + s * own: 1 + (s + 1) * own, 0].reshape(-1, 64)[: n - front].double()
+        want, mag = v.mean(0), v.abs().mean(0)
+        off = (out[s, 0].double() - want).abs()
+        assert bool((off <= half_step(torch.float16) * want.abs() * 1.001 + sums_error(64, n - front, 200.0) * mag + tiny(torch.float16)).all()), s
