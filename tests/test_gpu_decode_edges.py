@@ -7,7 +7,7 @@ import math
 import pytest
 import torch
 
-from test_gpu_decode import grouped
+from test_gpu_decode import check, grouped
 from test_gpu_handoff import DEV, TYPES, gen, half_step, ints, mb, randn, tiny  # noqa: F401
 
 pytestmark = pytest.mark.gpu
@@ -174,3 +174,23 @@ def test_attend_shared_at_lengths_just_below_32_bits(mb, page):  # noqa: F811
         want, mag = v.mean(0), v.abs().mean(0)
         off = (out[s, 0].double() - want).abs()
         assert bool((off <= half_step(torch.float16) * want.abs() * 1.001 + sums_error(64, n - front, 200.0) * mag + tiny(torch.float16)).all()), s
+
+
+# ----------------------------------------------------------------------------- many groups
+
+def test_attend_shared_of_groups_of_which_few_share(mb):  # noqa: F811
+    """60001 groups: the first, the second, one in the middle and the last one share rows, the others are single sequences of a row."""
+    cache = grouped(mb, torch.bfloat16, 64, 2, 16, [(1000, [5, 40, 1]), (0, [1])], 2)
+    groups = [[0, 1], [2, 0, 1]] + [[3]] * 29998 + [[1, 2]] + [[3]] * 29999 + [[0, 2]]
+    seqs, starts = sum(groups, []), [0]
+    for g in groups:
+        starts.append(starts[-1] + len(g))
+    q = randn(gen(1), 1, 4, 64, typ=torch.bfloat16).expand(len(seqs), -1, -1).contiguous()
+    out = cache.attend_shared(q, ints(seqs), 0, ints(starts))
+    cache.check()
+    v = cache.pool[0, 1, cache.table[3, 0].long(), :, 0].repeat_interleave(2, 0)
+    alone = torch.tensor(seqs, device=DEV) == 3
+    assert bool((out[alone] == v).all())
+    several = (~alone).nonzero()[:, 0]
+    check(out[several], q[several], cache, 0, [seqs[i] for i in several.tolist()], 0.125, torch.bfloat16)
+    assert torch.equal(cache.attend_shared(q, ints(seqs), 0, ints(starts)), out)
