@@ -3,12 +3,15 @@
 Tolerances as in test_gpu_decode.py, and: fp16's halves of a weight above zero are raised to 2^-24 of 2^15 each, so that a row adds
 2^-38 of the base's weight at most (bf16: 2^-125, nothing beside the smallest numbers)."""
 import math
+import threading
 
+import numpy as np
 import pytest
 import torch
 
-from test_gpu_decode import check, grouped
-from test_gpu_handoff import DEV, TYPES, gen, half_step, ints, mb, randn, tiny  # noqa: F401
+from oracle import handoff_oracle as H
+from test_gpu_decode import check, grouped, slots_of
+from test_gpu_handoff import DEV, TYPES, f64, filled, gen, half_step, ints, mb, randn, rows_of, tiny  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -194,3 +197,185 @@ def test_attend_shared_of_groups_of_which_few_share(mb):  # noqa: F811
     several = (~alone).nonzero()[:, 0]
     check(out[several], q[several], cache, 0, [seqs[i] for i in several.tolist()], 0.125, torch.bfloat16)
     assert torch.equal(cache.attend_shared(q, ints(seqs), 0, ints(starts)), out)
+
+
+@pytest.mark.parametrize("typ", ["f16", "bf16"])
+def test_attend_shared_of_values_without_weight(mb, typ):  # noqa: F811
+    """An infinite value of a row whose weight is zero in fp32 is no number in the sum, as in map_cache_attend."""
+    cache = grouped(mb, TYPES[typ], 64, 1, 16, [(320, [4, 9])], 2)
+    cache.pool[0, 0] = torch.nan_to_num(cache.pool[0, 0]) * 0
+    cache.pool[0, 0, cache.table[0, 0].long(), 0, 3, 0] = 1600.0     # a row that takes all, by 288 powers of two
+    cache.pool[0, 1, cache.table[0, 2].long(), 0, 5, 7] = float("inf")
+    q = torch.ones(2, 2, 64, dtype=TYPES[typ], device=DEV)
+    for out in (cache.attend(q, ints([0, 1]), 0), cache.attend_shared(q, ints([0, 1]), 0, ints([0, 2]))):
+        assert bool(torch.isnan(out[:, :, 7]).all())
+        out[:, :, 7] = 0.0
+        assert bool(torch.isfinite(out).all())
+
+
+# ----------------------------------------------------------------------------- eviction: variants, refusals, replaced pages
+
+def evicted(cache, weights, s, first, last, k):
+    """Rows [layers, 2, rows, heads, dh] and weights [layers, heads, rows] that sequence s is to have afterwards."""
+    slots = torch.tensor(slots_of(cache, s), device=DEV)
+    n, layers, heads = len(slots), weights.shape[0], weights.shape[2]
+    rows = cache.pool[:, :, slots // cache.page, :, slots % cache.page].permute(1, 2, 3, 0, 4)       # [layers, 2, heads, rows, dh]
+    w = weights[:, s, :, :n]
+    kept = w[..., first: n - last].sort(dim=-1, descending=True, stable=True).indices[..., :k].sort(dim=-1).values + first
+    front, behind = (torch.arange(*r, device=DEV).expand(layers, heads, -1) for r in ((0, first), (n - last, n)))
+    src = torch.cat((front, kept, behind), -1)
+    return rows.gather(3, src[:, None, :, :, None].expand(-1, 2, -1, -1, rows.shape[-1])).transpose(2, 3), w.gather(-1, src)
+
+
+VARIANTS = [
+    # layers, heads, page, lens, first, last, k
+    (38, 8, 16, [1000], 4, 100, 300), (38, 8, 16, [2000], 0, 0, 1500), (38, 8, 24, [3000], 35, 1, 700),
+    (38, 8, 16, [4000], 1, 50, 2049), (38, 8, 5, [9000], 4, 9, 4000), (1, 2, 16, [70000], 35, 100, 30000),
+    (2, 1, 64, [140001, 9], 0, 1, 100), (1, 1, 1024, [66000, 65000, 8193], 7, 0, 8100)]
+
+
+@pytest.mark.parametrize("case", VARIANTS, ids=["-".join(str(v) for v in c) for c in VARIANTS])
+def test_evict_of_every_number_of_candidates_a_thread(mb, case):  # noqa: F811
+    """304 units a CTA each, with 4, 8, 13 and 16 candidates a thread and more than it holds; few units in clusters of eight CTAs, whose
+    shares are looked at in several pieces.  Thousands of equal weights at the border."""
+    layers, hk, page, lens, first, last, k = case
+    cache = filled(mb, torch.float16, 8, hk, page, lens, 3, layers=layers)
+    weights = torch.exp(2.5 * torch.randn(layers, len(lens), hk, cache.table.shape[1] * page, generator=gen(1), device=DEV))
+    weights[:, :, hk // 2:] = (weights[:, :, hk // 2:] * 4).floor()
+    was = [n if n - first - last <= k else first + k + last for n in lens]
+    want = [evicted(cache, weights, s, first, last, k) if left < lens[s] else None for s, left in enumerate(was)]
+    n = len(lens)
+    cache.evict(weights, ints(range(n)), ints([first] * n), ints([last] * n), k)
+    cache.check()
+    assert cache.length.cpu().tolist() == was
+    for s, left in enumerate(was):
+        if want[s] is not None:
+            assert torch.equal(rows_of(cache.pool, slots_of(cache, s)), want[s][0])
+            assert torch.equal(weights[:, s, :, :left], want[s][1]) and bool((weights[:, s, :, left: lens[s]] == 0).all())
+
+
+def test_evict_that_is_refused_leaves_the_table(mb):  # noqa: F811
+    def refused(code, *args):
+        state = [t.clone() for t in (cache.table, cache.length, cache.refs, cache.pool.view(torch.int16), weights)]
+        cache.evict(weights, *args)
+        assert cache.status() == code
+        for a, b in zip(state, (cache.table, cache.length, cache.refs, cache.pool.view(torch.int16), weights)):
+            assert torch.equal(a, b)
+
+    cache = grouped(mb, torch.float16, 64, 1, 16, [(64, [5, 40]), (0, [100])], 1, spare=-2)          # two pages are free
+    weights = torch.rand(1, 3, 1, cache.table.shape[1] * 16, generator=gen(1), device=DEV)
+    refused(mb.MAP_ENOMEM, ints([0, 2]), None, None, 40)             # three shared pages to replace
+    refused(mb.MAP_EINTERNAL, ints([0, 2, 0]), ints([32] * 3), None, 4)
+    refused(mb.MAP_EINTERNAL, ints([0, 3]), ints([32] * 2), None, 4)
+    refused(mb.MAP_EINTERNAL, ints([0, 2]), ints([32, -1]), None, 4)
+    cache.length[2] = 1 << 20
+    refused(mb.MAP_EINTERNAL, ints([0, 2]), ints([32, 0]), None, 4)
+    cache.length[2] = 100
+    for bad in (-1, cache.pool.shape[2]):
+        good, cache.table[2, 5] = int(cache.table[2, 5]), bad
+        refused(mb.MAP_EINTERNAL, ints([0, 2]), ints([32, 0]), None, 4)
+        cache.table[2, 5] = good
+    cache.evict(weights, ints([0, 2]), ints([32, 0]), None, 4)       # what was refused with them
+    cache.check()
+    assert cache.length.cpu().tolist() == [36, 104, 4]
+
+
+def test_evict_replaces_the_shared_page_that_it_cuts(mb):  # noqa: F811
+    """Nothing stays behind row 20: the shared page of rows 16 to 19 is replaced all the same, so that rows appended later
+    are the sequence's own, and the call is refused where no page is free."""
+    for spare in (-3, -4):                                           # one page free, none
+        cache = grouped(mb, torch.float16, 64, 2, 16, [(64, [5, 40])], 1, spare=spare)
+        weights = torch.rand(1, 2, 2, cache.table.shape[1] * 16, generator=gen(1), device=DEV)
+        pages, rows = cache.table[0].clone(), rows_of(cache.pool, slots_of(cache, 0))
+        other = rows_of(cache.pool, slots_of(cache, 1))
+        cache.evict(weights, ints([0]), ints([20]), None, 0)
+        if spare == -4:
+            assert cache.status() == mb.MAP_ENOMEM and torch.equal(cache.table[0], pages) and int(cache.length[0]) == 69
+            continue
+        cache.check()
+        assert int(cache.length[0]) == 20 and cache.table[0, 0] == pages[0] and cache.table[0, 1] != pages[1]
+        assert cache.refs[pages[:5].long()].tolist() == [2, 1, 1, 1, 0] and int(cache.refs[cache.table[0, 1].long()]) == 1
+        cache.pool[0, :, cache.table[0, 1].long(), :, 4:] = 9.0      # where rows behind come
+        assert torch.equal(rows_of(cache.pool, slots_of(cache, 0)), rows[:, :, :20])
+        assert torch.equal(rows_of(cache.pool, slots_of(cache, 1)), other)
+
+
+# ----------------------------------------------------------------------------- together
+
+def test_positions_go_on_after_an_eviction(mb):  # noqa: F811
+    """Kept keys stay rotated by the positions they were appended with: the caller counts on from the tokens, not from the length."""
+    dh, hk, hq, page, plan_freq = 64, 2, 4, 16, [0.9 ** i for i in range(32)]
+    plan, cache = mb.Rope(dh, plan_freq), mb.Cache.empty(1, 8, hk, page, dh, 1, 5, torch.float16)
+    weights = torch.zeros(1, 1, hk, 5 * page, device=DEV)
+    one, first, last, budget, tokens = ints([0]), ints([4]), ints([8]), 20, 150
+    raw = [randn(gen(i), tokens, h, dh, typ=torch.float16) for i, h in enumerate((hq, hk, hk))]
+    token = torch.zeros(1, 1, dtype=torch.int32, device=DEV)         # positions: tokens so far, whatever has been evicted
+    held = [[] for _ in range(hk)]                                   # tokens that a head holds
+    for t in range(tokens):
+        q, k, v = (x[t: t + 1] for x in raw)
+        q = plan.append(q, k, v, token, cache, 0, cache.extend(one))
+        out = cache.attend_weigh(q, one, 0, weights)
+        token += 1
+        for h in range(hk):
+            held[h].append(t)
+        n = len(held[0])
+        assert n == int(cache.length[0])
+        if n == 40:                                                  # back to first + budget + last
+            for h in range(hk):
+                kept = 4 + weights[0, 0, h, 4: n - 8].sort(descending=True, stable=True).indices[:budget].sort().values
+                held[h] = held[h][:4] + [held[h][i] for i in kept.tolist()] + held[h][n - 8:]
+            cache.evict(weights, one, first, last, budget)
+    cache.check()
+    assert int(cache.length[0]) < 40 < tokens
+    for h in range(hk):
+        pos = np.array([held[h]], dtype=np.int64)
+        keys = H.rotate(f64(raw[1])[held[h]], None, pos, plan_freq, np.zeros(32, int), False, 0.0)[0][:, h: h + 1]
+        want, mag, dz = H.attend(H.rotate(f64(raw[0])[-1:], None, np.array([[tokens - 1]]), plan_freq, np.zeros(32, int), False, 0.0)[0][0, 2 * h: 2 * h + 2],
+                                 keys, f64(raw[2])[held[h]][:, h: h + 1], dh ** -0.5)
+        # q and k are rotated and rounded once: 32 2^-24 and half a step each of the scores' products, which p has twice
+        e = sums_error(dh, 40, dz) + 4.2 * half_step(torch.float16) * dz + 128 * 2.0 ** -24 * dz
+        assert (np.abs(f64(out[0, 2 * h: 2 * h + 2]) - want) <= half_step(torch.float16) * np.abs(want) + e * mag + tiny(torch.float16)).all()
+
+
+def test_evictions_of_several_caches_from_several_threads(mb):  # noqa: F811
+    """Steps of rows appended, weighed and evicted, in caches whose calls take more and less shared memory than is had without asking:
+    each cache ends as it does alone."""
+    budget, steps, sets = 6, 150, []
+    for n, dh, group in ((3000, 64, 16), (2, 64, 1), (3000, 256, 1), (2, 256, 2)):
+        c = mb.Cache.empty(1, 4 * n, 1, 4, dh, n, 5, torch.float16)
+        c.pool.normal_(generator=gen(n + dh))
+        sets.append((n, c, randn(gen(dh), n, group, dh, typ=torch.float16), torch.cuda.Stream()))
+
+    def work(n, c, q, weights, stream):
+        seqs, first, last, counts = ints(range(n)), ints([1] * n), ints([2] * n), ints([3] * n)
+        stream.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(stream):
+            for step in range(steps):
+                c.extend(seqs, counts, rows=3 * n)
+                c.attend_weigh(q, seqs, 0, weights)
+                c.evict(weights, seqs, first, last, budget)
+        stream.synchronize()
+
+    results = []
+    for threads in (False, True):
+        copies, jobs = [], []
+        for n, c, q, stream in sets:
+            d = mb.Cache(*(t.clone() for t in (c.pool, c.table, c.length, c.refs)))
+            w = torch.zeros(1, n, 1, 20, device=DEV)
+            copies.append((d, w))
+            jobs.append(threading.Thread(target=work, args=(n, d, q, w, stream)))
+        torch.cuda.synchronize()
+        for j in jobs:
+            j.start()
+            if not threads:
+                j.join()
+        for j in jobs:
+            j.join()
+        torch.cuda.synchronize()
+        for d, _ in copies:
+            d.check()
+            assert bool((d.length == 1 + budget + 2).all())
+        results.append([(d.pool.view(torch.int16), d.table, d.length, d.refs, w) for d, w in copies])
+    for alone, beside in zip(*results):
+        assert all(torch.equal(a, b) for a, b in zip(alone, beside))
+        assert float(alone[-1].abs().sum()) > 0
