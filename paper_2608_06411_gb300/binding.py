@@ -741,6 +741,8 @@ class Cache:
         larger one is a call's own, and so is one of a call that is captured, whose memory then belongs to the graph."""
         size = self._sizes.get((call, args))
         if size is None:
+            if len(self._sizes) >= 4096:     # (calls of ever other sizes)
+                self._sizes.clear()
             size = self._sizes[call, args] = int(getattr(lib, call + "_workspace")(self.desc, *args))
         if size > _KEEP or _capturing():
             return torch.empty(max(size, 256), dtype=torch.uint8, device=self.device)

@@ -379,3 +379,12 @@ def test_evictions_of_several_caches_from_several_threads(mb):  # noqa: F811
     for alone, beside in zip(*results):
         assert all(torch.equal(a, b) for a, b in zip(alone, beside))
         assert float(alone[-1].abs().sum()) > 0
+
+
+def test_what_a_cache_remembers_of_its_calls_is_bounded(mb):  # noqa: F811
+    cache = mb.Cache.empty(1, 8, 1, 4, 8, 2, 4)
+    weights = torch.zeros(1, 2, 1, 16, device=DEV)
+    for k in range(5000):
+        cache.evict(weights, ints([-1]), None, None, k)
+    cache.check()
+    assert len(cache._sizes) <= 4096
