@@ -800,6 +800,8 @@ class Cache:
         if stream is not None or dev.index != _current_device():
             with _on(dev, stream, weights, seqs, first, last):
                 return self.evict(weights, seqs, first, last, k)
+        if k >= 1 << 31:                     # (a C int would be what is left of it, and fewer rows stay)
+            raise ValueError("k must be below 2^31")
         n, i32 = seqs.shape[0], torch.int32
         ws = self._scratch("map_cache_evict", n, k)
         _check(lib.map_cache_evict(self.desc, _dense(weights, torch.float32, dev, self._weights_shape, "weights"),

@@ -388,3 +388,15 @@ def test_what_a_cache_remembers_of_its_calls_is_bounded(mb):  # noqa: F811
         cache.evict(weights, ints([-1]), None, None, k)
     cache.check()
     assert len(cache._sizes) <= 4096
+
+
+def test_evict_refuses_a_k_that_no_int_holds(mb):  # noqa: F811
+    cache = mb.Cache.empty(1, 8, 1, 4, 8, 1, 4)
+    weights = torch.zeros(1, 1, 1, 16, device=DEV)
+    cache.extend(ints([0]), ints([10]), rows=10)
+    for k in (1 << 31, 1 << 32, (1 << 40) + 1):
+        with pytest.raises(ValueError):
+            cache.evict(weights, ints([0]), None, None, k)
+    cache.evict(weights, ints([0]), None, None, (1 << 31) - 1)
+    cache.check()
+    assert int(cache.length[0]) == 10
