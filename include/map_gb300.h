@@ -490,7 +490,7 @@ int map_cache_attend_shared(const map_cache *cache, int layer, const map_heads *
  *             or freed; a row that is appended must find its weight as the caller wants it to begin.  What lies at or behind a
  *             sequence's length is not read or written.
  *   ws        device scratch of map_cache_attend_weigh_workspace(cache, q heads, n) bytes, 16-byte aligned, the caller's until
- *             the call's work completes; 4 bytes for each row that a sequence can have and query head.
+ *             the call's work completes; 4 bytes for each row that a sequence can have (not those that it has) and query head.
  * A sequence that appears in several rows gets the weights of all, added up in their order.  Everything else as for
  * map_cache_attend.
  */
@@ -508,9 +508,12 @@ int map_cache_attend_weigh(const map_cache *cache, int layer, const map_heads *q
  *   weights      as map_cache_attend_weigh's; those behind the new length, up to the old one, become 0.
  *   ws           device scratch of map_cache_evict_workspace(cache, n, k) bytes, 16-byte aligned, the caller's until the call's work
  *                completes.
- * Pages that other sequences hold as well keep their rows: where rows move (or stay beside ones that do) the sequence gets new
- * pages instead, taken before any is given up.  Pages behind the new length lose a holder.  n <= 4096, n * max_pages < 2^31,
- * n * layers * heads <= 2^24 (MAP_EUNSUPPORTED beyond).
+ * Pages that other sequences hold as well keep their rows: of a sequence that loses rows, those from row first[i]'s page up to the
+ * new length are replaced by new ones, taken before any is given up (row first[i]'s also where only rows before it are left of it:
+ * what is appended next goes there).  Pages behind the new length lose a holder.
+ * Keys stay rotated by the positions that they were appended with: the next token's position follows from the tokens so far,
+ * not from len, which an eviction has made smaller.
+ * n <= 4096, n * max_pages < 2^31, n * layers * heads <= 2^24 (MAP_EUNSUPPORTED beyond).
  */
 size_t map_cache_evict_workspace(const map_cache *cache, int n, int k);
 int map_cache_evict(const map_cache *cache, float *weights, const int32_t *seqs, int n, const int32_t *first,

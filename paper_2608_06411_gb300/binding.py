@@ -795,7 +795,8 @@ class Cache:
     def evict(self, weights, seqs, first, last, k: int, stream=None) -> None:
         """map_cache_evict: of rows first[i] .. length - last[i] - 1 of sequence seqs[i] the k with the greatest weights stay,
         for each layer and head by itself; the rows behind move up, their weights with them (all int32 on the device, first
-        and last None for 0)."""
+        and last None for 0).  Keys stay rotated by the positions they were appended with: count the next token's position
+        from the tokens so far, not from `length`."""
         dev = self.device
         if stream is not None or dev.index != _current_device():
             with _on(dev, stream, weights, seqs, first, last):

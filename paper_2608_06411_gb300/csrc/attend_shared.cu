@@ -8,11 +8,11 @@
 // weights in two halves), on the tensor cores as much as the loads from about 200 query heads a key head on; for groups of a few
 // sequences the chain of four launches.
 // The launches: what is shared, the shared rows, the sequences' own rows, the join.  The own rows' kernel starts on the SMs that the
-// shared rows leave free.  (The other order took 47 us for 64 questions and 74 for the video below, where 41 and 64 are taken.)
+// shared rows leave free.  (The other order took 3 us more for 64 questions and 6 more for the video below.)
 // Measured, 128 columns: 4 questions on 611 rows, 32 heads over 32: 22 us (plan 4, shared rows 9, join 5, launches); 64 questions on
-// 2915 rows, 32 over 8: 41 us (plan 6, shared rows done at 22 and own rows at 30, join 7 of 17 MB of parts); 8 groups of 8 on up to
-// 1315 rows, 28 over 4: 32 us; 32 answers on 60001 rows, 28 over 4, fp16: 64 us, of which the shared rows take 43, 123 MB at
-// 2.8 TB/s and tensor cores 57 % busy.
+// 2915 rows, 32 over 8: 42.5 us (plan 6, shared rows done at 22 and own rows at 30, join 7 of 17 MB of parts); 8 groups of 8 on up to
+// 1315 rows, 28 over 4: 33 us; 32 answers on 60001 rows, 28 over 4, fp16: 69 us, of which the shared rows take 48, 123 MB at
+// 2.5 TB/s and tensor cores 48 % busy.
 #include <type_traits>
 
 #include "attend.cuh"
@@ -238,7 +238,7 @@ __device__ __forceinline__ float2 add2(float2 a, float2 b) {
 // number, those of a weight of zero are zero.  Weights are 2^kLift times what they are to the row's base, which the largest score
 // passes by kSlack at most: sums are scaled only then, not whenever a tile has a greater score.  fp16 has room for a little less
 // than 2^16, so that a half that is raised adds 2^-39 of the base's weight there as in split_weights.  (A smaller lift under a
-// slack of 4 and halves raised whatever the weight took 4 us less of the video's 69 above and added 2^-34 a row.)
+// slack of 4 and halves raised whatever the weight took 4 to 5 us less of the video's 69 above and added 2^-34 a row.)
 template <typename T> constexpr float kSlack = 8.f;
 template <> constexpr float kSlack<__half> = 0.99f;
 __device__ __forceinline__ uint32_t min_u16x2(uint32_t a, uint32_t b) {
@@ -893,7 +893,7 @@ int shared_box(const AttendArgs& a, CUtensorMap* map) {
 }
 
 // Rows of an item: 256, on an SM of its own, where groups have more than 128 on average (32 answers of 7 heads a key head on a
-// video: 64 us; with 128, which read the keys and values twice, 86).
+// video took a third more with 128, which read the keys and values twice).
 int shared_rows(const map_cache* c, long long heads, long long n, long long groups) {
   return c->dh <= 128 && n * (heads / c->heads) > kM * groups ? 2 * kM : kM;
 }

@@ -13,10 +13,10 @@
 // the rows move.  (One kernel, a CTA a unit, took 65, 223, 229 and 621 us for the cases below; that kernel with 2048 units in
 // two halves, the select of some beside the moves of others, gained nothing.)
 // Measured (28 layers of 4 key heads, 128 columns, unless said otherwise; with the copies of tables and weights that the
-// measurement makes): one sequence of 1100 rows to 512: 26 us, a chain of launches; 6 of 3001 to 4096 rows to 1315: 172 us, of
-// which the move of 858 MB of DRAM traffic takes 141 to 147, 5.8 to 6.1 TB/s; 8 questions of 2915 to 3000 rows on one image in
-// 32 layers of 8 heads to 245: 120 us, the move of rows at random places 77 (5.5 TB/s), the select 28, bound by its
-// instructions; one of 60001 rows in 8 layers to 16900: 146 us, of which the move of 64-byte slices takes 113 (4.7 TB/s).
+// measurement makes): one sequence of 1100 rows to 512: 26 us, a chain of launches; 6 of 3001 to 4096 rows to 1315: 170 us, of
+// which the move of 854 MB of DRAM traffic takes 141 to 148, 5.8 to 6.1 TB/s; 8 questions of 2915 to 3000 rows on one image in
+// 32 layers of 8 heads to 245: 119 us, the move of rows at random places 77 (5.5 TB/s), the select 28, bound by its
+// instructions; one of 60001 rows in 8 layers to 16900: 144 us, of which the move of 64-byte slices takes 108 (4.9 TB/s).
 #include <algorithm>
 
 #include "pages.cuh"
@@ -496,7 +496,9 @@ int map_cache_evict(const map_cache* c, float* weights, const int32_t* seqs, int
   cudaError_t e = allow_smem(reinterpret_cast<const void*>(evict_plan_kernel), smem);
   if (e == cudaSuccess) e = launch_k(evict_plan_kernel, dim3(1), dim3(kPlanThreads), smem, st, a);
   const long long units = static_cast<long long>(n) * c->layers * c->heads, max_rows = static_cast<long long>(c->max_pages) * c->page;
-  // CTAs that look for a unit's rows, and slices that its columns move in: as many as fill the chip where the units do not
+  // CTAs that look for a unit's rows, and slices that its columns move in: as many as fill the chip where the units do not.  What a
+  // sequence can hold counts, for its length is not known here: one of 1100 rows to 512 takes 28 to 30 us in a cache of 1120 to 4112
+  // rows, 32 in one of 16384 and 37 in one of 131072.
   int ranks = 1, slices = 1;
   while (ranks < 8 && units * ranks < 2 * 152 && max_rows / ranks > 2048) ranks *= 2;
   while (slices < 4 && units * (4 * slices + 1) <= 4 * 152 && c->dh / 8 / slices >= 8) slices *= 2;
